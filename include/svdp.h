@@ -272,6 +272,93 @@ svdp_status svdp_ffn_step_glued(const svdp_layer *layer, const void *x_prev, con
                                 uint64_t *mask_out, int32_t *idx_out, int32_t *nnz_out,
                                 void *ws, size_t ws_bytes, void *stream);
 
+/* ---- decoding with drafted tokens ----
+ *
+ * A program that verifies drafted tokens decodes a small tree of tokens for each request in one pass and keeps the
+ * branch that its own answers agree with.  Per step: svdp_tree_attn in every layer, svdp_tree_accept on the logits,
+ * svdp_kv_plan for the slots of the accepted tokens, svdp_kv_commit for their K and V of all layers.  Only accepted
+ * tokens ever enter the cache, so nothing in it has to be moved or taken back.
+ *
+ * Rows and trees.  T rows (tokens) of R requests, one request after the other: request r has the rows
+ * starts[r] .. starts[r + 1], its nodes 0, 1, ...; starts: device [R + 1] int32, ascending, starts[0] = 0; rows from
+ * starts[R] to T are padding.  tree: device [T] 64-bit words, bit j of tree[t]: row t sees node j of its own request;
+ * NULL: every node sees the nodes before it and itself.  A request has up to max_nodes <= SVDP_MAX_NODES nodes.
+ * Nodes come after their ancestors (node 0 first: the newest certain token).
+ *
+ * Pages.  A request's tokens lie in pages of `page` tokens: token i in page table[r][i / page], at i % page.
+ * table: device [R][max_pages] int32; entries past a request's length are not read.  A slot is page id * page + place.
+ *
+ * Limits (else SVDP_ERR_UNSUPPORTED): page 32, 64, 128 or 256; dim 64, 128 or 256; R <= SVDP_MAX_REQUESTS;
+ * pages * page, R * max_pages and max_pages * page below 2^31.  Values read from device memory that lie outside their
+ * range never lead outside a buffer: lengths are clamped to the table's width, a page id outside [0, pages) is
+ * skipped with its tokens.                                                                                     */
+#define SVDP_MAX_NODES 64
+#define SVDP_MAX_REQUESTS 4096
+
+/* K and V of the cached tokens, all layers.  With e = 16 bytes / element size, V holds e tokens of a channel side by
+ * side: what a lane of the matrix cores multiplies the weights of e tokens with is then one 16-byte load.        */
+typedef struct svdp_kv_cache {
+    int32_t layers, pages, page, heads, dim;
+    int32_t dtype;         /* svdp_dtype of K and V, and of q, k, v and out           */
+    void *K;               /* [layers][pages][heads][page][dim], 16-byte aligned      */
+    void *V;               /* [layers][pages][heads][page / e][dim][e], 16-byte aligned */
+} svdp_kv_cache;
+
+/* Attention of every row over its request's cached tokens 0 .. lens[r] and over the nodes that it sees:
+ *   out[t][h] = sum_j softmax_j(scale q[t][h] . k_j[c]) v_j[c],  c = h / (heads_q / heads).
+ * q: device rows of [heads_q][dim], q_stride elements apart; k, v: device rows of [heads][dim], the step's own tokens
+ * (not in the cache), k_stride and v_stride elements apart; the three pointers 16-byte aligned, the strides whole
+ * 16-byte vectors.  lens: device [R] int32.  out: device [T][heads_q][dim] in the cache's type, rows of requests
+ * written (padding and nodes past max_nodes are not).  lse: device [T][heads_q] fp32, nullable: the natural logarithm
+ * of the softmax's denominator (with its maximum), for joining with attention over other tokens.
+ * A row that sees nothing: out 0, lse -inf; so too where every weight is zero (all scores -inf).  Tokens that a row
+ * does not see have no influence on it, NaN and infinities included.  Scores, softmax and sums are fp32; the weights are
+ * rounded to the cache's type for their product with V.
+ * ws: >= svdp_tree_attn_workspace_bytes() (0 for arguments it does not take).                                      */
+size_t svdp_tree_attn_workspace_bytes(const svdp_kv_cache *cache, int32_t heads_q, int32_t R, int32_t max_pages,
+                                      int32_t max_nodes);
+svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void *q, int64_t q_stride, const void *k,
+                           int64_t k_stride, const void *v, int64_t v_stride, const uint64_t *tree, const int32_t *table,
+                           int32_t max_pages, const int32_t *lens, const int32_t *starts, int32_t R, int32_t T,
+                           int32_t max_nodes, int32_t heads_q, float scale, void *out, float *lse, void *ws,
+                           size_t ws_bytes, void *stream);
+
+/* Greedy acceptance.  logits: device rows of [V] in `dtype`, `stride` elements apart (aligned to their elements).
+ * best [T]: the index of a row's largest logit, the lowest one among equals; NaN counts as largest (as it does for
+ * torch.argmax).  tokens: device [T] int32, the drafted tokens.  From node 0, which is always kept, the walk goes to the
+ * lowest node whose parent (the last node before it that it sees) is the current one and whose token is best of the
+ * current one, until there is none.  The sets of `tree` have to be trees: node j sees itself, its parent, and what its parent sees.
+ * keep [T]: a row's place in the branch (0, 1, ...), -1 for a row that is not in it.  counts [R]: length of the branch
+ * (0 for a request without rows).  next [R]: best of the branch's last node, the token that follows it (-1 without rows).
+ * All outputs device int32, fully written.  ws: >= svdp_tree_accept_workspace_bytes() (0 for arguments it does not take). */
+size_t svdp_tree_accept_workspace_bytes(int32_t T, int32_t V, int32_t dtype);
+svdp_status svdp_tree_accept(const void *logits, int64_t stride, int32_t dtype, int32_t V, const int32_t *tokens,
+                             const uint64_t *tree, const int32_t *starts, int32_t R, int32_t T, int32_t max_nodes,
+                             int32_t *keep, int32_t *counts, int32_t *next, int32_t *best, void *ws, size_t ws_bytes,
+                             void *stream);
+
+/* Block tables and slots of a step, from the requests' lengths.  Free pages are the `pool[1]` entries of the ring
+ * ring[pages] from place pool[0] on (cyclic).  add[r] >= 0: request r, of lens[r] tokens, takes the pages that add[r] more need, in the
+ * order of the requests, from the ring's front, and its new entries of `table` are written.  add[r] = -1: the
+ * request ends, its pages go to the ring's end in the order of the requests and of its table row (they are free from
+ * the next call on).  A request whose pages would not fit the table, or are not there after those of the requests before
+ * it, is refused: refused[r] = 1 (else 0), its length stays, its rows get no slots (nor do those after it, unless they need no page).
+ * lens_out [R] int32: the lengths after the step.  pool_out [2]: place and number of the free pages after it.
+ * keep: device [T], the place of row t among its request's added tokens, -1 for a row that is not added (as
+ * svdp_tree_accept writes it); NULL: row starts[r] + i has place i.  slots: device [T] 64-bit, the slot of each row, -1 where it has none.
+ * table and ring are changed in place; pool_out and lens_out must not overlap the inputs.  Every other array is device int32.
+ * A repeated call with the same inputs writes the same values.                                                        */
+svdp_status svdp_kv_plan(int32_t *table, int32_t max_pages, int32_t *ring, int32_t pages, int32_t page, const int32_t *pool,
+                         const int32_t *lens, const int32_t *add, const int32_t *starts, const int32_t *keep, int32_t R,
+                         int32_t T, int64_t *slots, int32_t *lens_out, int32_t *pool_out, int32_t *refused, void *stream);
+
+/* K and V of new tokens into their slots, all layers: k, v: device, row t of layer l is [heads][dim] at
+ * l * layer_stride + t * row_stride elements (whole 16-byte vectors, pointers 16-byte aligned).  slots: device [T]; a
+ * slot outside [0, pages * page) is skipped, no two rows may have the same one.                                       */
+svdp_status svdp_kv_commit(const svdp_kv_cache *cache, const void *k, int64_t k_layer_stride, int64_t k_row_stride,
+                           const void *v, int64_t v_layer_stride, int64_t v_row_stride, const int64_t *slots, int32_t T,
+                           void *stream);
+
 /* Static string for a status code.  Never NULL. */
 const char *svdp_status_string(svdp_status st);
 

@@ -20,6 +20,8 @@ SVDP_F32, SVDP_BF16 = 0, 1
 FLAG_DRELU, FLAG_REVALIDATE, FLAG_ENGINE_VECTOR, FLAG_ENGINE_MATRIX = 1, 2, 4, 8
 MAX_BATCH = 8
 STATIC_SCRATCH_BYTES = 8 << 20
+MAX_NODES = 64
+MAX_REQUESTS = 4096
 
 EXPORTS = [
     "svdp_workspace_bytes", "svdp_predict", "svdp_compact", "svdp_sparse_ffn", "svdp_dense_ffn",
@@ -27,6 +29,8 @@ EXPORTS = [
     "svdp_active_rows", "svdp_calib_workspace_bytes", "svdp_calib_need", "svdp_calib_bias",
     "svdp_calib_stats_workspace_bytes", "svdp_calib_stats", "svdp_ffn_step_glued",
     "svdp_whiten_workspace_bytes", "svdp_whiten_factors",
+    "svdp_tree_attn_workspace_bytes", "svdp_tree_attn", "svdp_tree_accept_workspace_bytes", "svdp_tree_accept",
+    "svdp_kv_plan", "svdp_kv_commit",
 ]
 
 
@@ -40,6 +44,13 @@ class svdp_layer(ctypes.Structure):
         ("P", ctypes.c_void_p), ("Q", ctypes.c_void_p), ("b", ctypes.c_void_p),
         ("W_gate", ctypes.c_void_p), ("W_up", ctypes.c_void_p), ("W_downT", ctypes.c_void_p),
         ("flags", ctypes.c_uint32),
+    ]
+
+
+class svdp_kv_cache(ctypes.Structure):
+    _fields_ = [
+        ("layers", ctypes.c_int32), ("pages", ctypes.c_int32), ("page", ctypes.c_int32), ("heads", ctypes.c_int32),
+        ("dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p),
     ]
 
 
@@ -92,6 +103,20 @@ def lib() -> ctypes.CDLL:
     L.svdp_whiten_factors.restype = ctypes.c_int
     L.svdp_ffn_step_glued.argtypes = [lp, vp, vp, vp, ctypes.c_float, vp, i32, vp, vp, vp, vp, vp, sz, vp]
     L.svdp_ffn_step_glued.restype = ctypes.c_int
+    cp, i64 = ctypes.POINTER(svdp_kv_cache), ctypes.c_int64
+    L.svdp_tree_attn_workspace_bytes.argtypes = [cp, i32, i32, i32, i32]
+    L.svdp_tree_attn_workspace_bytes.restype = sz
+    L.svdp_tree_attn.argtypes = [cp, i32, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, vp, i32, i32, i32, i32,
+                                 ctypes.c_float, vp, vp, vp, sz, vp]
+    L.svdp_tree_attn.restype = ctypes.c_int
+    L.svdp_tree_accept_workspace_bytes.argtypes = [i32, i32, i32]
+    L.svdp_tree_accept_workspace_bytes.restype = sz
+    L.svdp_tree_accept.argtypes = [vp, i64, i32, i32, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.svdp_tree_accept.restype = ctypes.c_int
+    L.svdp_kv_plan.argtypes = [vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+    L.svdp_kv_plan.restype = ctypes.c_int
+    L.svdp_kv_commit.argtypes = [cp, vp, i64, i64, vp, i64, i64, vp, i32, vp]
+    L.svdp_kv_commit.restype = ctypes.c_int
     _lib = L
     return L
 
@@ -359,6 +384,162 @@ def whiten_factors(W_gate: torch.Tensor, X: torch.Tensor, r: int):
     _check(lib().svdp_whiten_factors(_ptr(W_gate), _ptr(X), d, D, T, int(r), dt, _ptr(P), _ptr(Q), sigma, sweeps,
                                      _ptr(ws), ws.numel(), _stream()), "svdp_whiten_factors")
     return P, Q, np.array(sigma[:], dtype=np.float32), (int(sweeps[0]), int(sweeps[1]))
+
+
+# ---- decoding with drafted tokens -----------------------------------------------------------------------------------
+
+
+class KVCache:
+    """K and V of the cached tokens of every layer, in pages: owns the tensors and the C struct that points at them.
+
+    K [layers][pages][heads][page][dim]; V [layers][pages][heads][page / e][dim][e], e = 8 (bfloat16) or 4 (float32)
+    tokens of a channel side by side."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor):
+        if K.dtype not in (torch.float32, torch.bfloat16) or V.dtype != K.dtype:
+            raise SvdpError(f"unsupported cache dtypes {K.dtype}, {V.dtype}")
+        if K.dim() != 5 or not all(t.is_cuda and t.is_contiguous() for t in (K, V)):
+            raise SvdpError("K, V: expected contiguous device tensors, K of five dimensions")
+        self.layers, self.pages, self.heads, self.page, self.dim = K.shape
+        e = 16 // K.element_size()
+        if tuple(V.shape) != (self.layers, self.pages, self.heads, self.page // e, self.dim, e):
+            raise SvdpError(f"V: shape {tuple(V.shape)} does not go with K's {tuple(K.shape)}")
+        self.K, self.V, self.dtype = K, V, K.dtype
+        self.c = svdp_kv_cache(self.layers, self.pages, self.page, self.heads, self.dim,
+                               SVDP_BF16 if K.dtype == torch.bfloat16 else SVDP_F32, K.data_ptr(), V.data_ptr())
+
+    @classmethod
+    def empty(cls, layers: int, pages: int, page: int, heads: int, dim: int, dtype=torch.bfloat16, device="cuda") -> "KVCache":
+        e = 16 // torch.empty(0, dtype=dtype).element_size()
+        return cls(torch.empty((layers, pages, heads, page, dim), dtype=dtype, device=device),
+                   torch.empty((layers, pages, heads, page // e, dim, e), dtype=dtype, device=device))
+
+
+def _typed(t: Optional[torch.Tensor], dtype, what: str, shape=None) -> Optional[int]:
+    """Address of a contiguous device tensor of one type (and shape); None stays None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise SvdpError(f"{what}: expected a contiguous device tensor of {dtype}"
+                        f"{'' if shape is None else ' ' + str(tuple(shape))}, got {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
+
+
+def _heads_rows(t: torch.Tensor, cache: KVCache, heads: Optional[int], what: str) -> int:
+    """Stride of the rows [heads][dim] of q, k or v (a slice of a wider projection is fine)."""
+    if (t.dim() != 3 or t.dtype != cache.dtype or not t.is_cuda or t.shape[2] != cache.dim or
+            (heads is not None and t.shape[1] != heads)):
+        raise SvdpError(f"{what}: expected [rows][{'heads' if heads is None else heads}][{cache.dim}] of {cache.dtype} on the "
+                        f"device, got {tuple(t.shape)} {t.dtype}")
+    row, head, one = t.stride()
+    if t.shape[0] and (one != 1 or (head != cache.dim and t.shape[1] > 1)):
+        raise SvdpError(f"{what}: the heads of a row have to lie side by side")
+    # one row: its stride says nothing
+    return row if t.shape[0] > 1 else t.shape[1] * cache.dim
+
+
+def tree_attn_workspace_bytes(cache: KVCache, heads_q: int, R: int, max_pages: int, max_nodes: int = MAX_NODES) -> int:
+    n = lib().svdp_tree_attn_workspace_bytes(ctypes.byref(cache.c), heads_q, R, max_pages, max_nodes)
+    if n == 0:
+        raise SvdpError("svdp_tree_attn_workspace_bytes: unsupported cache, heads or sizes")
+    return int(n)
+
+
+def tree_attn(cache: KVCache, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor,
+              lens: torch.Tensor, starts: torch.Tensor, tree: Optional[torch.Tensor] = None,
+              max_nodes: Optional[int] = None, scale: Optional[float] = None, want_lse: bool = False,
+              out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """Attention of each request's new rows over its pages and over the rows of its tree that each one sees.
+
+    q [T][heads_q][dim], k, v [T][heads][dim] (rows may be slices of a wider projection); table [R][max_pages], lens [R],
+    starts [R + 1] int32; tree [T] int64 (bit j: the row sees node j of its request; None: the nodes up to itself).
+    max_nodes: the most rows a request has (default: T, at most 64).  scale: default dim ** -0.5.
+    Returns out [T][heads_q][dim] (and lse [T][heads_q] fp32 with want_lse)."""
+    T, R, heads_q = q.shape[0], lens.numel(), q.shape[1]
+    if k.shape[0] != T or v.shape[0] != T or table.dim() != 2 or table.shape[0] != R or starts.numel() != R + 1:
+        raise SvdpError(f"svdp_tree_attn: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, table "
+                        f"{tuple(table.shape)}, lens [{R}] and starts [{starts.numel()}] do not go together")
+    qs, ks, vs = (_heads_rows(q, cache, None, "q"), _heads_rows(k, cache, cache.heads, "k"),
+                  _heads_rows(v, cache, cache.heads, "v"))
+    max_pages = table.shape[1]
+    max_nodes = max(1, min(T, MAX_NODES)) if max_nodes is None else int(max_nodes)
+    if out is None:
+        out = torch.empty((T, heads_q, cache.dim), dtype=cache.dtype, device=q.device)
+    if want_lse and lse is None:
+        lse = torch.empty((T, heads_q), dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = torch.empty(tree_attn_workspace_bytes(cache, heads_q, R, max_pages, max_nodes), dtype=torch.uint8, device=q.device)
+    i32 = torch.int32
+    _check(lib().svdp_tree_attn(
+        ctypes.byref(cache.c), layer, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+        _typed(tree, torch.int64, "tree", (T,)), _typed(table, i32, "table"), max_pages, _typed(lens, i32, "lens"),
+        _typed(starts, i32, "starts"), R, T, max_nodes, heads_q, cache.dim ** -0.5 if scale is None else scale,
+        _typed(out, cache.dtype, "out", (T, heads_q, cache.dim)), _typed(lse, torch.float32, "lse", (T, heads_q)), _ptr(ws),
+        ws.numel(), _stream()), "svdp_tree_attn")
+    return (out, lse) if want_lse else out
+
+
+def tree_accept(logits: torch.Tensor, tokens: torch.Tensor, starts: torch.Tensor, tree: Optional[torch.Tensor] = None,
+                max_nodes: Optional[int] = None, ws: Optional[torch.Tensor] = None):
+    """Greedy acceptance of drafted tokens: logits [T][V] (rows may be strided), tokens [T], starts [R + 1] int32,
+    tree [T] int64 or None (chains).  Returns (keep [T], counts [R], next [R], best [T]), all int32."""
+    if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or not logits.is_cuda or logits.stride(1) != 1:
+        raise SvdpError(f"logits: expected [T][V] of float32 or bfloat16 on the device, got {tuple(logits.shape)} {logits.dtype}")
+    T, V = logits.shape
+    R = starts.numel() - 1
+    dt = SVDP_BF16 if logits.dtype == torch.bfloat16 else SVDP_F32
+    max_nodes = max(1, min(T, MAX_NODES)) if max_nodes is None else int(max_nodes)
+    nbytes = lib().svdp_tree_accept_workspace_bytes(T, V, dt)
+    if nbytes == 0:
+        raise SvdpError(f"svdp_tree_accept: unsupported sizes T={T} V={V}")
+    if ws is None:
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
+    made = torch.empty(2 * T + 2 * max(R, 0), dtype=torch.int32, device=logits.device)
+    keep, best, counts, following = made.split((T, T, max(R, 0), max(R, 0)))
+    _check(lib().svdp_tree_accept(
+        logits.data_ptr(), logits.stride(0) if T > 1 else V, dt, V, _typed(tokens, torch.int32, "tokens", (T,)),
+        _typed(tree, torch.int64, "tree", (T,)), _typed(starts, torch.int32, "starts"), R, T, max_nodes, keep.data_ptr(),
+        counts.data_ptr(), following.data_ptr(), best.data_ptr(), _ptr(ws), ws.numel(), _stream()), "svdp_tree_accept")
+    return keep, counts, following, best
+
+
+def kv_plan(table: torch.Tensor, ring: torch.Tensor, pool: torch.Tensor, lens: torch.Tensor, add: torch.Tensor,
+            starts: torch.Tensor, page: int, keep: Optional[torch.Tensor] = None, rows: Optional[int] = None):
+    """Pages for add[r] more tokens of each request (-1: the request ends, its pages are free again), and the rows' slots.
+
+    table [R][max_pages] and ring [pages] are changed in place; pool [2], lens, add [R], starts [R + 1], keep [T] are read,
+    all int32.  keep: as tree_accept returns it; None: every row is kept, ``rows`` of them.
+    Returns (slots [T] int64, lens [R], pool [2], refused [R])."""
+    R = lens.numel()
+    if table.dim() != 2 or table.shape[0] != R or add.numel() != R or starts.numel() != R + 1 or pool.numel() != 2:
+        raise SvdpError(f"svdp_kv_plan: table {tuple(table.shape)}, lens [{R}], add [{add.numel()}], starts [{starts.numel()}] "
+                        f"and pool [{pool.numel()}] do not go together")
+    if keep is None and rows is None:
+        raise SvdpError("svdp_kv_plan: without keep the number of rows has to be given")
+    T = keep.numel() if keep is not None else int(rows)
+    slots = torch.empty(T, dtype=torch.int64, device=lens.device)
+    lens_out, refused, pool_out = torch.empty(2 * R + 2, dtype=torch.int32, device=lens.device).split((R, R, 2))
+    i32 = torch.int32
+    _check(lib().svdp_kv_plan(
+        _typed(table, i32, "table"), table.shape[1], _typed(ring, i32, "ring"), ring.numel(), int(page), _typed(pool, i32, "pool"),
+        _typed(lens, i32, "lens"), _typed(add, i32, "add"), _typed(starts, i32, "starts"), _typed(keep, i32, "keep"), R, T,
+        slots.data_ptr(), lens_out.data_ptr(), pool_out.data_ptr(), refused.data_ptr(), _stream()), "svdp_kv_plan")
+    return slots, lens_out, pool_out, refused
+
+
+def kv_commit(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """K and V of new rows, k, v [layers][T][heads][dim], into the cache at slots [T] (int64; negative: not stored)."""
+    shape = (cache.layers, slots.numel(), cache.heads, cache.dim)
+    for what, t in (("k", k), ("v", v)):
+        if (t.shape != shape or t.dtype != cache.dtype or not t.is_cuda or
+                (t.numel() and (t.stride(3) != 1 or (cache.heads > 1 and t.stride(2) != cache.dim)))):
+            raise SvdpError(f"{what}: expected {shape} of {cache.dtype} on the device, heads side by side, got {tuple(t.shape)} "
+                            f"{t.dtype}")
+    T, row = slots.numel(), cache.heads * cache.dim
+    # a dimension of one entry: its stride says nothing
+    steps = lambda t: (t.stride(0) if cache.layers > 1 else 0, t.stride(1) if T > 1 else row)
+    _check(lib().svdp_kv_commit(ctypes.byref(cache.c), k.data_ptr(), *steps(k), v.data_ptr(), *steps(v),
+                                _typed(slots, torch.int64, "slots"), T, _stream()), "svdp_kv_commit")
 
 
 def version() -> str:

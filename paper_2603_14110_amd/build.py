@@ -8,8 +8,9 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "svdp.hip")
-# every file the translation unit includes, and this one with the compiler's options: the library is rebuilt when any of them is newer
-DEPS = [os.path.abspath(__file__), SRC, os.path.join(os.path.dirname(HERE), "include", "svdp.h")] + sorted(glob.glob(os.path.join(HERE, "csrc", "*.h")))
+DRAFT_SRC = os.path.join(HERE, "csrc", "svdp_draft.hip")
+# every file the translation units include, and this one with the compiler's options: the library is rebuilt when any of them is newer
+DEPS = [os.path.abspath(__file__), SRC, DRAFT_SRC, os.path.join(os.path.dirname(HERE), "include", "svdp.h")] + sorted(glob.glob(os.path.join(HERE, "csrc", "*.h")))
 LIB = os.path.join(HERE, "libsvdp.so")
 # a matrix product that the device refused must not go unnoticed ([[nodiscard]])
 WARNINGS = ["-Wall", "-Wno-unused-function", "-Werror=unused-result"]
@@ -26,9 +27,9 @@ def hipcc_path() -> str:
     return shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
 
 
-def _hipcc(src: str, out: str, verbose: bool) -> None:
+def _hipcc(src: list, out: str, verbose: bool) -> None:
     cmd = [hipcc_path(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", *PRELOAD, *WARNINGS, "-o", out, src]
+           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", *PRELOAD, *WARNINGS, "-o", out, *src]
     if verbose:
         print(" ".join(cmd))
     subprocess.run(cmd, check=True)
@@ -38,7 +39,7 @@ def build_lib(force: bool = True, verbose: bool = False) -> str:
     """Compile the C-ABI library.  Packed-fp32 instructions are disabled on purpose."""
     if not force and os.path.exists(LIB) and all(os.path.getmtime(LIB) >= os.path.getmtime(p) for p in DEPS):
         return LIB
-    _hipcc(SRC, LIB, verbose)
+    _hipcc([SRC, DRAFT_SRC], LIB, verbose)
     return LIB
 
 
@@ -46,7 +47,7 @@ def build_probe(force: bool = True, verbose: bool = False) -> str:
     """Compile the benchmark's measurement helpers (include/svdp_probe.h)."""
     if not force and os.path.exists(PROBE_LIB) and all(os.path.getmtime(PROBE_LIB) >= os.path.getmtime(p) for p in PROBE_DEPS):
         return PROBE_LIB
-    _hipcc(PROBE_SRC, PROBE_LIB, verbose)
+    _hipcc([PROBE_SRC], PROBE_LIB, verbose)
     return PROBE_LIB
 
 

@@ -7,6 +7,8 @@
 
 namespace svdp {
 
+constexpr size_t LDS_MAX = 160 * 1024;    // bytes of LDS of one gfx950 compute unit
+
 // bfloat16 storage element (bit pattern only; all arithmetic is fp32, the
 // "full precision registers, half precision memory" policy of the paper's App. C).
 struct bf16 {

@@ -1,0 +1,250 @@
+// C-ABI entry points of decoding with drafted tokens (see include/svdp.h): host-side validation and kernel launches.  No
+// allocation, no synchronisation, no state kept between calls.
+#include "../../include/svdp.h"
+
+#include <hip/hip_runtime.h>
+
+#include "svdp_draft_kernels.h"
+#include "svdp_host.h"
+#include "svdp_tree_attn.h"
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+namespace {
+
+using namespace svdp;
+
+constexpr int64_t INT_LIMIT = (int64_t)1 << 31;
+
+template <typename T>
+struct Type {
+    using type = T;
+};
+// f(W tag) for a storage type
+template <typename F>
+auto on_type(int dt, F &&f)
+{
+    return dt == SVDP_F32 ? f(Type<float>{}) : f(Type<bf16>{});
+}
+
+inline int bytes_of(int dt) { return dt == SVDP_F32 ? 4 : 2; }
+inline bool aligned_to(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+inline bool whole_vectors(int64_t stride, int dt) { return stride % (16 / bytes_of(dt)) == 0; }
+inline bool good_page(int page) { return page == 32 || page == 64 || page == 128 || page == 256; }
+inline int bits_of(int page) { return page == 32 ? 5 : page == 64 ? 6 : page == 128 ? 7 : 8; }
+inline int tiles(int64_t n, int per) { return (int)((n + per - 1) / per); }
+
+bool overlap(const void *a, size_t an, const void *b, size_t bn)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + bn && y < x + an;
+}
+
+svdp_status check_cache(const svdp_kv_cache *c)
+{
+    if (c == nullptr || c->layers < 1 || c->pages < 1 || c->heads < 1) return SVDP_ERR_INVALID_ARG;
+    if (c->dtype != SVDP_F32 && c->dtype != SVDP_BF16) return SVDP_ERR_UNSUPPORTED;
+    if (!good_page(c->page) || (c->dim != 64 && c->dim != 128 && c->dim != 256)) return SVDP_ERR_UNSUPPORTED;
+    if ((int64_t)c->pages * c->page >= INT_LIMIT || c->heads > 65535 || c->layers > 65535) return SVDP_ERR_UNSUPPORTED;
+    return SVDP_OK;
+}
+svdp_status check_cache_memory(const svdp_kv_cache *c)
+{
+    if (!c->K || !c->V || !aligned16(c->K) || !aligned16(c->V)) return SVDP_ERR_INVALID_ARG;
+    return SVDP_OK;
+}
+svdp_status check_requests(int R, int T, int max_nodes)
+{
+    if (R < 1 || T < 0 || max_nodes < 1) return SVDP_ERR_INVALID_ARG;
+    if (R > SVDP_MAX_REQUESTS || max_nodes > SVDP_MAX_NODES) return SVDP_ERR_UNSUPPORTED;
+    return SVDP_OK;
+}
+svdp_status check_table(int R, int max_pages, int page)
+{
+    if (max_pages < 1) return SVDP_ERR_INVALID_ARG;
+    if ((int64_t)R * max_pages >= INT_LIMIT || (int64_t)max_pages * page >= INT_LIMIT) return SVDP_ERR_UNSUPPORTED;
+    return SVDP_OK;
+}
+svdp_status check_ws(void *ws, size_t ws_bytes, size_t need)
+{
+    return ws == nullptr || !aligned_to(ws, ALIGN) || ws_bytes < need ? SVDP_ERR_WORKSPACE : SVDP_OK;
+}
+
+// Parts that a row of logits is cut into: about a thousand blocks altogether, each of 8 to 32 KB.
+int best_parts(int T, int V, int dt)
+{
+    const int64_t row = (int64_t)V * bytes_of(dt);
+    const int64_t part = std::min<int64_t>(std::max<int64_t>(row * T / 1024, 8 << 10), 32 << 10);
+    return (int)std::min<int64_t>((row + part - 1) / part, 65535);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t svdp_tree_attn_workspace_bytes(const svdp_kv_cache *cache, int32_t heads_q, int32_t R, int32_t max_pages,
+                                      int32_t max_nodes)
+{
+    if (check_cache(cache) != SVDP_OK || check_requests(R, 0, max_nodes) != SVDP_OK ||
+        check_table(R, max_pages, cache->page) != SVDP_OK || heads_q < 1 || heads_q % cache->heads != 0)
+        return 0;
+    return ALIGN;
+}
+
+svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void *q, int64_t q_stride, const void *k,
+                           int64_t k_stride, const void *v, int64_t v_stride, const uint64_t *tree, const int32_t *table,
+                           int32_t max_pages, const int32_t *lens, const int32_t *starts, int32_t R, int32_t T,
+                           int32_t max_nodes, int32_t heads_q, float scale, void *out, float *lse, void *ws,
+                           size_t ws_bytes, void *stream)
+{
+    svdp_status st = check_cache(cache);
+    if (st == SVDP_OK) st = check_cache_memory(cache);
+    if (st == SVDP_OK) st = check_requests(R, T, max_nodes);
+    if (st == SVDP_OK) st = check_table(R, max_pages, cache->page);
+    if (st != SVDP_OK) return st;
+    const int dt = cache->dtype, dim = cache->dim;
+    if (layer < 0 || layer >= cache->layers || heads_q < 1 || heads_q % cache->heads != 0 || !std::isfinite(scale))
+        return SVDP_ERR_INVALID_ARG;
+    if (heads_q > 65535) return SVDP_ERR_UNSUPPORTED;
+    if (T == 0) return SVDP_OK;
+    if (!q || !k || !v || !out || !table || !lens || !starts || !aligned16(q) || !aligned16(k) || !aligned16(v) ||
+        !aligned16(out) || !aligned_to(table, 4) || !aligned_to(lens, 4) || !aligned_to(starts, 4) ||
+        !aligned_to(tree, 8) || !aligned_to(lse, 4))
+        return SVDP_ERR_INVALID_ARG;
+    if (q_stride < (int64_t)heads_q * dim || k_stride < (int64_t)cache->heads * dim ||
+        v_stride < (int64_t)cache->heads * dim || !whole_vectors(q_stride, dt) || !whole_vectors(k_stride, dt) ||
+        !whole_vectors(v_stride, dt))
+        return SVDP_ERR_INVALID_ARG;
+    st = check_ws(ws, ws_bytes, svdp_tree_attn_workspace_bytes(cache, heads_q, R, max_pages, max_nodes));
+    if (st != SVDP_OK) return st;
+    const size_t layer_bytes = (size_t)cache->pages * cache->heads * cache->page * dim * bytes_of(dt);
+    TreeAttnArgs A{};
+    A.K = static_cast<const char *>(cache->K) + layer * layer_bytes;
+    A.V = static_cast<const char *>(cache->V) + layer * layer_bytes;
+    A.q = q;
+    A.k = k;
+    A.v = v;
+    A.q_stride = q_stride;
+    A.k_stride = k_stride;
+    A.v_stride = v_stride;
+    A.tree = tree;
+    A.table = table;
+    A.lens = lens;
+    A.starts = starts;
+    A.out = out;
+    A.lse = lse;
+    A.scale = scale;
+    A.max_pages = max_pages;
+    A.pages = cache->pages;
+    A.page_bits = bits_of(cache->page);
+    A.heads = cache->heads;
+    A.group = heads_q / cache->heads;
+    A.R = R;
+    A.T = T;
+    A.max_nodes = max_nodes;
+    return on_type(dt, [&](auto wt) {
+        using W = typename decltype(wt)::type;
+        hipStream_t hs = static_cast<hipStream_t>(stream);
+        if (dim == 64) launch(k_tree_attn<W, 64>, dim3(T, heads_q), dim3(64), 0, hs, A);
+        else if (dim == 128) launch(k_tree_attn<W, 128>, dim3(T, heads_q), dim3(64), 0, hs, A);
+        else launch(k_tree_attn<W, 256>, dim3(T, heads_q), dim3(64), 0, hs, A);
+        return hip_status(hipSuccess);
+    });
+}
+
+size_t svdp_tree_accept_workspace_bytes(int32_t T, int32_t V, int32_t dtype)
+{
+    if (T < 0 || V < 1 || (dtype != SVDP_F32 && dtype != SVDP_BF16)) return 0;
+    return std::max(align_up((size_t)T * best_parts(T, V, dtype) * 8), ALIGN);
+}
+
+svdp_status svdp_tree_accept(const void *logits, int64_t stride, int32_t dtype, int32_t V, const int32_t *tokens,
+                             const uint64_t *tree, const int32_t *starts, int32_t R, int32_t T, int32_t max_nodes,
+                             int32_t *keep, int32_t *counts, int32_t *next, int32_t *best, void *ws, size_t ws_bytes,
+                             void *stream)
+{
+    svdp_status st = check_requests(R, T, max_nodes);
+    if (st != SVDP_OK) return st;
+    if (V < 1 || stride < V) return SVDP_ERR_INVALID_ARG;
+    if (dtype != SVDP_F32 && dtype != SVDP_BF16) return SVDP_ERR_UNSUPPORTED;
+    if (V > (1 << 30)) return SVDP_ERR_UNSUPPORTED;
+    if (!starts || !counts || !next || !aligned_to(starts, 4) || !aligned_to(counts, 4) || !aligned_to(next, 4))
+        return SVDP_ERR_INVALID_ARG;
+    if (T > 0 && (!logits || !tokens || !keep || !best || !aligned_to(logits, bytes_of(dtype)) || !aligned_to(tokens, 4) ||
+                  !aligned_to(tree, 8) || !aligned_to(keep, 4) || !aligned_to(best, 4)))
+        return SVDP_ERR_INVALID_ARG;
+    st = check_ws(ws, ws_bytes, svdp_tree_accept_workspace_bytes(T, V, dtype));
+    if (st != SVDP_OK) return st;
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    uint64_t *parts = static_cast<uint64_t *>(ws);
+    const int n_parts = best_parts(T, V, dtype);
+    if (T > 0)
+        on_type(dtype, [&](auto wt) {
+            using W = typename decltype(wt)::type;
+            // one vector more than the row has where it begins between two of them
+            const int per = tiles(tiles(V, Elem<W>::VEC) + 1, n_parts);
+            launch(k_logits_best<W>, dim3(T, n_parts), dim3(BEST_THREADS), 0, hs, static_cast<const W *>(logits), stride, V,
+                   per, parts);
+        });
+    launch(k_tree_walk, dim3(R + 1), dim3(64), 0, hs, parts, n_parts, tokens, tree, starts, R, T, max_nodes, keep, counts,
+           next, best);
+    return hip_status(hipSuccess);
+}
+
+svdp_status svdp_kv_plan(int32_t *table, int32_t max_pages, int32_t *ring, int32_t pages, int32_t page, const int32_t *pool,
+                         const int32_t *lens, const int32_t *add, const int32_t *starts, const int32_t *keep, int32_t R,
+                         int32_t T, int64_t *slots, int32_t *lens_out, int32_t *pool_out, int32_t *refused, void *stream)
+{
+    svdp_status st = check_requests(R, T, 1);
+    if (st != SVDP_OK) return st;
+    if (pages < 1) return SVDP_ERR_INVALID_ARG;
+    if (!good_page(page) || (int64_t)pages * page >= INT_LIMIT) return SVDP_ERR_UNSUPPORTED;
+    st = check_table(R, max_pages, page);
+    if (st != SVDP_OK) return st;
+    const void *words[] = {table, ring, pool, lens, add, starts, lens_out, pool_out, refused};
+    for (const void *p : words)
+        if (p == nullptr || !aligned_to(p, 4)) return SVDP_ERR_INVALID_ARG;
+    if (!aligned_to(keep, 4) || (T > 0 && slots == nullptr) || !aligned_to(slots, 8)) return SVDP_ERR_INVALID_ARG;
+    const size_t rows = (size_t)R * 4;
+    for (const void *o : {static_cast<const void *>(lens_out), static_cast<const void *>(refused)})
+        if (overlap(o, rows, lens, rows) || overlap(o, rows, add, rows) || overlap(o, rows, pool, 8) ||
+            overlap(o, rows, starts, rows + 4))
+            return SVDP_ERR_INVALID_ARG;
+    if (overlap(pool_out, 8, pool, 8) || overlap(pool_out, 8, lens, rows) || overlap(pool_out, 8, add, rows))
+        return SVDP_ERR_INVALID_ARG;
+    const size_t lds = plan_lds(R);
+    if (!grant_lds<k_kv_plan>(lds)) return SVDP_ERR_UNSUPPORTED;
+    const int blocks = std::min(std::max(tiles(T, 2 * PLAN_THREADS), tiles(R, 4 * PLAN_WAVES)), 256);
+    launch(k_kv_plan, dim3(blocks), dim3(PLAN_THREADS), lds, static_cast<hipStream_t>(stream), table, max_pages, ring, pages,
+           bits_of(page), pool, lens, add, starts, keep, R, T, slots, lens_out, pool_out, refused);
+    return hip_status(hipSuccess);
+}
+
+svdp_status svdp_kv_commit(const svdp_kv_cache *cache, const void *k, int64_t k_layer_stride, int64_t k_row_stride,
+                           const void *v, int64_t v_layer_stride, int64_t v_row_stride, const int64_t *slots, int32_t T,
+                           void *stream)
+{
+    svdp_status st = check_cache(cache);
+    if (st == SVDP_OK) st = check_cache_memory(cache);
+    if (st != SVDP_OK) return st;
+    if (T < 0) return SVDP_ERR_INVALID_ARG;
+    if (T == 0) return SVDP_OK;
+    const int dt = cache->dtype;
+    const int64_t row = (int64_t)cache->heads * cache->dim;
+    if (!k || !v || !slots || !aligned16(k) || !aligned16(v) || !aligned_to(slots, 8) || k_row_stride < row ||
+        v_row_stride < row || k_layer_stride < 0 || v_layer_stride < 0 || !whole_vectors(k_row_stride, dt) ||
+        !whole_vectors(v_row_stride, dt) || !whole_vectors(k_layer_stride, dt) || !whole_vectors(v_layer_stride, dt))
+        return SVDP_ERR_INVALID_ARG;
+    return on_type(dt, [&](auto wt) {
+        using W = typename decltype(wt)::type;
+        launch(k_kv_commit<W>, dim3(tiles(T, COMMIT_ROWS), cache->layers), dim3(COMMIT_THREADS), 0,
+               static_cast<hipStream_t>(stream), static_cast<W *>(cache->K), static_cast<W *>(cache->V),
+               static_cast<const W *>(k), k_layer_stride, k_row_stride, static_cast<const W *>(v), v_layer_stride,
+               v_row_stride, slots, T, cache->pages, bits_of(cache->page), cache->heads, cache->dim);
+        return hip_status(hipSuccess);
+    });
+}
+
+}  // extern "C"
