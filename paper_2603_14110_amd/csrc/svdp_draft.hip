@@ -72,6 +72,46 @@ svdp_status check_ws(void *ws, size_t ws_bytes, size_t need)
     return ws == nullptr || !aligned_to(ws, ALIGN) || ws_bytes < need ? SVDP_ERR_WORKSPACE : SVDP_OK;
 }
 
+// Row tiles of attention: 16 NT rows a wave, as many as a request may have, up to what a wave holds in registers.
+struct AttnPlan {
+    int nt, block_bits;
+    size_t bytes;
+};
+AttnPlan attn_plan(int dim, int group, int max_nodes)
+{
+    const int64_t rows = (int64_t)group * max_nodes;
+    AttnPlan p;
+    p.nt = rows <= 16 ? 1 : rows <= 32 || dim == 256 ? 2 : 4;
+    p.block_bits = p.nt * dim <= 256 ? 9 : 8;
+    p.bytes = align_up(((size_t)2 << p.block_bits) * 16 * p.nt * (dim + 2) * 4);
+    return p;
+}
+// Units of the longest request that the table has room for.
+int64_t attn_steps(int max_pages, int page, int max_nodes)
+{
+    const int64_t tiles = (int64_t)max_pages * page / TA_TILE + (max_nodes + TA_TILE - 1) / TA_TILE;
+    return (tiles + TA_WAVES - 1) / TA_WAVES;
+}
+bool attn_units_fit(const svdp_kv_cache *c, int heads_q, int R, int max_pages, int max_nodes, int nt)
+{
+    const int64_t rows = (int64_t)(heads_q / c->heads) * max_nodes;
+    return attn_steps(max_pages, c->page, max_nodes) * ((rows + 16 * nt - 1) / (16 * nt)) * c->heads * R < INT_LIMIT;
+}
+template <typename F>
+void on_attn(int dt, int dim, int nt, F &&f)
+{
+    on_type(dt, [&](auto wt) {
+        const auto on_nt = [&](auto dc) {
+            if (nt == 1) f(wt, dc, std::integral_constant<int, 1>{});
+            else if (nt == 2) f(wt, dc, std::integral_constant<int, 2>{});
+            else if constexpr (decltype(dc)::value <= 128) f(wt, dc, std::integral_constant<int, 4>{});
+        };
+        if (dim == 64) on_nt(std::integral_constant<int, 64>{});
+        else if (dim == 128) on_nt(std::integral_constant<int, 128>{});
+        else on_nt(std::integral_constant<int, 256>{});
+    });
+}
+
 // Parts that a row of logits is cut into: about a thousand blocks altogether, each of 8 to 32 KB.
 int best_parts(int T, int V, int dt)
 {
@@ -90,7 +130,8 @@ size_t svdp_tree_attn_workspace_bytes(const svdp_kv_cache *cache, int32_t heads_
     if (check_cache(cache) != SVDP_OK || check_requests(R, 0, max_nodes) != SVDP_OK ||
         check_table(R, max_pages, cache->page) != SVDP_OK || heads_q < 1 || heads_q % cache->heads != 0)
         return 0;
-    return ALIGN;
+    const AttnPlan plan = attn_plan(cache->dim, heads_q / cache->heads, max_nodes);
+    return attn_units_fit(cache, heads_q, R, max_pages, max_nodes, plan.nt) ? plan.bytes : 0;
 }
 
 svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void *q, int64_t q_stride, const void *k,
@@ -117,7 +158,9 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
         v_stride < (int64_t)cache->heads * dim || !whole_vectors(q_stride, dt) || !whole_vectors(k_stride, dt) ||
         !whole_vectors(v_stride, dt))
         return SVDP_ERR_INVALID_ARG;
-    st = check_ws(ws, ws_bytes, svdp_tree_attn_workspace_bytes(cache, heads_q, R, max_pages, max_nodes));
+    const AttnPlan plan = attn_plan(dim, heads_q / cache->heads, max_nodes);
+    if (!attn_units_fit(cache, heads_q, R, max_pages, max_nodes, plan.nt)) return SVDP_ERR_UNSUPPORTED;
+    st = check_ws(ws, ws_bytes, plan.bytes);
     if (st != SVDP_OK) return st;
     const size_t layer_bytes = (size_t)cache->pages * cache->heads * cache->page * dim * bytes_of(dt);
     TreeAttnArgs A{};
@@ -144,14 +187,18 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     A.R = R;
     A.T = T;
     A.max_nodes = max_nodes;
-    return on_type(dt, [&](auto wt) {
+    A.parts = static_cast<float *>(ws);
+    A.block_bits = plan.block_bits;
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    on_attn(dt, dim, plan.nt, [&](auto wt, auto dc, auto nc) {
         using W = typename decltype(wt)::type;
-        hipStream_t hs = static_cast<hipStream_t>(stream);
-        if (dim == 64) launch(k_tree_attn<W, 64>, dim3(T, heads_q), dim3(64), 0, hs, A);
-        else if (dim == 128) launch(k_tree_attn<W, 128>, dim3(T, heads_q), dim3(64), 0, hs, A);
-        else launch(k_tree_attn<W, 256>, dim3(T, heads_q), dim3(64), 0, hs, A);
-        return hip_status(hipSuccess);
+        constexpr int DIM = decltype(dc)::value, NT = decltype(nc)::value;
+        launch((k_tree_attn<W, DIM, NT>), dim3(1 << plan.block_bits), dim3(TA_THREADS), 0, hs, A);
+        // a request of one unit is never cut
+        if (attn_steps(max_pages, cache->page, max_nodes) > 1)
+            launch((k_tree_join<W, DIM, NT>), dim3(T, heads_q), dim3(TA_THREADS), 0, hs, A);
     });
+    return hip_status(hipSuccess);
 }
 
 size_t svdp_tree_accept_workspace_bytes(int32_t T, int32_t V, int32_t dtype)

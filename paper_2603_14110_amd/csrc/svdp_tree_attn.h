@@ -1,12 +1,38 @@
-// Attention of drafted tokens over paged K and V and over their own tree.
+// Attention of drafted tokens over paged K and V and over their own tree:
+//   out[t][h] = sum_j softmax_j(scale q[t][h] . k_j) v_j
+// over the cached tokens of t's request and the nodes of its tree that t sees.
+//
+// Rows and tiles.  The query heads that share a head of K and V, times the nodes of a request, are the rows of one matrix
+// product: K and V are read once for all of them.  A wave takes tiles of 32 tokens and 16 NT rows, on the matrix cores:
+//   S^T = K Q^T     A operand: tokens x channels, B operand: channels x rows; a lane ends up with 8 scores of ONE row
+//   O^T += V^T P^T  A operand: channels x tokens, B operand: tokens x rows
+// The tokens that a lane's K rows stand for are chosen so that the 8 weights which a lane then holds are the 8 tokens
+// that the second product's B operand wants in that lane: the weights never leave their registers.  V is kept with e tokens of a channel
+// side by side, so its operand is a 16-byte load as well: neither K nor V passes through LDS, and a tile of each is one contiguous
+// piece of memory (8 KB for bf16 and 128 channels).
+//
+// Division of the work.  A unit is four tiles (one a wave).  All units of all requests, heads and row tiles stand in a
+// row, and each block takes an equal piece of it, whatever the requests' lengths are (they are known on the device only).  What a block
+// has of a (request, head, row tile) goes to the output where it is the whole of it, and otherwise, as a sum with its maximum, to
+// the workspace, where k_tree_join puts the parts together.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "svdp_device.h"
 
 namespace svdp {
+
+constexpr int TA_THREADS = 256;
+constexpr int TA_WAVES = TA_THREADS / 64;
+constexpr int TA_TILE = 32;                      // tokens of a tile; divides every page
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+typedef __bf16 ta_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float ta_f32x8 __attribute__((ext_vector_type(8)));
 
 struct TreeAttnArgs {
     const void *K, *V;                  // of the layer
@@ -16,83 +42,535 @@ struct TreeAttnArgs {
     const int32_t *table, *lens, *starts;
     void *out;
     float *lse;
+    float *parts;                       // [2 << block_bits] parts of (dim + 2) floats a row
     float scale;
     int max_pages, pages, page_bits, heads, group, R, T, max_nodes;
+    int block_bits;                     // there are 1 << block_bits blocks
 };
 
-__device__ __forceinline__ float wave_max(float v)
+// One request's share: rows, tiles and units.
+struct TreeSpan {
+    int len, start, n, tiles, steps, row_tiles, units;
+};
+template <int ROWS>
+__device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs &A, int r)
 {
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
-    return v;
+    TreeSpan s;
+    s.len = min(max(A.lens[r], 0), A.max_pages << A.page_bits);
+    s.start = min(max(A.starts[r], 0), A.T);
+    s.n = min(min(max(A.starts[r + 1] - s.start, 0), A.max_nodes), A.T - s.start);
+    s.tiles = (s.len + TA_TILE - 1) / TA_TILE;
+    s.steps = (s.tiles + (s.n + TA_TILE - 1) / TA_TILE + TA_WAVES - 1) / TA_WAVES;
+    s.row_tiles = (s.n * A.group + ROWS - 1) / ROWS;
+    s.units = s.row_tiles * s.steps * A.heads;
+    return s;
 }
 
-// One wave a row and query head: 64 tokens at a time, a lane a token for the scores and a lane every 64th channel for the sum.
-template <typename W, int DIM>
-__global__ __launch_bounds__(64) void k_tree_attn(TreeAttnArgs A)
+__device__ __forceinline__ int lane_of_first(uint64_t ballot) { return __ffsll((unsigned long long)ballot) - 1; }
+
+// Units of all requests; `upto`: the inclusive sums of the first 64, a lane each.
+template <int ROWS>
+__device__ __forceinline__ int tree_units(const TreeAttnArgs &A, int lane, int *own, int *upto)
 {
-    constexpr int E = Elem<W>::VEC, PER = DIM / 64;
-    const int lane = threadIdx.x, t = blockIdx.x, hq = blockIdx.y, h = hq / A.group;
-    int lo = 0, hi = A.R;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (A.starts[mid] <= t) lo = mid;
-        else hi = mid - 1;
+    *own = lane < A.R ? tree_span<ROWS>(A, lane).units : 0;
+    *upto = wave_inclusive_scan(*own);
+    int all = __builtin_amdgcn_readlane(*upto, 63);
+    for (int c = 64; c < A.R; c += 64) {
+        const int u = c + lane < A.R ? tree_span<ROWS>(A, c + lane).units : 0;
+        all += __builtin_amdgcn_readlane(wave_inclusive_scan(u), 63);
     }
-    if (lo >= A.R) return;
-    const int a = max(A.starts[lo], 0), n = min(min(A.starts[lo + 1], A.T) - a, A.max_nodes), node = t - a;
-    if (node < 0 || node >= n) return;
-    const int page = 1 << A.page_bits, len = min(max(A.lens[lo], 0), A.max_pages << A.page_bits);
-    const int heads_q = A.heads * A.group;
-    const W *q = static_cast<const W *>(A.q) + t * A.q_stride + (int64_t)hq * DIM;
-    const W *K = static_cast<const W *>(A.K), *V = static_cast<const W *>(A.V);
-    const int32_t *table = A.table + (size_t)lo * A.max_pages;
-    const uint64_t sees = A.tree != nullptr ? A.tree[t] : ~0ull >> (63 - node);
-    float top = -INFINITY, total = 0.f, acc[PER] = {};
-    for (int at = 0; at < len + n; at += 64) {
-        const int j = at + lane;
-        const W *key = nullptr, *value = nullptr;
-        int64_t value_step = 0;
-        if (j < len) {
-            const int id = table[j >> A.page_bits];
-            if (id >= 0 && id < A.pages) {
-                const int place = j & (page - 1);
-                const int64_t base = (((int64_t)id * A.heads + h) << A.page_bits) * DIM;
-                key = K + base + (int64_t)place * DIM;
-                value = V + base + (int64_t)(place / E) * DIM * E + (place & (E - 1));
-                value_step = E;
+    return all;
+}
+
+// The unit where block b begins: an equal share for each, or one unit each for the first blocks.  No block in between has none.
+__device__ __forceinline__ int tree_begin(int b, int units, int bits)
+{
+    return units >> bits == 0 ? min(b, units) : (int)(((int64_t)b * units) >> bits);
+}
+// The block that has unit u: the first one whose successor begins behind u.
+__device__ __forceinline__ int tree_block_of(int u, int units, int bits)
+{
+    return units >> bits == 0 ? u : (int)(((((int64_t)u + 1) << bits) + units - 1) / units) - 1;
+}
+
+// ---- operands, by storage type --------------------------------------------------------------------------------------------
+// Lane = 16 g + m.  KEY(t, m): the token of a tile whose K row m of the t-th product comes from; the result's rows 4 g + i lie
+// in lane group g, so that this lane group ends up with the tokens KEY(t, 4 g + i), which are those it has of V below.
+template <typename W, int DIM>
+struct TreeTile;
+
+template <int DIM>
+struct TreeTile<bf16, DIM> {
+    static constexpr int E = 8, KC = DIM / 32, VT = 1;
+    static __device__ __forceinline__ int key(int t, int m) { return (m >> 2) * 8 + (m & 3) + 4 * t; }
+    static __device__ __forceinline__ int pack(int, int g) { return g; }          // of 8 tokens
+    static __device__ __forceinline__ f32x4_t score(const uint4 &k, const uint4 &q, f32x4_t s)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ta_bf16x8, k), __builtin_bit_cast(ta_bf16x8, q), s, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x4_t sum(const uint4 (&v)[1], const float (&p)[8], f32x4_t o)
+    {
+        const ta_f32x8 w = {p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]};
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ta_bf16x8, v[0]), __builtin_convertvector(w, ta_bf16x8), o, 0, 0, 0);
+    }
+    static __device__ __forceinline__ bool finite(const uint4 &v)
+    {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        bool ok = true;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ok = ok && (w[i] & 0x7f80u) != 0x7f80u && (w[i] & 0x7f800000u) != 0x7f800000u;
+        return ok;
+    }
+    // the first n of 8 tokens, zeros behind them
+    static __device__ __forceinline__ uint4 first(const uint4 &v, int n)
+    {
+        const auto keep = [&](uint32_t w, int at) { return n >= at + 2 ? w : n == at + 1 ? w & 0xffffu : 0u; };
+        return make_uint4(keep(v.x, 0), keep(v.y, 2), keep(v.z, 4), keep(v.w, 6));
+    }
+};
+
+template <int DIM>
+struct TreeTile<float, DIM> {
+    static constexpr int E = 4, KC = DIM / 16, VT = 2;
+    static __device__ __forceinline__ int key(int t, int m) { return 16 * t + m; }
+    static __device__ __forceinline__ int pack(int t, int g) { return 4 * t + g; } // of 4 tokens
+    static __device__ __forceinline__ f32x4_t score(const uint4 &k, const uint4 &q, f32x4_t s)
+    {
+        const float4 a = as_float4(k), b = as_float4(q);
+        s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x, b.x, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.y, b.y, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.z, b.z, s, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x4f32(a.w, b.w, s, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x4_t sum(const uint4 (&v)[2], const float (&p)[8], f32x4_t o)
+    {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const float4 a = as_float4(v[t]);
+            o = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x, p[4 * t], o, 0, 0, 0);
+            o = __builtin_amdgcn_mfma_f32_16x16x4f32(a.y, p[4 * t + 1], o, 0, 0, 0);
+            o = __builtin_amdgcn_mfma_f32_16x16x4f32(a.z, p[4 * t + 2], o, 0, 0, 0);
+            o = __builtin_amdgcn_mfma_f32_16x16x4f32(a.w, p[4 * t + 3], o, 0, 0, 0);
+        }
+        return o;
+    }
+    static __device__ __forceinline__ bool finite(const uint4 &v)
+    {
+        return (v.x & 0x7f800000u) != 0x7f800000u && (v.y & 0x7f800000u) != 0x7f800000u && (v.z & 0x7f800000u) != 0x7f800000u &&
+               (v.w & 0x7f800000u) != 0x7f800000u;
+    }
+    static __device__ __forceinline__ uint4 first(const uint4 &v, int n)
+    {
+        return make_uint4(n > 0 ? v.x : 0u, n > 1 ? v.y : 0u, n > 2 ? v.z : 0u, n > 3 ? v.w : 0u);
+    }
+};
+
+__device__ __forceinline__ float max_xor16(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_xor32(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+// what exponents are taken relative to: a maximum of -inf (nothing but zero weights so far) must not make -inf - -inf
+__device__ __forceinline__ float shift_of(float top) { return top == -INFINITY ? 0.f : top; }
+
+// What a wave has of its rows: the sum O^T (channels 16 dt + 4 g + i of row m), the maximum of the scores in base two and the lane
+// group's part of the denominator.
+template <typename W, int DIM, int NT>
+struct TreeWave {
+    using X = TreeTile<W, DIM>;
+    static constexpr int DT = DIM / 16;
+    f32x4_t o[DT][NT];
+    float top[NT], total[NT];
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            top[nt] = -INFINITY;
+            total[nt] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[dt][nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    // scores in base two -> weights; earlier sums come down to the new maximum
+    __device__ __forceinline__ void weights(float (&z)[NT][8])
+    {
+        float next[NT];
+        bool grew = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float t = fmaxf(fmaxf(fmaxf(z[nt][0], z[nt][1]), fmaxf(z[nt][2], z[nt][3])),
+                            fmaxf(fmaxf(z[nt][4], z[nt][5]), fmaxf(z[nt][6], z[nt][7])));
+            next[nt] = fmaxf(top[nt], max_xor32(max_xor16(t)));
+            grew = grew || next[nt] > top[nt];
+        }
+        if (__any(grew)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float old = exp2_fast(top[nt] - shift_of(next[nt]));
+                top[nt] = next[nt];
+                total[nt] *= old;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[dt][nt] *= old;
             }
-        } else if (j < len + n && ((sees >> (j - len)) & 1)) {
-            key = static_cast<const W *>(A.k) + (a + j - len) * A.k_stride + (int64_t)h * DIM;
-            value = static_cast<const W *>(A.v) + (a + j - len) * A.v_stride + (int64_t)h * DIM;
-            value_step = 1;
         }
-        float s = -INFINITY;
-        if (key != nullptr) {
-            s = 0.f;
-            for (int c = 0; c < DIM; ++c) s = fmaf(to_f32(q[c]), to_f32(key[c]), s);
-            s *= A.scale;
-        }
-        const float next = fmaxf(top, wave_max(s)), shift = next == -INFINITY ? 0.f : next;
-        const float p = key != nullptr ? __expf(s - shift) : 0.f, old = __expf(top - shift);
-        top = next;
-        total = total * old + wave_sum(p);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) acc[i] *= old;
-        for (int o = 0; o < 64; ++o) {
-            const W *from = reinterpret_cast<const W *>(__shfl((unsigned long long)(uintptr_t)value, o));
-            const int64_t step = __shfl(value_step, o);
-            const float w = __shfl(p, o);
-            if (from == nullptr) continue;
+        for (int nt = 0; nt < NT; ++nt) {
+            const float shift = shift_of(top[nt]);
 #pragma unroll
-            for (int i = 0; i < PER; ++i) acc[i] = fmaf(w, to_f32(from[(lane + 64 * i) * step]), acc[i]);
+            for (int i = 0; i < 8; ++i) {
+                z[nt][i] = exp2_fast(z[nt][i] - shift);
+                total[nt] += z[nt][i];
+            }
         }
     }
-    W *out = static_cast<W *>(A.out) + ((int64_t)t * heads_q + hq) * DIM;
+};
+
+// One block: its piece of the row of units, a segment (what it has of one request, head and row tile) after the other.
+template <typename W, int DIM, int NT>
+__global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
+{
+    using X = TreeTile<W, DIM>;
+    constexpr int ROWS = 16 * NT, E = X::E, KC = X::KC, VT = X::VT, DT = DIM / 16;
+    constexpr int DC = DIM * NT <= 128 ? DIM : 128 / NT;          // channels that the waves' sums meet in LDS by: 32 KB
+    __shared__ float s_top[TA_WAVES][ROWS], s_total[TA_WAVES][ROWS];
+    __shared__ __align__(16) float s_sum[TA_WAVES][ROWS][DC + 4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, m = lane & 15;
+    const int heads_q = A.heads * A.group;
+
+    int own, upto;
+    const int units = tree_units<ROWS>(A, lane, &own, &upto);
+    int u = tree_begin(blockIdx.x, units, A.block_bits);
+    const int u1 = tree_begin(blockIdx.x + 1, units, A.block_bits);
+    if (u >= u1) return;
+    // the request that unit u belongs to, and the units in front of that request
+    int r = 0, rem = 0;
+    for (int c = 0, base = 0;; c += 64) {
+        if (c > 0) {
+            own = c + lane < A.R ? tree_span<ROWS>(A, c + lane).units : 0;
+            upto = wave_inclusive_scan(own);
+        }
+        const uint64_t behind = __ballot(base + upto > u);
+        if (behind != 0) {
+            const int l = lane_of_first(behind);
+            r = c + l;
+            rem = u - base - __builtin_amdgcn_readlane(upto, l) + __builtin_amdgcn_readlane(own, l);
+            break;
+        }
+        base += __builtin_amdgcn_readlane(upto, 63);
+    }
+
+    for (bool first = true; u < u1; ++r, rem = 0) {
+        const TreeSpan S = tree_span<ROWS>(A, __builtin_amdgcn_readfirstlane(r));
+        if (S.units == 0) continue;
+        const int32_t *table = A.table + (size_t)r * A.max_pages;
+        int task = rem / S.steps, s0 = rem - task * S.steps;
+        for (; task < A.heads * S.row_tiles && u < u1; ++task, s0 = 0, first = false) {
+            const int s1 = min(S.steps, s0 + u1 - u);
+            const int h = task / S.row_tiles, row0 = (task - h * S.row_tiles) * ROWS, rows = S.n * A.group;
+            const bool whole = s0 == 0 && s1 == S.steps;
+
+            // Q of the rows (a row past the last one repeats it: computed and never written)
+            uint4 q[KC][NT];
+            uint64_t sees[NT];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) from_f32(total == 0.f ? 0.f : acc[i] / total, out + lane + 64 * i);
-    if (A.lse != nullptr && lane == 0)
-        A.lse[(int64_t)t * heads_q + hq] = total == 0.f ? -INFINITY : top + logf(total);
+            for (int nt = 0; nt < NT; ++nt) {
+                const int row = min(row0 + 16 * nt + m, rows - 1), node = row / A.group, head = h * A.group + row - node * A.group;
+                const W *from = static_cast<const W *>(A.q) + (S.start + node) * A.q_stride + (int64_t)head * DIM + g * E;
+#pragma unroll
+                for (int c = 0; c < KC; ++c) q[c][nt] = load_raw(from + c * 4 * E);
+                sees[nt] = A.tree != nullptr ? A.tree[S.start + node] : ~0ull >> (63 - node);
+            }
+            TreeWave<W, DIM, NT> mine;
+            mine.clear();
+
+            const auto scores = [&](const uint4 (&k)[2][KC], float (&z)[NT][8]) {
+                const float to_log2 = A.scale * LOG2E;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int c = 0; c < KC; ++c) s = X::score(k[t][c], q[c][nt], s);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) z[nt][4 * t + i] = s[i] * to_log2;
+                    }
+            };
+            const auto add = [&](const uint4 (&v)[DT][VT], const float (&p)[NT][8]) {
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mine.o[dt][nt] = X::sum(v[dt], p[nt], mine.o[dt][nt]);
+            };
+
+            // cached tokens: K of the next tile is requested when this one's has been used, and so is V
+            int i = s0 * TA_WAVES + wave;
+            const int i_end = min(s1 * TA_WAVES, S.tiles), per_page = A.page_bits - 5;
+            if (i < i_end) {
+                const auto page_of = [&](int tile) { return table[min(tile, S.tiles - 1) >> per_page]; };
+                const auto real = [&](int id) { return (uint32_t)id < (uint32_t)A.pages; };
+                const auto tile_at = [&](int tile, int id) {
+                    const int64_t page = (int64_t)(real(id) ? id : 0) * A.heads + h;
+                    return (((page << per_page) + (tile & ((1 << per_page) - 1))) * TA_TILE) * DIM;
+                };
+                uint4 k[2][KC], v[DT][VT];
+                const auto load_k = [&](int64_t at) {
+                    const W *from = static_cast<const W *>(A.K) + at;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int c = 0; c < KC; ++c) k[t][c] = load_raw(from + X::key(t, m) * DIM + (4 * c + g) * E);
+                };
+                const auto load_v = [&](int64_t at) {
+                    const W *from = static_cast<const W *>(A.V) + at;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int t = 0; t < VT; ++t) v[dt][t] = load_raw(from + (X::pack(t, g) * DIM + dt * 16 + m) * E);
+                };
+                int id = __builtin_amdgcn_readfirstlane(page_of(i)), id_next = page_of(i + TA_WAVES);
+                load_k(tile_at(i, id));
+                load_v(tile_at(i, id));
+                for (; i < i_end; i += TA_WAVES) {
+                    const int count = real(id) ? min(S.len - i * TA_TILE, TA_TILE) : 0;
+                    id = __builtin_amdgcn_readfirstlane(id_next);
+                    id_next = page_of(i + 2 * TA_WAVES);
+                    const int64_t at = tile_at(min(i + TA_WAVES, S.tiles - 1), id);
+                    float z[NT][8];
+                    scores(k, z);
+                    if (i + TA_WAVES < i_end) load_k(at);
+                    if (count < TA_TILE) {
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+                                    if (X::key(t, 4 * g + j) >= count) z[nt][4 * t + j] = -INFINITY;
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                            for (int t = 0; t < VT; ++t) v[dt][t] = X::first(v[dt][t], count - X::pack(t, g) * E);
+                    }
+                    mine.weights(z);
+                    add(v, z);
+                    if (i + TA_WAVES < i_end) load_v(at);
+                }
+            }
+
+            // the tree's own tokens
+            for (; i < min(s1 * TA_WAVES, S.tiles + (S.n + TA_TILE - 1) / TA_TILE); i += TA_WAVES) {
+                const int node0 = (i - S.tiles) * TA_TILE;
+                const W *key = static_cast<const W *>(A.k) + (int64_t)h * DIM, *value = static_cast<const W *>(A.v) + (int64_t)h * DIM;
+                uint4 k[2][KC], v[DT][VT];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const W *from = key + (S.start + min(node0 + X::key(t, m), S.n - 1)) * A.k_stride + g * E;
+#pragma unroll
+                    for (int c = 0; c < KC; ++c) k[t][c] = load_raw(from + c * 4 * E);
+                }
+                // these rows lie token by token: an operand is put together from its elements
+                bool finite = true;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int t = 0; t < VT; ++t) {
+                        const int node = node0 + X::pack(t, g) * E;
+                        W in[E];
+#pragma unroll
+                        for (int j = 0; j < E; ++j) in[j] = value[(S.start + min(node + j, S.n - 1)) * A.v_stride + dt * 16 + m];
+                        __builtin_memcpy(&v[dt][t], in, 16);
+                        v[dt][t] = X::first(v[dt][t], S.n - node);
+                        finite = finite && X::finite(v[dt][t]);
+                    }
+                float z[NT][8];
+                scores(k, z);
+                uint32_t mask[NT];                               // of the lane's 8 tokens
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    mask[nt] = 0;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int node = node0 + X::key(t, 4 * g + j);
+                            if (node < S.n && ((sees[nt] >> node) & 1)) mask[nt] |= 1u << (4 * t + j);
+                            else z[nt][4 * t + j] = -INFINITY;
+                        }
+                }
+                mine.weights(z);
+                if (__all(finite)) {
+                    add(v, z);
+                } else {
+                    // A weight of zero does not hide an infinite or NaN value from a product: only what a row sees is added.
+                    for (int og = 0; og < 4; ++og)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int node = node0 + X::key(j >> 2, 4 * og + (j & 3));
+                            const W *from = value + (S.start + min(node, S.n - 1)) * A.v_stride + 4 * g;
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                const float p = __shfl(z[nt][j], 16 * og + m);
+                                if (((uint32_t)__shfl((int)mask[nt], 16 * og + m) >> j) & 1)
+#pragma unroll
+                                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                                        for (int c = 0; c < 4; ++c)
+                                            mine.o[dt][nt][c] = fmaf(p, to_f32(from[dt * 16 + c]), mine.o[dt][nt][c]);
+                            }
+                        }
+                }
+            }
+
+            // the waves' sums together, DC channels at a time
+            __syncthreads();
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float all = add_xor32(add_xor16(mine.total[nt]));
+                if (g == 0) {
+                    s_top[wave][16 * nt + m] = mine.top[nt];
+                    s_total[wave][16 * nt + m] = all;
+                }
+            }
+            __syncthreads();
+            const auto top_of = [&](int row) {
+                return fmaxf(fmaxf(s_top[0][row], s_top[1][row]), fmaxf(s_top[2][row], s_top[3][row]));
+            };
+            const auto total_of = [&](int row, float shift) {
+                float t = 0.f;
+#pragma unroll
+                for (int w = 0; w < TA_WAVES; ++w) t += s_total[w][row] * exp2_fast(s_top[w][row] - shift);
+                return t;
+            };
+            float mine_by[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mine_by[nt] = exp2_fast(mine.top[nt] - shift_of(top_of(16 * nt + m)));
+            float *part = A.parts + (size_t)(2 * blockIdx.x + (first ? 0 : 1)) * ROWS * (DIM + 2);
+#pragma unroll
+            for (int d0 = 0; d0 < DIM; d0 += DC) {
+                if (d0 > 0) __syncthreads();
+#pragma unroll
+                for (int dt = 0; dt < DC / 16; ++dt)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const f32x4_t o = mine.o[d0 / 16 + dt][nt];
+                        *reinterpret_cast<float4 *>(&s_sum[wave][16 * nt + m][16 * dt + 4 * g]) =
+                            make_float4(o[0] * mine_by[nt], o[1] * mine_by[nt], o[2] * mine_by[nt], o[3] * mine_by[nt]);
+                    }
+                __syncthreads();
+                for (int e = tid; e < ROWS * (DC / 4); e += TA_THREADS) {
+                    const int row = e / (DC / 4), c = (e - row * (DC / 4)) * 4;
+                    if (row0 + row >= rows) continue;
+                    float4 a = *reinterpret_cast<const float4 *>(&s_sum[0][row][c]);
+#pragma unroll
+                    for (int w = 1; w < TA_WAVES; ++w) {
+                        const float4 b = *reinterpret_cast<const float4 *>(&s_sum[w][row][c]);
+                        a.x += b.x;
+                        a.y += b.y;
+                        a.z += b.z;
+                        a.w += b.w;
+                    }
+                    if (whole) {
+                        const float top = top_of(row), total = total_of(row, shift_of(top));
+                        const float by = total == 0.f ? 0.f : 1.f / total;
+                        const int node = (row0 + row) / A.group, head = h * A.group + row0 + row - node * A.group;
+                        const int64_t at = (int64_t)(S.start + node) * heads_q + head;
+                        W to[4];
+                        from_f32(a.x * by, to);
+                        from_f32(a.y * by, to + 1);
+                        from_f32(a.z * by, to + 2);
+                        from_f32(a.w * by, to + 3);
+                        __builtin_memcpy(__builtin_assume_aligned(static_cast<W *>(A.out) + at * DIM + d0 + c, sizeof(to)), to, sizeof(to));
+                        if (d0 + c == 0 && A.lse != nullptr) A.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
+                    } else {
+                        *reinterpret_cast<float4 *>(part + (size_t)row * DIM + d0 + c) = a;
+                    }
+                }
+            }
+            if (!whole && tid < ROWS) {
+                const float top = top_of(tid);
+                part[(size_t)ROWS * DIM + 2 * tid] = top;
+                part[(size_t)ROWS * DIM + 2 * tid + 1] = total_of(tid, shift_of(top));
+            }
+            u += s1 - s0;
+        }
+    }
+}
+
+// Parts of one row and head, where there are more than one: a block each, its waves taking every fourth part.
+template <typename W, int DIM, int NT>
+__global__ __launch_bounds__(TA_THREADS) void k_tree_join(TreeAttnArgs A)
+{
+    constexpr int ROWS = 16 * NT, PER = DIM / 64;
+    __shared__ float s_top[TA_WAVES], s_total[TA_WAVES], s_sum[TA_WAVES][DIM];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, heads_q = A.heads * A.group;
+    const int t = blockIdx.x, hq = blockIdx.y, h = hq / A.group;
+
+    int own, upto;
+    const int units = tree_units<ROWS>(A, lane, &own, &upto);
+    int r = -1, base = 0;
+    for (int c = 0; c < A.R; c += 64) {
+        if (c > 0) {
+            own = c + lane < A.R ? tree_span<ROWS>(A, c + lane).units : 0;
+            upto = wave_inclusive_scan(own);
+        }
+        const bool here = c + lane < A.R && A.starts[c + lane] <= t && t < A.starts[c + lane + 1];
+        const uint64_t found = __ballot(here);
+        if (found != 0) {
+            const int l = lane_of_first(found);
+            r = c + l;
+            base += __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(own, l);
+            break;
+        }
+        base += __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (r < 0) return;
+    const TreeSpan S = tree_span<ROWS>(A, r);
+    const int node = t - S.start;
+    if (node < 0 || node >= S.n) return;
+    const int row = node * A.group + hq - h * A.group, u0 = base + (h * S.row_tiles + row / ROWS) * S.steps;
+    const int b0 = tree_block_of(u0, units, A.block_bits), b1 = tree_block_of(u0 + S.steps - 1, units, A.block_bits);
+    if (b0 == b1) return;                                        // one block had the whole and has written it
+    // a block's first segment is its part 0: that of b0 is if b0 begins with this task
+    const int part0 = tree_begin(b0, units, A.block_bits) == u0 ? 0 : 1;
+
+    float top = -INFINITY, total = 0.f, sum[PER] = {};
+    for (int b = b0 + wave; b <= b1; b += TA_WAVES) {
+        const float *part = A.parts + (size_t)(2 * b + (b == b0 ? part0 : 0)) * ROWS * (DIM + 2);
+        const float other = part[(size_t)ROWS * DIM + 2 * (row % ROWS)], weight = part[(size_t)ROWS * DIM + 2 * (row % ROWS) + 1];
+        const float next = fmaxf(top, other), shift = shift_of(next);
+        const float old = exp2_fast(top - shift), by = exp2_fast(other - shift);
+        top = next;
+        total = total * old + weight * by;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) sum[i] = sum[i] * old + part[(size_t)(row % ROWS) * DIM + lane + 64 * i] * by;
+    }
+    if (lane == 0) {
+        s_top[wave] = top;
+        s_total[wave] = total;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) s_sum[wave][lane + 64 * i] = sum[i];
+    __syncthreads();
+    if (tid >= DIM) return;
+    const float all = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])), shift = shift_of(all);
+    float denominator = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 0; w < TA_WAVES; ++w) {
+        const float by = exp2_fast(s_top[w] - shift);
+        denominator += s_total[w] * by;
+        o += s_sum[w][tid] * by;
+    }
+    const int64_t at = (int64_t)t * heads_q + hq;
+    from_f32(denominator == 0.f ? 0.f : o / denominator, static_cast<W *>(A.out) + at * DIM + tid);
+    if (tid == 0 && A.lse != nullptr) A.lse[at] = denominator == 0.f ? -INFINITY : (all + log2f(denominator)) * LN2;
 }
 
 }  // namespace svdp
