@@ -7,6 +7,7 @@
 #include "svdp_draft_kernels.h"
 #include "svdp_host.h"
 #include "svdp_tree_attn.h"
+#include "svdp_tree_wide.h"
 
 #include <algorithm>
 #include <cmath>
@@ -72,44 +73,47 @@ svdp_status check_ws(void *ws, size_t ws_bytes, size_t need)
     return ws == nullptr || !aligned_to(ws, ALIGN) || ws_bytes < need ? SVDP_ERR_WORKSPACE : SVDP_OK;
 }
 
-// Row tiles of attention: 16 NT rows a wave, as many as a request may have, up to what a wave holds in registers.
+// Which attention kernel: rows are the nodes of a request times the query heads that share a head of K and V.
 struct AttnPlan {
-    int nt, block_bits;
+    bool wide;              // rows over the waves of a block (k_tree_attn_wide), or tokens (k_tree_attn)
+    int nt, block_bits, block_rows, part_rows;
     size_t bytes;
 };
-AttnPlan attn_plan(int dim, int group, int max_nodes)
+AttnPlan attn_plan(int dt, int dim, int group, int max_nodes)
 {
     const int64_t rows = (int64_t)group * max_nodes;
     AttnPlan p;
-    p.nt = rows <= 16 ? 1 : rows <= 32 || dim == 256 ? 2 : 4;
-    p.block_bits = p.nt * dim <= 256 ? 9 : 8;
-    p.bytes = align_up(((size_t)2 << p.block_bits) * 16 * p.nt * (dim + 2) * 4);
+    p.wide = dt == SVDP_BF16 && dim <= 128 && rows > 64;
+    p.nt = rows <= 16 || dim == 256 ? 1 : rows <= 32 || dt == SVDP_F32 ? 2 : 4;
+    p.block_bits = !p.wide && p.nt * dim <= 256 ? 9 : 8;
+    p.block_rows = p.wide ? TW_ROWS : 16 * p.nt;
+    p.part_rows = (int)std::min<int64_t>(rows, p.block_rows);
+    p.bytes = align_up(((size_t)2 << p.block_bits) * p.part_rows * (dim + 2) * 4);
     return p;
 }
-// Units of the longest request that the table has room for.
-int64_t attn_steps(int max_pages, int page, int max_nodes)
+// Units of the longest request that the table has room for, at most.
+int64_t attn_steps(int max_pages, int page, int max_nodes, int tiles_of_unit)
 {
-    const int64_t tiles = (int64_t)max_pages * page / TA_TILE + (max_nodes + TA_TILE - 1) / TA_TILE;
-    return (tiles + TA_WAVES - 1) / TA_WAVES;
+    return tiles((int64_t)max_pages * page / TA_TILE, tiles_of_unit) + tiles(tiles(max_nodes, TA_TILE), tiles_of_unit);
 }
-bool attn_units_fit(const svdp_kv_cache *c, int heads_q, int R, int max_pages, int max_nodes, int nt)
+bool attn_units_fit(const svdp_kv_cache *c, int heads_q, int R, int max_pages, int max_nodes, const AttnPlan &p)
 {
     const int64_t rows = (int64_t)(heads_q / c->heads) * max_nodes;
-    return attn_steps(max_pages, c->page, max_nodes) * ((rows + 16 * nt - 1) / (16 * nt)) * c->heads * R < INT_LIMIT;
+    return attn_steps(max_pages, c->page, max_nodes, 1) * ((rows + p.block_rows - 1) / p.block_rows) * c->heads * R < INT_LIMIT;
 }
 template <typename F>
-void on_attn(int dt, int dim, int nt, F &&f)
+void on_dim(int dim, F &&f)
 {
-    on_type(dt, [&](auto wt) {
-        const auto on_nt = [&](auto dc) {
-            if (nt == 1) f(wt, dc, std::integral_constant<int, 1>{});
-            else if (nt == 2) f(wt, dc, std::integral_constant<int, 2>{});
-            else if constexpr (decltype(dc)::value <= 128) f(wt, dc, std::integral_constant<int, 4>{});
-        };
-        if (dim == 64) on_nt(std::integral_constant<int, 64>{});
-        else if (dim == 128) on_nt(std::integral_constant<int, 128>{});
-        else on_nt(std::integral_constant<int, 256>{});
-    });
+    if (dim == 64) f(std::integral_constant<int, 64>{});
+    else if (dim == 128) f(std::integral_constant<int, 128>{});
+    else f(std::integral_constant<int, 256>{});
+}
+template <typename F>
+void on_tiles(int nt, F &&f)
+{
+    if (nt == 1) f(std::integral_constant<int, 1>{});
+    else if (nt == 2) f(std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 4>{});
 }
 
 // Parts that a row of logits is cut into: about a thousand blocks altogether, each of 8 to 32 KB.
@@ -130,8 +134,8 @@ size_t svdp_tree_attn_workspace_bytes(const svdp_kv_cache *cache, int32_t heads_
     if (check_cache(cache) != SVDP_OK || check_requests(R, 0, max_nodes) != SVDP_OK ||
         check_table(R, max_pages, cache->page) != SVDP_OK || heads_q < 1 || heads_q % cache->heads != 0)
         return 0;
-    const AttnPlan plan = attn_plan(cache->dim, heads_q / cache->heads, max_nodes);
-    return attn_units_fit(cache, heads_q, R, max_pages, max_nodes, plan.nt) ? plan.bytes : 0;
+    const AttnPlan plan = attn_plan(cache->dtype, cache->dim, heads_q / cache->heads, max_nodes);
+    return attn_units_fit(cache, heads_q, R, max_pages, max_nodes, plan) ? plan.bytes : 0;
 }
 
 svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void *q, int64_t q_stride, const void *k,
@@ -146,7 +150,7 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     if (st == SVDP_OK) st = check_table(R, max_pages, cache->page);
     if (st != SVDP_OK) return st;
     const int dt = cache->dtype, dim = cache->dim;
-    if (layer < 0 || layer >= cache->layers || heads_q < 1 || heads_q % cache->heads != 0 || !std::isfinite(scale))
+    if (layer < 0 || layer >= cache->layers || heads_q < 1 || heads_q % cache->heads != 0 || !std::isfinite(scale * LOG2E))
         return SVDP_ERR_INVALID_ARG;
     if (heads_q > 65535) return SVDP_ERR_UNSUPPORTED;
     if (T == 0) return SVDP_OK;
@@ -158,8 +162,8 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
         v_stride < (int64_t)cache->heads * dim || !whole_vectors(q_stride, dt) || !whole_vectors(k_stride, dt) ||
         !whole_vectors(v_stride, dt))
         return SVDP_ERR_INVALID_ARG;
-    const AttnPlan plan = attn_plan(dim, heads_q / cache->heads, max_nodes);
-    if (!attn_units_fit(cache, heads_q, R, max_pages, max_nodes, plan.nt)) return SVDP_ERR_UNSUPPORTED;
+    const AttnPlan plan = attn_plan(dt, dim, heads_q / cache->heads, max_nodes);
+    if (!attn_units_fit(cache, heads_q, R, max_pages, max_nodes, plan)) return SVDP_ERR_UNSUPPORTED;
     st = check_ws(ws, ws_bytes, plan.bytes);
     if (st != SVDP_OK) return st;
     const size_t layer_bytes = (size_t)cache->pages * cache->heads * cache->page * dim * bytes_of(dt);
@@ -189,16 +193,38 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     A.max_nodes = max_nodes;
     A.parts = static_cast<float *>(ws);
     A.block_bits = plan.block_bits;
+    A.part_rows = plan.part_rows;
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    on_attn(dt, dim, plan.nt, [&](auto wt, auto dc, auto nc) {
-        using W = typename decltype(wt)::type;
-        constexpr int DIM = decltype(dc)::value, NT = decltype(nc)::value;
-        launch((k_tree_attn<W, DIM, NT>), dim3(1 << plan.block_bits), dim3(TA_THREADS), 0, hs, A);
-        // a request of one unit is never cut
-        if (attn_steps(max_pages, cache->page, max_nodes) > 1)
-            launch((k_tree_join<W, DIM, NT>), dim3(T, heads_q), dim3(TA_THREADS), 0, hs, A);
+    const dim3 blocks(1 << plan.block_bits);
+    bool granted = true;
+    // a request of one unit is never cut
+    const auto join = [&](auto wt, auto dc, auto cut, int tiles_of_unit) {
+        if (attn_steps(max_pages, cache->page, max_nodes, tiles_of_unit) > 1)
+            launch((k_tree_join<typename decltype(wt)::type, decltype(dc)::value, decltype(cut)>), dim3(T, heads_q), dim3(TA_THREADS),
+                   0, hs, A);
+    };
+    on_dim(dim, [&](auto dc) {
+        constexpr int DIM = decltype(dc)::value;
+        if constexpr (DIM <= 128)
+            if (plan.wide) {
+                granted = grant_lds<k_tree_attn_wide<DIM>>(TW_LDS);
+                if (!granted) return;
+                launch(k_tree_attn_wide<DIM>, blocks, dim3(TW_THREADS), TW_LDS, hs, A);
+                join(Type<bf16>{}, dc, TreeCut<TW_ROWS, tw_tiles<DIM>(), true>{}, tw_tiles<DIM>());
+                return;
+            }
+        on_tiles(plan.nt, [&](auto nc) {
+            constexpr int NT = decltype(nc)::value;
+            on_type(dt, [&](auto wt) {
+                using W = typename decltype(wt)::type;
+                if constexpr (NT == 1 || (DIM <= 128 && (NT == 2 || std::is_same<W, bf16>::value))) {
+                    launch((k_tree_attn<W, DIM, NT>), blocks, dim3(TA_THREADS), 0, hs, A);
+                    join(wt, dc, TreeCut<16 * NT, TA_WAVES, false>{}, TA_WAVES);
+                }
+            });
+        });
     });
-    return hip_status(hipSuccess);
+    return granted ? hip_status(hipSuccess) : SVDP_ERR_UNSUPPORTED;
 }
 
 size_t svdp_tree_accept_workspace_bytes(int32_t T, int32_t V, int32_t dtype)

@@ -42,25 +42,41 @@ struct TreeAttnArgs {
     const int32_t *table, *lens, *starts;
     void *out;
     float *lse;
-    float *parts;                       // [2 << block_bits] parts of (dim + 2) floats a row
+    float *parts;                       // [2 << block_bits] parts of part_rows (dim + 2) floats
     float scale;
     int max_pages, pages, page_bits, heads, group, R, T, max_nodes;
     int block_bits;                     // there are 1 << block_bits blocks
+    int part_rows;                      // rows of a part: no more than a request has, nor a block
 };
+
+// How a kernel cuts the work: ROWS rows a block, units of TILES tiles; the tree's own tiles follow the cached ones, or begin a
+// unit of their own.
+template <int ROWS_, int TILES, bool APART>
+struct TreeCut {
+    static constexpr int ROWS = ROWS_;
+    static __device__ __forceinline__ int steps(int tiles, int n)
+    {
+        const int more = (n + TA_TILE - 1) / TA_TILE;
+        return APART ? (tiles + TILES - 1) / TILES + (more + TILES - 1) / TILES : (tiles + more + TILES - 1) / TILES;
+    }
+};
+
+typedef const __attribute__((address_space(4))) int32_t *table_t;            // read through the scalar cache
 
 // One request's share: rows, tiles and units.
 struct TreeSpan {
     int len, start, n, tiles, steps, row_tiles, units;
 };
-template <int ROWS>
+template <typename Cut>
 __device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs &A, int r)
 {
+    constexpr int ROWS = Cut::ROWS;
     TreeSpan s;
     s.len = min(max(A.lens[r], 0), A.max_pages << A.page_bits);
     s.start = min(max(A.starts[r], 0), A.T);
     s.n = min(min(max(A.starts[r + 1] - s.start, 0), A.max_nodes), A.T - s.start);
     s.tiles = (s.len + TA_TILE - 1) / TA_TILE;
-    s.steps = (s.tiles + (s.n + TA_TILE - 1) / TA_TILE + TA_WAVES - 1) / TA_WAVES;
+    s.steps = Cut::steps(s.tiles, s.n);
     s.row_tiles = (s.n * A.group + ROWS - 1) / ROWS;
     s.units = s.row_tiles * s.steps * A.heads;
     return s;
@@ -69,14 +85,14 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs &A, int r)
 __device__ __forceinline__ int lane_of_first(uint64_t ballot) { return __ffsll((unsigned long long)ballot) - 1; }
 
 // Units of all requests; `upto`: the inclusive sums of the first 64, a lane each.
-template <int ROWS>
+template <typename Cut>
 __device__ __forceinline__ int tree_units(const TreeAttnArgs &A, int lane, int *own, int *upto)
 {
-    *own = lane < A.R ? tree_span<ROWS>(A, lane).units : 0;
+    *own = lane < A.R ? tree_span<Cut>(A, lane).units : 0;
     *upto = wave_inclusive_scan(*own);
     int all = __builtin_amdgcn_readlane(*upto, 63);
     for (int c = 64; c < A.R; c += 64) {
-        const int u = c + lane < A.R ? tree_span<ROWS>(A, c + lane).units : 0;
+        const int u = c + lane < A.R ? tree_span<Cut>(A, c + lane).units : 0;
         all += __builtin_amdgcn_readlane(wave_inclusive_scan(u), 63);
     }
     return all;
@@ -93,6 +109,31 @@ __device__ __forceinline__ int tree_block_of(int u, int units, int bits)
     return units >> bits == 0 ? u : (int)(((((int64_t)u + 1) << bits) + units - 1) / units) - 1;
 }
 
+// The request that unit u belongs to, and how far into it that is; own, upto as tree_units left them.
+template <typename Cut>
+__device__ __forceinline__ int tree_request(const TreeAttnArgs &A, int u, int lane, int own, int upto, int *rem)
+{
+    for (int c = 0, base = 0;; c += 64) {
+        if (c > 0) {
+            own = c + lane < A.R ? tree_span<Cut>(A, c + lane).units : 0;
+            upto = wave_inclusive_scan(own);
+        }
+        const uint64_t behind = __ballot(base + upto > u);
+        if (behind != 0) {
+            const int l = lane_of_first(behind);
+            *rem = u - base - __builtin_amdgcn_readlane(upto, l) + __builtin_amdgcn_readlane(own, l);
+            return c + l;
+        }
+        base += __builtin_amdgcn_readlane(upto, 63);
+    }
+}
+
+// A part's address: block b has two, of part_rows rows of DIM sums and behind them the rows' maxima and denominators.
+__device__ __forceinline__ float *tree_part(const TreeAttnArgs &A, int b, int which, int dim)
+{
+    return A.parts + (size_t)(2 * b + which) * A.part_rows * (dim + 2);
+}
+
 // ---- operands, by storage type --------------------------------------------------------------------------------------------
 // Lane = 16 g + m.  KEY(t, m): the token of a tile whose K row m of the t-th product comes from; the result's rows 4 g + i lie
 // in lane group g, so that this lane group ends up with the tokens KEY(t, 4 g + i), which are those it has of V below.
@@ -101,6 +142,7 @@ struct TreeTile;
 
 template <int DIM>
 struct TreeTile<bf16, DIM> {
+    static constexpr uint32_t SIGNS = 0x80008000u;
     static constexpr int E = 8, KC = DIM / 32, VT = 1;
     static __device__ __forceinline__ int key(int t, int m) { return (m >> 2) * 8 + (m & 3) + 4 * t; }
     static __device__ __forceinline__ int pack(int, int g) { return g; }          // of 8 tokens
@@ -108,10 +150,22 @@ struct TreeTile<bf16, DIM> {
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ta_bf16x8, k), __builtin_bit_cast(ta_bf16x8, q), s, 0, 0, 0);
     }
-    static __device__ __forceinline__ f32x4_t sum(const uint4 (&v)[1], const float (&p)[8], f32x4_t o)
+    typedef ta_bf16x8 Weights;                  // of a lane's 8 tokens: rounded once, for their product with V
+    static __device__ __forceinline__ Weights pack_weights(const float (&p)[8])
     {
         const ta_f32x8 w = {p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]};
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ta_bf16x8, v[0]), __builtin_convertvector(w, ta_bf16x8), o, 0, 0, 0);
+        return __builtin_convertvector(w, ta_bf16x8);
+    }
+    static __device__ __forceinline__ f32x4_t sum(const uint4 (&v)[1], const Weights &p, f32x4_t o)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ta_bf16x8, v[0]), p, o, 0, 0, 0);
+    }
+    // each element: f(its bits in front of 16 zeros) as a new element
+    template <typename F>
+    static __device__ __forceinline__ uint4 each(const uint4 &v, F &&f)
+    {
+        const auto two = [&](uint32_t w) { return (f(w << 16) >> 16) | (f(w & 0xffff0000u) & 0xffff0000u); };
+        return make_uint4(two(v.x), two(v.y), two(v.z), two(v.w));
     }
     static __device__ __forceinline__ bool finite(const uint4 &v)
     {
@@ -131,6 +185,7 @@ struct TreeTile<bf16, DIM> {
 
 template <int DIM>
 struct TreeTile<float, DIM> {
+    static constexpr uint32_t SIGNS = 0x80000000u;
     static constexpr int E = 4, KC = DIM / 16, VT = 2;
     static __device__ __forceinline__ int key(int t, int m) { return 16 * t + m; }
     static __device__ __forceinline__ int pack(int t, int g) { return 4 * t + g; } // of 4 tokens
@@ -142,8 +197,24 @@ struct TreeTile<float, DIM> {
         s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.z, b.z, s, 0, 0, 0);
         return __builtin_amdgcn_mfma_f32_16x16x4f32(a.w, b.w, s, 0, 0, 0);
     }
-    static __device__ __forceinline__ f32x4_t sum(const uint4 (&v)[2], const float (&p)[8], f32x4_t o)
+    struct Weights {
+        float p[8];
+    };
+    static __device__ __forceinline__ Weights pack_weights(const float (&p)[8])
     {
+        Weights w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w.p[i] = p[i];
+        return w;
+    }
+    template <typename F>
+    static __device__ __forceinline__ uint4 each(const uint4 &v, F &&f)
+    {
+        return make_uint4(f(v.x), f(v.y), f(v.z), f(v.w));
+    }
+    static __device__ __forceinline__ f32x4_t sum(const uint4 (&v)[2], const Weights &w, f32x4_t o)
+    {
+        const float (&p)[8] = w.p;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const float4 a = as_float4(v[t]);
@@ -176,59 +247,140 @@ __device__ __forceinline__ float max_xor32(float v)
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
-// what exponents are taken relative to: a maximum of -inf (nothing but zero weights so far) must not make -inf - -inf
-__device__ __forceinline__ float shift_of(float top) { return top == -INFINITY ? 0.f : top; }
+// Scores are taken relative to a `base` that follows their maximum: it moves only where a score exceeds it by more than SLACK in
+// base two (then to the maximum), so that the sums are rarely brought down to a new one.  A weight is then below 2^SLACK, far from any
+// limit of fp32 (nor of bf16, which has the same exponents).  The base is where the score products' accumulators start, so
+// that a score costs one multiplication in front of its exponential.
+constexpr float SLACK = 8.f;
+// -inf (nothing but zero weights so far) must not make -inf - -inf
+__device__ __forceinline__ float finite_shift(float shift) { return shift == -INFINITY ? 0.f : shift; }
 
-// What a wave has of its rows: the sum O^T (channels 16 dt + 4 g + i of row m), the maximum of the scores in base two and the lane
-// group's part of the denominator.
+// Infinities and NaN in V where not every row sees every token: a weight of zero would not hide them from a product.  So that is
+// taken over the finite elements, and for each of +inf, -inf and NaN it is counted how many of them a row sees.
+__device__ __forceinline__ bool is_finite_bits(uint32_t u) { return (u & 0x7f800000u) != 0x7f800000u; }
+template <typename X>
+__device__ __forceinline__ uint4 only_finite(const uint4 &v)
+{
+    return X::each(v, [](uint32_t u) { return is_finite_bits(u) ? u : 0u; });
+}
+__device__ __forceinline__ float value_of_kind(int kind) { return kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN; }
+template <typename X>
+__device__ __forceinline__ uint4 ones_of_kind(const uint4 &v, int kind)
+{
+    const uint32_t inf = kind == 0 ? 0x7f800000u : 0xff800000u;
+    return X::each(v, [&](uint32_t u) {
+        return (kind == 2 ? !is_finite_bits(u) && (u & 0x007fffffu) != 0 : u == inf) ? 0x3f800000u : 0u;
+    });
+}
+
+// What a wave has of its rows: the sum O^T (channels 16 dt + 4 g + i of row m), the base, and the lane group's part of the denominator.
 template <typename W, int DIM, int NT>
 struct TreeWave {
     using X = TreeTile<W, DIM>;
-    static constexpr int DT = DIM / 16;
+    using Weights = typename X::Weights;
+    static constexpr int DT = DIM / 16, VT = X::VT;
     f32x4_t o[DT][NT];
-    float top[NT], total[NT];
+    float base[NT], total[NT];          // base: in units of `unit`; zero for a row that has not seen anything
+    float limit[NT];                    // what a relative score has to exceed for the base to move: -inf for such a row
 
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            top[nt] = -INFINITY;
+            base[nt] = 0.f;
+            limit[nt] = -INFINITY;
             total[nt] = 0.f;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[dt][nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
     }
-    // scores in base two -> weights; earlier sums come down to the new maximum
-    __device__ __forceinline__ void weights(float (&z)[NT][8])
+    // where the accumulators of row tile nt's scores start
+    __device__ __forceinline__ f32x4_t start(int nt) const { return f32x4_t{-base[nt], -base[nt], -base[nt], -base[nt]}; }
+    // the base in base two, -inf for a row that has not seen anything
+    __device__ __forceinline__ float shift(int nt, float unit) const { return limit[nt] == -INFINITY ? -INFINITY : base[nt] * unit; }
+
+    // Scores relative to the base, times unit (> 0), in base two -> weights.
+    template <int N>
+    __device__ __forceinline__ void weights(float (&z)[NT][8 * N], float unit, Weights (&w)[NT][N])
     {
-        float next[NT];
+        float top[NT];
         bool grew = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float t = fmaxf(fmaxf(fmaxf(z[nt][0], z[nt][1]), fmaxf(z[nt][2], z[nt][3])),
-                            fmaxf(fmaxf(z[nt][4], z[nt][5]), fmaxf(z[nt][6], z[nt][7])));
-            next[nt] = fmaxf(top[nt], max_xor32(max_xor16(t)));
-            grew = grew || next[nt] > top[nt];
+            float t = z[nt][0];
+#pragma unroll
+            for (int i = 1; i < 8 * N; ++i) t = fmaxf(t, z[nt][i]);
+            top[nt] = max_xor32(max_xor16(t));
+            grew = grew || top[nt] > limit[nt];
         }
         if (__any(grew)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const float old = exp2_fast(top[nt] - shift_of(next[nt]));
-                top[nt] = next[nt];
+                const float to = top[nt] > limit[nt] ? base[nt] + top[nt] / unit : base[nt];
+                // nothing so far: there is nothing to bring down, and the base may come down itself
+                const float down = (to - base[nt]) * unit, old = limit[nt] == -INFINITY ? 0.f : exp2_fast(-down);
+                base[nt] = to;
+                limit[nt] = top[nt] > limit[nt] ? SLACK : limit[nt];
                 total[nt] *= old;
+#pragma unroll
+                for (int i = 0; i < 8 * N; ++i) z[nt][i] -= down;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) o[dt][nt] *= old;
             }
         }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const float shift = shift_of(top[nt]);
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                z[nt][i] = exp2_fast(z[nt][i] - shift);
-                total[nt] += z[nt][i];
+            for (int n = 0; n < N; ++n) {
+                float e[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = exp2_fast(z[nt][8 * n + i]);
+                total[nt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+                w[nt][n] = X::pack_weights(e);
+            }
+    }
+    // One V operand (16 channels) against the weights of all rows.
+    template <int N>
+    __device__ __forceinline__ void add(int dt, const uint4 (&v)[VT], const Weights (&w)[NT][N], int n = 0)
+    {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) o[dt][nt] = X::sum(v, w[nt][n], o[dt][nt]);
+    }
+    // What V's infinities and NaN add (see only_finite).
+    __device__ __forceinline__ void add_special(int dt, const uint4 (&v)[VT], const uint32_t (&mask)[NT])
+    {
+        uint4 part[VT];
+#pragma unroll 1
+        for (int kind = 0; kind < 3; ++kind) {
+#pragma unroll
+            for (int t = 0; t < VT; ++t) part[t] = ones_of_kind<X>(v[t], kind);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float seen[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) seen[i] = (mask[nt] >> i) & 1 ? 1.f : 0.f;
+                const f32x4_t count = X::sum(part, X::pack_weights(seen), f32x4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                for (int c = 0; c < 4; ++c) o[dt][nt][c] += count[c] > 0.f ? value_of_kind(kind) : 0.f;
             }
         }
+    }
+};
+
+// Scores stay in units of |scale| > 0, so that the sign goes to Q; for a scale of zero Q is zero, and the unit one.
+struct TreeScale {
+    float unit;
+    uint32_t stays, flip;
+    __device__ __forceinline__ TreeScale(float scale, uint32_t signs)
+    {
+        unit = fabsf(scale) * LOG2E;
+        stays = unit == 0.f ? 0u : ~0u;
+        unit = unit == 0.f ? 1.f : unit;
+        flip = scale < 0.f ? signs : 0u;
+    }
+    __device__ __forceinline__ uint4 of(const uint4 &q) const
+    {
+        return make_uint4((q.x & stays) ^ flip, (q.y & stays) ^ flip, (q.z & stays) ^ flip, (q.w & stays) ^ flip);
     }
 };
 
@@ -237,7 +389,8 @@ template <typename W, int DIM, int NT>
 __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
 {
     using X = TreeTile<W, DIM>;
-    constexpr int ROWS = 16 * NT, E = X::E, KC = X::KC, VT = X::VT, DT = DIM / 16;
+    using Cut = TreeCut<16 * NT, TA_WAVES, false>;
+    constexpr int ROWS = Cut::ROWS, E = X::E, KC = X::KC, VT = X::VT, DT = DIM / 16;
     constexpr int DC = DIM * NT <= 128 ? DIM : 128 / NT;          // channels that the waves' sums meet in LDS by: 32 KB
     __shared__ float s_top[TA_WAVES][ROWS], s_total[TA_WAVES][ROWS];
     __shared__ __align__(16) float s_sum[TA_WAVES][ROWS][DC + 4];
@@ -245,31 +398,15 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
     const int heads_q = A.heads * A.group;
 
     int own, upto;
-    const int units = tree_units<ROWS>(A, lane, &own, &upto);
+    const int units = tree_units<Cut>(A, lane, &own, &upto);
     int u = tree_begin(blockIdx.x, units, A.block_bits);
     const int u1 = tree_begin(blockIdx.x + 1, units, A.block_bits);
     if (u >= u1) return;
-    // the request that unit u belongs to, and the units in front of that request
-    int r = 0, rem = 0;
-    for (int c = 0, base = 0;; c += 64) {
-        if (c > 0) {
-            own = c + lane < A.R ? tree_span<ROWS>(A, c + lane).units : 0;
-            upto = wave_inclusive_scan(own);
-        }
-        const uint64_t behind = __ballot(base + upto > u);
-        if (behind != 0) {
-            const int l = lane_of_first(behind);
-            r = c + l;
-            rem = u - base - __builtin_amdgcn_readlane(upto, l) + __builtin_amdgcn_readlane(own, l);
-            break;
-        }
-        base += __builtin_amdgcn_readlane(upto, 63);
-    }
-
+    int rem, r = tree_request<Cut>(A, u, lane, own, upto, &rem);
     for (bool first = true; u < u1; ++r, rem = 0) {
-        const TreeSpan S = tree_span<ROWS>(A, __builtin_amdgcn_readfirstlane(r));
+        const TreeSpan S = tree_span<Cut>(A, __builtin_amdgcn_readfirstlane(r));
         if (S.units == 0) continue;
-        const int32_t *table = A.table + (size_t)r * A.max_pages;
+        const table_t table = (table_t)(uintptr_t)(A.table + (size_t)r * A.max_pages);
         int task = rem / S.steps, s0 = rem - task * S.steps;
         for (; task < A.heads * S.row_tiles && u < u1; ++task, s0 = 0, first = false) {
             const int s1 = min(S.steps, s0 + u1 - u);
@@ -279,35 +416,30 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
             // Q of the rows (a row past the last one repeats it: computed and never written)
             uint4 q[KC][NT];
             uint64_t sees[NT];
+            const TreeScale scale(A.scale, X::SIGNS);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int row = min(row0 + 16 * nt + m, rows - 1), node = row / A.group, head = h * A.group + row - node * A.group;
                 const W *from = static_cast<const W *>(A.q) + (S.start + node) * A.q_stride + (int64_t)head * DIM + g * E;
 #pragma unroll
-                for (int c = 0; c < KC; ++c) q[c][nt] = load_raw(from + c * 4 * E);
+                for (int c = 0; c < KC; ++c) q[c][nt] = scale.of(load_raw(from + c * 4 * E));
                 sees[nt] = A.tree != nullptr ? A.tree[S.start + node] : ~0ull >> (63 - node);
             }
             TreeWave<W, DIM, NT> mine;
+            typename X::Weights p[NT][1];
             mine.clear();
 
             const auto scores = [&](const uint4 (&k)[2][KC], float (&z)[NT][8]) {
-                const float to_log2 = A.scale * LOG2E;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+                        f32x4_t s = mine.start(nt);
 #pragma unroll
                         for (int c = 0; c < KC; ++c) s = X::score(k[t][c], q[c][nt], s);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) z[nt][4 * t + i] = s[i] * to_log2;
+                        for (int i = 0; i < 4; ++i) z[nt][4 * t + i] = s[i] * scale.unit;
                     }
-            };
-            const auto add = [&](const uint4 (&v)[DT][VT], const float (&p)[NT][8]) {
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mine.o[dt][nt] = X::sum(v[dt], p[nt], mine.o[dt][nt]);
             };
 
             // cached tokens: K of the next tile is requested when this one's has been used, and so is V
@@ -335,12 +467,12 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
 #pragma unroll
                         for (int t = 0; t < VT; ++t) v[dt][t] = load_raw(from + (X::pack(t, g) * DIM + dt * 16 + m) * E);
                 };
-                int id = __builtin_amdgcn_readfirstlane(page_of(i)), id_next = page_of(i + TA_WAVES);
+                int id = page_of(i), id_next = page_of(i + TA_WAVES);
                 load_k(tile_at(i, id));
                 load_v(tile_at(i, id));
                 for (; i < i_end; i += TA_WAVES) {
                     const int count = real(id) ? min(S.len - i * TA_TILE, TA_TILE) : 0;
-                    id = __builtin_amdgcn_readfirstlane(id_next);
+                    id = id_next;
                     id_next = page_of(i + 2 * TA_WAVES);
                     const int64_t at = tile_at(min(i + TA_WAVES, S.tiles - 1), id);
                     float z[NT][8];
@@ -348,48 +480,34 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
                     if (i + TA_WAVES < i_end) load_k(at);
                     if (count < TA_TILE) {
 #pragma unroll
-                        for (int t = 0; t < 2; ++t)
+                        for (int j = 0; j < 8; ++j)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt)
-                                    if (X::key(t, 4 * g + j) >= count) z[nt][4 * t + j] = -INFINITY;
+                            for (int nt = 0; nt < NT; ++nt)
+                                if (X::key(j >> 2, 4 * g + (j & 3)) >= count) z[nt][j] = -INFINITY;
 #pragma unroll
                         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                             for (int t = 0; t < VT; ++t) v[dt][t] = X::first(v[dt][t], count - X::pack(t, g) * E);
                     }
-                    mine.weights(z);
-                    add(v, z);
+                    mine.template weights<1>(z, scale.unit, p);
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) mine.add(dt, v[dt], p);
                     if (i + TA_WAVES < i_end) load_v(at);
                 }
             }
 
             // the tree's own tokens
+#pragma unroll 1
             for (; i < min(s1 * TA_WAVES, S.tiles + (S.n + TA_TILE - 1) / TA_TILE); i += TA_WAVES) {
                 const int node0 = (i - S.tiles) * TA_TILE;
                 const W *key = static_cast<const W *>(A.k) + (int64_t)h * DIM, *value = static_cast<const W *>(A.v) + (int64_t)h * DIM;
-                uint4 k[2][KC], v[DT][VT];
+                uint4 k[2][KC];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const W *from = key + (S.start + min(node0 + X::key(t, m), S.n - 1)) * A.k_stride + g * E;
 #pragma unroll
                     for (int c = 0; c < KC; ++c) k[t][c] = load_raw(from + c * 4 * E);
                 }
-                // these rows lie token by token: an operand is put together from its elements
-                bool finite = true;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int t = 0; t < VT; ++t) {
-                        const int node = node0 + X::pack(t, g) * E;
-                        W in[E];
-#pragma unroll
-                        for (int j = 0; j < E; ++j) in[j] = value[(S.start + min(node + j, S.n - 1)) * A.v_stride + dt * 16 + m];
-                        __builtin_memcpy(&v[dt][t], in, 16);
-                        v[dt][t] = X::first(v[dt][t], S.n - node);
-                        finite = finite && X::finite(v[dt][t]);
-                    }
                 float z[NT][8];
                 scores(k, z);
                 uint32_t mask[NT];                               // of the lane's 8 tokens
@@ -397,35 +515,34 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
                 for (int nt = 0; nt < NT; ++nt) {
                     mask[nt] = 0;
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int node = node0 + X::key(t, 4 * g + j);
-                            if (node < S.n && ((sees[nt] >> node) & 1)) mask[nt] |= 1u << (4 * t + j);
-                            else z[nt][4 * t + j] = -INFINITY;
-                        }
+                    for (int j = 0; j < 8; ++j) {
+                        const int node = node0 + X::key(j >> 2, 4 * g + (j & 3));
+                        if (node < S.n && ((sees[nt] >> node) & 1)) mask[nt] |= 1u << j;
+                        else z[nt][j] = -INFINITY;
+                    }
                 }
-                mine.weights(z);
-                if (__all(finite)) {
-                    add(v, z);
-                } else {
-                    // A weight of zero does not hide an infinite or NaN value from a product: only what a row sees is added.
-                    for (int og = 0; og < 4; ++og)
+                mine.template weights<1>(z, scale.unit, p);
+                // these rows of V lie token by token: an operand is put together from its elements
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int node = node0 + X::key(j >> 2, 4 * og + (j & 3));
-                            const W *from = value + (S.start + min(node, S.n - 1)) * A.v_stride + 4 * g;
+                for (int dt = 0; dt < DT; ++dt) {
+                    uint4 v[VT];
+                    bool finite = true;
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                const float p = __shfl(z[nt][j], 16 * og + m);
-                                if (((uint32_t)__shfl((int)mask[nt], 16 * og + m) >> j) & 1)
+                    for (int t = 0; t < VT; ++t) {
+                        const int node = node0 + X::pack(t, g) * E;
+                        W in[E];
 #pragma unroll
-                                    for (int dt = 0; dt < DT; ++dt)
+                        for (int j = 0; j < E; ++j) in[j] = value[(S.start + min(node + j, S.n - 1)) * A.v_stride + dt * 16 + m];
+                        __builtin_memcpy(&v[t], in, 16);
+                        v[t] = X::first(v[t], S.n - node);
+                        finite = finite && X::finite(v[t]);
+                    }
+                    if (!__all(finite)) {
+                        mine.add_special(dt, v, mask);
 #pragma unroll
-                                        for (int c = 0; c < 4; ++c)
-                                            mine.o[dt][nt][c] = fmaf(p, to_f32(from[dt * 16 + c]), mine.o[dt][nt][c]);
-                            }
-                        }
+                        for (int t = 0; t < VT; ++t) v[t] = only_finite<X>(v[t]);
+                    }
+                    mine.add(dt, v, p);
                 }
             }
 
@@ -435,7 +552,7 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
             for (int nt = 0; nt < NT; ++nt) {
                 const float all = add_xor32(add_xor16(mine.total[nt]));
                 if (g == 0) {
-                    s_top[wave][16 * nt + m] = mine.top[nt];
+                    s_top[wave][16 * nt + m] = mine.shift(nt, scale.unit);
                     s_total[wave][16 * nt + m] = all;
                 }
             }
@@ -451,8 +568,8 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
             };
             float mine_by[NT];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mine_by[nt] = exp2_fast(mine.top[nt] - shift_of(top_of(16 * nt + m)));
-            float *part = A.parts + (size_t)(2 * blockIdx.x + (first ? 0 : 1)) * ROWS * (DIM + 2);
+            for (int nt = 0; nt < NT; ++nt) mine_by[nt] = exp2_fast(mine.shift(nt, scale.unit) - finite_shift(top_of(16 * nt + m)));
+            float *part = tree_part(A, blockIdx.x, first ? 0 : 1, DIM);
 #pragma unroll
             for (int d0 = 0; d0 < DIM; d0 += DC) {
                 if (d0 > 0) __syncthreads();
@@ -478,7 +595,7 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
                         a.w += b.w;
                     }
                     if (whole) {
-                        const float top = top_of(row), total = total_of(row, shift_of(top));
+                        const float top = top_of(row), total = total_of(row, finite_shift(top));
                         const float by = total == 0.f ? 0.f : 1.f / total;
                         const int node = (row0 + row) / A.group, head = h * A.group + row0 + row - node * A.group;
                         const int64_t at = (int64_t)(S.start + node) * heads_q + head;
@@ -494,10 +611,10 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
                     }
                 }
             }
-            if (!whole && tid < ROWS) {
+            if (!whole && tid < min(ROWS, A.part_rows)) {
                 const float top = top_of(tid);
-                part[(size_t)ROWS * DIM + 2 * tid] = top;
-                part[(size_t)ROWS * DIM + 2 * tid + 1] = total_of(tid, shift_of(top));
+                part[(size_t)A.part_rows * DIM + 2 * tid] = top;
+                part[(size_t)A.part_rows * DIM + 2 * tid + 1] = total_of(tid, finite_shift(top));
             }
             u += s1 - s0;
         }
@@ -505,20 +622,20 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
 }
 
 // Parts of one row and head, where there are more than one: a block each, its waves taking every fourth part.
-template <typename W, int DIM, int NT>
+template <typename W, int DIM, typename Cut>
 __global__ __launch_bounds__(TA_THREADS) void k_tree_join(TreeAttnArgs A)
 {
-    constexpr int ROWS = 16 * NT, PER = DIM / 64;
+    constexpr int ROWS = Cut::ROWS, PER = DIM / 64;
     __shared__ float s_top[TA_WAVES], s_total[TA_WAVES], s_sum[TA_WAVES][DIM];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, heads_q = A.heads * A.group;
     const int t = blockIdx.x, hq = blockIdx.y, h = hq / A.group;
 
     int own, upto;
-    const int units = tree_units<ROWS>(A, lane, &own, &upto);
+    const int units = tree_units<Cut>(A, lane, &own, &upto);
     int r = -1, base = 0;
     for (int c = 0; c < A.R; c += 64) {
         if (c > 0) {
-            own = c + lane < A.R ? tree_span<ROWS>(A, c + lane).units : 0;
+            own = c + lane < A.R ? tree_span<Cut>(A, c + lane).units : 0;
             upto = wave_inclusive_scan(own);
         }
         const bool here = c + lane < A.R && A.starts[c + lane] <= t && t < A.starts[c + lane + 1];
@@ -532,7 +649,7 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_join(TreeAttnArgs A)
         base += __builtin_amdgcn_readlane(upto, 63);
     }
     if (r < 0) return;
-    const TreeSpan S = tree_span<ROWS>(A, r);
+    const TreeSpan S = tree_span<Cut>(A, r);
     const int node = t - S.start;
     if (node < 0 || node >= S.n) return;
     const int row = node * A.group + hq - h * A.group, u0 = base + (h * S.row_tiles + row / ROWS) * S.steps;
@@ -543,9 +660,10 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_join(TreeAttnArgs A)
 
     float top = -INFINITY, total = 0.f, sum[PER] = {};
     for (int b = b0 + wave; b <= b1; b += TA_WAVES) {
-        const float *part = A.parts + (size_t)(2 * b + (b == b0 ? part0 : 0)) * ROWS * (DIM + 2);
-        const float other = part[(size_t)ROWS * DIM + 2 * (row % ROWS)], weight = part[(size_t)ROWS * DIM + 2 * (row % ROWS) + 1];
-        const float next = fmaxf(top, other), shift = shift_of(next);
+        const float *part = tree_part(A, b, b == b0 ? part0 : 0, DIM);
+        const float2 head = *reinterpret_cast<const float2 *>(part + (size_t)A.part_rows * DIM + 2 * (row % ROWS));
+        const float other = head.x, weight = head.y;
+        const float next = fmaxf(top, other), shift = finite_shift(next);
         const float old = exp2_fast(top - shift), by = exp2_fast(other - shift);
         top = next;
         total = total * old + weight * by;
@@ -560,7 +678,7 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_join(TreeAttnArgs A)
     for (int i = 0; i < PER; ++i) s_sum[wave][lane + 64 * i] = sum[i];
     __syncthreads();
     if (tid >= DIM) return;
-    const float all = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])), shift = shift_of(all);
+    const float all = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])), shift = finite_shift(all);
     float denominator = 0.f, o = 0.f;
 #pragma unroll
     for (int w = 0; w < TA_WAVES; ++w) {

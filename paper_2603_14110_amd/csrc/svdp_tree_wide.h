@@ -1,0 +1,337 @@
+// Attention of drafted tokens where a request has many rows (svdp_tree_attn.h holds the division of the work and the join).
+//
+// The waves of a block take different rows of the SAME tokens, 32 each: K and V come from memory once for 256 rows.
+// Their tiles pass through LDS, in three stages of 32 KB that are filled straight from memory, two stages ahead, with one
+// barrier a stage; each wave keeps its own rows' base, denominator and sum, and nothing is exchanged between waves.
+// Products are 32 x 32 x 16: S^T = K Q^T leaves a lane with 16 scores of one row (token of result register i in lane half f:
+// 16 (i / 8) + 8 f + i % 8, by the choice of K rows), which are the tokens that O^T += V^T P^T wants of that lane.
+// LDS: K rows of DIM channels, 16-byte chunk c of token i at slot c ^ swizzle(i), so that the tokens of an operand read lie in different
+// banks; V as in memory, of which 32 lanes read consecutive 512 bytes.
+#pragma once
+
+#include "svdp_tree_attn.h"
+
+namespace svdp {
+
+constexpr int TW_THREADS = 512, TW_WAVES = TW_THREADS / 64, TW_ROWS = 32 * TW_WAVES;
+constexpr int TW_STAGE = 32 << 10, TW_STAGES = 3, TW_LDS = TW_STAGES * TW_STAGE;
+template <int DIM>
+constexpr int tw_tiles() { return TW_STAGE / 2 / (TA_TILE * DIM * 2); }          // of a stage: 4 or 2
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16_t mfma_32(const uint4 &a, const uint4 &b, const f32x16_t &c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(ta_bf16x8, a), __builtin_bit_cast(ta_bf16x8, b), c, 0, 0, 0);
+}
+
+// The same value, of which the compiler knows nothing: what is computed from it stays where it is written.  Without it, what the
+// rare parts of a loop need per lane is kept in registers that the products' operands could be read ahead into.
+__device__ __forceinline__ int here(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// Token (of 32) that row `at` of K's operand stands for, and what its chunks are moved by.
+__device__ __forceinline__ int tw_token(int at) { return (at >> 4) * 16 + ((at >> 2) & 1) * 8 + ((at >> 3) & 1) * 4 + (at & 3); }
+__device__ __forceinline__ int tw_swizzle(int token, int dim) { return dim == 64 ? token & 7 : token & 15; }
+
+template <int DIM>
+__global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_tree_attn_wide(TreeAttnArgs A)
+{
+    using X = TreeTile<bf16, DIM>;
+    constexpr int TILES = tw_tiles<DIM>(), KC = DIM / 16, DT = DIM / 32;
+    using Cut = TreeCut<TW_ROWS, TILES, true>;
+    constexpr int TILE_BYTES = TA_TILE * DIM * 2, CHUNKS = DIM / 8;
+    extern __shared__ __align__(16) char tw_smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), f = lane >> 5, m = lane & 31;
+    const int heads_q = A.heads * A.group;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t *)tw_smem;
+
+    int own, upto;
+    const int units = tree_units<Cut>(A, lane, &own, &upto);
+    int u = tree_begin(blockIdx.x, units, A.block_bits);
+    const int u1 = tree_begin(blockIdx.x + 1, units, A.block_bits);
+    if (u >= u1) return;
+    int rem, r = tree_request<Cut>(A, u, lane, own, upto, &rem);
+
+    // where a lane's operands lie in a tile
+    int k_at[KC];
+#pragma unroll
+    for (int c = 0; c < KC; ++c) k_at[c] = (tw_token(m) * CHUNKS + ((2 * c + f) ^ tw_swizzle(tw_token(m), DIM))) * 16;
+    const int v_at = (f * DIM + m) * 16;
+
+    for (bool first = true; u < u1; ++r, rem = 0) {
+        const TreeSpan S = tree_span<Cut>(A, __builtin_amdgcn_readfirstlane(r));
+        if (S.units == 0) continue;
+        const int cached_steps = (S.tiles + TILES - 1) / TILES, per_page = A.page_bits - 5;
+        int task = rem / S.steps, s0 = rem - task * S.steps;
+        for (; task < A.heads * S.row_tiles && u < u1; ++task, s0 = 0, first = false) {
+            const int s1 = min(S.steps, s0 + u1 - u), s_end = min(s1, cached_steps);
+            const int h = task / S.row_tiles, rows = S.n * A.group, block_row0 = (task - h * S.row_tiles) * TW_ROWS;
+            const int row0 = block_row0 + wave * 32;
+            const bool whole = s0 == 0 && s1 == S.steps, active = row0 < rows;
+
+            // Page ids: a lane each for 64 pages, read out per tile.  (Read one by one through the scalar cache, the wait for
+            // them also holds up the reads from LDS.)
+            int window = -64, window_ids = 0;
+            const auto pages_of = [&](int step, int (&ids)[TILES]) {
+                const int last = min(step * TILES + TILES - 1, S.tiles - 1) >> per_page;
+                if (last >= window + 64) {
+                    window = min(step * TILES, S.tiles - 1) >> per_page;
+                    window_ids = here(A.table[(size_t)r * A.max_pages + min(window + lane, (S.tiles - 1) >> per_page)]);
+                }
+#pragma unroll
+                for (int j = 0; j < TILES; ++j)
+                    ids[j] = __builtin_amdgcn_readlane(window_ids, (min(step * TILES + j, S.tiles - 1) >> per_page) - window);
+            };
+            const auto real = [&](int id) { return (uint32_t)id < (uint32_t)A.pages; };
+            // a stage from memory: 16 bytes a thread, four times
+            const auto fill = [&](int step, int buffer, const int (&ids)[TILES]) {
+#pragma unroll
+                for (int part = 0; part < 4; ++part) {           // K, K, V, V
+                    constexpr int IN_TILE = TILE_BYTES / 16;
+                    const int p0 = (part & 1) * TW_THREADS + wave * 64, j = p0 / IN_TILE;
+                    int id = ids[0];
+#pragma unroll
+                    for (int i = 1; i < TILES; ++i) id = i == j ? ids[i] : id;
+                    const int tile = min(step * TILES + j, S.tiles - 1), p = p0 % IN_TILE + lane;
+                    const int64_t page = (int64_t)(real(id) ? id : 0) * A.heads + h;
+                    const int64_t at = ((page << per_page) + (tile & ((1 << per_page) - 1))) * TILE_BYTES;
+                    const int token = p / CHUNKS, slot = p % CHUNKS;
+                    const int piece = part < 2 ? token * CHUNKS + (slot ^ tw_swizzle(token, DIM)) : p;
+                    load_to_lds(static_cast<const char *>(part < 2 ? A.K : A.V) + at + piece * 16,
+                                lds0 + buffer * TW_STAGE + (part >> 1) * (TW_STAGE / 2) + p0 * 16);
+                }
+            };
+
+            stage_barrier<0>();                                  // the last segment's stages and stores are done with
+            int buffer = 0;
+            int ids[TILES], ids_1[TILES], ids_2[TILES];          // of this stage and of the next two
+            if (s0 < s_end) {
+                pages_of(s0, ids);
+                pages_of(s0 + 1, ids_1);
+                pages_of(s0 + 2, ids_2);
+                fill(s0, 0, ids);
+                if (s0 + 1 < s_end) fill(s0 + 1, 1, ids_1);
+            }
+
+            const TreeScale scale(A.scale, X::SIGNS);
+            uint4 q[KC], k[KC], v[DT][2];
+            {
+                const int row = min(row0 + (here(lane) & 31), rows - 1), node = row / A.group, head = h * A.group + row - node * A.group;
+                const bf16 *from = static_cast<const bf16 *>(A.q) + (S.start + node) * A.q_stride + (int64_t)head * DIM + f * 8;
+#pragma unroll
+                for (int c = 0; c < KC; ++c) q[c] = scale.of(load_raw(from + c * 16));
+            }
+            // as in TreeWave: sum, base, denominator (the lane half's part), and what a score has to exceed for the base to move
+            f32x16_t o[DT];
+            float base = 0.f, total = 0.f, limit = -INFINITY;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+
+            for (int step = s0; step < s1; ++step) {
+                const bool own_tokens = step >= cached_steps;    // the tree's
+                const int spare = buffer == TW_STAGES - 1 ? 0 : buffer + 1;
+                bool full = true, finite = true;
+                char *stage = tw_smem + buffer * TW_STAGE;
+                int counts[TILES], n_tiles = TILES;              // tokens of each tile: fewer at the end, none where there is no page
+                const int node0 = (step - cached_steps) * TILES * TA_TILE;
+                if (!own_tokens) {
+                    if (step + 1 < s_end) stage_barrier<4>();
+                    else stage_barrier<0>();
+                    if (step + 2 < s_end) fill(step + 2, buffer >= 1 ? buffer - 1 : buffer + 2, ids_2);
+                    buffer = spare;
+#pragma unroll
+                    for (int j = 0; j < TILES; ++j) {
+                        counts[j] = real(ids[j]) ? min(max(S.len - (step * TILES + j) * TA_TILE, 0), TA_TILE) : 0;
+                        full = full && counts[j] == TA_TILE;
+                        ids[j] = ids_1[j];
+                        ids_1[j] = ids_2[j];
+                    }
+                    pages_of(step + 3, ids_2);
+                    if (!full) {                                 // what lies behind them in V must not be NaN
+                        for (int e = here(tid); e < TW_STAGE / 32; e += TW_THREADS) {
+                            const int tile = e / (TILE_BYTES / 16), pack = e % (TILE_BYTES / 16) / DIM;
+                            uint4 *at = reinterpret_cast<uint4 *>(stage + TW_STAGE / 2) + e;
+                            int count = counts[0];
+#pragma unroll
+                            for (int i = 1; i < TILES; ++i) count = i == tile ? counts[i] : count;
+                            *at = X::first(*at, count - pack * 8);
+                        }
+                        __syncthreads();
+                    }
+                } else {                                         // into the same layout, V's packs element by element
+                    const int there = min(S.n - node0, TILES * TA_TILE);
+                    n_tiles = (there + TA_TILE - 1) / TA_TILE;
+                    full = false;
+#pragma unroll
+                    for (int j = 0; j < TILES; ++j) counts[j] = min(max(there - j * TA_TILE, 0), TA_TILE);
+                    stage_barrier<0>();
+                    int odd = 0;
+                    for (int e = here(tid); e < n_tiles * TA_TILE * CHUNKS; e += TW_THREADS) {
+                        const int i = e / CHUNKS, c = e - i * CHUNKS, tile = i / TA_TILE, token = i % TA_TILE;
+                        uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+                        if (i < there) {
+                            a = load_raw(static_cast<const bf16 *>(A.k) + (S.start + node0 + i) * A.k_stride + (int64_t)h * DIM + c * 8);
+                            b = load_raw(static_cast<const bf16 *>(A.v) + (S.start + node0 + i) * A.v_stride + (int64_t)h * DIM + c * 8);
+                        }
+                        *reinterpret_cast<uint4 *>(stage + tile * TILE_BYTES + (token * CHUNKS + (c ^ tw_swizzle(token, DIM))) * 16) = a;
+                        const int at = TW_STAGE / 2 + tile * TILE_BYTES + (((token >> 3) * DIM + c * 8) * 8 + (token & 7)) * 2;
+                        const auto put = [&](char *to, const uint4 &what) {
+                            const uint32_t w[4] = {what.x, what.y, what.z, what.w};
+#pragma unroll
+                            for (int d = 0; d < 8; ++d) *reinterpret_cast<uint16_t *>(to + d * 16) = (uint16_t)(w[d >> 1] >> (16 * (d & 1)));
+                        };
+                        put(stage + at, only_finite<X>(b));
+                        put(tw_smem + spare * TW_STAGE + at, b);
+                        odd |= X::finite(b) ? 0 : 1;
+                    }
+                    finite = __syncthreads_or(odd) == 0;
+                }
+                if (!active) continue;
+
+                // which of the lane's 16 tokens its row sees
+                const auto mask_of = [&](int j) {
+                    const int f = here(lane) >> 5, m = here(lane) & 31;
+                    int count = counts[0];
+#pragma unroll
+                    for (int i = 1; i < TILES; ++i) count = i == j ? counts[i] : count;
+                    uint32_t seen = (uint32_t)((1ull << count) - 1);
+                    if (own_tokens) {
+                        const int node = min(row0 + m, rows - 1) / A.group;
+                        const uint64_t sees = A.tree != nullptr ? A.tree[S.start + node] : ~0ull >> (63 - node);
+                        seen &= (uint32_t)(sees >> (node0 + j * TA_TILE));
+                    }
+                    return ((seen >> (8 * f)) & 0xffu) | ((seen >> (16 + 8 * f)) & 0xffu) << 8;
+                };
+                const auto read_k = [&](const char *at) {
+#pragma unroll
+                    for (int c = 0; c < KC; ++c) k[c] = *reinterpret_cast<const uint4 *>(at + k_at[c]);
+                };
+                // A tile's operands are read ahead of their use by hand, V's while the weights are formed and the next tile's K
+                // in front of the second product: left alone, the compiler reads each just before its products, and the
+                // wave stands for the whole way to LDS every time.
+                read_k(stage);
+#pragma unroll 1
+                for (int j = 0; j < n_tiles; ++j) {
+                    f32x16_t s;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = -base;
+#pragma unroll
+                    for (int c = 0; c < KC; ++c) s = mfma_32(k[c], q[c], s);
+                    __builtin_amdgcn_sched_barrier(0);
+                    const char *v_from = stage + TW_STAGE / 2 + j * TILE_BYTES + v_at;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) v[dt][t] = *reinterpret_cast<const uint4 *>(v_from + (2 * t * DIM + dt * 32) * 16);
+                    read_k(stage + min(j + 1, n_tiles - 1) * TILE_BYTES);
+                    __builtin_amdgcn_sched_barrier(0);
+                    float z[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] = s[i] * scale.unit;
+                    if (!full) {
+                        const uint32_t mask = mask_of(j);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (!((mask >> i) & 1)) z[i] = -INFINITY;
+                    }
+                    float top = z[0];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
+                    top = max_xor32(top);
+                    if (__any(top > limit)) {
+                        const float to = top > limit ? base + top / scale.unit : base;
+                        const float down = (to - base) * scale.unit, old = limit == -INFINITY ? 0.f : exp2_fast(-down);
+                        base = to;
+                        limit = top > limit ? SLACK : limit;
+                        total *= old;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) z[i] -= down;
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) o[dt] *= old;
+                    }
+                    float sum = 0.f;
+                    uint4 p[2];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        float e[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) e[i] = exp2_fast(z[8 * t + i]);
+                        sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+                        p[t] = __builtin_bit_cast(uint4, X::pack_weights(e));
+                    }
+                    total += sum;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) o[dt] = mfma_32(v[dt][t], p[t], o[dt]);
+                }
+                if (finite) continue;
+                // infinities and NaN that a row sees (see TreeWave::add_special)
+#pragma unroll 1
+                for (int j = 0; j < n_tiles; ++j) {
+                    const uint32_t mask = mask_of(j);
+                    const char *from = tw_smem + spare * TW_STAGE + TW_STAGE / 2 + j * TILE_BYTES + v_at;
+#pragma unroll 1
+                    for (int kind = 0; kind < 3; ++kind)
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) {
+                            f32x16_t count;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) count[i] = 0.f;
+#pragma unroll
+                            for (int t = 0; t < 2; ++t) {
+                                float seen[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) seen[i] = (mask >> (8 * t + i)) & 1 ? 1.f : 0.f;
+                                const uint4 all = *reinterpret_cast<const uint4 *>(from + (2 * t * DIM + dt * 32) * 16);
+                                count = mfma_32(ones_of_kind<X>(all, kind), __builtin_bit_cast(uint4, X::pack_weights(seen)), count);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[dt][i] += count[i] > 0.f ? value_of_kind(kind) : 0.f;
+                        }
+                }
+            }
+
+            // result register i of a lane: channel 32 dt + 8 (i / 4) + 4 f + i % 4 of row m
+            if (active) {
+                const int f = here(lane) >> 5, row = row0 + (here(lane) & 31);
+                const float all = add_xor32(total), up = limit == -INFINITY ? -INFINITY : base * scale.unit;
+                if (row < rows) {
+                    if (whole) {
+                        const float by = all == 0.f ? 0.f : 1.f / all;
+                        const int node = row / A.group, head = h * A.group + row - node * A.group;
+                        const int64_t at = (int64_t)(S.start + node) * heads_q + head;
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) {
+                                bf16 to[4];
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) from_f32(o[dt][4 * b + c] * by, to + c);
+                                __builtin_memcpy(__builtin_assume_aligned(static_cast<bf16 *>(A.out) + at * DIM + dt * 32 + 8 * b + 4 * f, 8), to, 8);
+                            }
+                        if (f == 0 && A.lse != nullptr) A.lse[at] = all == 0.f ? -INFINITY : (up + log2f(all)) * LN2;
+                    } else {
+                        float *part = tree_part(A, blockIdx.x, first ? 0 : 1, DIM);
+                        const int at = row - block_row0;
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                            for (int b = 0; b < 4; ++b)
+                                *reinterpret_cast<float4 *>(part + (size_t)at * DIM + dt * 32 + 8 * b + 4 * f) =
+                                    make_float4(o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]);
+                        if (f == 0) *reinterpret_cast<float2 *>(part + (size_t)A.part_rows * DIM + 2 * at) = make_float2(up, all);
+                    }
+                }
+            }
+            u += s1 - s0;
+        }
+    }
+}
+
+}  // namespace svdp
