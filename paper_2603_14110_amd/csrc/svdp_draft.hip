@@ -77,30 +77,27 @@ svdp_status check_ws(void *ws, size_t ws_bytes, size_t need)
 struct AttnPlan {
     bool wide;              // rows over the waves of a block (k_tree_attn_wide), or tokens (k_tree_attn)
     int nt, block_bits, block_rows, part_rows;
+    int64_t steps, tasks;   // units of a request and head, and requests times heads times row tiles, at most
     size_t bytes;
 };
-AttnPlan attn_plan(int dt, int dim, int group, int max_nodes)
+AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, int max_nodes)
 {
-    const int64_t rows = (int64_t)group * max_nodes;
+    const int dt = c->dtype, dim = c->dim, group = heads_q / c->heads;
+    const int64_t rows = (int64_t)group * max_nodes, room = (int64_t)max_pages * c->page / TA_TILE, own = tiles(max_nodes, TA_TILE);
     AttnPlan p;
     p.wide = dt == SVDP_BF16 && dim <= 128 && rows > 64;
     p.nt = rows <= 16 || dim == 256 ? 1 : rows <= 32 || dt == SVDP_F32 ? 2 : 4;
-    p.block_bits = !p.wide && p.nt * dim <= 256 ? 9 : 8;
+    const bool two_waves = ta_waves(bytes_of(dt), dim, p.nt) >= 2;       // of a SIMD
+    p.block_bits = !p.wide && two_waves ? 9 : 8;
     p.block_rows = p.wide ? TW_ROWS : 16 * p.nt;
     p.part_rows = (int)std::min<int64_t>(rows, p.block_rows);
+    const int unit = p.wide ? (dim == 64 ? tw_tiles<64>() : tw_tiles<128>()) : TA_WAVES;
+    p.steps = p.wide ? tiles(room, unit) + tiles(own, unit) : tiles(room + own, unit);
+    p.tasks = (rows + p.block_rows - 1) / p.block_rows * c->heads * R;
     p.bytes = align_up(((size_t)2 << p.block_bits) * p.part_rows * (dim + 2) * 4);
     return p;
 }
-// Units of the longest request that the table has room for, at most.
-int64_t attn_steps(int max_pages, int page, int max_nodes, int tiles_of_unit)
-{
-    return tiles((int64_t)max_pages * page / TA_TILE, tiles_of_unit) + tiles(tiles(max_nodes, TA_TILE), tiles_of_unit);
-}
-bool attn_units_fit(const svdp_kv_cache *c, int heads_q, int R, int max_pages, int max_nodes, const AttnPlan &p)
-{
-    const int64_t rows = (int64_t)(heads_q / c->heads) * max_nodes;
-    return attn_steps(max_pages, c->page, max_nodes, 1) * ((rows + p.block_rows - 1) / p.block_rows) * c->heads * R < INT_LIMIT;
-}
+constexpr int JOIN_WAVES = 2048;        // rows and heads from which the join has a wave for each, whatever the parts
 template <typename F>
 void on_dim(int dim, F &&f)
 {
@@ -134,8 +131,8 @@ size_t svdp_tree_attn_workspace_bytes(const svdp_kv_cache *cache, int32_t heads_
     if (check_cache(cache) != SVDP_OK || check_requests(R, 0, max_nodes) != SVDP_OK ||
         check_table(R, max_pages, cache->page) != SVDP_OK || heads_q < 1 || heads_q % cache->heads != 0)
         return 0;
-    const AttnPlan plan = attn_plan(cache->dtype, cache->dim, heads_q / cache->heads, max_nodes);
-    return attn_units_fit(cache, heads_q, R, max_pages, max_nodes, plan) ? plan.bytes : 0;
+    const AttnPlan plan = attn_plan(cache, heads_q, R, max_pages, max_nodes);
+    return plan.steps * plan.tasks < INT_LIMIT ? plan.bytes : 0;
 }
 
 svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void *q, int64_t q_stride, const void *k,
@@ -152,7 +149,7 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     const int dt = cache->dtype, dim = cache->dim;
     if (layer < 0 || layer >= cache->layers || heads_q < 1 || heads_q % cache->heads != 0 || !std::isfinite(scale * LOG2E))
         return SVDP_ERR_INVALID_ARG;
-    if (heads_q > 65535) return SVDP_ERR_UNSUPPORTED;
+    if ((int64_t)T * heads_q >= INT_LIMIT) return SVDP_ERR_UNSUPPORTED;
     if (T == 0) return SVDP_OK;
     if (!q || !k || !v || !out || !table || !lens || !starts || !aligned16(q) || !aligned16(k) || !aligned16(v) ||
         !aligned16(out) || !aligned_to(table, 4) || !aligned_to(lens, 4) || !aligned_to(starts, 4) ||
@@ -162,8 +159,8 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
         v_stride < (int64_t)cache->heads * dim || !whole_vectors(q_stride, dt) || !whole_vectors(k_stride, dt) ||
         !whole_vectors(v_stride, dt))
         return SVDP_ERR_INVALID_ARG;
-    const AttnPlan plan = attn_plan(dt, dim, heads_q / cache->heads, max_nodes);
-    if (!attn_units_fit(cache, heads_q, R, max_pages, max_nodes, plan)) return SVDP_ERR_UNSUPPORTED;
+    const AttnPlan plan = attn_plan(cache, heads_q, R, max_pages, max_nodes);
+    if (plan.steps * plan.tasks >= INT_LIMIT) return SVDP_ERR_UNSUPPORTED;
     st = check_ws(ws, ws_bytes, plan.bytes);
     if (st != SVDP_OK) return st;
     const size_t layer_bytes = (size_t)cache->pages * cache->heads * cache->page * dim * bytes_of(dt);
@@ -197,11 +194,15 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const dim3 blocks(1 << plan.block_bits);
     bool granted = true;
-    // a request of one unit is never cut
-    const auto join = [&](auto wt, auto dc, auto cut, int tiles_of_unit) {
-        if (attn_steps(max_pages, cache->page, max_nodes, tiles_of_unit) > 1)
-            launch((k_tree_join<typename decltype(wt)::type, decltype(dc)::value, decltype(cut)>), dim3(T, heads_q), dim3(TA_THREADS),
-                   0, hs, A);
+    // A request of one unit is never cut.  A row has at most blocks / heads parts and two more: few, or many rows, a wave each.
+    const int items = T * heads_q;
+    const bool shared = items < JOIN_WAVES && (1 << plan.block_bits) / cache->heads + 2 > 8;
+    const auto join = [&](auto wt, auto dc, auto cut) {
+        using W = typename decltype(wt)::type;
+        constexpr int DIM = decltype(dc)::value;
+        if (plan.steps <= 1) return;
+        if (shared) launch((k_tree_join<W, DIM, decltype(cut), true>), dim3(items), dim3(TA_THREADS), 0, hs, A);
+        else launch((k_tree_join<W, DIM, decltype(cut), false>), dim3(tiles(items, TA_WAVES)), dim3(TA_THREADS), 0, hs, A);
     };
     on_dim(dim, [&](auto dc) {
         constexpr int DIM = decltype(dc)::value;
@@ -210,7 +211,7 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
                 granted = grant_lds<k_tree_attn_wide<DIM>>(TW_LDS);
                 if (!granted) return;
                 launch(k_tree_attn_wide<DIM>, blocks, dim3(TW_THREADS), TW_LDS, hs, A);
-                join(Type<bf16>{}, dc, TreeCut<TW_ROWS, tw_tiles<DIM>(), true>{}, tw_tiles<DIM>());
+                join(Type<bf16>{}, dc, TreeCut<TW_ROWS, tw_tiles<DIM>(), true>{});
                 return;
             }
         on_tiles(plan.nt, [&](auto nc) {
@@ -219,7 +220,7 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
                 using W = typename decltype(wt)::type;
                 if constexpr (NT == 1 || (DIM <= 128 && (NT == 2 || std::is_same<W, bf16>::value))) {
                     launch((k_tree_attn<W, DIM, NT>), blocks, dim3(TA_THREADS), 0, hs, A);
-                    join(wt, dc, TreeCut<16 * NT, TA_WAVES, false>{}, TA_WAVES);
+                    join(wt, dc, TreeCut<16 * NT, TA_WAVES, false>{});
                 }
             });
         });

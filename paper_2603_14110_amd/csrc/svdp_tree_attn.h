@@ -26,8 +26,7 @@
 
 namespace svdp {
 
-constexpr int TA_THREADS = 256;
-constexpr int TA_WAVES = TA_THREADS / 64;
+constexpr int TA_WAVES = 4, TA_THREADS = 64 * TA_WAVES;
 constexpr int TA_TILE = 32;                      // tokens of a tile; divides every page
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -80,6 +79,14 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs &A, int r)
     s.row_tiles = (s.n * A.group + ROWS - 1) / ROWS;
     s.units = s.row_tiles * s.steps * A.heads;
     return s;
+}
+
+// The same value, of which the compiler knows nothing: what is computed from it stays where it is written.  Without it, what the
+// rare parts of a loop need per lane is kept in registers that the products' operands could be read ahead into.
+__device__ __forceinline__ int here(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
 }
 
 __device__ __forceinline__ int lane_of_first(uint64_t ballot) { return __ffsll((unsigned long long)ballot) - 1; }
@@ -385,13 +392,19 @@ struct TreeScale {
 };
 
 // One block: its piece of the row of units, a segment (what it has of one request, head and row tile) after the other.
+// Waves of a SIMD that its registers have room for: the sum, Q, and one tile of K and of V.  (Three where they would fit measured
+// the same as two.)
+constexpr int ta_waves(int element, int dim, int nt)
+{
+    return nt * (dim / 4 + dim * element / 16) + 2 * dim * element / 8 <= 200 ? 2 : 1;
+}
 template <typename W, int DIM, int NT>
-__global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
+__global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tree_attn(TreeAttnArgs A)
 {
     using X = TreeTile<W, DIM>;
     using Cut = TreeCut<16 * NT, TA_WAVES, false>;
     constexpr int ROWS = Cut::ROWS, E = X::E, KC = X::KC, VT = X::VT, DT = DIM / 16;
-    constexpr int DC = DIM * NT <= 128 ? DIM : 128 / NT;          // channels that the waves' sums meet in LDS by: 32 KB
+    constexpr int DC = DIM * NT <= 128 ? DIM : 128 / NT;       // channels that the waves' sums meet in LDS by: 32 KB
     __shared__ float s_top[TA_WAVES][ROWS], s_total[TA_WAVES][ROWS];
     __shared__ __align__(16) float s_sum[TA_WAVES][ROWS][DC + 4];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, m = lane & 15;
@@ -403,6 +416,7 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
     const int u1 = tree_begin(blockIdx.x + 1, units, A.block_bits);
     if (u >= u1) return;
     int rem, r = tree_request<Cut>(A, u, lane, own, upto, &rem);
+
     for (bool first = true; u < u1; ++r, rem = 0) {
         const TreeSpan S = tree_span<Cut>(A, __builtin_amdgcn_readfirstlane(r));
         if (S.units == 0) continue;
@@ -415,20 +429,33 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
 
             // Q of the rows (a row past the last one repeats it: computed and never written)
             uint4 q[KC][NT];
-            uint64_t sees[NT];
-            const TreeScale scale(A.scale, X::SIGNS);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int row = min(row0 + 16 * nt + m, rows - 1), node = row / A.group, head = h * A.group + row - node * A.group;
                 const W *from = static_cast<const W *>(A.q) + (S.start + node) * A.q_stride + (int64_t)head * DIM + g * E;
 #pragma unroll
-                for (int c = 0; c < KC; ++c) q[c][nt] = scale.of(load_raw(from + c * 4 * E));
-                sees[nt] = A.tree != nullptr ? A.tree[S.start + node] : ~0ull >> (63 - node);
+                for (int c = 0; c < KC; ++c) q[c][nt] = load_raw(from + c * 4 * E);
             }
+
+            // cached tokens: K of the next tile is requested when this one's has been used, and so is V
+            int i = s0 * TA_WAVES + wave, id = -1, id_next = -1;
+            const int i_end = min(s1 * TA_WAVES, S.tiles), per_page = A.page_bits - 5;
+            const auto page_of = [&](int tile) { return table[min(tile, S.tiles - 1) >> per_page]; };
+            const auto real = [&](int id) { return (uint32_t)id < (uint32_t)A.pages; };
+            const auto tile_at = [&](int tile, int id) {
+                const int64_t page = (int64_t)(real(id) ? id : 0) * A.heads + h;
+                return (((page << per_page) + (tile & ((1 << per_page) - 1))) * TA_TILE) * DIM;
+            };
+            const TreeScale scale(A.scale, X::SIGNS);
+            const auto scale_q = [&] {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < KC; ++c) q[c][nt] = scale.of(q[c][nt]);
+            };
             TreeWave<W, DIM, NT> mine;
             typename X::Weights p[NT][1];
             mine.clear();
-
             const auto scores = [&](const uint4 (&k)[2][KC], float (&z)[NT][8]) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -442,16 +469,9 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
                     }
             };
 
-            // cached tokens: K of the next tile is requested when this one's has been used, and so is V
-            int i = s0 * TA_WAVES + wave;
-            const int i_end = min(s1 * TA_WAVES, S.tiles), per_page = A.page_bits - 5;
-            if (i < i_end) {
-                const auto page_of = [&](int tile) { return table[min(tile, S.tiles - 1) >> per_page]; };
-                const auto real = [&](int id) { return (uint32_t)id < (uint32_t)A.pages; };
-                const auto tile_at = [&](int tile, int id) {
-                    const int64_t page = (int64_t)(real(id) ? id : 0) * A.heads + h;
-                    return (((page << per_page) + (tile & ((1 << per_page) - 1))) * TA_TILE) * DIM;
-                };
+            if (i >= i_end) {
+                scale_q();
+            } else {
                 uint4 k[2][KC], v[DT][VT];
                 const auto load_k = [&](int64_t at) {
                     const W *from = static_cast<const W *>(A.K) + at;
@@ -467,9 +487,11 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
 #pragma unroll
                         for (int t = 0; t < VT; ++t) v[dt][t] = load_raw(from + (X::pack(t, g) * DIM + dt * 16 + m) * E);
                 };
-                int id = page_of(i), id_next = page_of(i + TA_WAVES);
+                id = page_of(i);
+                id_next = page_of(i + TA_WAVES);
                 load_k(tile_at(i, id));
                 load_v(tile_at(i, id));
+                scale_q();                                       // only now what waits for Q
                 for (; i < i_end; i += TA_WAVES) {
                     const int count = real(id) ? min(S.len - i * TA_TILE, TA_TILE) : 0;
                     id = id_next;
@@ -499,14 +521,39 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
             // the tree's own tokens
 #pragma unroll 1
             for (; i < min(s1 * TA_WAVES, S.tiles + (S.n + TA_TILE - 1) / TA_TILE); i += TA_WAVES) {
+                const int g = here(lane) >> 4, m = here(lane) & 15;
                 const int node0 = (i - S.tiles) * TA_TILE;
                 const W *key = static_cast<const W *>(A.k) + (int64_t)h * DIM, *value = static_cast<const W *>(A.v) + (int64_t)h * DIM;
-                uint4 k[2][KC];
+                // K, what the rows see, and (where the registers have room) V, all requested before anything is waited for
+                constexpr bool EARLY = NT * DIM <= 128 && DIM * (int)sizeof(W) <= 256;
+                uint4 k[2][KC], v[DT][VT];
+                uint64_t sees[NT];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const W *from = key + (S.start + min(node0 + X::key(t, m), S.n - 1)) * A.k_stride + g * E;
 #pragma unroll
                     for (int c = 0; c < KC; ++c) k[t][c] = load_raw(from + c * 4 * E);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int node = min(row0 + 16 * nt + m, rows - 1) / A.group;
+                    sees[nt] = A.tree != nullptr ? A.tree[S.start + node] : ~0ull >> (63 - node);
+                }
+                // these rows of V lie token by token: an operand is put together from its elements
+                const auto read_v = [&](int dt, uint4 (&to)[VT]) {
+#pragma unroll
+                    for (int t = 0; t < VT; ++t) {
+                        const int node = node0 + X::pack(t, g) * E;
+                        W in[E];
+#pragma unroll
+                        for (int j = 0; j < E; ++j) in[j] = value[(S.start + min(node + j, S.n - 1)) * A.v_stride + dt * 16 + m];
+                        __builtin_memcpy(&to[t], in, 16);
+                    }
+                };
+                if constexpr (EARLY) {
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) read_v(dt, v[dt]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
                 float z[NT][8];
                 scores(k, z);
@@ -522,31 +569,32 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
                     }
                 }
                 mine.template weights<1>(z, scale.unit, p);
-                // these rows of V lie token by token: an operand is put together from its elements
+                bool finite = true;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
-                    uint4 v[VT];
-                    bool finite = true;
+                    if constexpr (!EARLY) read_v(dt, v[dt]);
 #pragma unroll
                     for (int t = 0; t < VT; ++t) {
-                        const int node = node0 + X::pack(t, g) * E;
-                        W in[E];
-#pragma unroll
-                        for (int j = 0; j < E; ++j) in[j] = value[(S.start + min(node + j, S.n - 1)) * A.v_stride + dt * 16 + m];
-                        __builtin_memcpy(&v[t], in, 16);
-                        v[t] = X::first(v[t], S.n - node);
-                        finite = finite && X::finite(v[t]);
+                        v[dt][t] = X::first(v[dt][t], S.n - node0 - X::pack(t, g) * E);
+                        finite = finite && X::finite(v[dt][t]);
+                        v[dt][t] = only_finite<X>(v[dt][t]);
                     }
-                    if (!__all(finite)) {
-                        mine.add_special(dt, v, mask);
+                    mine.add(dt, v[dt], p);
+                }
+                if (!__all(finite)) {
 #pragma unroll
-                        for (int t = 0; t < VT; ++t) v[t] = only_finite<X>(v[t]);
+                    for (int dt = 0; dt < DT; ++dt) {
+                        uint4 all[VT];
+                        read_v(dt, all);
+#pragma unroll
+                        for (int t = 0; t < VT; ++t) all[t] = X::first(all[t], S.n - node0 - X::pack(t, g) * E);
+                        mine.add_special(dt, all, mask);
                     }
-                    mine.add(dt, v, p);
                 }
             }
 
             // the waves' sums together, DC channels at a time
+            const int g = here(lane) >> 4, m = here(lane) & 15;
             __syncthreads();
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -558,7 +606,10 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
             }
             __syncthreads();
             const auto top_of = [&](int row) {
-                return fmaxf(fmaxf(s_top[0][row], s_top[1][row]), fmaxf(s_top[2][row], s_top[3][row]));
+                float top = s_top[0][row];
+#pragma unroll
+                for (int w = 1; w < TA_WAVES; ++w) top = fmaxf(top, s_top[w][row]);
+                return top;
             };
             const auto total_of = [&](int row, float shift) {
                 float t = 0.f;
@@ -621,14 +672,16 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_attn(TreeAttnArgs A)
     }
 }
 
-// Parts of one row and head, where there are more than one: a block each, its waves taking every fourth part.
-template <typename W, int DIM, typename Cut>
+// The parts of a row and head, where there are more than one: a wave each (SHARED false), or a block each, whose waves take every
+// fourth part (few rows with many parts).
+template <typename W, int DIM, typename Cut, bool SHARED>
 __global__ __launch_bounds__(TA_THREADS) void k_tree_join(TreeAttnArgs A)
 {
-    constexpr int ROWS = Cut::ROWS, PER = DIM / 64;
-    __shared__ float s_top[TA_WAVES], s_total[TA_WAVES], s_sum[TA_WAVES][DIM];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, heads_q = A.heads * A.group;
-    const int t = blockIdx.x, hq = blockIdx.y, h = hq / A.group;
+    constexpr int ROWS = Cut::ROWS, PER = DIM / 64, STEP = SHARED ? TA_WAVES : 1, AHEAD = SHARED && DIM <= 128 ? 16 : 8;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), heads_q = A.heads * A.group;
+    const int item = SHARED ? blockIdx.x : blockIdx.x * TA_WAVES + wave, t = item / heads_q, hq = item - t * heads_q;
+    if (t >= A.T) return;
+    const int h = hq / A.group;
 
     int own, upto;
     const int units = tree_units<Cut>(A, lane, &own, &upto);
@@ -652,43 +705,75 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_join(TreeAttnArgs A)
     const TreeSpan S = tree_span<Cut>(A, r);
     const int node = t - S.start;
     if (node < 0 || node >= S.n) return;
-    const int row = node * A.group + hq - h * A.group, u0 = base + (h * S.row_tiles + row / ROWS) * S.steps;
+    const int row = node * A.group + hq - h * A.group, in_part = row % ROWS, u0 = base + (h * S.row_tiles + row / ROWS) * S.steps;
     const int b0 = tree_block_of(u0, units, A.block_bits), b1 = tree_block_of(u0 + S.steps - 1, units, A.block_bits);
     if (b0 == b1) return;                                        // one block had the whole and has written it
     // a block's first segment is its part 0: that of b0 is if b0 begins with this task
     const int part0 = tree_begin(b0, units, A.block_bits) == u0 ? 0 : 1;
 
-    float top = -INFINITY, total = 0.f, sum[PER] = {};
-    for (int b = b0 + wave; b <= b1; b += TA_WAVES) {
-        const float *part = tree_part(A, b, b == b0 ? part0 : 0, DIM);
-        const float2 head = *reinterpret_cast<const float2 *>(part + (size_t)A.part_rows * DIM + 2 * (row % ROWS));
-        const float other = head.x, weight = head.y;
-        const float next = fmaxf(top, other), shift = finite_shift(next);
-        const float old = exp2_fast(top - shift), by = exp2_fast(other - shift);
+    float top = -INFINITY, total = 0.f, sum[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum[i] = 0.f;
+    for (int b = b0 + (SHARED ? wave : 0); b <= b1; b += STEP * AHEAD) {
+        float2 head[AHEAD];
+        float in[AHEAD][PER];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int at = min(b + j * STEP, b1);
+            const float *part = tree_part(A, at, at == b0 ? part0 : 0, DIM);
+            head[j] = *reinterpret_cast<const float2 *>(part + (size_t)A.part_rows * DIM + 2 * in_part);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) in[j][i] = part[(size_t)in_part * DIM + lane * PER + i];
+        }
+        float next = top;
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (b + j * STEP > b1) head[j] = make_float2(-INFINITY, 0.f);
+            next = fmaxf(next, head[j].x);
+        }
+        const float shift = finite_shift(next), old = exp2_fast(top - shift);
         top = next;
-        total = total * old + weight * by;
+        total *= old;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) sum[i] = sum[i] * old + part[(size_t)(row % ROWS) * DIM + lane + 64 * i] * by;
+        for (int i = 0; i < PER; ++i) sum[i] *= old;
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (b + j * STEP > b1) break;
+            const float by = exp2_fast(head[j].x - shift);
+            total += head[j].y * by;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) sum[i] += in[j][i] * by;
+        }
     }
-    if (lane == 0) {
-        s_top[wave] = top;
-        s_total[wave] = total;
-    }
+    if constexpr (SHARED) {
+        __shared__ float s_top[TA_WAVES], s_total[TA_WAVES], s_sum[TA_WAVES][DIM];
+        if (lane == 0) {
+            s_top[wave] = top;
+            s_total[wave] = total;
+        }
 #pragma unroll
-    for (int i = 0; i < PER; ++i) s_sum[wave][lane + 64 * i] = sum[i];
-    __syncthreads();
-    if (tid >= DIM) return;
-    const float all = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])), shift = finite_shift(all);
-    float denominator = 0.f, o = 0.f;
+        for (int i = 0; i < PER; ++i) s_sum[wave][lane * PER + i] = sum[i];
+        __syncthreads();
+        if (wave > 0) return;
+        top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+        total = 0.f;
 #pragma unroll
-    for (int w = 0; w < TA_WAVES; ++w) {
-        const float by = exp2_fast(s_top[w] - shift);
-        denominator += s_total[w] * by;
-        o += s_sum[w][tid] * by;
+        for (int i = 0; i < PER; ++i) sum[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < TA_WAVES; ++w) {
+            const float by = exp2_fast(s_top[w] - finite_shift(top));
+            total += s_total[w] * by;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) sum[i] += s_sum[w][lane * PER + i] * by;
+        }
     }
     const int64_t at = (int64_t)t * heads_q + hq;
-    from_f32(denominator == 0.f ? 0.f : o / denominator, static_cast<W *>(A.out) + at * DIM + tid);
-    if (tid == 0 && A.lse != nullptr) A.lse[at] = denominator == 0.f ? -INFINITY : (all + log2f(denominator)) * LN2;
+    const float by = total == 0.f ? 0.f : 1.f / total;
+    W to[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) from_f32(sum[i] * by, to + i);
+    __builtin_memcpy(__builtin_assume_aligned(static_cast<W *>(A.out) + at * DIM + lane * PER, sizeof(to)), to, sizeof(to));
+    if (lane == 0 && A.lse != nullptr) A.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
 }
 
 }  // namespace svdp

@@ -24,14 +24,6 @@ __device__ __forceinline__ f32x16_t mfma_32(const uint4 &a, const uint4 &b, cons
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(ta_bf16x8, a), __builtin_bit_cast(ta_bf16x8, b), c, 0, 0, 0);
 }
 
-// The same value, of which the compiler knows nothing: what is computed from it stays where it is written.  Without it, what the
-// rare parts of a loop need per lane is kept in registers that the products' operands could be read ahead into.
-__device__ __forceinline__ int here(int v)
-{
-    asm volatile("" : "+v"(v));
-    return v;
-}
-
 // Token (of 32) that row `at` of K's operand stands for, and what its chunks are moved by.
 __device__ __forceinline__ int tw_token(int at) { return (at >> 4) * 16 + ((at >> 2) & 1) * 8 + ((at >> 3) & 1) * 4 + (at & 3); }
 __device__ __forceinline__ int tw_swizzle(int token, int dim) { return dim == 64 ? token & 7 : token & 15; }
