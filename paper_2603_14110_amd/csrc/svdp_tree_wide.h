@@ -1,12 +1,15 @@
 // Attention of drafted tokens where a request has many rows (svdp_tree_attn.h holds the division of the work and the join).
 //
 // The waves of a block take different rows of the SAME tokens, 32 each: K and V come from memory once for 256 rows.
-// Their tiles pass through LDS, in three stages of 32 KB that are filled straight from memory, two stages ahead, with one
-// barrier a stage; each wave keeps its own rows' base, denominator and sum, and nothing is exchanged between waves.
+// Their tiles pass through LDS, in two stages of 64 KB that are filled straight from memory, one while the other is worked on, with
+// one barrier a stage; each wave keeps its own rows' base, denominator and sum, and nothing is exchanged between waves.
 // Products are 32 x 32 x 16: S^T = K Q^T leaves a lane with 16 scores of one row (token of result register i in lane half f:
 // 16 (i / 8) + 8 f + i % 8, by the choice of K rows), which are the tokens that O^T += V^T P^T wants of that lane.
 // LDS: K rows of DIM channels, 16-byte chunk c of token i at slot c ^ swizzle(i), so that the tokens of an operand read lie in different
 // banks; V as in memory, of which 32 lanes read consecutive 512 bytes.
+// What bounds it: a tile of 32 tokens is 528 cycles of a SIMD's matrix unit for each of its two waves, and about 600 of its
+// vector unit (16 exponentials and some 70 other instructions), side by side; what a stage costs besides (its barrier, addresses,
+// the first read of K) is why a stage is as large as LDS allows.
 #pragma once
 
 #include "svdp_tree_attn.h"
@@ -14,10 +17,9 @@
 namespace svdp {
 
 constexpr int TW_THREADS = 512, TW_WAVES = TW_THREADS / 64, TW_ROWS = 32 * TW_WAVES;
-constexpr int TW_STAGE = 32 << 10, TW_STAGES = 3, TW_LDS = TW_STAGES * TW_STAGE;
+constexpr int TW_STAGE = 64 << 10, TW_LDS = 2 * TW_STAGE;
 template <int DIM>
-constexpr int tw_tiles() { return TW_STAGE / 2 / (TA_TILE * DIM * 2); }          // of a stage: 4 or 2
-
+constexpr int tw_tiles() { return TW_STAGE / 2 / (TA_TILE * DIM * 2); }          // of a stage: 8 or 4
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16_t mfma_32(const uint4 &a, const uint4 &b, const f32x16_t &c)
 {
@@ -32,12 +34,15 @@ template <int DIM>
 __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_tree_attn_wide(TreeAttnArgs A)
 {
     using X = TreeTile<bf16, DIM>;
-    constexpr int TILES = tw_tiles<DIM>(), KC = DIM / 16, DT = DIM / 32;
+    constexpr int TILES = tw_tiles<DIM>(), KC = DIM / 16, DT = DIM / 32, CHUNKS = DIM / 8;
     using Cut = TreeCut<TW_ROWS, TILES, true>;
-    constexpr int TILE_BYTES = TA_TILE * DIM * 2, CHUNKS = DIM / 8;
+    constexpr int TILE_BYTES = TA_TILE * DIM * 2, V_AT = TW_STAGE / 2;
+    static_assert(TILES * TA_TILE >= 64, "the tree's tokens are one stage");
+    // a stage of the tree's tokens: K where it always is; V as it comes, then in packs (finite elements), and as it is in packs
+    constexpr int OWN_RAW = V_AT, OWN_PACKS = V_AT + TW_STAGE / 4, OWN_ALL = TW_STAGE / 4;
     extern __shared__ __align__(16) char tw_smem[];
+    __shared__ uint64_t s_sees[64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), f = lane >> 5, m = lane & 31;
-    const int heads_q = A.heads * A.group;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t *)tw_smem;
 
     int own, upto;
@@ -47,11 +52,12 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
     if (u >= u1) return;
     int rem, r = tree_request<Cut>(A, u, lane, own, upto, &rem);
 
-    // where a lane's operands lie in a tile
-    int k_at[KC];
-#pragma unroll
-    for (int c = 0; c < KC; ++c) k_at[c] = (tw_token(m) * CHUNKS + ((2 * c + f) ^ tw_swizzle(tw_token(m), DIM))) * 16;
+    // where a lane's operands lie in a tile (chunk c of K: ^ 32 c)
+    const int k_at = tw_token(m) * CHUNKS * 16 + ((f ^ tw_swizzle(tw_token(m), DIM)) * 16);
     const int v_at = (f * DIM + m) * 16;
+    // what a wave brings of a stage, 1 KB eight times: 128 channels: K or V of a tile; 64 channels: K and V of a tile
+    const int fill_tile = DIM == 128 ? wave >> 1 : wave;
+    const int fill_k = (lane / CHUNKS) * CHUNKS * 16 + (((lane % CHUNKS) ^ tw_swizzle(lane / CHUNKS, DIM)) * 16);
 
     for (bool first = true; u < u1; ++r, rem = 0) {
         const TreeSpan S = tree_span<Cut>(A, __builtin_amdgcn_readfirstlane(r));
@@ -67,46 +73,54 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
             // Page ids: a lane each for 64 pages, read out per tile.  (Read one by one through the scalar cache, the wait for
             // them also holds up the reads from LDS.)
             int window = -64, window_ids = 0;
-            const auto pages_of = [&](int step, int (&ids)[TILES]) {
-                const int last = min(step * TILES + TILES - 1, S.tiles - 1) >> per_page;
-                if (last >= window + 64) {
-                    window = min(step * TILES, S.tiles - 1) >> per_page;
-                    window_ids = here(A.table[(size_t)r * A.max_pages + min(window + lane, (S.tiles - 1) >> per_page)]);
+            bool window_whole = true;                            // no page of it is missing
+            const auto see_pages = [&](int step) {
+                const int last_page = (S.tiles - 1) >> per_page;
+                if (min((step * TILES + TILES - 1) >> per_page, last_page) >= window + 64) {
+                    window = (max(step - 1, s0) * TILES) >> per_page;            // the stage that is worked on as well
+                    window_ids = here(A.table[(size_t)r * A.max_pages + min(window + (tid & 63), last_page)]);
+                    window_whole = __all((uint32_t)window_ids < (uint32_t)A.pages);
                 }
-#pragma unroll
-                for (int j = 0; j < TILES; ++j)
-                    ids[j] = __builtin_amdgcn_readlane(window_ids, (min(step * TILES + j, S.tiles - 1) >> per_page) - window);
             };
-            const auto real = [&](int id) { return (uint32_t)id < (uint32_t)A.pages; };
-            // a stage from memory: 16 bytes a thread, four times
-            const auto fill = [&](int step, int buffer, const int (&ids)[TILES]) {
+            const auto page_of = [&](int tile) {
+                return __builtin_amdgcn_readlane(window_ids, (min(tile, S.tiles - 1) >> per_page) - window);
+            };
+            const auto fill = [&](int step, int stage) {
+                see_pages(step);
+                const int tile = min(step * TILES + fill_tile, S.tiles - 1), id = page_of(tile);
+                const int64_t page = (int64_t)((uint32_t)id < (uint32_t)A.pages ? id : 0) * A.heads + h;
+                const int64_t at = ((page << per_page) + (tile & ((1 << per_page) - 1))) * TILE_BYTES;
+                const uint32_t to = lds0 + stage + fill_tile * TILE_BYTES;
+                if constexpr (DIM == 128) {
+                    const char *from = static_cast<const char *>(wave & 1 ? A.V : A.K) + at;
+                    const int off = wave & 1 ? lane * 16 : fill_k, turn = wave & 1 ? 0 : 64;     // rows of 16 chunks: four of them in 1 KB
 #pragma unroll
-                for (int part = 0; part < 4; ++part) {           // K, K, V, V
-                    constexpr int IN_TILE = TILE_BYTES / 16;
-                    const int p0 = (part & 1) * TW_THREADS + wave * 64, j = p0 / IN_TILE;
-                    int id = ids[0];
+                    for (int i = 0; i < 8; ++i) load_to_lds(from + i * 1024 + (off ^ ((i & 3) * turn)), to + (wave & 1 ? V_AT : 0) + i * 1024);
+                } else {
 #pragma unroll
-                    for (int i = 1; i < TILES; ++i) id = i == j ? ids[i] : id;
-                    const int tile = min(step * TILES + j, S.tiles - 1), p = p0 % IN_TILE + lane;
-                    const int64_t page = (int64_t)(real(id) ? id : 0) * A.heads + h;
-                    const int64_t at = ((page << per_page) + (tile & ((1 << per_page) - 1))) * TILE_BYTES;
-                    const int token = p / CHUNKS, slot = p % CHUNKS;
-                    const int piece = part < 2 ? token * CHUNKS + (slot ^ tw_swizzle(token, DIM)) : p;
-                    load_to_lds(static_cast<const char *>(part < 2 ? A.K : A.V) + at + piece * 16,
-                                lds0 + buffer * TW_STAGE + (part >> 1) * (TW_STAGE / 2) + p0 * 16);
+                    for (int i = 0; i < 4; ++i) {
+                        load_to_lds(static_cast<const char *>(A.K) + at + i * 1024 + fill_k, to + i * 1024);
+                        load_to_lds(static_cast<const char *>(A.V) + at + i * 1024 + lane * 16, to + V_AT + i * 1024);
+                    }
+                }
+            };
+            // the tree's own tokens: rows of K and of V as they are (those past the last one repeat it)
+            const auto fill_own = [&](int stage) {
+                const int lane = here(tid) & 63;
+                for (int p0 = wave * 64; p0 < (S.n + TA_TILE - 1) / TA_TILE * TA_TILE * CHUNKS; p0 += TW_THREADS) {
+                    const int p = p0 + lane, token = p / CHUNKS, slot = p % CHUNKS;
+                    const int64_t row = S.start + min(token, S.n - 1);
+                    const int piece = (slot ^ tw_swizzle(token, DIM)) * 8;
+                    load_to_lds(static_cast<const bf16 *>(A.k) + row * A.k_stride + h * DIM + piece, lds0 + stage + p0 * 16);
+                    load_to_lds(static_cast<const bf16 *>(A.v) + row * A.v_stride + h * DIM + slot * 8, lds0 + stage + OWN_RAW + p0 * 16);
                 }
             };
 
             stage_barrier<0>();                                  // the last segment's stages and stores are done with
-            int buffer = 0;
-            int ids[TILES], ids_1[TILES], ids_2[TILES];          // of this stage and of the next two
-            if (s0 < s_end) {
-                pages_of(s0, ids);
-                pages_of(s0 + 1, ids_1);
-                pages_of(s0 + 2, ids_2);
-                fill(s0, 0, ids);
-                if (s0 + 1 < s_end) fill(s0 + 1, 1, ids_1);
-            }
+            int stage = 0;
+            if (s0 < s_end) fill(s0, 0);
+            else fill_own(0);
+            if (s1 > cached_steps && tid < S.n) s_sees[tid] = A.tree != nullptr ? A.tree[S.start + tid] : ~0ull >> (63 - tid);
 
             const TreeScale scale(A.scale, X::SIGNS);
             uint4 q[KC], k[KC], v[DT][2];
@@ -124,103 +138,81 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
 
-            for (int step = s0; step < s1; ++step) {
+            for (int step = s0; step < s1; ++step, stage ^= TW_STAGE) {
                 const bool own_tokens = step >= cached_steps;    // the tree's
-                const int spare = buffer == TW_STAGES - 1 ? 0 : buffer + 1;
-                bool full = true, finite = true;
-                char *stage = tw_smem + buffer * TW_STAGE;
-                int counts[TILES], n_tiles = TILES;              // tokens of each tile: fewer at the end, none where there is no page
-                const int node0 = (step - cached_steps) * TILES * TA_TILE;
-                if (!own_tokens) {
-                    if (step + 1 < s_end) stage_barrier<4>();
-                    else stage_barrier<0>();
-                    if (step + 2 < s_end) fill(step + 2, buffer >= 1 ? buffer - 1 : buffer + 2, ids_2);
-                    buffer = spare;
-#pragma unroll
+                stage_barrier<0>();
+                const bool full = !own_tokens && window_whole && (step + 1) * TILES * TA_TILE <= S.len;
+                uint64_t counts = 0;                             // where it is not full: tokens of each tile, eight bits each
+                bool finite = true;
+                if (!full) {
                     for (int j = 0; j < TILES; ++j) {
-                        counts[j] = real(ids[j]) ? min(max(S.len - (step * TILES + j) * TA_TILE, 0), TA_TILE) : 0;
-                        full = full && counts[j] == TA_TILE;
-                        ids[j] = ids_1[j];
-                        ids_1[j] = ids_2[j];
+                        const int tile = step * TILES + j;
+                        const int count = own_tokens ? S.n - j * TA_TILE : (uint32_t)page_of(tile) < (uint32_t)A.pages ? S.len - tile * TA_TILE : 0;
+                        counts |= (uint64_t)min(max(count, 0), TA_TILE) << (8 * j);
                     }
-                    pages_of(step + 3, ids_2);
-                    if (!full) {                                 // what lies behind them in V must not be NaN
-                        for (int e = here(tid); e < TW_STAGE / 32; e += TW_THREADS) {
-                            const int tile = e / (TILE_BYTES / 16), pack = e % (TILE_BYTES / 16) / DIM;
-                            uint4 *at = reinterpret_cast<uint4 *>(stage + TW_STAGE / 2) + e;
-                            int count = counts[0];
-#pragma unroll
-                            for (int i = 1; i < TILES; ++i) count = i == tile ? counts[i] : count;
-                            *at = X::first(*at, count - pack * 8);
-                        }
-                        __syncthreads();
-                    }
-                } else {                                         // into the same layout, V's packs element by element
-                    const int there = min(S.n - node0, TILES * TA_TILE);
-                    n_tiles = (there + TA_TILE - 1) / TA_TILE;
-                    full = false;
-#pragma unroll
-                    for (int j = 0; j < TILES; ++j) counts[j] = min(max(there - j * TA_TILE, 0), TA_TILE);
-                    stage_barrier<0>();
+                }
+                const auto count_of = [&](int j) { return (int)(counts >> (8 * j)) & 0xff; };
+                if (step + 1 < s_end) fill(step + 1, stage ^ TW_STAGE);
+                else if (step + 1 < s1) fill_own(stage ^ TW_STAGE);
+                char *const lds = tw_smem + stage;
+                const int n_tiles = own_tokens ? (S.n + TA_TILE - 1) / TA_TILE : TILES;
+                if (own_tokens) {                                // V into packs
                     int odd = 0;
                     for (int e = here(tid); e < n_tiles * TA_TILE * CHUNKS; e += TW_THREADS) {
-                        const int i = e / CHUNKS, c = e - i * CHUNKS, tile = i / TA_TILE, token = i % TA_TILE;
-                        uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
-                        if (i < there) {
-                            a = load_raw(static_cast<const bf16 *>(A.k) + (S.start + node0 + i) * A.k_stride + (int64_t)h * DIM + c * 8);
-                            b = load_raw(static_cast<const bf16 *>(A.v) + (S.start + node0 + i) * A.v_stride + (int64_t)h * DIM + c * 8);
-                        }
-                        *reinterpret_cast<uint4 *>(stage + tile * TILE_BYTES + (token * CHUNKS + (c ^ tw_swizzle(token, DIM))) * 16) = a;
-                        const int at = TW_STAGE / 2 + tile * TILE_BYTES + (((token >> 3) * DIM + c * 8) * 8 + (token & 7)) * 2;
+                        const int i = e / CHUNKS, c = e - i * CHUNKS;
+                        uint4 all = *reinterpret_cast<const uint4 *>(lds + OWN_RAW + e * 16);
+                        if (i >= S.n) all = make_uint4(0u, 0u, 0u, 0u);
+                        const int at = (i / TA_TILE) * TILE_BYTES + ((((i % TA_TILE) >> 3) * DIM + c * 8) * 8 + (i & 7)) * 2;
                         const auto put = [&](char *to, const uint4 &what) {
                             const uint32_t w[4] = {what.x, what.y, what.z, what.w};
 #pragma unroll
                             for (int d = 0; d < 8; ++d) *reinterpret_cast<uint16_t *>(to + d * 16) = (uint16_t)(w[d >> 1] >> (16 * (d & 1)));
                         };
-                        put(stage + at, only_finite<X>(b));
-                        put(tw_smem + spare * TW_STAGE + at, b);
-                        odd |= X::finite(b) ? 0 : 1;
+                        put(lds + OWN_PACKS + at, only_finite<X>(all));
+                        put(lds + OWN_ALL + at, all);
+                        odd |= X::finite(all) ? 0 : 1;
                     }
                     finite = __syncthreads_or(odd) == 0;
+                } else if (!full) {                              // what lies behind the tokens in V must not be NaN
+                    for (int e = here(tid); e < V_AT / 16; e += TW_THREADS) {
+                        const int tile = e / (TILE_BYTES / 16), pack = e % (TILE_BYTES / 16) / DIM;
+                        uint4 *at = reinterpret_cast<uint4 *>(lds + V_AT) + e;
+                        *at = X::first(*at, count_of(tile) - pack * 8);
+                    }
+                    __syncthreads();
                 }
                 if (!active) continue;
 
                 // which of the lane's 16 tokens its row sees
                 const auto mask_of = [&](int j) {
                     const int f = here(lane) >> 5, m = here(lane) & 31;
-                    int count = counts[0];
-#pragma unroll
-                    for (int i = 1; i < TILES; ++i) count = i == j ? counts[i] : count;
-                    uint32_t seen = (uint32_t)((1ull << count) - 1);
-                    if (own_tokens) {
-                        const int node = min(row0 + m, rows - 1) / A.group;
-                        const uint64_t sees = A.tree != nullptr ? A.tree[S.start + node] : ~0ull >> (63 - node);
-                        seen &= (uint32_t)(sees >> (node0 + j * TA_TILE));
-                    }
+                    uint32_t seen = (uint32_t)((1ull << count_of(j)) - 1);
+                    if (own_tokens) seen &= (uint32_t)(s_sees[min(row0 + m, rows - 1) / A.group] >> (j * TA_TILE));
                     return ((seen >> (8 * f)) & 0xffu) | ((seen >> (16 + 8 * f)) & 0xffu) << 8;
-                };
-                const auto read_k = [&](const char *at) {
-#pragma unroll
-                    for (int c = 0; c < KC; ++c) k[c] = *reinterpret_cast<const uint4 *>(at + k_at[c]);
                 };
                 // A tile's operands are read ahead of their use by hand, V's while the weights are formed and the next tile's K
                 // in front of the second product: left alone, the compiler reads each just before its products, and the
                 // wave stands for the whole way to LDS every time.
-                read_k(stage);
+                const char *k_from = lds, *v_from = lds + (own_tokens ? OWN_PACKS : V_AT) + v_at;
+                const auto read_k = [&] {
+#pragma unroll
+                    for (int c = 0; c < KC; ++c) k[c] = *reinterpret_cast<const uint4 *>(k_from + (k_at ^ (c * 32)));
+                };
+                read_k();
 #pragma unroll 1
-                for (int j = 0; j < n_tiles; ++j) {
+                for (int j = 0; j < n_tiles; ++j, v_from += TILE_BYTES) {
                     f32x16_t s;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = -base;
 #pragma unroll
                     for (int c = 0; c < KC; ++c) s = mfma_32(k[c], q[c], s);
                     __builtin_amdgcn_sched_barrier(0);
-                    const char *v_from = stage + TW_STAGE / 2 + j * TILE_BYTES + v_at;
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                         for (int t = 0; t < 2; ++t) v[dt][t] = *reinterpret_cast<const uint4 *>(v_from + (2 * t * DIM + dt * 32) * 16);
-                    read_k(stage + min(j + 1, n_tiles - 1) * TILE_BYTES);
+                    if (j + 1 < n_tiles) k_from += TILE_BYTES;
+                    read_k();
                     __builtin_amdgcn_sched_barrier(0);
                     float z[16];
 #pragma unroll
@@ -267,7 +259,7 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
 #pragma unroll 1
                 for (int j = 0; j < n_tiles; ++j) {
                     const uint32_t mask = mask_of(j);
-                    const char *from = tw_smem + spare * TW_STAGE + TW_STAGE / 2 + j * TILE_BYTES + v_at;
+                    const char *from = lds + OWN_ALL + j * TILE_BYTES + v_at;
 #pragma unroll 1
                     for (int kind = 0; kind < 3; ++kind)
 #pragma unroll
@@ -297,7 +289,7 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                     if (whole) {
                         const float by = all == 0.f ? 0.f : 1.f / all;
                         const int node = row / A.group, head = h * A.group + row - node * A.group;
-                        const int64_t at = (int64_t)(S.start + node) * heads_q + head;
+                        const int64_t at = (int64_t)(S.start + node) * A.heads * A.group + head;
 #pragma unroll
                         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
