@@ -254,10 +254,9 @@ __device__ __forceinline__ float max_xor32(float v)
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
-// Scores are taken relative to a `base` that follows their maximum: it moves only where a score exceeds it by more than SLACK in
-// base two (then to the maximum), so that the sums are rarely brought down to a new one.  A weight is then below 2^SLACK, far from any
-// limit of fp32 (nor of bf16, which has the same exponents).  The base is where the score products' accumulators start, so
-// that a score costs one multiplication in front of its exponential.
+// Scores are taken relative to a `shift` that follows their maximum, in base two: it moves only where a score exceeds it by more than
+// SLACK (then to the maximum), so that the sums are rarely brought down to a new one.  A weight is then below 2^SLACK, far from any
+// limit of fp32 (nor of bf16, which has the same exponents).
 constexpr float SLACK = 8.f;
 // -inf (nothing but zero weights so far) must not make -inf - -inf
 __device__ __forceinline__ float finite_shift(float shift) { return shift == -INFINITY ? 0.f : shift; }
@@ -280,35 +279,33 @@ __device__ __forceinline__ uint4 ones_of_kind(const uint4 &v, int kind)
     });
 }
 
-// What a wave has of its rows: the sum O^T (channels 16 dt + 4 g + i of row m), the base, and the lane group's part of the denominator.
+// What a wave has of its rows: the sum O^T (channels 16 dt + 4 g + i of row m), the shift, and the lane group's part of the denominator.
 template <typename W, int DIM, int NT>
 struct TreeWave {
     using X = TreeTile<W, DIM>;
     using Weights = typename X::Weights;
     static constexpr int DT = DIM / 16, VT = X::VT;
     f32x4_t o[DT][NT];
-    float base[NT], total[NT];          // base: in units of `unit`; zero for a row that has not seen anything
-    float limit[NT];                    // what a relative score has to exceed for the base to move: -inf for such a row
+    float shift[NT], total[NT];         // shift: zero for a row that has not seen anything
+    float limit[NT];                    // what a relative score has to exceed for the shift to move: -inf for such a row
 
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            base[nt] = 0.f;
+            shift[nt] = 0.f;
             limit[nt] = -INFINITY;
             total[nt] = 0.f;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[dt][nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
     }
-    // where the accumulators of row tile nt's scores start
-    __device__ __forceinline__ f32x4_t start(int nt) const { return f32x4_t{-base[nt], -base[nt], -base[nt], -base[nt]}; }
-    // the base in base two, -inf for a row that has not seen anything
-    __device__ __forceinline__ float shift(int nt, float unit) const { return limit[nt] == -INFINITY ? -INFINITY : base[nt] * unit; }
+    // the maximum that others compare theirs with: -inf for a row that has not seen anything
+    __device__ __forceinline__ float top(int nt) const { return limit[nt] == -INFINITY ? -INFINITY : shift[nt]; }
 
-    // Scores relative to the base, times unit (> 0), in base two -> weights.
+    // Scores in base two, relative to the shift -> weights.
     template <int N>
-    __device__ __forceinline__ void weights(float (&z)[NT][8 * N], float unit, Weights (&w)[NT][N])
+    __device__ __forceinline__ void weights(float (&z)[NT][8 * N], Weights (&w)[NT][N])
     {
         float top[NT];
         bool grew = false;
@@ -323,10 +320,10 @@ struct TreeWave {
         if (__any(grew)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const float to = top[nt] > limit[nt] ? base[nt] + top[nt] / unit : base[nt];
-                // nothing so far: there is nothing to bring down, and the base may come down itself
-                const float down = (to - base[nt]) * unit, old = limit[nt] == -INFINITY ? 0.f : exp2_fast(-down);
-                base[nt] = to;
+                const float to = top[nt] > limit[nt] ? shift[nt] + top[nt] : shift[nt];
+                // nothing so far: there is nothing to bring down, and the shift may come down itself
+                const float down = to - shift[nt], old = limit[nt] == -INFINITY ? 0.f : exp2_fast(-down);
+                shift[nt] = to;
                 limit[nt] = top[nt] > limit[nt] ? SLACK : limit[nt];
                 total[nt] *= old;
 #pragma unroll
@@ -461,11 +458,11 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        f32x4_t s = mine.start(nt);
+                        f32x4_t s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int c = 0; c < KC; ++c) s = X::score(k[t][c], q[c][nt], s);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) z[nt][4 * t + i] = s[i] * scale.unit;
+                        for (int i = 0; i < 4; ++i) z[nt][4 * t + i] = fmaf(s[i], scale.unit, -mine.shift[nt]);
                     }
             };
 
@@ -511,7 +508,7 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
 #pragma unroll
                             for (int t = 0; t < VT; ++t) v[dt][t] = X::first(v[dt][t], count - X::pack(t, g) * E);
                     }
-                    mine.template weights<1>(z, scale.unit, p);
+                    mine.template weights<1>(z, p);
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) mine.add(dt, v[dt], p);
                     if (i + TA_WAVES < i_end) load_v(at);
@@ -568,7 +565,7 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
                         else z[nt][j] = -INFINITY;
                     }
                 }
-                mine.template weights<1>(z, scale.unit, p);
+                mine.template weights<1>(z, p);
                 bool finite = true;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
@@ -600,7 +597,7 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
             for (int nt = 0; nt < NT; ++nt) {
                 const float all = add_xor32(add_xor16(mine.total[nt]));
                 if (g == 0) {
-                    s_top[wave][16 * nt + m] = mine.shift(nt, scale.unit);
+                    s_top[wave][16 * nt + m] = mine.top(nt);
                     s_total[wave][16 * nt + m] = all;
                 }
             }
@@ -619,7 +616,7 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
             };
             float mine_by[NT];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mine_by[nt] = exp2_fast(mine.shift(nt, scale.unit) - finite_shift(top_of(16 * nt + m)));
+            for (int nt = 0; nt < NT; ++nt) mine_by[nt] = exp2_fast(mine.top(nt) - finite_shift(top_of(16 * nt + m)));
             float *part = tree_part(A, blockIdx.x, first ? 0 : 1, DIM);
 #pragma unroll
             for (int d0 = 0; d0 < DIM; d0 += DC) {

@@ -2,7 +2,7 @@
 //
 // The waves of a block take different rows of the SAME tokens, 32 each: K and V come from memory once for 256 rows.
 // Their tiles pass through LDS, in two stages of 64 KB that are filled straight from memory, one while the other is worked on, with
-// one barrier a stage; each wave keeps its own rows' base, denominator and sum, and nothing is exchanged between waves.
+// one barrier a stage; each wave keeps its own rows' shift, denominator and sum, and nothing is exchanged between waves.
 // Products are 32 x 32 x 16: S^T = K Q^T leaves a lane with 16 scores of one row (token of result register i in lane half f:
 // 16 (i / 8) + 8 f + i % 8, by the choice of K rows), which are the tokens that O^T += V^T P^T wants of that lane.
 // LDS: K rows of DIM channels, 16-byte chunk c of token i at slot c ^ swizzle(i), so that the tokens of an operand read lie in different
@@ -130,9 +130,9 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
 #pragma unroll
                 for (int c = 0; c < KC; ++c) q[c] = scale.of(load_raw(from + c * 16));
             }
-            // as in TreeWave: sum, base, denominator (the lane half's part), and what a score has to exceed for the base to move
+            // as in TreeWave: sum, shift, denominator (the lane half's part), and what a score has to exceed for the shift to move
             f32x16_t o[DT];
-            float base = 0.f, total = 0.f, limit = -INFINITY;
+            float shift = 0.f, total = 0.f, limit = -INFINITY;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -193,30 +193,32 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                 // A tile's operands are read ahead of their use by hand, V's while the weights are formed and the next tile's K
                 // in front of the second product: left alone, the compiler reads each just before its products, and the
                 // wave stands for the whole way to LDS every time.
-                const char *k_from = lds, *v_from = lds + (own_tokens ? OWN_PACKS : V_AT) + v_at;
-                const auto read_k = [&] {
+                const char *v_from = lds + (own_tokens ? OWN_PACKS : V_AT) + v_at, *k_from[KC];
 #pragma unroll
-                    for (int c = 0; c < KC; ++c) k[c] = *reinterpret_cast<const uint4 *>(k_from + (k_at ^ (c * 32)));
+                for (int c = 0; c < KC; ++c) k_from[c] = lds + (k_at ^ (c * 32));
+                const auto read_k = [&](int j) {
+#pragma unroll
+                    for (int c = 0; c < KC; ++c) k[c] = *reinterpret_cast<const uint4 *>(k_from[c] + j * TILE_BYTES);
                 };
-                read_k();
-#pragma unroll 1
-                for (int j = 0; j < n_tiles; ++j, v_from += TILE_BYTES) {
+                read_k(0);
+#pragma unroll
+                for (int j = 0; j < TILES; ++j) {
+                    if (j >= n_tiles) break;
                     f32x16_t s;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = -base;
+                    for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
                     for (int c = 0; c < KC; ++c) s = mfma_32(k[c], q[c], s);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                        for (int t = 0; t < 2; ++t) v[dt][t] = *reinterpret_cast<const uint4 *>(v_from + (2 * t * DIM + dt * 32) * 16);
-                    if (j + 1 < n_tiles) k_from += TILE_BYTES;
-                    read_k();
+                        for (int t = 0; t < 2; ++t) v[dt][t] = *reinterpret_cast<const uint4 *>(v_from + j * TILE_BYTES + (2 * t * DIM + dt * 32) * 16);
+                    if (j + 1 < TILES) read_k(j + 1);
                     __builtin_amdgcn_sched_barrier(0);
                     float z[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] = s[i] * scale.unit;
+                    for (int i = 0; i < 16; ++i) z[i] = fmaf(s[i], scale.unit, -shift);
                     if (!full) {
                         const uint32_t mask = mask_of(j);
 #pragma unroll
@@ -228,9 +230,9 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                     for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
                     top = max_xor32(top);
                     if (__any(top > limit)) {
-                        const float to = top > limit ? base + top / scale.unit : base;
-                        const float down = (to - base) * scale.unit, old = limit == -INFINITY ? 0.f : exp2_fast(-down);
-                        base = to;
+                        const float to = top > limit ? shift + top : shift;
+                        const float down = to - shift, old = limit == -INFINITY ? 0.f : exp2_fast(-down);
+                        shift = to;
                         limit = top > limit ? SLACK : limit;
                         total *= old;
 #pragma unroll
@@ -284,7 +286,7 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
             // result register i of a lane: channel 32 dt + 8 (i / 4) + 4 f + i % 4 of row m
             if (active) {
                 const int f = here(lane) >> 5, row = row0 + (here(lane) & 31);
-                const float all = add_xor32(total), up = limit == -INFINITY ? -INFINITY : base * scale.unit;
+                const float all = add_xor32(total), up = limit == -INFINITY ? -INFINITY : shift;
                 if (row < rows) {
                     if (whole) {
                         const float by = all == 0.f ? 0.f : 1.f / all;
