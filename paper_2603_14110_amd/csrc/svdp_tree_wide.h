@@ -41,7 +41,7 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
     // a stage of the tree's tokens: K where it always is; V as it comes, then in packs (finite elements), and as it is in packs
     constexpr int OWN_RAW = V_AT, OWN_PACKS = V_AT + TW_STAGE / 4, OWN_ALL = TW_STAGE / 4;
     extern __shared__ __align__(16) char tw_smem[];
-    __shared__ uint64_t s_sees[64];
+    __shared__ uint64_t s_sees[TW_WAVES * 32];                   // what a row sees of its tree
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), f = lane >> 5, m = lane & 31;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t *)tw_smem;
 
@@ -116,20 +116,23 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                 }
             };
 
-            stage_barrier<0>();                                  // the last segment's stages and stores are done with
-            int stage = 0;
-            if (s0 < s_end) fill(s0, 0);
-            else fill_own(0);
-            if (s1 > cached_steps && tid < S.n) s_sees[tid] = A.tree != nullptr ? A.tree[S.start + tid] : ~0ull >> (63 - tid);
-
+            // Q, and what the rows see of their tree, requested in front of the first stage and waited for behind it
             const TreeScale scale(A.scale, X::SIGNS);
             uint4 q[KC], k[KC], v[DT][2];
             {
                 const int row = min(row0 + (here(lane) & 31), rows - 1), node = row / A.group, head = h * A.group + row - node * A.group;
                 const bf16 *from = static_cast<const bf16 *>(A.q) + (S.start + node) * A.q_stride + (int64_t)head * DIM + f * 8;
 #pragma unroll
-                for (int c = 0; c < KC; ++c) q[c] = scale.of(load_raw(from + c * 16));
+                for (int c = 0; c < KC; ++c) q[c] = load_raw(from + c * 16);
+                const uint64_t sees = A.tree != nullptr ? A.tree[S.start + node] : ~0ull >> (63 - node);
+                stage_barrier<0>();                              // the last segment's stages and stores are done with
+                if (f == 0) s_sees[wave * 32 + m] = sees;
             }
+            int stage = 0;
+            if (s0 < s_end) fill(s0, 0);
+            else fill_own(0);
+#pragma unroll
+            for (int c = 0; c < KC; ++c) q[c] = scale.of(q[c]);
             // as in TreeWave: sum, shift, denominator (the lane half's part), and what a score has to exceed for the shift to move
             f32x16_t o[DT];
             float shift = 0.f, total = 0.f, limit = -INFINITY;
@@ -158,18 +161,18 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                 const int n_tiles = own_tokens ? (S.n + TA_TILE - 1) / TA_TILE : TILES;
                 if (own_tokens) {                                // V into packs
                     int odd = 0;
-                    for (int e = here(tid); e < n_tiles * TA_TILE * CHUNKS; e += TW_THREADS) {
-                        const int i = e / CHUNKS, c = e - i * CHUNKS;
-                        uint4 all = *reinterpret_cast<const uint4 *>(lds + OWN_RAW + e * 16);
-                        if (i >= S.n) all = make_uint4(0u, 0u, 0u, 0u);
-                        const int at = (i / TA_TILE) * TILE_BYTES + ((((i % TA_TILE) >> 3) * DIM + c * 8) * 8 + (i & 7)) * 2;
-                        const auto put = [&](char *to, const uint4 &what) {
-                            const uint32_t w[4] = {what.x, what.y, what.z, what.w};
+                    for (int e = here(tid); e < n_tiles * 4 * DIM; e += TW_THREADS) {
+                        const int pack = e / DIM, c = e - pack * DIM;
+                        uint32_t w[4];
 #pragma unroll
-                            for (int d = 0; d < 8; ++d) *reinterpret_cast<uint16_t *>(to + d * 16) = (uint16_t)(w[d >> 1] >> (16 * (d & 1)));
-                        };
-                        put(lds + OWN_PACKS + at, only_finite<X>(all));
-                        put(lds + OWN_ALL + at, all);
+                        for (int i = 0; i < 8; ++i) {
+                            uint32_t x = *reinterpret_cast<const uint16_t *>(lds + OWN_RAW + ((pack * 8 + i) * DIM + c) * 2);
+                            x = pack * 8 + i < S.n ? x : 0u;
+                            w[i >> 1] = i & 1 ? w[i >> 1] | x << 16 : x;
+                        }
+                        const uint4 all = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4 *>(lds + OWN_PACKS + e * 16) = only_finite<X>(all);
+                        *reinterpret_cast<uint4 *>(lds + OWN_ALL + e * 16) = all;
                         odd |= X::finite(all) ? 0 : 1;
                     }
                     finite = __syncthreads_or(odd) == 0;
@@ -187,7 +190,7 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                 const auto mask_of = [&](int j) {
                     const int f = here(lane) >> 5, m = here(lane) & 31;
                     uint32_t seen = (uint32_t)((1ull << count_of(j)) - 1);
-                    if (own_tokens) seen &= (uint32_t)(s_sees[min(row0 + m, rows - 1) / A.group] >> (j * TA_TILE));
+                    if (own_tokens) seen &= (uint32_t)(s_sees[wave * 32 + m] >> (j * TA_TILE));
                     return ((seen >> (8 * f)) & 0xffu) | ((seen >> (16 + 8 * f)) & 0xffu) << 8;
                 };
                 // A tile's operands are read ahead of their use by hand, V's while the weights are formed and the next tile's K
