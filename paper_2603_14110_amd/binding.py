@@ -7,6 +7,7 @@ or eager fallback: if the library has not been built, ``lib()`` raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Tuple
 
@@ -405,6 +406,7 @@ class KVCache:
         if tuple(V.shape) != (self.layers, self.pages, self.heads, self.page // e, self.dim, e):
             raise SvdpError(f"V: shape {tuple(V.shape)} does not go with K's {tuple(K.shape)}")
         self.K, self.V, self.dtype = K, V, K.dtype
+        self._sizes = {}          # workspace bytes of the sizes asked for
         self.c = svdp_kv_cache(self.layers, self.pages, self.page, self.heads, self.dim,
                                SVDP_BF16 if K.dtype == torch.bfloat16 else SVDP_F32, K.data_ptr(), V.data_ptr())
 
@@ -419,30 +421,33 @@ def _typed(t: Optional[torch.Tensor], dtype, what: str, shape=None) -> Optional[
     """Address of a contiguous device tensor of one type (and shape); None stays None."""
     if t is None:
         return None
-    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or (shape is not None and t.shape != shape):
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise SvdpError(f"{what}: expected a contiguous device tensor of {dtype}"
                         f"{'' if shape is None else ' ' + str(tuple(shape))}, got {tuple(t.shape)} {t.dtype}")
     return t.data_ptr()
 
 
-def _heads_rows(t: torch.Tensor, cache: KVCache, heads: Optional[int], what: str) -> int:
+def _heads_rows(t: torch.Tensor, cache: KVCache, heads: int, what: str) -> int:
     """Stride of the rows [heads][dim] of q, k or v (a slice of a wider projection is fine)."""
-    if (t.dim() != 3 or t.dtype != cache.dtype or not t.is_cuda or t.shape[2] != cache.dim or
-            (heads is not None and t.shape[1] != heads)):
-        raise SvdpError(f"{what}: expected [rows][{'heads' if heads is None else heads}][{cache.dim}] of {cache.dtype} on the "
-                        f"device, got {tuple(t.shape)} {t.dtype}")
+    rows, _, dim = shape = t.shape
     row, head, one = t.stride()
-    if t.shape[0] and (one != 1 or (head != cache.dim and t.shape[1] > 1)):
+    if t.dtype != cache.dtype or not t.is_cuda or dim != cache.dim or shape[1] != heads:
+        raise SvdpError(f"{what}: expected [rows][{heads}][{cache.dim}] of {cache.dtype} on the device, got {tuple(shape)} {t.dtype}")
+    if rows and (one != 1 or (head != dim and heads > 1)):
         raise SvdpError(f"{what}: the heads of a row have to lie side by side")
     # one row: its stride says nothing
-    return row if t.shape[0] > 1 else t.shape[1] * cache.dim
+    return row if rows > 1 else heads * dim
 
 
 def tree_attn_workspace_bytes(cache: KVCache, heads_q: int, R: int, max_pages: int, max_nodes: int = MAX_NODES) -> int:
-    n = lib().svdp_tree_attn_workspace_bytes(ctypes.byref(cache.c), heads_q, R, max_pages, max_nodes)
-    if n == 0:
-        raise SvdpError("svdp_tree_attn_workspace_bytes: unsupported cache, heads or sizes")
-    return int(n)
+    key = (heads_q, R, max_pages, max_nodes)
+    n = cache._sizes.get(key)
+    if n is None:
+        n = int(lib().svdp_tree_attn_workspace_bytes(ctypes.byref(cache.c), *key))
+        if n == 0:
+            raise SvdpError("svdp_tree_attn_workspace_bytes: unsupported cache, heads or sizes")
+        cache._sizes[key] = n
+    return n
 
 
 def tree_attn(cache: KVCache, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor,
@@ -454,29 +459,48 @@ def tree_attn(cache: KVCache, layer: int, q: torch.Tensor, k: torch.Tensor, v: t
     q [T][heads_q][dim], k, v [T][heads][dim] (rows may be slices of a wider projection); table [R][max_pages], lens [R],
     starts [R + 1] int32; tree [T] int64 (bit j: the row sees node j of its request; None: the nodes up to itself).
     max_nodes: the most rows a request has (default: T, at most 64).  scale: default dim ** -0.5.
+    ws: tree_attn_workspace_bytes() bytes.
     Returns out [T][heads_q][dim] (and lse [T][heads_q] fp32 with want_lse)."""
-    T, R, heads_q = q.shape[0], lens.numel(), q.shape[1]
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        raise SvdpError("svdp_tree_attn: q, k, v are rows of heads of channels")
+    T, heads_q, dim = q.shape
+    R = lens.numel()
     if k.shape[0] != T or v.shape[0] != T or table.dim() != 2 or table.shape[0] != R or starts.numel() != R + 1:
         raise SvdpError(f"svdp_tree_attn: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, table "
                         f"{tuple(table.shape)}, lens [{R}] and starts [{starts.numel()}] do not go together")
-    qs, ks, vs = (_heads_rows(q, cache, None, "q"), _heads_rows(k, cache, cache.heads, "k"),
+    qs, ks, vs = (_heads_rows(q, cache, heads_q, "q"), _heads_rows(k, cache, cache.heads, "k"),
                   _heads_rows(v, cache, cache.heads, "v"))
     max_pages = table.shape[1]
     max_nodes = max(1, min(T, MAX_NODES)) if max_nodes is None else int(max_nodes)
     if out is None:
-        out = torch.empty((T, heads_q, cache.dim), dtype=cache.dtype, device=q.device)
+        out = torch.empty((T, heads_q, dim), dtype=cache.dtype, device=q.device)
+        out_at = out.data_ptr()
+    else:
+        out_at = _typed(out, cache.dtype, "out", (T, heads_q, dim))
     if want_lse and lse is None:
         lse = torch.empty((T, heads_q), dtype=torch.float32, device=q.device)
+        lse_at = lse.data_ptr()
+    else:
+        lse_at = _typed(lse, torch.float32, "lse", (T, heads_q))
     if ws is None:
         ws = torch.empty(tree_attn_workspace_bytes(cache, heads_q, R, max_pages, max_nodes), dtype=torch.uint8, device=q.device)
+    elif not (ws.is_cuda and ws.is_contiguous()):
+        raise SvdpError("ws: expected a contiguous device tensor")
     i32 = torch.int32
     _check(lib().svdp_tree_attn(
         ctypes.byref(cache.c), layer, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
         _typed(tree, torch.int64, "tree", (T,)), _typed(table, i32, "table"), max_pages, _typed(lens, i32, "lens"),
-        _typed(starts, i32, "starts"), R, T, max_nodes, heads_q, cache.dim ** -0.5 if scale is None else scale,
-        _typed(out, cache.dtype, "out", (T, heads_q, cache.dim)), _typed(lse, torch.float32, "lse", (T, heads_q)), _ptr(ws),
-        ws.numel(), _stream()), "svdp_tree_attn")
+        _typed(starts, i32, "starts"), R, T, max_nodes, heads_q, dim ** -0.5 if scale is None else scale, out_at, lse_at,
+        ws.data_ptr(), ws.numel(), _stream()), "svdp_tree_attn")
     return (out, lse) if want_lse else out
+
+
+@functools.lru_cache(maxsize=256)
+def tree_accept_workspace_bytes(T: int, V: int, dtype: int) -> int:
+    n = int(lib().svdp_tree_accept_workspace_bytes(T, V, dtype))
+    if n == 0:
+        raise SvdpError(f"svdp_tree_accept: unsupported sizes T={T} V={V}")
+    return n
 
 
 def tree_accept(logits: torch.Tensor, tokens: torch.Tensor, starts: torch.Tensor, tree: Optional[torch.Tensor] = None,
@@ -489,17 +513,19 @@ def tree_accept(logits: torch.Tensor, tokens: torch.Tensor, starts: torch.Tensor
     R = starts.numel() - 1
     dt = SVDP_BF16 if logits.dtype == torch.bfloat16 else SVDP_F32
     max_nodes = max(1, min(T, MAX_NODES)) if max_nodes is None else int(max_nodes)
-    nbytes = lib().svdp_tree_accept_workspace_bytes(T, V, dt)
-    if nbytes == 0:
-        raise SvdpError(f"svdp_tree_accept: unsupported sizes T={T} V={V}")
-    if ws is None:
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
-    made = torch.empty(2 * T + 2 * max(R, 0), dtype=torch.int32, device=logits.device)
-    keep, best, counts, following = made.split((T, T, max(R, 0), max(R, 0)))
+    nbytes = tree_accept_workspace_bytes(T, V, dt)
+    if ws is None:          # one allocation: the scratch in front of the outputs
+        at, keep, best, counts, following = torch.empty(
+            nbytes // 4 + 2 * T + 2 * max(R, 0), dtype=torch.int32, device=logits.device).split_with_sizes((nbytes // 4, T, T, max(R, 0), max(R, 0)))
+        at, room = at.data_ptr(), nbytes
+    else:
+        keep, best, counts, following = torch.empty(2 * T + 2 * max(R, 0), dtype=torch.int32, device=logits.device).split(
+            (T, T, max(R, 0), max(R, 0)))
+        at, room = _ptr(ws), ws.numel()
     _check(lib().svdp_tree_accept(
         logits.data_ptr(), logits.stride(0) if T > 1 else V, dt, V, _typed(tokens, torch.int32, "tokens", (T,)),
         _typed(tree, torch.int64, "tree", (T,)), _typed(starts, torch.int32, "starts"), R, T, max_nodes, keep.data_ptr(),
-        counts.data_ptr(), following.data_ptr(), best.data_ptr(), _ptr(ws), ws.numel(), _stream()), "svdp_tree_accept")
+        counts.data_ptr(), following.data_ptr(), best.data_ptr(), at, room, _stream()), "svdp_tree_accept")
     return keep, counts, following, best
 
 
@@ -518,7 +544,7 @@ def kv_plan(table: torch.Tensor, ring: torch.Tensor, pool: torch.Tensor, lens: t
         raise SvdpError("svdp_kv_plan: without keep the number of rows has to be given")
     T = keep.numel() if keep is not None else int(rows)
     slots = torch.empty(T, dtype=torch.int64, device=lens.device)
-    lens_out, refused, pool_out = torch.empty(2 * R + 2, dtype=torch.int32, device=lens.device).split((R, R, 2))
+    lens_out, refused, pool_out = torch.empty(2 * R + 2, dtype=torch.int32, device=lens.device).split_with_sizes((R, R, 2))
     i32 = torch.int32
     _check(lib().svdp_kv_plan(
         _typed(table, i32, "table"), table.shape[1], _typed(ring, i32, "ring"), ring.numel(), int(page), _typed(pool, i32, "pool"),

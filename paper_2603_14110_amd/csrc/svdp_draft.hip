@@ -34,7 +34,7 @@ inline int bytes_of(int dt) { return dt == SVDP_F32 ? 4 : 2; }
 inline bool aligned_to(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 inline bool whole_vectors(int64_t stride, int dt) { return stride % (16 / bytes_of(dt)) == 0; }
 inline bool good_page(int page) { return page == 32 || page == 64 || page == 128 || page == 256; }
-inline int bits_of(int page) { return page == 32 ? 5 : page == 64 ? 6 : page == 128 ? 7 : 8; }
+inline int bits_of(int n) { return n == 32 ? 5 : n == 64 ? 6 : n == 128 ? 7 : 8; }
 inline int tiles(int64_t n, int per) { return (int)((n + per - 1) / per); }
 
 bool overlap(const void *a, size_t an, const void *b, size_t bn)
@@ -112,6 +112,8 @@ void on_tiles(int nt, F &&f)
     else if (nt == 2) f(std::integral_constant<int, 2>{});
     else f(std::integral_constant<int, 4>{});
 }
+
+constexpr int COMMIT_BLOCKS = 4096;       // K and V of few rows: fewer channels a block, until there are so many blocks
 
 // Parts that a row of logits is cut into: about a thousand blocks altogether, each of 8 to 32 KB.
 int best_parts(int T, int V, int dt)
@@ -290,9 +292,10 @@ svdp_status svdp_kv_plan(int32_t *table, int32_t max_pages, int32_t *ring, int32
         return SVDP_ERR_INVALID_ARG;
     const size_t lds = plan_lds(R);
     if (!grant_lds<k_kv_plan>(lds)) return SVDP_ERR_UNSUPPORTED;
-    const int blocks = std::min(std::max(tiles(T, 2 * PLAN_THREADS), tiles(R, 4 * PLAN_WAVES)), 256);
-    launch(k_kv_plan, dim3(blocks), dim3(PLAN_THREADS), lds, static_cast<hipStream_t>(stream), table, max_pages, ring, pages,
-           bits_of(page), pool, lens, add, starts, keep, R, T, slots, lens_out, pool_out, refused);
+    const int row_blocks = tiles(R, PLAN_WAVES), slot_blocks = std::min(tiles(T, PLAN_THREADS), 256);
+    launch(k_kv_plan, dim3(row_blocks + slot_blocks), dim3(PLAN_THREADS), lds, static_cast<hipStream_t>(stream), table, max_pages, ring, pages,
+           bits_of(page), pool, lens, add, starts, keep, R, T, row_blocks, slots, lens_out, pool_out,
+           refused);
     return hip_status(hipSuccess);
 }
 
@@ -311,12 +314,16 @@ svdp_status svdp_kv_commit(const svdp_kv_cache *cache, const void *k, int64_t k_
         v_row_stride < row || k_layer_stride < 0 || v_layer_stride < 0 || !whole_vectors(k_row_stride, dt) ||
         !whole_vectors(v_row_stride, dt) || !whole_vectors(k_layer_stride, dt) || !whole_vectors(v_layer_stride, dt))
         return SVDP_ERR_INVALID_ARG;
+    const int groups = tiles(T, COMMIT_ROWS);
+    int channels = (int)row;
+    while (channels > COMMIT_CHANNELS && tiles(row, channels) < COMMIT_BLOCKS / (2 * (int64_t)groups * cache->layers))
+        channels = tiles(channels, 2 * COMMIT_CHANNELS) * COMMIT_CHANNELS;
     return on_type(dt, [&](auto wt) {
         using W = typename decltype(wt)::type;
-        launch(k_kv_commit<W>, dim3(tiles(T, COMMIT_ROWS), cache->layers), dim3(COMMIT_THREADS), 0,
+        launch(k_kv_commit<W>, dim3(groups, cache->layers, 2 * tiles(row, channels)), dim3(COMMIT_THREADS), 0,
                static_cast<hipStream_t>(stream), static_cast<W *>(cache->K), static_cast<W *>(cache->V),
                static_cast<const W *>(k), k_layer_stride, k_row_stride, static_cast<const W *>(v), v_layer_stride,
-               v_row_stride, slots, T, cache->pages, bits_of(cache->page), cache->heads, cache->dim);
+               v_row_stride, slots, T, cache->pages, bits_of(cache->page), cache->heads, bits_of(cache->dim), channels);
         return hip_status(hipSuccess);
     });
 }

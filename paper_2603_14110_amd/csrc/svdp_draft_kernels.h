@@ -11,19 +11,23 @@ namespace svdp {
 
 // ---- block tables and slots -----------------------------------------------------------------------------------------------
 
-constexpr int PLAN_THREADS = 256;
+constexpr int PLAN_THREADS = 1024;
 constexpr int PLAN_WAVES = PLAN_THREADS / 64;
+constexpr int PLAN_EACH = 4;                // requests of a thread, at most
 // LDS of a block: starts [R + 1], then lens, limit and first [R] (below)
 inline size_t plan_lds(int R) { return ((size_t)4 * R + 1) * 4; }
 
 // Pages are handed out by a prefix sum of the requests' needs, and so are places at the ring's end for pages that come
 // back.  Every block forms the whole sums (R <= 4096 lengths, a few microseconds' worth of arithmetic at most) and then does
 // its share of table rows and of slots, so that nothing waits for another block and nothing but the inputs is read: a new entry
-// of the table is taken from the ring again by the rows that lie in it.
+// of the table is taken from the ring again by the rows that lie in it.  Blocks for table rows and blocks for slots follow each
+// other in the grid.  What bounds it is the chain of loads (lengths, then the ring or the table), not bytes: 3.4 us for 8
+// requests, 7.0 us for 700 requests and 93 500 rows (7.8 us where a block does rows and then slots, 8.7 us with blocks of 256
+// threads, whose threads have three requests each).
 __global__ __launch_bounds__(PLAN_THREADS) void k_kv_plan(
     int32_t *table, int max_pages, int32_t *ring, int pages, int page_bits, const int32_t *pool, const int32_t *lens,
-    const int32_t *add, const int32_t *starts, const int32_t *keep, int R, int T, int64_t *slots, int32_t *lens_out,
-    int32_t *pool_out, int32_t *refused)
+    const int32_t *add, const int32_t *starts, const int32_t *keep, int R, int T, int row_blocks, int64_t *slots,
+    int32_t *lens_out, int32_t *pool_out, int32_t *refused)
 {
     extern __shared__ __align__(16) char plan_smem[];
     int *s_starts = reinterpret_cast<int *>(plan_smem);
@@ -34,25 +38,39 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_kv_plan(
     __shared__ int s_taken;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int page = 1 << page_bits;
+    const int per = (R + PLAN_THREADS - 1) / PLAN_THREADS, r0 = tid * per, mine = min(per, R - r0);
+    int raw[PLAN_EACH], more[PLAN_EACH];
+#pragma unroll
+    for (int j = 0; j < PLAN_EACH; ++j) {
+        if (j >= per) break;
+        raw[j] = lens[min(r0 + j, R - 1)];
+        more[j] = add[min(r0 + j, R - 1)];
+    }
     const int free_pages = min(max(pool[1], 0), pages);
     const int head = (int)(((uint32_t)max(pool[0], 0)) % (uint32_t)pages);
+    // slots of the blocks behind those that do the table's rows, and what is kept of the first of them
+    const int64_t slot_step = (int64_t)(gridDim.x - row_blocks) * PLAN_THREADS;
+    int64_t t = ((int64_t)blockIdx.x - row_blocks) * PLAN_THREADS + tid;
+    int kept = t >= 0 && t < T && keep != nullptr ? keep[t] : 0;
     if (tid == 0) s_taken = 0;
     for (int r = tid; r <= R; r += PLAN_THREADS) s_starts[r] = starts[r];
 
-    // pages held, and pages needed, of request r; more pages than the table is wide: refused (need 0)
+    // pages held, and pages needed, of a request; more pages than the table is wide: refused
     const auto pages_of = [&](int n) { return (n + page - 1) >> page_bits; };
-    const int per = (R + PLAN_THREADS - 1) / PLAN_THREADS, r0 = min(tid * per, R), r1 = min(r0 + per, R);
-    int need_sum = 0, give_sum = 0;
-    for (int r = r0; r < r1; ++r) {
-        const int len = min(max(lens[r], 0), max_pages << page_bits), a = add[r];
-        const int before = pages_of(len);
-        const bool ends = a < 0, wide = (int64_t)len + a > (int64_t)max_pages << page_bits;
-        const int need = ends || wide ? 0 : pages_of(len + a) - before;
-        s_lens[r] = len;
-        s_limit[r] = ends ? -1 : wide ? -2 : need;          // until the sums are known
-        need_sum += need;
-        give_sum += ends ? before : 0;
-    }
+    int len[PLAN_EACH], need[PLAN_EACH], need_sum = 0, give_sum = 0;
+    bool wide[PLAN_EACH];
+#pragma unroll
+    for (int j = 0; j < PLAN_EACH; ++j)
+        if (j < mine) {
+            len[j] = min(max(raw[j], 0), max_pages << page_bits);
+            const int before = pages_of(len[j]);
+            const bool ends = more[j] < 0;
+            wide[j] = !ends && (int64_t)len[j] + more[j] > (int64_t)max_pages << page_bits;
+            need[j] = ends || wide[j] ? 0 : pages_of(len[j] + more[j]) - before;
+            s_lens[r0 + j] = len[j];
+            need_sum += need[j];
+            give_sum += ends ? before : 0;
+        }
     const int need_upto = wave_inclusive_scan(need_sum), give_upto = wave_inclusive_scan(give_sum);
     if (lane == 63) {
         s_wave[0][wave] = need_upto;
@@ -60,27 +78,28 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_kv_plan(
     }
     __syncthreads();
     int taken_before = need_upto - need_sum, given_before = give_upto - give_sum, given = 0;
+#pragma unroll
     for (int w = 0; w < PLAN_WAVES; ++w) {
         taken_before += w < wave ? s_wave[0][w] : 0;
         given_before += w < wave ? s_wave[1][w] : 0;
         given += s_wave[1][w];
     }
     int taken = 0;
-    for (int r = r0; r < r1; ++r) {
-        const int kind = s_limit[r], len = s_lens[r];
-        const bool ends = kind == -1;
-        const int need = max(kind, 0);
-        const bool no = kind == -2 || (need > 0 && taken_before + need > free_pages);
-        s_first[r] = ends ? given_before : taken_before;
-        s_limit[r] = ends ? -1 : no ? 0 : add[r];
-        taken_before += need;
-        given_before += ends ? pages_of(len) : 0;
-        if (need > 0 && !no) taken = taken_before;          // sums only grow: the last granted one is the largest
-        if (blockIdx.x == 0) {
-            lens_out[r] = ends ? 0 : no ? lens[r] : len + add[r];
-            refused[r] = no ? 1 : 0;
+#pragma unroll
+    for (int j = 0; j < PLAN_EACH; ++j)
+        if (j < mine) {
+            const int r = r0 + j;
+            const bool ends = more[j] < 0, no = wide[j] || (need[j] > 0 && taken_before + need[j] > free_pages);
+            s_first[r] = ends ? given_before : taken_before;
+            s_limit[r] = ends ? -1 : no ? 0 : more[j];
+            taken_before += need[j];
+            given_before += ends ? pages_of(len[j]) : 0;
+            if (need[j] > 0 && !no) taken = taken_before;   // sums only grow: the last granted one is the largest
+            if (blockIdx.x == 0) {
+                lens_out[r] = ends ? 0 : no ? raw[j] : len[j] + more[j];
+                refused[r] = no ? 1 : 0;
+            }
         }
-    }
     if (taken > 0) atomicMax(&s_taken, taken);
     __syncthreads();
     if (blockIdx.x == 0 && tid == 0) {
@@ -89,22 +108,25 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_kv_plan(
     }
 
     // table rows, one wave each: new entries in, or the pages of a request that ends to the ring's end
-    for (int r = blockIdx.x * PLAN_WAVES + wave; r < R; r += gridDim.x * PLAN_WAVES) {
-        const int limit = s_limit[r], before = pages_of(s_lens[r]), first = s_first[r];
-        int32_t *row = table + (size_t)r * max_pages;
-        if (limit < 0) {
-            for (int i = lane; i < before; i += 64)
-                if (first + i < pages - free_pages)         // no more than there are places for
-                    ring[((uint32_t)head + (uint32_t)free_pages + (uint32_t)(first + i)) % (uint32_t)pages] = row[i];
-        } else {
-            const int after = pages_of(s_lens[r] + limit);
-            for (int i = before + lane; i < after; i += 64)
-                row[i] = ring[((uint32_t)head + (uint32_t)(first + i - before)) % (uint32_t)pages];
+    if ((int)blockIdx.x < row_blocks) {
+        for (int r = blockIdx.x * PLAN_WAVES + wave; r < R; r += row_blocks * PLAN_WAVES) {
+            const int limit = s_limit[r], before = pages_of(s_lens[r]), first = s_first[r];
+            int32_t *row = table + (size_t)r * max_pages;
+            if (limit < 0) {
+                for (int i = lane; i < before; i += 64)
+                    if (first + i < pages - free_pages)     // no more than there are places for
+                        ring[((uint32_t)head + (uint32_t)free_pages + (uint32_t)(first + i)) % (uint32_t)pages] = row[i];
+            } else {
+                const int after = pages_of(s_lens[r] + limit);
+                for (int i = before + lane; i < after; i += 64)
+                    row[i] = ring[((uint32_t)head + (uint32_t)(first + i - before)) % (uint32_t)pages];
+            }
         }
+        return;
     }
 
     // slots
-    for (int64_t t = (int64_t)blockIdx.x * PLAN_THREADS + tid; t < T; t += (int64_t)gridDim.x * PLAN_THREADS) {
+    for (; t < T; t += slot_step, kept = t < T && keep != nullptr ? keep[t] : 0) {
         int lo = 0, hi = R;                                 // the last request that starts at or before t
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -113,7 +135,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_kv_plan(
         }
         int64_t slot = -1;
         if (lo < R) {
-            const int place = keep != nullptr ? keep[t] : (int)t - s_starts[lo];
+            const int place = keep != nullptr ? kept : (int)t - s_starts[lo];
             if (place >= 0 && place < s_limit[lo]) {
                 const int at = s_lens[lo] + place, i = at >> page_bits, before = pages_of(s_lens[lo]);
                 const int id = i < before
@@ -130,12 +152,15 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_kv_plan(
 
 constexpr int BEST_THREADS = 256;
 
-// A value and its index as one word that grows with the value and falls with the index: NaN above all, -0 equal to 0.
-__device__ __forceinline__ uint64_t best_key(float v, uint32_t index)
+// A word that grows with the value: NaN above all, -0 equal to 0; and one that then falls with the index.
+__device__ __forceinline__ uint32_t best_order(float v)
 {
     const uint32_t u = __float_as_uint(v + 0.f);
-    const uint32_t o = (u & 0x7fffffffu) > 0x7f800000u ? 0xffffffffu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
-    return ((uint64_t)o << 32) | (0xffffffffu - index);
+    return (u & 0x7fffffffu) > 0x7f800000u ? 0xffffffffu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ uint64_t best_key(float v, uint32_t index)
+{
+    return ((uint64_t)best_order(v) << 32) | (0xffffffffu - index);
 }
 __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v)
 {
@@ -148,34 +173,65 @@ __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v)
 }
 
 // The largest logit of a part of a row.  A row is cut where 16-byte vectors begin, whatever its own alignment: part p has the
-// vectors [p per, (p + 1) per) counted from the aligned address at or before the row.
+// vectors [p per, (p + 1) per) counted from the aligned address at or before the row.  A lane keeps its best vector by the
+// largest of its values, a few operations for a vector, and looks for the place in it once, at the end.  Bound by reading:
+// 439 MB of bf16 logits in 77 us, 5.7 TB/s (90.7 us, by arithmetic, with an order and an index for every element); 8 rows of
+// 32 000 in 3.2 us, by the latency of one load and the launch.
 template <typename W>
 __global__ __launch_bounds__(BEST_THREADS) void k_logits_best(const W *logits, int64_t stride, int V, int per, uint64_t *parts)
 {
-    constexpr int VEC = Elem<W>::VEC;
+    constexpr int VEC = Elem<W>::VEC, AHEAD = 4;
     __shared__ uint64_t s_best[BEST_THREADS / 64];
     const W *row = logits + (int64_t)blockIdx.x * stride;
     const int skew = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / Elem<W>::BYTES);
     const int vectors = (V + skew + VEC - 1) / VEC;
-    const int end = min((int)(blockIdx.y + 1) * per, vectors);
-    uint64_t best = 0;
-    for (int i = blockIdx.y * per + threadIdx.x; i < end; i += BEST_THREADS) {
-        const int at = i * VEC - skew;
-        if (at >= 0 && at + VEC <= V) {
-            float v[VEC];
-            load_vec(row + at, v);
+    const int begin = blockIdx.y * per, end = min(begin + per, vectors);
+    // vectors that lie in the row as a whole
+    const int inner = max(begin, skew > 0 ? 1 : 0), outer = min(end, (V + skew) / VEC);
+    uint4 kept = make_uint4(0, 0, 0, 0);
+    uint32_t top = 0;                                       // order of the largest value, above 0 once there is one
+    int place = 0;
+    for (int i0 = inner + threadIdx.x; i0 < outer; i0 += AHEAD * BEST_THREADS) {
+        uint4 in[AHEAD];
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const uint64_t key = best_key(v[j], at + j);
-                best = key > best ? key : best;
+        for (int a = 0; a < AHEAD; ++a) in[a] = load_raw(row + (min(i0 + a * BEST_THREADS, outer - 1) * VEC - skew));
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            float v[VEC];
+            widen(in[a], v, row);
+            float m = v[0];
+            bool nan = false;
+#pragma unroll
+            for (int j = 0; j < VEC; j += 2) {
+                m = fmaxf(m, fmaxf(v[j], v[j + 1]));
+                nan |= __builtin_isunordered(v[j], v[j + 1]);
             }
-        } else {
-            for (int j = max(at, 0); j < min(at + VEC, V); ++j) {
-                const uint64_t key = best_key(to_f32(row[j]), j);
-                best = key > best ? key : best;
+            const uint32_t o = nan ? 0xffffffffu : best_order(m);
+            if (o > top) {
+                top = o;
+                place = min(i0 + a * BEST_THREADS, outer - 1);
+                kept = in[a];
             }
         }
     }
+    uint64_t best = 0;
+    if (top > 0) {
+        float v[VEC];
+        widen(kept, v, row);
+#pragma unroll
+        for (int j = VEC - 1; j >= 0; --j)
+            if (best_order(v[j]) == top) best = best_key(v[j], place * VEC - skew + j);
+    }
+    // the row's ends: the first and the last vector of the row, where they reach over it
+    const auto edge = [&](int i) {
+        if (i < begin || i >= end || threadIdx.x >= VEC) return;
+        const int at = i * VEC - skew + (int)threadIdx.x;
+        if (at < 0 || at >= V) return;
+        const uint64_t key = best_key(to_f32(row[at]), at);
+        best = key > best ? key : best;
+    };
+    if (skew > 0) edge(0);
+    if ((V + skew) % VEC != 0) edge(vectors - 1);
     best = wave_max_u64(best);
     if ((threadIdx.x & 63) == 0) s_best[threadIdx.x >> 6] = best;
     __syncthreads();
@@ -186,16 +242,21 @@ __global__ __launch_bounds__(BEST_THREADS) void k_logits_best(const W *logits, i
 }
 
 // One wave a request, a lane a node: the rows' answers from their parts, then down the tree; the last block has the padding.
+// Bound by the latency of two loads after each other: 1.6 us for one tree of 8, 4.2 us for 32 trees and 10 parts a row.
 __global__ __launch_bounds__(64) void k_tree_walk(const uint64_t *parts, int n_parts, const int32_t *tokens, const uint64_t *tree,
                                                   const int32_t *starts, int R, int T, int max_nodes, int32_t *keep,
                                                   int32_t *counts, int32_t *next, int32_t *best)
 {
     const int r = blockIdx.x, lane = threadIdx.x;
     const auto answer = [&](int t) {
+        constexpr int AHEAD = 16;
         uint64_t k = 0;
-        for (int p = 0; p < n_parts; ++p) {
-            const uint64_t o = parts[(size_t)t * n_parts + p];
-            k = o > k ? o : k;
+        for (int p = 0; p < n_parts; p += AHEAD) {
+            uint64_t o[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) o[i] = parts[(size_t)t * n_parts + min(p + i, n_parts - 1)];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) k = o[i] > k ? o[i] : k;
         }
         return (int)(0xffffffffu - (uint32_t)k);
     };
@@ -204,24 +265,24 @@ __global__ __launch_bounds__(64) void k_tree_walk(const uint64_t *parts, int n_p
     const bool node = lane < n;
     int mine = -1, token = -2, parent = -1;
     if (node) {
-        mine = answer(a + lane);
-        best[a + lane] = mine;
-        token = tokens[a + lane];
         const uint64_t before = (1ull << lane) - 1;
         const uint64_t up = tree != nullptr ? tree[a + lane] & before : before;
+        token = tokens[a + lane];
+        mine = answer(a + lane);
+        best[a + lane] = mine;
         parent = up != 0 ? 63 - __clzll((long long)up) : -1;
     }
     if (r < R) {
         int place = lane == 0 ? 0 : -1, count = n > 0 ? 1 : 0, at = 0;
         while (count > 0) {                                 // at grows with every step
-            const int answered = __shfl(mine, at);
+            const int answered = __builtin_amdgcn_readlane(mine, at);
             const uint64_t agree = __ballot(node && lane > at && parent == at && token == answered);
             if (agree == 0) break;
             at = __ffsll((unsigned long long)agree) - 1;
             if (lane == at) place = count;
             ++count;
         }
-        const int following = __shfl(mine, at);
+        const int following = __builtin_amdgcn_readlane(mine, at);
         if (node) keep[a + lane] = place;
         if (lane == 0) {
             counts[r] = count;
@@ -239,59 +300,96 @@ __global__ __launch_bounds__(64) void k_tree_walk(const uint64_t *parts, int n_p
 constexpr int COMMIT_THREADS = 256;
 constexpr int COMMIT_ROWS = 8;
 
-// Rows [8 blockIdx.x, + 8) of layer blockIdx.y.  K is copied in 16-byte vectors.  V lies with e tokens of a channel side by side:
-// where e rows in a row fill such a pack (prompts), their elements are exchanged between registers and written as whole
-// packs by the rows of the pack's first token; other rows (branches of a tree) write their elements one by one.
+constexpr int COMMIT_CHANNELS = 256;        // the least a block has of them, unless a row has fewer
+
+// Rows [8 blockIdx.x, + 8) of layer blockIdx.y, channels [blockIdx.z / 2 channels, + channels) of all heads side by side.
+// Even blockIdx.z: K, odd: V.  K is
+// copied in 16-byte vectors.  V lies with e tokens of a channel side by side: where e rows in a row fill such a pack
+// (prompts), they are read together and written as whole packs, by the row of the pack's first token; other rows (branches of
+// a tree) write their elements one by one.  A lane has two channels of V, so that the packs of a wave lie side by side.  Bound
+// by reading and writing: a prompt's 618 MB (half read, half written) in 113 us, 5.5 TB/s (144 us with eight channels a lane,
+// packs 128 bytes apart); a branch of a tree of 8, in 32 layers, in 3.9 us, by latency, with its channels over many blocks
+// (6.5 us with one block for all of them and for K and V).
 template <typename W>
 __global__ __launch_bounds__(COMMIT_THREADS) void k_kv_commit(W *K, W *V, const W *k, int64_t k_layer, int64_t k_row,
                                                               const W *v, int64_t v_layer, int64_t v_row,
                                                               const int64_t *slots, int T, int pages, int page_bits, int heads,
-                                                              int dim)
+                                                              int dim_bits, int channels)
 {
-    constexpr int E = Elem<W>::VEC;
-    __shared__ int64_t s_slot[COMMIT_ROWS];
-    __shared__ int s_whole[COMMIT_ROWS];          // 0: element by element, 1: writes a pack, 2: another row writes it
+    constexpr int E = Elem<W>::VEC, AHEAD = 4;
+    __shared__ int64_t s_near[COMMIT_ROWS + 2 * E];         // slots from row t0 - E on
+    __shared__ int s_rows[COMMIT_ROWS];                     // rows that write V: row, or row | 8 for whole packs
     const int tid = threadIdx.x, t0 = blockIdx.x * COMMIT_ROWS, layer = blockIdx.y;
     const int64_t all = (int64_t)pages << page_bits;
-    if (tid < COMMIT_ROWS) {
-        const int t = t0 + tid;
-        const int64_t s = t < T ? slots[t] : -1;
-        const bool real = s >= 0 && s < all;
-        const int j = (int)(s & (E - 1)), first = t - j;
-        bool whole = real && first >= 0 && first + E <= T;
-        for (int i = 0; i < E && whole; ++i) whole = slots[first + i] == s - j + i;
-        s_slot[tid] = real ? s : -1;
-        s_whole[tid] = whole ? (j == 0 ? 1 : 2) : 0;
+    if (tid < COMMIT_ROWS + 2 * E) {
+        const int t = t0 - E + tid;
+        const int64_t s = t >= 0 && t < T ? slots[t] : -1;
+        s_near[tid] = s < all ? s : -1;
     }
     __syncthreads();
-    const int page = 1 << page_bits, vectors = heads * dim / E;
-    k += (int64_t)layer * k_layer;
-    v += (int64_t)layer * v_layer;
+    const int page = 1 << page_bits, c0 = (int)(blockIdx.z >> 1) * channels, cn = min(channels, (heads << dim_bits) - c0);
+    k += (int64_t)layer * k_layer + (int64_t)t0 * k_row + c0;
+    v += (int64_t)layer * v_layer + (int64_t)t0 * v_row + c0;
     const int64_t layer_at = (int64_t)layer * pages * heads;
-    for (int i = tid; i < COMMIT_ROWS * vectors; i += COMMIT_THREADS) {
-        const int row = i / vectors, at = (i - row * vectors) * E, h = at / dim, c = at - h * dim;
-        const int64_t slot = s_slot[row];
-        if (slot < 0) continue;
-        const int t = t0 + row, place = (int)(slot & (page - 1));
-        const int64_t base = ((layer_at + (slot >> page_bits) * heads + h) << page_bits) * dim;
-        *reinterpret_cast<uint4 *>(K + base + (int64_t)place * dim + c) = load_raw(k + t * k_row + at);
-        W *to = V + base + ((int64_t)(place / E) * dim + c) * E;
-        if (s_whole[row] == 1) {
-            W in[E][E];
+    // element of the cache at which channel c of a slot's head begins its page
+    const auto page_at = [&](int64_t slot, int c) {
+        return (((layer_at + (slot >> page_bits) * heads + (c >> dim_bits)) << page_bits) << dim_bits);
+    };
+    const int mask = (1 << dim_bits) - 1;
+    const bool of_v = blockIdx.z & 1;
+    bool writes = false, whole = false;
+    if (of_v && tid < 64) {
+        if (tid < COMMIT_ROWS) {
+            const int64_t s = s_near[E + tid];
+            const int j = (int)(s & (E - 1));
+            whole = s >= 0;
 #pragma unroll
-            for (int j = 0; j < E; ++j) __builtin_memcpy(in[j], __builtin_assume_aligned(v + (t + j) * v_row + at, 16), 16);
+            for (int i = 0; i < E; ++i) whole &= s_near[E + tid - j + i] == s - j + i;
+            writes = s >= 0 && (!whole || j == 0);
+        }
+        const uint64_t who = __ballot(writes);
+        if (writes) s_rows[__popcll(who & ((1ull << tid) - 1))] = tid | (whole ? COMMIT_ROWS : 0);
+        if (tid == 0) s_near[0] = __popcll(who);            // row t0 - E is in no pack of these rows
+    }
+    const int vectors = cn / E, items = of_v ? 0 : min(COMMIT_ROWS, T - t0) * vectors;
+    for (int i0 = tid; i0 < items; i0 += AHEAD * COMMIT_THREADS) {
+        uint4 in[AHEAD];
+        W *to[AHEAD];
+        bool real[AHEAD];
 #pragma unroll
-            for (int d = 0; d < E; ++d) {
-                W out[E];
+        for (int a = 0; a < AHEAD; ++a) {                   // no branch around a load: they are on their way together
+            const int i = min(i0 + a * COMMIT_THREADS, items - 1), row = i / vectors, c = (i - row * vectors) * E;
+            const int64_t slot = s_near[E + row];
+            real[a] = slot >= 0 && i0 + a * COMMIT_THREADS < items;
+            in[a] = load_raw(k + (int64_t)row * k_row + c);
+            to[a] = K + page_at(slot, c0 + c) + (((slot & (page - 1)) << dim_bits) + ((c0 + c) & mask));
+        }
 #pragma unroll
-                for (int j = 0; j < E; ++j) out[j] = in[j][d];
-                __builtin_memcpy(__builtin_assume_aligned(to + d * E, 16), out, 16);
+        for (int a = 0; a < AHEAD; ++a)
+            if (real[a]) *reinterpret_cast<uint4 *>(to[a]) = in[a];
+    }
+    if (!of_v) return;
+    __syncthreads();
+    const int pairs = cn / 2, jobs = (int)s_near[0] * pairs;
+    for (int i = tid; i < jobs; i += COMMIT_THREADS) {
+        const int job = i / pairs, c = (i - job * pairs) * 2, row = s_rows[job] & (COMMIT_ROWS - 1);
+        const int64_t slot = s_near[E + row];
+        const int place = (int)(slot & (page - 1));
+        const W *from = v + (int64_t)row * v_row + c;
+        W *to = V + page_at(slot, c0 + c) + ((((int64_t)(place / E) << dim_bits) + ((c0 + c) & mask)) * E);
+        if (s_rows[job] & COMMIT_ROWS) {
+            W in[E][2], out[2][E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) __builtin_memcpy(in[j], __builtin_assume_aligned(from + j * v_row, sizeof(in[j])), sizeof(in[j]));
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                out[0][j] = in[j][0];
+                out[1][j] = in[j][1];
             }
-        } else if (s_whole[row] == 0) {
-            W in[E];
-            __builtin_memcpy(in, __builtin_assume_aligned(v + t * v_row + at, 16), 16);
-#pragma unroll
-            for (int d = 0; d < E; ++d) to[d * E + (place & (E - 1))] = in[d];
+            __builtin_memcpy(__builtin_assume_aligned(to, 16), out, sizeof(out));
+        } else {
+            to[place & (E - 1)] = from[0];
+            to[E + (place & (E - 1))] = from[1];
         }
     }
 }
