@@ -76,28 +76,11 @@ svdp_status check_ws(void *ws, size_t ws_bytes, size_t need)
 // Which attention kernel: rows are the nodes of a request times the query heads that share a head of K and V.
 struct AttnPlan {
     bool wide;              // rows over the waves of a block (k_tree_attn_wide), or tokens (k_tree_attn)
-    int nt, block_bits, block_rows, part_rows;
+    int nt;                 // row tiles of 16 in k_tree_attn
+    int block_bits, part_rows;
     int64_t steps, tasks;   // units of a request and head, and requests times heads times row tiles, at most
     size_t bytes;
 };
-AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, int max_nodes)
-{
-    const int dt = c->dtype, dim = c->dim, group = heads_q / c->heads;
-    const int64_t rows = (int64_t)group * max_nodes, room = (int64_t)max_pages * c->page / TA_TILE, own = tiles(max_nodes, TA_TILE);
-    AttnPlan p;
-    p.wide = dt == SVDP_BF16 && dim <= 128 && rows > 64;
-    p.nt = rows <= 16 || dim == 256 ? 1 : rows <= 32 || dt == SVDP_F32 ? 2 : 4;
-    const bool two_waves = ta_waves(bytes_of(dt), dim, p.nt) >= 2;       // of a SIMD
-    p.block_bits = !p.wide && two_waves ? 9 : 8;
-    p.block_rows = p.wide ? TW_ROWS : 16 * p.nt;
-    p.part_rows = (int)std::min<int64_t>(rows, p.block_rows);
-    const int unit = p.wide ? (dim == 64 ? tw_tiles<64>() : tw_tiles<128>()) : TA_WAVES;
-    p.steps = p.wide ? tiles(room, unit) + tiles(own, unit) : tiles(room + own, unit);
-    p.tasks = (rows + p.block_rows - 1) / p.block_rows * c->heads * R;
-    p.bytes = align_up(((size_t)2 << p.block_bits) * p.part_rows * (dim + 2) * 4);
-    return p;
-}
-constexpr int JOIN_WAVES = 2048;        // rows and heads from which the join has a wave for each, whatever the parts
 template <typename F>
 void on_dim(int dim, F &&f)
 {
@@ -105,14 +88,50 @@ void on_dim(int dim, F &&f)
     else if (dim == 128) f(std::integral_constant<int, 128>{});
     else f(std::integral_constant<int, 256>{});
 }
+// f(W tag, DIM, cut) of the kernel that a plan takes
 template <typename F>
-void on_tiles(int nt, F &&f)
+void on_kernel(const AttnPlan &p, int dt, int dim, F &&f)
 {
-    if (nt == 1) f(std::integral_constant<int, 1>{});
-    else if (nt == 2) f(std::integral_constant<int, 2>{});
-    else f(std::integral_constant<int, 4>{});
+    on_dim(dim, [&](auto dc) {
+        constexpr int DIM = decltype(dc)::value;
+        if constexpr (DIM <= 128)
+            if (p.wide) return f(Type<bf16>{}, dc, WideCut<DIM>{});
+        on_type(dt, [&](auto wt) {
+            using W = typename decltype(wt)::type;
+            if constexpr (DIM <= 128)
+                if (p.nt == 2) return f(wt, dc, NarrowCut<W, DIM, 2>{});
+            f(wt, dc, NarrowCut<W, DIM, 1>{});
+        });
+    });
 }
-
+AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, int max_nodes)
+{
+    const int dt = c->dtype, dim = c->dim, group = heads_q / c->heads;
+    const int64_t rows = (int64_t)group * max_nodes, room = (int64_t)max_pages * c->page / TA_TILE, own = tiles(max_nodes, TA_TILE);
+    AttnPlan p;
+    // More than 32 rows: over the waves, 32 each (36 rows, 135 MB: 31 us, where tiles of 64 rows over the waves' tokens took 34, and
+    // 10 us against 14 for 500 tokens).  At 32 rows: 28.6 us for one request of 30 000 tokens, 45 for 24 of 150, where
+    // k_tree_attn takes 25.4 and 24.5.
+    p.wide = dt == SVDP_BF16 && dim <= 128 && rows > 32;
+    // Two row tiles of 16 read K and V once for 32 rows (8 requests of 4096 tokens, 135 MB: 28.5 us, one after the other 38.8); with
+    // 256 channels a second one does not fit the registers.
+    p.nt = rows <= 16 || dim == 256 ? 1 : 2;
+    int unit, block_rows;
+    on_kernel(p, dt, dim, [&](auto, auto, auto cut) {
+        using Cut = decltype(cut);
+        unit = Cut::UNIT;
+        block_rows = Cut::ROWS;
+        p.block_bits = Cut::BITS;
+    });
+    p.part_rows = (int)std::min<int64_t>(rows, block_rows);
+    p.steps = p.wide ? tiles(room, unit) + tiles(own, unit) : tiles(room + own, unit);
+    p.tasks = (rows + block_rows - 1) / block_rows * c->heads * R;
+    p.bytes = align_up(((size_t)2 << p.block_bits) * p.part_rows * (dim + 2) * 4);
+    return p;
+}
+// Rows and heads from which the join has a wave for each, whatever the parts (2048 of 10 parts: 6.6 us, with a block each 9.9; 256
+// of 64 parts: 23 us, with a block each 6.3).
+constexpr int JOIN_WAVES = 1024;
 constexpr int COMMIT_BLOCKS = 4096;       // K and V of few rows: fewer channels a block, until there are so many blocks
 
 // Parts that a row of logits is cut into: about a thousand blocks altogether, each of 8 to 32 KB.
@@ -191,7 +210,6 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     A.T = T;
     A.max_nodes = max_nodes;
     A.parts = static_cast<float *>(ws);
-    A.block_bits = plan.block_bits;
     A.part_rows = plan.part_rows;
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const dim3 blocks(1 << plan.block_bits);
@@ -199,33 +217,20 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     // A request of one unit is never cut.  A row has at most blocks / heads parts and two more: few, or many rows, a wave each.
     const int items = T * heads_q;
     const bool shared = items < JOIN_WAVES && (1 << plan.block_bits) / cache->heads + 2 > 8;
-    const auto join = [&](auto wt, auto dc, auto cut) {
+    on_kernel(plan, dt, dim, [&](auto wt, auto dc, auto cut) {
         using W = typename decltype(wt)::type;
+        using Cut = decltype(cut);
         constexpr int DIM = decltype(dc)::value;
+        if constexpr (Cut::ROWS == TW_ROWS) {
+            granted = grant_lds<k_tree_attn_wide<DIM>>(TW_LDS);
+            if (!granted) return;
+            launch(k_tree_attn_wide<DIM>, blocks, dim3(TW_THREADS), TW_LDS, hs, A);
+        } else {
+            launch((k_tree_attn<W, DIM, Cut::ROWS / 16>), blocks, dim3(TA_THREADS), 0, hs, A);
+        }
         if (plan.steps <= 1) return;
-        if (shared) launch((k_tree_join<W, DIM, decltype(cut), true>), dim3(items), dim3(TA_THREADS), 0, hs, A);
-        else launch((k_tree_join<W, DIM, decltype(cut), false>), dim3(tiles(items, TA_WAVES)), dim3(TA_THREADS), 0, hs, A);
-    };
-    on_dim(dim, [&](auto dc) {
-        constexpr int DIM = decltype(dc)::value;
-        if constexpr (DIM <= 128)
-            if (plan.wide) {
-                granted = grant_lds<k_tree_attn_wide<DIM>>(TW_LDS);
-                if (!granted) return;
-                launch(k_tree_attn_wide<DIM>, blocks, dim3(TW_THREADS), TW_LDS, hs, A);
-                join(Type<bf16>{}, dc, TreeCut<TW_ROWS, tw_tiles<DIM>(), true>{});
-                return;
-            }
-        on_tiles(plan.nt, [&](auto nc) {
-            constexpr int NT = decltype(nc)::value;
-            on_type(dt, [&](auto wt) {
-                using W = typename decltype(wt)::type;
-                if constexpr (NT == 1 || (DIM <= 128 && (NT == 2 || std::is_same<W, bf16>::value))) {
-                    launch((k_tree_attn<W, DIM, NT>), blocks, dim3(TA_THREADS), 0, hs, A);
-                    join(wt, dc, TreeCut<16 * NT, TA_WAVES, false>{});
-                }
-            });
-        });
+        if (shared) launch((k_tree_join<W, DIM, Cut, true>), dim3(items), dim3(64 * tj_waves<true>()), 0, hs, A);
+        else launch((k_tree_join<W, DIM, Cut, false>), dim3(tiles(items, tj_waves<false>())), dim3(64 * tj_waves<false>()), 0, hs, A);
     });
     return granted ? hip_status(hipSuccess) : SVDP_ERR_UNSUPPORTED;
 }

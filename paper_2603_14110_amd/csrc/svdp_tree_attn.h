@@ -41,18 +41,17 @@ struct TreeAttnArgs {
     const int32_t *table, *lens, *starts;
     void *out;
     float *lse;
-    float *parts;                       // [2 << block_bits] parts of part_rows (dim + 2) floats
+    float *parts;                       // [2 << Cut::BITS] parts of part_rows (dim + 2) floats
     float scale;
     int max_pages, pages, page_bits, heads, group, R, T, max_nodes;
-    int block_bits;                     // there are 1 << block_bits blocks
     int part_rows;                      // rows of a part: no more than a request has, nor a block
 };
 
-// How a kernel cuts the work: ROWS rows a block, units of TILES tiles; the tree's own tiles follow the cached ones, or begin a
-// unit of their own.
-template <int ROWS_, int TILES, bool APART>
+// How a kernel cuts the work: ROWS rows a block, units of TILES tiles, 1 << BITS blocks; the tree's own tiles follow the cached
+// ones, or begin a unit of their own.
+template <int ROWS_, int TILES, int BITS_, bool APART>
 struct TreeCut {
-    static constexpr int ROWS = ROWS_;
+    static constexpr int ROWS = ROWS_, UNIT = TILES, BITS = BITS_;
     static __device__ __forceinline__ int steps(int tiles, int n)
     {
         const int more = (n + TA_TILE - 1) / TA_TILE;
@@ -106,14 +105,16 @@ __device__ __forceinline__ int tree_units(const TreeAttnArgs &A, int lane, int *
 }
 
 // The unit where block b begins: an equal share for each, or one unit each for the first blocks.  No block in between has none.
-__device__ __forceinline__ int tree_begin(int b, int units, int bits)
+template <typename Cut>
+__device__ __forceinline__ int tree_begin(int b, int units)
 {
-    return units >> bits == 0 ? min(b, units) : (int)(((int64_t)b * units) >> bits);
+    return units >> Cut::BITS == 0 ? min(b, units) : (int)(((int64_t)b * units) >> Cut::BITS);
 }
 // The block that has unit u: the first one whose successor begins behind u.
-__device__ __forceinline__ int tree_block_of(int u, int units, int bits)
+template <typename Cut>
+__device__ __forceinline__ int tree_block_of(int u, int units)
 {
-    return units >> bits == 0 ? u : (int)(((((int64_t)u + 1) << bits) + units - 1) / units) - 1;
+    return units >> Cut::BITS == 0 ? u : (int)(((((int64_t)u + 1) << Cut::BITS) + units - 1) / units) - 1;
 }
 
 // The request that unit u belongs to, and how far into it that is; own, upto as tree_units left them.
@@ -395,11 +396,17 @@ constexpr int ta_waves(int element, int dim, int nt)
 {
     return nt * (dim / 4 + dim * element / 16) + 2 * dim * element / 8 <= 200 ? 2 : 1;
 }
+// One block a compute unit, so that there are few parts to join (32 rows over 30 000 tokens: 25.4 + 5.1 us; with 512 blocks
+// 25.9 + 6.6).  Two where the registers have room and the parts are small: their starts and ends overlap (a ragged batch
+// of one row a head, 592 MB: 105 us; with 256 blocks 110).
+template <typename W, int DIM, int NT>
+using NarrowCut = TreeCut<16 * NT, TA_WAVES, NT == 1 && ta_waves(sizeof(W), DIM, NT) == 2 ? 9 : 8, false>;
+
 template <typename W, int DIM, int NT>
 __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tree_attn(TreeAttnArgs A)
 {
     using X = TreeTile<W, DIM>;
-    using Cut = TreeCut<16 * NT, TA_WAVES, false>;
+    using Cut = NarrowCut<W, DIM, NT>;
     constexpr int ROWS = Cut::ROWS, E = X::E, KC = X::KC, VT = X::VT, DT = DIM / 16;
     constexpr int DC = DIM * NT <= 128 ? DIM : 128 / NT;       // channels that the waves' sums meet in LDS by: 32 KB
     __shared__ float s_top[TA_WAVES][ROWS], s_total[TA_WAVES][ROWS];
@@ -409,8 +416,8 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
 
     int own, upto;
     const int units = tree_units<Cut>(A, lane, &own, &upto);
-    int u = tree_begin(blockIdx.x, units, A.block_bits);
-    const int u1 = tree_begin(blockIdx.x + 1, units, A.block_bits);
+    int u = tree_begin<Cut>(blockIdx.x, units);
+    const int u1 = tree_begin<Cut>(blockIdx.x + 1, units);
     if (u >= u1) return;
     int rem, r = tree_request<Cut>(A, u, lane, own, upto, &rem);
 
@@ -669,14 +676,18 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
     }
 }
 
-// The parts of a row and head, where there are more than one: a wave each (SHARED false), or a block each, whose waves take every
-// fourth part (few rows with many parts).
+// The parts of a row and head, where there are more than one: a wave each (SHARED false), or a block each, whose eight waves take
+// parts in turn (few rows with many parts).  Bound by latency, of the lengths and then of the parts, which other XCDs have written:
+// 3.5 us at the least; 5.1 us for 256 rows and heads with 32 parts each (a wave each: 23 us).
+template <bool SHARED>
+constexpr int tj_waves() { return SHARED ? 8 : 4; }
 template <typename W, int DIM, typename Cut, bool SHARED>
-__global__ __launch_bounds__(TA_THREADS) void k_tree_join(TreeAttnArgs A)
+__global__ __launch_bounds__(64 * tj_waves<SHARED>()) void k_tree_join(TreeAttnArgs A)
 {
-    constexpr int ROWS = Cut::ROWS, PER = DIM / 64, STEP = SHARED ? TA_WAVES : 1, AHEAD = SHARED && DIM <= 128 ? 16 : 8;
+    constexpr int WAVES = tj_waves<SHARED>();
+    constexpr int ROWS = Cut::ROWS, PER = DIM / 64, STEP = SHARED ? WAVES : 1, AHEAD = 8;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), heads_q = A.heads * A.group;
-    const int item = SHARED ? blockIdx.x : blockIdx.x * TA_WAVES + wave, t = item / heads_q, hq = item - t * heads_q;
+    const int item = SHARED ? blockIdx.x : blockIdx.x * WAVES + wave, t = item / heads_q, hq = item - t * heads_q;
     if (t >= A.T) return;
     const int h = hq / A.group;
 
@@ -703,10 +714,10 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_join(TreeAttnArgs A)
     const int node = t - S.start;
     if (node < 0 || node >= S.n) return;
     const int row = node * A.group + hq - h * A.group, in_part = row % ROWS, u0 = base + (h * S.row_tiles + row / ROWS) * S.steps;
-    const int b0 = tree_block_of(u0, units, A.block_bits), b1 = tree_block_of(u0 + S.steps - 1, units, A.block_bits);
+    const int b0 = tree_block_of<Cut>(u0, units), b1 = tree_block_of<Cut>(u0 + S.steps - 1, units);
     if (b0 == b1) return;                                        // one block had the whole and has written it
     // a block's first segment is its part 0: that of b0 is if b0 begins with this task
-    const int part0 = tree_begin(b0, units, A.block_bits) == u0 ? 0 : 1;
+    const int part0 = tree_begin<Cut>(b0, units) == u0 ? 0 : 1;
 
     float top = -INFINITY, total = 0.f, sum[PER];
 #pragma unroll
@@ -743,7 +754,7 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_join(TreeAttnArgs A)
         }
     }
     if constexpr (SHARED) {
-        __shared__ float s_top[TA_WAVES], s_total[TA_WAVES], s_sum[TA_WAVES][DIM];
+        __shared__ float s_top[WAVES], s_total[WAVES], s_sum[WAVES][DIM];
         if (lane == 0) {
             s_top[wave] = top;
             s_total[wave] = total;
@@ -752,12 +763,13 @@ __global__ __launch_bounds__(TA_THREADS) void k_tree_join(TreeAttnArgs A)
         for (int i = 0; i < PER; ++i) s_sum[wave][lane * PER + i] = sum[i];
         __syncthreads();
         if (wave > 0) return;
-        top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, s_top[w]);
         total = 0.f;
 #pragma unroll
         for (int i = 0; i < PER; ++i) sum[i] = 0.f;
 #pragma unroll
-        for (int w = 0; w < TA_WAVES; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float by = exp2_fast(s_top[w] - finite_shift(top));
             total += s_total[w] * by;
 #pragma unroll

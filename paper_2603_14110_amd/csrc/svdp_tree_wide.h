@@ -20,6 +20,8 @@ constexpr int TW_THREADS = 512, TW_WAVES = TW_THREADS / 64, TW_ROWS = 32 * TW_WA
 constexpr int TW_STAGE = 64 << 10, TW_LDS = 2 * TW_STAGE;
 template <int DIM>
 constexpr int tw_tiles() { return TW_STAGE / 2 / (TA_TILE * DIM * 2); }          // of a stage: 8 or 4
+template <int DIM>
+using WideCut = TreeCut<TW_ROWS, tw_tiles<DIM>(), 8, true>;
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16_t mfma_32(const uint4 &a, const uint4 &b, const f32x16_t &c)
 {
@@ -35,7 +37,7 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
 {
     using X = TreeTile<bf16, DIM>;
     constexpr int TILES = tw_tiles<DIM>(), KC = DIM / 16, DT = DIM / 32, CHUNKS = DIM / 8;
-    using Cut = TreeCut<TW_ROWS, TILES, true>;
+    using Cut = WideCut<DIM>;
     constexpr int TILE_BYTES = TA_TILE * DIM * 2, V_AT = TW_STAGE / 2;
     static_assert(TILES * TA_TILE >= 64, "the tree's tokens are one stage");
     // a stage of the tree's tokens: K where it always is; V as it comes, then in packs (finite elements), and as it is in packs
@@ -47,8 +49,8 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
 
     int own, upto;
     const int units = tree_units<Cut>(A, lane, &own, &upto);
-    int u = tree_begin(blockIdx.x, units, A.block_bits);
-    const int u1 = tree_begin(blockIdx.x + 1, units, A.block_bits);
+    int u = tree_begin<Cut>(blockIdx.x, units);
+    const int u1 = tree_begin<Cut>(blockIdx.x + 1, units);
     if (u >= u1) return;
     int rem, r = tree_request<Cut>(A, u, lane, own, upto, &rem);
 
