@@ -1,0 +1,114 @@
+"""The small decoder that runs tree attention, sparse FFN, acceptance, block tables and commit together."""
+import pytest
+
+
+def _follow(history, tokens, parents):
+    """The text that a node stands for is the history and its branch."""
+    texts = []
+    for t, p in zip(tokens, parents):
+        texts.append((texts[p] if p >= 0 else list(history)) + [t])
+    return texts
+
+
+@pytest.mark.parametrize("history,nodes", [([7], 5), ([1, 2, 1], 5), ([3, 1, 4, 1, 5, 9, 1], 6), ([2] * 9, 7), (list(range(20)) * 3, 63),
+                                           ([1, 2, 1], 0)])
+def test_lookup_proposes_what_followed_before(history, nodes):
+    from paper_2603_14110_amd.draft import lookup
+
+    tokens, parents = lookup(history, nodes)
+    assert len(tokens) == len(parents) <= nodes
+    assert all(-1 <= p < j for j, p in enumerate(parents))
+    assert len(set(zip(tokens, parents))) == len(tokens)
+    if history.count(history[-1]) > 1 and nodes:
+        assert tokens
+    for text in _follow(history[-1:], tokens, parents):
+        assert any(history[i:i + len(text)] == text for i in range(len(history)))
+
+
+PROMPTS = [[5], [17, 4, 4, 250, 17], [(7 * i * i + 3) % 300 for i in range(150)]]
+NEW = 40
+
+
+def _decoder(**over):
+    import torch
+    from paper_2603_14110_amd.draft import random_decoder
+
+    made = dict(layers=2, V=300, dtype=torch.float32, requests=len(PROMPTS), pages=24, page=32, max_len=256)
+    return random_decoder(**{**made, **over})
+
+
+def _all_free(decoder):
+    assert decoder.lens.tolist() == [0] * len(PROMPTS)
+    assert int(decoder.pool[1]) == decoder.ring.numel()
+    assert sorted(decoder.ring.tolist()) == list(range(decoder.ring.numel()))
+
+
+@pytest.mark.gpu
+def test_drafts_do_not_change_the_tokens_and_pages_come_back():
+    """fp32 and every neuron active, so that neither other orders of the same sums nor lists that tokens share change an answer."""
+    decoder = _decoder(bias=1e4)
+    plain, steps = decoder.generate(PROMPTS, NEW, nodes=1)
+    assert steps == NEW and [len(o) for o in plain] == [NEW] * len(PROMPTS)
+    assert min(len(set(o)) for o in plain) > 3
+    _all_free(decoder)
+    for nodes in (2, 8, 33, 64):
+        out, steps = decoder.generate(PROMPTS, NEW, nodes=nodes)
+        assert out == plain and steps <= NEW
+        _all_free(decoder)
+    # drafts that are right: as many tokens a step as there are nodes
+    texts = [p + o for p, o in zip(PROMPTS, plain)]
+
+    def right(history, nodes):
+        text = next(t for t in texts if t[:len(history)] == list(history))
+        more = text[len(history):len(history) + nodes]
+        return more, list(range(-1, len(more) - 1))
+
+    out, steps = decoder.generate(PROMPTS, NEW, nodes=8, draft=right)
+    assert out == plain and steps == -(-NEW // 8)
+    _all_free(decoder)
+
+
+@pytest.mark.gpu
+def test_tokens_are_those_of_a_plain_decoder_in_64_bits():
+    """Every neuron active: the FFN is the dense one, and the whole text can be computed at once with a causal mask.  A token has
+    to be the largest logit's wherever the second is more than 1e-3 of the logits' spread behind (fp32 through two layers is off
+    by some 1e-5 of it)."""
+    import torch
+
+    decoder = _decoder(bias=1e4)
+    out, _ = decoder.generate(PROMPTS, NEW, nodes=12)
+    f64 = lambda t: t.double().cpu()
+    norm = lambda x: x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-6)
+    checked = 0
+    for prompt, more in zip(PROMPTS, out):
+        text = torch.tensor(prompt + more[:-1])
+        T, hq, h, dim = len(text), decoder.heads_q, decoder.heads, decoder.dim
+        x = f64(decoder.embed)[text] + f64(decoder.where)[:T]
+        for layer, Wqkv, Wo in zip(decoder.ffn, decoder.Wqkv, decoder.Wo):
+            q, k, v = (norm(x) @ f64(Wqkv)).view(T, hq + 2 * h, dim).split((hq, h, h), dim=1)
+            k, v = k.repeat_interleave(hq // h, 1), v.repeat_interleave(hq // h, 1)
+            s = (q.transpose(0, 1) @ k.permute(1, 2, 0)) * dim ** -0.5
+            s = s.masked_fill(torch.ones(T, T).triu(1).bool(), float("-inf")).softmax(-1)
+            x = x + (s @ v.transpose(0, 1)).transpose(0, 1).reshape(T, hq * dim) @ f64(Wo)
+            w = {n: f64(layer.tensors[n]) for n in ("W_gate", "W_up", "W_downT")}
+            z = norm(x)
+            x = x + ((z @ w["W_gate"].t()).relu() * (z @ w["W_up"].t())) @ w["W_downT"]
+        logits = (norm(x) @ f64(decoder.head).t())[len(prompt) - 1:]
+        best = logits.topk(2, dim=-1)
+        clear = best.values[:, 0] - best.values[:, 1] > 1e-3 * logits.std()
+        assert torch.equal(best.indices[clear, 0], torch.tensor(more)[clear])
+        checked += int(clear.sum())
+    assert checked > 0.9 * NEW * len(PROMPTS)
+
+
+@pytest.mark.gpu
+def test_bf16_decodes_and_too_few_pages_are_an_error():
+    import torch
+
+    decoder = _decoder(dtype=torch.bfloat16, page=64)
+    out, steps = decoder.generate(PROMPTS, NEW, nodes=16)
+    assert [len(o) for o in out] == [NEW] * len(PROMPTS) and steps <= NEW
+    assert all(0 <= t < 300 for o in out for t in o)
+    _all_free(decoder)
+    with pytest.raises(RuntimeError, match="too few pages"):
+        _decoder(pages=4).generate(PROMPTS, NEW)
