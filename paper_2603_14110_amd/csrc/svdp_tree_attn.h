@@ -66,19 +66,39 @@ struct TreeSpan {
     int len, start, n, tiles, steps, row_tiles, units;
 };
 template <typename Cut>
-__device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs &A, int r)
+__device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs &A, int len, int start, int n)
 {
     constexpr int ROWS = Cut::ROWS;
-    TreeSpan s;
-    s.len = min(max(A.lens[r], 0), A.max_pages << A.page_bits);
-    s.start = min(max(A.starts[r], 0), A.T);
-    s.n = min(min(max(A.starts[r + 1] - s.start, 0), A.max_nodes), A.T - s.start);
+    TreeSpan s{len, start, n};
     s.tiles = (s.len + TA_TILE - 1) / TA_TILE;
     s.steps = Cut::steps(s.tiles, s.n);
     s.row_tiles = (s.n * A.group + ROWS - 1) / ROWS;
     s.units = s.row_tiles * s.steps * A.heads;
     return s;
 }
+// 64 requests, a lane each: what there is of them, their units and the inclusive sums of these.  They are read once, all
+// together; a request's share is then read out of its lane.
+template <typename Cut>
+struct TreeChunk {
+    int first, len, start, n, units, upto;
+    __device__ __forceinline__ void load(const TreeAttnArgs &A, int lane, int at)
+    {
+        const int r = at + lane, i = min(r, A.R - 1);
+        const int raw_len = A.lens[i], raw_start = A.starts[i], raw_end = A.starts[i + 1];
+        first = at;
+        len = min(max(raw_len, 0), A.max_pages << A.page_bits);
+        start = min(max(raw_start, 0), A.T);
+        n = r < A.R ? min(min(max(raw_end - start, 0), A.max_nodes), A.T - start) : 0;
+        units = tree_span<Cut>(A, len, start, n).units;              // none without rows
+        upto = wave_inclusive_scan(units);
+    }
+    __device__ __forceinline__ int all() const { return __builtin_amdgcn_readlane(upto, 63); }
+    __device__ __forceinline__ int before(int l) const { return __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(units, l); }
+    __device__ __forceinline__ TreeSpan span(const TreeAttnArgs &A, int l) const
+    {
+        return tree_span<Cut>(A, __builtin_amdgcn_readlane(len, l), __builtin_amdgcn_readlane(start, l), __builtin_amdgcn_readlane(n, l));
+    }
+};
 
 // The same value, of which the compiler knows nothing: what is computed from it stays where it is written.  Without it, what the
 // rare parts of a loop need per lane is kept in registers that the products' operands could be read ahead into.
@@ -90,16 +110,16 @@ __device__ __forceinline__ int here(int v)
 
 __device__ __forceinline__ int lane_of_first(uint64_t ballot) { return __ffsll((unsigned long long)ballot) - 1; }
 
-// Units of all requests; `upto`: the inclusive sums of the first 64, a lane each.
+// Units of all requests; the first 64 of them stay in the chunk.
 template <typename Cut>
-__device__ __forceinline__ int tree_units(const TreeAttnArgs &A, int lane, int *own, int *upto)
+__device__ __forceinline__ int tree_units(const TreeAttnArgs &A, int lane, TreeChunk<Cut> &chunk)
 {
-    *own = lane < A.R ? tree_span<Cut>(A, lane).units : 0;
-    *upto = wave_inclusive_scan(*own);
-    int all = __builtin_amdgcn_readlane(*upto, 63);
+    chunk.load(A, lane, 0);
+    int all = chunk.all();
     for (int c = 64; c < A.R; c += 64) {
-        const int u = c + lane < A.R ? tree_span<Cut>(A, c + lane).units : 0;
-        all += __builtin_amdgcn_readlane(wave_inclusive_scan(u), 63);
+        TreeChunk<Cut> other;
+        other.load(A, lane, c);
+        all += other.all();
     }
     return all;
 }
@@ -117,22 +137,17 @@ __device__ __forceinline__ int tree_block_of(int u, int units)
     return units >> Cut::BITS == 0 ? u : (int)(((((int64_t)u + 1) << Cut::BITS) + units - 1) / units) - 1;
 }
 
-// The request that unit u belongs to, and how far into it that is; own, upto as tree_units left them.
+// The request that unit u belongs to, as the lane that has it in the chunk, and how far into it that is.
 template <typename Cut>
-__device__ __forceinline__ int tree_request(const TreeAttnArgs &A, int u, int lane, int own, int upto, int *rem)
+__device__ __forceinline__ int tree_request(const TreeAttnArgs &A, int u, int lane, TreeChunk<Cut> &chunk, int *rem)
 {
-    for (int c = 0, base = 0;; c += 64) {
-        if (c > 0) {
-            own = c + lane < A.R ? tree_span<Cut>(A, c + lane).units : 0;
-            upto = wave_inclusive_scan(own);
-        }
-        const uint64_t behind = __ballot(base + upto > u);
+    for (int base = 0;; base += chunk.all(), chunk.load(A, lane, chunk.first + 64)) {
+        const uint64_t behind = __ballot(base + chunk.upto > u);
         if (behind != 0) {
             const int l = lane_of_first(behind);
-            *rem = u - base - __builtin_amdgcn_readlane(upto, l) + __builtin_amdgcn_readlane(own, l);
-            return c + l;
+            *rem = u - base - chunk.before(l);
+            return l;
         }
-        base += __builtin_amdgcn_readlane(upto, 63);
     }
 }
 
@@ -414,16 +429,21 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, m = lane & 15;
     const int heads_q = A.heads * A.group;
 
-    int own, upto;
-    const int units = tree_units<Cut>(A, lane, &own, &upto);
+    TreeChunk<Cut> chunk;
+    const int units = tree_units(A, lane, chunk);
     int u = tree_begin<Cut>(blockIdx.x, units);
     const int u1 = tree_begin<Cut>(blockIdx.x + 1, units);
     if (u >= u1) return;
-    int rem, r = tree_request<Cut>(A, u, lane, own, upto, &rem);
+    int rem, l = tree_request(A, u, lane, chunk, &rem);
 
-    for (bool first = true; u < u1; ++r, rem = 0) {
-        const TreeSpan S = tree_span<Cut>(A, __builtin_amdgcn_readfirstlane(r));
+    for (bool first = true; u < u1; ++l, rem = 0) {
+        if (l == 64) {
+            chunk.load(A, lane, chunk.first + 64);
+            l = 0;
+        }
+        const TreeSpan S = chunk.span(A, l);
         if (S.units == 0) continue;
+        const int r = chunk.first + l;
         const table_t table = (table_t)(uintptr_t)(A.table + (size_t)r * A.max_pages);
         int task = rem / S.steps, s0 = rem - task * S.steps;
         for (; task < A.heads * S.row_tiles && u < u1; ++task, s0 = 0, first = false) {
@@ -691,28 +711,19 @@ __global__ __launch_bounds__(64 * tj_waves<SHARED>()) void k_tree_join(TreeAttnA
     if (t >= A.T) return;
     const int h = hq / A.group;
 
-    int own, upto;
-    const int units = tree_units<Cut>(A, lane, &own, &upto);
-    int r = -1, base = 0;
-    for (int c = 0; c < A.R; c += 64) {
-        if (c > 0) {
-            own = c + lane < A.R ? tree_span<Cut>(A, c + lane).units : 0;
-            upto = wave_inclusive_scan(own);
-        }
-        const bool here = c + lane < A.R && A.starts[c + lane] <= t && t < A.starts[c + lane + 1];
-        const uint64_t found = __ballot(here);
-        if (found != 0) {
-            const int l = lane_of_first(found);
-            r = c + l;
-            base += __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(own, l);
-            break;
-        }
-        base += __builtin_amdgcn_readlane(upto, 63);
+    TreeChunk<Cut> chunk;
+    const int units = tree_units(A, lane, chunk);
+    int base = 0;
+    uint64_t found;
+    while ((found = __ballot(t >= chunk.start && t < chunk.start + chunk.n)) == 0) {
+        if (chunk.first + 64 >= A.R) return;                     // a row of no request
+        base += chunk.all();
+        chunk.load(A, lane, chunk.first + 64);
     }
-    if (r < 0) return;
-    const TreeSpan S = tree_span<Cut>(A, r);
+    const int l = lane_of_first(found);
+    const TreeSpan S = chunk.span(A, l);
+    base += chunk.before(l);
     const int node = t - S.start;
-    if (node < 0 || node >= S.n) return;
     const int row = node * A.group + hq - h * A.group, in_part = row % ROWS, u0 = base + (h * S.row_tiles + row / ROWS) * S.steps;
     const int b0 = tree_block_of<Cut>(u0, units), b1 = tree_block_of<Cut>(u0 + S.steps - 1, units);
     if (b0 == b1) return;                                        // one block had the whole and has written it

@@ -47,12 +47,12 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), f = lane >> 5, m = lane & 31;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t *)tw_smem;
 
-    int own, upto;
-    const int units = tree_units<Cut>(A, lane, &own, &upto);
+    TreeChunk<Cut> chunk;
+    const int units = tree_units(A, lane, chunk);
     int u = tree_begin<Cut>(blockIdx.x, units);
     const int u1 = tree_begin<Cut>(blockIdx.x + 1, units);
     if (u >= u1) return;
-    int rem, r = tree_request<Cut>(A, u, lane, own, upto, &rem);
+    int rem, l = tree_request(A, u, lane, chunk, &rem);
 
     // where a lane's operands lie in a tile (chunk c of K: ^ 32 c)
     const int k_at = tw_token(m) * CHUNKS * 16 + ((f ^ tw_swizzle(tw_token(m), DIM)) * 16);
@@ -61,9 +61,14 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
     const int fill_tile = DIM == 128 ? wave >> 1 : wave;
     const int fill_k = (lane / CHUNKS) * CHUNKS * 16 + (((lane % CHUNKS) ^ tw_swizzle(lane / CHUNKS, DIM)) * 16);
 
-    for (bool first = true; u < u1; ++r, rem = 0) {
-        const TreeSpan S = tree_span<Cut>(A, __builtin_amdgcn_readfirstlane(r));
+    for (bool first = true; u < u1; ++l, rem = 0) {
+        if (l == 64) {
+            chunk.load(A, lane, chunk.first + 64);
+            l = 0;
+        }
+        const TreeSpan S = chunk.span(A, l);
         if (S.units == 0) continue;
+        const int r = chunk.first + l;
         const int cached_steps = (S.tiles + TILES - 1) / TILES, per_page = A.page_bits - 5;
         int task = rem / S.steps, s0 = rem - task * S.steps;
         for (; task < A.heads * S.row_tiles && u < u1; ++task, s0 = 0, first = false) {
