@@ -280,3 +280,42 @@ def test_binding_refuses_what_does_not_go_together(env):
     odd = binding.KVCache.empty(1, 1, 48, 1, 64)
     with pytest.raises(E, match="unsupported"):
         binding.tree_attn_workspace_bytes(odd, 1, 1, 1, 1)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_requests_of_many_rows(env, dim):
+    """More requests than a wave has lanes, for the kernel whose waves take different rows."""
+    torch, binding, draft = env
+    rng = np.random.default_rng(4)
+    lens = [int(v) for v in rng.integers(0, 200, 100)]
+    nodes = [24] + [int(v) for v in rng.integers(0, 25, 99)]
+    c = Attn(torch, binding, dtype="bf16", dim=dim, heads=2, group=3, page=32, lens=lens, nodes=nodes, tree="random", seed=6)
+    out, lse = c.call(binding)
+    c.check(draft, out, lse)
+
+
+@pytest.mark.parametrize("dtype,dim,group", [("bf16", 64, 2), ("bf16", 128, 2), ("bf16", 128, 4), ("bf16", 256, 4), ("f32", 64, 2), ("f32", 128, 4)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_few_rows_do_not_see_what_is_hidden(env, dtype, dim, group, bad):
+    """One and two row tiles: the places behind a length and a node that not every row sees."""
+    torch, binding, draft = env
+    c = Attn(torch, binding, dtype=dtype, dim=dim, heads=2, group=group, page=64, lens=[70, 0, 33], nodes=[7, 4, 5], seed=12)
+    out, lse = c.call(binding)
+    c.check(draft, out, lse)
+    e = 8 if dtype == "bf16" else 4
+    K, V = c.cache.K, c.cache.V
+    for r, n in enumerate(c.lens):
+        for j in range(n, -(-n // c.page) * c.page):
+            K[1, c.table[r][j // c.page], :, j % c.page] = bad
+            V[1, c.table[r][j // c.page], :, j % c.page // e, :, j % e] = bad
+    out2, lse2 = c.call(binding)
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+    t = c.starts[0] + 6
+    c.k[t] = bad
+    c.v[t] = bad
+    out3, lse3 = c.call(binding)
+    blind = torch.tensor([i >= c.starts[1] or not (c.words[i] >> 6) & 1 for i in range(c.starts[-1])], device="cuda")
+    scale = out.float().abs().amax()
+    assert float((out3.float() - out.float()).abs()[blind].amax()) <= (2.0 ** -7 if dtype == "bf16" else 1e-5) * scale
+    assert float((lse3 - lse).abs()[blind].amax()) <= 1e-5
+    assert not bool(torch.isfinite(out3[t].float()).any())
