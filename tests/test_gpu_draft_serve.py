@@ -387,3 +387,11 @@ def test_commit_in_a_graph(env):
         graph.replay()
         torch.cuda.synchronize()
         assert np.array_equal(cache.K.cpu().numpy(), K) and np.array_equal(cache.V.cpu().numpy(), V)
+
+
+@pytest.mark.parametrize("R,page,width,pages,rows,free", [(1024, 32, 4, 5000, 700, None), (1025, 64, 4, 5000, 300, None), (2500, 32, 3, 9000, 2600, 1500),
+                                                          (4096, 32, 2, 9000, 50, 700)])
+def test_plan_of_more_requests_than_threads(env, R, page, width, pages, rows, free):
+    torch, binding, draft = env
+    c = make_plan(R, R, page, width, pages, rows, free, padded=3)
+    assert run_plan(torch, binding, c) == tuple(draft.plan(**c, rows=len(c["keep"])))
