@@ -704,8 +704,9 @@ constexpr int tj_waves() { return SHARED ? 8 : 4; }
 template <typename W, int DIM, typename Cut, bool SHARED>
 __global__ __launch_bounds__(64 * tj_waves<SHARED>()) void k_tree_join(TreeAttnArgs A)
 {
-    constexpr int WAVES = tj_waves<SHARED>();
-    constexpr int ROWS = Cut::ROWS, PER = DIM / 64, STEP = SHARED ? WAVES : 1, AHEAD = 8;
+    // a lane has four channels; where that leaves lanes over, groups of them take different parts
+    constexpr int WAVES = tj_waves<SHARED>(), ROWS = Cut::ROWS, LANES = DIM / 4, GROUPS = 64 / LANES;
+    constexpr int STEP = (SHARED ? WAVES : 1) * GROUPS, AHEAD = GROUPS == 1 ? 8 : 4;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), heads_q = A.heads * A.group;
     const int item = SHARED ? blockIdx.x : blockIdx.x * WAVES + wave, t = item / heads_q, hq = item - t * heads_q;
     if (t >= A.T) return;
@@ -730,19 +731,18 @@ __global__ __launch_bounds__(64 * tj_waves<SHARED>()) void k_tree_join(TreeAttnA
     // a block's first segment is its part 0: that of b0 is if b0 begins with this task
     const int part0 = tree_begin<Cut>(b0, units) == u0 ? 0 : 1;
 
-    float top = -INFINITY, total = 0.f, sum[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) sum[i] = 0.f;
-    for (int b = b0 + (SHARED ? wave : 0); b <= b1; b += STEP * AHEAD) {
+    float top = -INFINITY, total = 0.f;
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+    const int c = lane % LANES * 4;
+    for (int b = b0 + (SHARED ? wave * GROUPS : 0) + lane / LANES; b <= b1; b += STEP * AHEAD) {
         float2 head[AHEAD];
-        float in[AHEAD][PER];
+        f32x4_t in[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
             const int at = min(b + j * STEP, b1);
             const float *part = tree_part(A, at, at == b0 ? part0 : 0, DIM);
             head[j] = *reinterpret_cast<const float2 *>(part + (size_t)A.part_rows * DIM + 2 * in_part);
-#pragma unroll
-            for (int i = 0; i < PER; ++i) in[j][i] = part[(size_t)in_part * DIM + lane * PER + i];
+            in[j] = *reinterpret_cast<const f32x4_t *>(part + (size_t)in_part * DIM + c);
         }
         float next = top;
 #pragma unroll
@@ -753,46 +753,59 @@ __global__ __launch_bounds__(64 * tj_waves<SHARED>()) void k_tree_join(TreeAttnA
         const float shift = finite_shift(next), old = exp2_fast(top - shift);
         top = next;
         total *= old;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) sum[i] *= old;
+        sum *= old;
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
             if (b + j * STEP > b1) break;
             const float by = exp2_fast(head[j].x - shift);
             total += head[j].y * by;
+            sum += in[j] * by;
+        }
+    }
+    // the groups together: all lanes of the same channels end up with the same
+    if constexpr (GROUPS > 1) {
+        float all = top;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) sum[i] += in[j][i] * by;
+        for (int m = LANES; m < 64; m *= 2) all = fmaxf(all, __shfl_xor(all, m));
+        const float by = exp2_fast(top - finite_shift(all));
+        top = all;
+        total *= by;
+        sum *= by;
+#pragma unroll
+        for (int m = LANES; m < 64; m *= 2) {
+            total += __shfl_xor(total, m);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], m);
         }
     }
     if constexpr (SHARED) {
-        __shared__ float s_top[WAVES], s_total[WAVES], s_sum[WAVES][DIM];
+        __shared__ float s_top[WAVES], s_total[WAVES];
+        __shared__ __align__(16) float s_sum[WAVES][DIM];
         if (lane == 0) {
             s_top[wave] = top;
             s_total[wave] = total;
         }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) s_sum[wave][lane * PER + i] = sum[i];
+        if (lane < LANES) *reinterpret_cast<f32x4_t *>(&s_sum[wave][c]) = sum;
         __syncthreads();
         if (wave > 0) return;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) top = fmaxf(top, s_top[w]);
         total = 0.f;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) sum[i] = 0.f;
+        sum = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
             const float by = exp2_fast(s_top[w] - finite_shift(top));
             total += s_total[w] * by;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) sum[i] += s_sum[w][lane * PER + i] * by;
+            sum += *reinterpret_cast<const f32x4_t *>(&s_sum[w][c]) * by;
         }
     }
+    if (lane >= LANES) return;
     const int64_t at = (int64_t)t * heads_q + hq;
     const float by = total == 0.f ? 0.f : 1.f / total;
-    W to[PER];
+    W to[4];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) from_f32(sum[i] * by, to + i);
-    __builtin_memcpy(__builtin_assume_aligned(static_cast<W *>(A.out) + at * DIM + lane * PER, sizeof(to)), to, sizeof(to));
+    for (int i = 0; i < 4; ++i) from_f32(sum[i] * by, to + i);
+    __builtin_memcpy(__builtin_assume_aligned(static_cast<W *>(A.out) + at * DIM + c, sizeof(to)), to, sizeof(to));
     if (lane == 0 && A.lse != nullptr) A.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
 }
 
