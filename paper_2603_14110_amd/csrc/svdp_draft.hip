@@ -129,9 +129,9 @@ AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, in
     p.bytes = align_up(((size_t)2 << p.block_bits) * p.part_rows * (dim + 2) * 4);
     return p;
 }
-// Rows and heads from which the join has a wave for each, whatever the parts (2048 of 10 parts: 6.6 us, with a block each 9.9; 256
-// of 64 parts: 23 us, with a block each 6.3).
-constexpr int JOIN_WAVES = 1024;
+// Rows and heads from which the join has a wave for each, whatever the parts (768 of 24 requests: 4.2 us, with a block each 5.2; 256
+// of one request, with 32 parts: 8.2 us, with a block each 4.5).
+constexpr int JOIN_WAVES = 512;
 constexpr int COMMIT_BLOCKS = 4096;       // K and V of few rows: fewer channels a block, until there are so many blocks
 
 // Parts that a row of logits is cut into: about a thousand blocks altogether, each of 8 to 32 KB.
@@ -214,7 +214,8 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const dim3 blocks(1 << plan.block_bits);
     bool granted = true;
-    // A request of one unit is never cut.  A row has at most blocks / heads parts and two more: few, or many rows, a wave each.
+    // A request of one unit is never cut.  A row has at most blocks / heads parts and two more: up to eight, which a wave reads at
+    // once, or many rows, a wave each.
     const int items = T * heads_q;
     const bool shared = items < JOIN_WAVES && (1 << plan.block_bits) / cache->heads + 2 > 8;
     on_kernel(plan, dt, dim, [&](auto wt, auto dc, auto cut) {

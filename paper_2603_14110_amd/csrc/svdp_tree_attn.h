@@ -15,6 +15,10 @@
 // row, and each block takes an equal piece of it, whatever the requests' lengths are (they are known on the device only).  What a block
 // has of a (request, head, row tile) goes to the output where it is the whole of it, and otherwise, as a sum with its maximum, to
 // the workspace, where k_tree_join puts the parts together.
+//
+// What bounds it: reading K and V.  24 requests of 3000 tokens, one row a head, bf16, 128 channels: 1180 MB in 197 us, 6.0 TB/s;
+// a ragged batch of 592 MB in 105 us; 32 rows over 30 000 tokens, 123 MB, in 25.6 us, of which some 5 go by before and behind the
+// reading.  One row over 780 tokens, 12.8 MB, takes 7.2 us, the latency of five loads after each other (lengths, page, K and V, parts).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -698,7 +702,7 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
 
 // The parts of a row and head, where there are more than one: a wave each (SHARED false), or a block each, whose eight waves take
 // parts in turn (few rows with many parts).  Bound by latency, of the lengths and then of the parts, which other XCDs have written:
-// 3.5 us at the least; 5.1 us for 256 rows and heads with 32 parts each (a wave each: 23 us).
+// 2.9 us at the least; 4.2 us for 256 rows and heads with 32 parts each; 5740 rows and heads of wide blocks, 34 MB, in 8.8 us.
 template <bool SHARED>
 constexpr int tj_waves() { return SHARED ? 8 : 4; }
 template <typename W, int DIM, typename Cut, bool SHARED>
