@@ -308,8 +308,8 @@ typedef struct svdp_kv_cache {
  *   out[t][h] = sum_j softmax_j(scale q[t][h] . k_j[c]) v_j[c],  c = h / (heads_q / heads).
  * q: device rows of [heads_q][dim], q_stride elements apart; k, v: device rows of [heads][dim], the step's own tokens
  * (not in the cache), k_stride and v_stride elements apart; the three pointers 16-byte aligned, the strides whole
- * 16-byte vectors.  scale: times log2(e) it has to be finite.  lens: device [R] int32.  out: device [T][heads_q][dim] in the cache's type, rows of requests
- * written (padding and nodes past max_nodes are not).  lse: device [T][heads_q] fp32, nullable: the natural logarithm
+ * 16-byte vectors.  scale: finite, and times log2(e) too.  lens: device [R] int32.  out: device [T][heads_q][dim] in the
+ * cache's type, rows of requests written (padding and nodes past max_nodes are not).  lse: device [T][heads_q] fp32, nullable: the natural logarithm
  * of the softmax's denominator (with its maximum), for joining with attention over other tokens.
  * A row that sees nothing: out 0, lse -inf; so too where every weight is zero (all scores -inf).  Tokens that a row
  * does not see have no influence on it, NaN and infinities included.  Scores, softmax and sums are fp32; the weights are

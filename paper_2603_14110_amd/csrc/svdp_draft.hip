@@ -201,6 +201,7 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     A.out = out;
     A.lse = lse;
     A.scale = scale;
+    A.room = max_pages << bits_of(cache->page);
     A.max_pages = max_pages;
     A.pages = cache->pages;
     A.page_bits = bits_of(cache->page);
@@ -208,9 +209,10 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     A.group = heads_q / cache->heads;
     A.R = R;
     A.T = T;
-    A.max_nodes = max_nodes;
+    A.max_nodes = (uint16_t)max_nodes;
     A.parts = static_cast<float *>(ws);
-    A.part_rows = plan.part_rows;
+    A.part_rows = (uint16_t)plan.part_rows;
+    const TreeJoinArgs J = A;
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const dim3 blocks(1 << plan.block_bits);
     bool granted = true;
@@ -230,8 +232,8 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
             launch((k_tree_attn<W, DIM, Cut::ROWS / 16>), blocks, dim3(TA_THREADS), 0, hs, A);
         }
         if (plan.steps <= 1) return;
-        if (shared) launch((k_tree_join<W, DIM, Cut, true>), dim3(items), dim3(64 * tj_waves<true>()), 0, hs, A);
-        else launch((k_tree_join<W, DIM, Cut, false>), dim3(tiles(items, tj_waves<false>())), dim3(64 * tj_waves<false>()), 0, hs, A);
+        if (shared) launch((k_tree_join<W, DIM, Cut, true>), dim3(items), dim3(64 * tj_waves<true>()), 0, hs, J);
+        else launch((k_tree_join<W, DIM, Cut, false>), dim3(tiles(items, tj_waves<false>())), dim3(64 * tj_waves<false>()), 0, hs, J);
     });
     return granted ? hip_status(hipSuccess) : SVDP_ERR_UNSUPPORTED;
 }
@@ -296,6 +298,7 @@ svdp_status svdp_kv_plan(int32_t *table, int32_t max_pages, int32_t *ring, int32
             return SVDP_ERR_INVALID_ARG;
     if (overlap(pool_out, 8, pool, 8) || overlap(pool_out, 8, lens, rows) || overlap(pool_out, 8, add, rows))
         return SVDP_ERR_INVALID_ARG;
+    static_assert(SVDP_MAX_REQUESTS <= PLAN_EACH * PLAN_THREADS, "every request has a thread");
     const size_t lds = plan_lds(R);
     if (!grant_lds<k_kv_plan>(lds)) return SVDP_ERR_UNSUPPORTED;
     const int row_blocks = tiles(R, PLAN_WAVES), slot_blocks = std::min(tiles(T, PLAN_THREADS), 256);

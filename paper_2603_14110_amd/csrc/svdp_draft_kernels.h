@@ -22,7 +22,7 @@ inline size_t plan_lds(int R) { return ((size_t)4 * R + 1) * 4; }
 // its share of table rows and of slots, so that nothing waits for another block and nothing but the inputs is read: a new entry
 // of the table is taken from the ring again by the rows that lie in it.  Blocks for table rows and blocks for slots follow each
 // other in the grid.  What bounds it is the chain of loads (lengths, then the ring or the table), not bytes: 3.4 us for 8
-// requests, 7.0 us for 700 requests and 93 500 rows (7.8 us where a block does rows and then slots, 8.7 us with blocks of 256
+// requests, 7.0 us for 700 requests and 93 289 rows (7.8 us where a block does rows and then slots, 8.7 us with blocks of 256
 // threads, whose threads have three requests each).
 __global__ __launch_bounds__(PLAN_THREADS) void k_kv_plan(
     int32_t *table, int max_pages, int32_t *ring, int pages, int page_bits, const int32_t *pool, const int32_t *lens,

@@ -37,18 +37,25 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 typedef __bf16 ta_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float ta_f32x8 __attribute__((ext_vector_type(8)));
 
-struct TreeAttnArgs {
+// What the division of the work and the join need, in front: 16 words, which a wave finds in its registers when it starts.
+struct TreeJoinArgs {
+    const int32_t *lens, *starts;
+    void *out;
+    float *lse;
+    float *parts;                       // [2 << Cut::BITS] parts of part_rows (dim + 2) floats
+    int room, heads, group, R, T;       // room: tokens that a request's row of the table can have
+    uint16_t max_nodes;
+    uint16_t part_rows;                 // rows of a part: no more than a request has, nor a block
+};
+static_assert(sizeof(TreeJoinArgs) == 64, "as many as are loaded ahead");
+struct TreeAttnArgs : TreeJoinArgs {
     const void *K, *V;                  // of the layer
     const void *q, *k, *v;
     int64_t q_stride, k_stride, v_stride;
     const uint64_t *tree;
-    const int32_t *table, *lens, *starts;
-    void *out;
-    float *lse;
-    float *parts;                       // [2 << Cut::BITS] parts of part_rows (dim + 2) floats
+    const int32_t *table;
     float scale;
-    int max_pages, pages, page_bits, heads, group, R, T, max_nodes;
-    int part_rows;                      // rows of a part: no more than a request has, nor a block
+    int max_pages, pages, page_bits;
 };
 
 // How a kernel cuts the work: ROWS rows a block, units of TILES tiles, 1 << BITS blocks; the tree's own tiles follow the cached
@@ -70,7 +77,7 @@ struct TreeSpan {
     int len, start, n, tiles, steps, row_tiles, units;
 };
 template <typename Cut>
-__device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs &A, int len, int start, int n)
+__device__ __forceinline__ TreeSpan tree_span(const TreeJoinArgs &A, int len, int start, int n)
 {
     constexpr int ROWS = Cut::ROWS;
     TreeSpan s{len, start, n};
@@ -85,20 +92,20 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs &A, int len, in
 template <typename Cut>
 struct TreeChunk {
     int first, len, start, n, units, upto;
-    __device__ __forceinline__ void load(const TreeAttnArgs &A, int lane, int at)
+    __device__ __forceinline__ void load(const TreeJoinArgs &A, int lane, int at)
     {
         const int r = at + lane, i = min(r, A.R - 1);
         const int raw_len = A.lens[i], raw_start = A.starts[i], raw_end = A.starts[i + 1];
         first = at;
-        len = min(max(raw_len, 0), A.max_pages << A.page_bits);
+        len = min(max(raw_len, 0), A.room);
         start = min(max(raw_start, 0), A.T);
-        n = r < A.R ? min(min(max(raw_end - start, 0), A.max_nodes), A.T - start) : 0;
+        n = r < A.R ? min(min(max(raw_end - start, 0), (int)A.max_nodes), A.T - start) : 0;
         units = tree_span<Cut>(A, len, start, n).units;              // none without rows
         upto = wave_inclusive_scan(units);
     }
     __device__ __forceinline__ int all() const { return __builtin_amdgcn_readlane(upto, 63); }
     __device__ __forceinline__ int before(int l) const { return __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(units, l); }
-    __device__ __forceinline__ TreeSpan span(const TreeAttnArgs &A, int l) const
+    __device__ __forceinline__ TreeSpan span(const TreeJoinArgs &A, int l) const
     {
         return tree_span<Cut>(A, __builtin_amdgcn_readlane(len, l), __builtin_amdgcn_readlane(start, l), __builtin_amdgcn_readlane(n, l));
     }
@@ -116,7 +123,7 @@ __device__ __forceinline__ int lane_of_first(uint64_t ballot) { return __ffsll((
 
 // Units of all requests; the first 64 of them stay in the chunk.
 template <typename Cut>
-__device__ __forceinline__ int tree_units(const TreeAttnArgs &A, int lane, TreeChunk<Cut> &chunk)
+__device__ __forceinline__ int tree_units(const TreeJoinArgs &A, int lane, TreeChunk<Cut> &chunk)
 {
     chunk.load(A, lane, 0);
     int all = chunk.all();
@@ -143,7 +150,7 @@ __device__ __forceinline__ int tree_block_of(int u, int units)
 
 // The request that unit u belongs to, as the lane that has it in the chunk, and how far into it that is.
 template <typename Cut>
-__device__ __forceinline__ int tree_request(const TreeAttnArgs &A, int u, int lane, TreeChunk<Cut> &chunk, int *rem)
+__device__ __forceinline__ int tree_request(const TreeJoinArgs &A, int u, int lane, TreeChunk<Cut> &chunk, int *rem)
 {
     for (int base = 0;; base += chunk.all(), chunk.load(A, lane, chunk.first + 64)) {
         const uint64_t behind = __ballot(base + chunk.upto > u);
@@ -156,7 +163,7 @@ __device__ __forceinline__ int tree_request(const TreeAttnArgs &A, int u, int la
 }
 
 // A part's address: block b has two, of part_rows rows of DIM sums and behind them the rows' maxima and denominators.
-__device__ __forceinline__ float *tree_part(const TreeAttnArgs &A, int b, int which, int dim)
+__device__ __forceinline__ float *tree_part(const TreeJoinArgs &A, int b, int which, int dim)
 {
     return A.parts + (size_t)(2 * b + which) * A.part_rows * (dim + 2);
 }
@@ -417,7 +424,7 @@ constexpr int ta_waves(int element, int dim, int nt)
 }
 // One block a compute unit, so that there are few parts to join (32 rows over 30 000 tokens: 25.4 + 5.1 us; with 512 blocks
 // 25.9 + 6.6).  Two where the registers have room and the parts are small: their starts and ends overlap (a ragged batch
-// of one row a head, 592 MB: 105 us; with 256 blocks 110).
+// of eight requests, 592 MB: 105 us; with 256 blocks 110).
 template <typename W, int DIM, int NT>
 using NarrowCut = TreeCut<16 * NT, TA_WAVES, NT == 1 && ta_waves(sizeof(W), DIM, NT) == 2 ? 9 : 8, false>;
 
@@ -690,7 +697,7 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
                     }
                 }
             }
-            if (!whole && tid < min(ROWS, A.part_rows)) {
+            if (!whole && tid < min(ROWS, (int)A.part_rows)) {
                 const float top = top_of(tid);
                 part[(size_t)A.part_rows * DIM + 2 * tid] = top;
                 part[(size_t)A.part_rows * DIM + 2 * tid + 1] = total_of(tid, finite_shift(top));
@@ -706,7 +713,7 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
 template <bool SHARED>
 constexpr int tj_waves() { return SHARED ? 8 : 4; }
 template <typename W, int DIM, typename Cut, bool SHARED>
-__global__ __launch_bounds__(64 * tj_waves<SHARED>()) void k_tree_join(TreeAttnArgs A)
+__global__ __launch_bounds__(64 * tj_waves<SHARED>()) void k_tree_join(TreeJoinArgs A)
 {
     // a lane has four channels; where that leaves lanes over, groups of them take different parts
     constexpr int WAVES = tj_waves<SHARED>(), ROWS = Cut::ROWS, LANES = DIM / 4, GROUPS = 64 / LANES;
