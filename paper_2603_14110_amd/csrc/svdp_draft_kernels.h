@@ -307,9 +307,9 @@ constexpr int COMMIT_CHANNELS = 256;        // the least a block has of them, un
 // copied in 16-byte vectors.  V lies with e tokens of a channel side by side: where e rows in a row fill such a pack
 // (prompts), they are read together and written as whole packs, by the row of the pack's first token; other rows (branches of
 // a tree) write their elements one by one.  A lane has two channels of V, so that the packs of a wave lie side by side.  Bound
-// by reading and writing: a prompt's 618 MB (half read, half written) in 113 us, 5.5 TB/s (144 us with eight channels a lane,
+// by reading and writing: a prompt's 618 MB (half read, half written) in 111 us, 5.5 TB/s (144 us with eight channels a lane,
 // packs 128 bytes apart); a branch of a tree of 8, in 32 layers, in 3.9 us, by latency, with its channels over many blocks
-// (6.5 us with one block for all of them and for K and V).
+// (6.5 us with one block for all of them and for K and V); branches of 723 rows in 12 layers, 8.8 MB, in 6.3 us.
 template <typename W>
 __global__ __launch_bounds__(COMMIT_THREADS) void k_kv_commit(W *K, W *V, const W *k, int64_t k_layer, int64_t k_row,
                                                               const W *v, int64_t v_layer, int64_t v_row,
@@ -318,7 +318,8 @@ __global__ __launch_bounds__(COMMIT_THREADS) void k_kv_commit(W *K, W *V, const 
 {
     constexpr int E = Elem<W>::VEC, AHEAD = 4;
     __shared__ int64_t s_near[COMMIT_ROWS + 2 * E];         // slots from row t0 - E on
-    __shared__ int s_rows[COMMIT_ROWS];                     // rows that write V: row, or row | 8 for whole packs
+    __shared__ int s_rows[COMMIT_ROWS];                     // V: from the front those that write whole packs, from the back one token; K: all
+    __shared__ int s_count[2];
     const int tid = threadIdx.x, t0 = blockIdx.x * COMMIT_ROWS, layer = blockIdx.y;
     const int64_t all = (int64_t)pages << page_bits;
     if (tid < COMMIT_ROWS + 2 * E) {
@@ -337,59 +338,77 @@ __global__ __launch_bounds__(COMMIT_THREADS) void k_kv_commit(W *K, W *V, const 
     };
     const int mask = (1 << dim_bits) - 1;
     const bool of_v = blockIdx.z & 1;
-    bool writes = false, whole = false;
-    if (of_v && tid < 64) {
+    if (tid < 64) {
+        bool real = false, whole = false, first = false;
         if (tid < COMMIT_ROWS) {
             const int64_t s = s_near[E + tid];
             const int j = (int)(s & (E - 1));
-            whole = s >= 0;
+            real = whole = s >= 0;
+            first = j == 0;
 #pragma unroll
             for (int i = 0; i < E; ++i) whole &= s_near[E + tid - j + i] == s - j + i;
-            writes = s >= 0 && (!whole || j == 0);
         }
-        const uint64_t who = __ballot(writes);
-        if (writes) s_rows[__popcll(who & ((1ull << tid) - 1))] = tid | (whole ? COMMIT_ROWS : 0);
-        if (tid == 0) s_near[0] = __popcll(who);            // row t0 - E is in no pack of these rows
-    }
-    const int vectors = cn / E, items = of_v ? 0 : min(COMMIT_ROWS, T - t0) * vectors;
-    for (int i0 = tid; i0 < items; i0 += AHEAD * COMMIT_THREADS) {
-        uint4 in[AHEAD];
-        W *to[AHEAD];
-        bool real[AHEAD];
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {                   // no branch around a load: they are on their way together
-            const int i = min(i0 + a * COMMIT_THREADS, items - 1), row = i / vectors, c = (i - row * vectors) * E;
-            const int64_t slot = s_near[E + row];
-            real[a] = slot >= 0 && i0 + a * COMMIT_THREADS < items;
-            in[a] = load_raw(k + (int64_t)row * k_row + c);
-            to[a] = K + page_at(slot, c0 + c) + (((slot & (page - 1)) << dim_bits) + ((c0 + c) & mask));
+        const bool in_front = real && (!of_v || (whole && first)), behind = real && of_v && !whole;
+        const uint64_t front = __ballot(in_front), back = __ballot(behind), before = (1ull << tid) - 1;
+        if (in_front) s_rows[__popcll(front & before)] = tid;
+        if (behind) s_rows[COMMIT_ROWS - 1 - __popcll(back & before)] = tid;
+        if (tid == 0) {
+            s_count[0] = __popcll(front);
+            s_count[1] = __popcll(back);
         }
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a)
-            if (real[a]) *reinterpret_cast<uint4 *>(to[a]) = in[a];
     }
-    if (!of_v) return;
     __syncthreads();
-    const int pairs = cn / 2, jobs = (int)s_near[0] * pairs;
-    for (int i = tid; i < jobs; i += COMMIT_THREADS) {
-        const int job = i / pairs, c = (i - job * pairs) * 2, row = s_rows[job] & (COMMIT_ROWS - 1);
-        const int64_t slot = s_near[E + row];
-        const int place = (int)(slot & (page - 1));
-        const W *from = v + (int64_t)row * v_row + c;
-        W *to = V + page_at(slot, c0 + c) + ((((int64_t)(place / E) << dim_bits) + ((c0 + c) & mask)) * E);
-        if (s_rows[job] & COMMIT_ROWS) {
-            W in[E][2], out[2][E];
+    if (!of_v) {
+        const int vectors = cn / E, items = s_count[0] * vectors;
+        for (int i0 = tid; i0 < items; i0 += AHEAD * COMMIT_THREADS) {
+            uint4 in[AHEAD];
+            W *to[AHEAD];
 #pragma unroll
-            for (int j = 0; j < E; ++j) __builtin_memcpy(in[j], __builtin_assume_aligned(from + j * v_row, sizeof(in[j])), sizeof(in[j]));
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                out[0][j] = in[j][0];
-                out[1][j] = in[j][1];
+            for (int a = 0; a < AHEAD; ++a) {                // no branch around a load: they are on their way together
+                const int i = min(i0 + a * COMMIT_THREADS, items - 1), job = i / vectors, c = (i - job * vectors) * E, row = s_rows[job];
+                const int64_t slot = s_near[E + row];
+                in[a] = load_raw(k + (int64_t)row * k_row + c);
+                to[a] = K + page_at(slot, c0 + c) + (((slot & (page - 1)) << dim_bits) + ((c0 + c) & mask));
             }
-            __builtin_memcpy(__builtin_assume_aligned(to, 16), out, sizeof(out));
-        } else {
-            to[place & (E - 1)] = from[0];
-            to[E + (place & (E - 1))] = from[1];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                if (i0 + a * COMMIT_THREADS >= items) break;
+                *reinterpret_cast<uint4 *>(to[a]) = in[a];
+            }
+        }
+        return;
+    }
+    const int pairs = cn / 2, whole_items = s_count[0] * pairs, one_items = s_count[1] * pairs;
+    const auto place_of = [&](int64_t slot, int c) {             // where V's pack of a slot and channel lies
+        return V + page_at(slot, c0 + c) + ((((slot & (page - 1)) / E << dim_bits) + ((c0 + c) & mask)) * E);
+    };
+    for (int i = tid; i < whole_items; i += COMMIT_THREADS) {
+        const int job = i / pairs, c = (i - job * pairs) * 2, row = s_rows[job];
+        const W *from = v + (int64_t)row * v_row + c;
+        W in[E][2], out[2][E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) __builtin_memcpy(in[j], __builtin_assume_aligned(from + j * v_row, sizeof(in[j])), sizeof(in[j]));
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            out[0][j] = in[j][0];
+            out[1][j] = in[j][1];
+        }
+        __builtin_memcpy(__builtin_assume_aligned(place_of(s_near[E + row], c), 16), out, sizeof(out));
+    }
+    for (int i0 = tid; i0 < one_items; i0 += AHEAD * COMMIT_THREADS) {
+        W in[AHEAD][2], *to[AHEAD];
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const int i = min(i0 + a * COMMIT_THREADS, one_items - 1), job = i / pairs, c = (i - job * pairs) * 2, row = s_rows[COMMIT_ROWS - 1 - job];
+            const int64_t slot = s_near[E + row];
+            __builtin_memcpy(in[a], __builtin_assume_aligned(v + (int64_t)row * v_row + c, sizeof(in[a])), sizeof(in[a]));
+            to[a] = place_of(slot, c) + (slot & (E - 1));
+        }
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            if (i0 + a * COMMIT_THREADS >= one_items) break;
+            to[a][0] = in[a][0];
+            to[a][E] = in[a][1];
         }
     }
 }
