@@ -289,11 +289,12 @@ svdp_status svdp_ffn_step_glued(const svdp_layer *layer, const void *x_prev, con
  * table: device [R][max_pages] int32; entries past a request's length are not read.  A slot is page id * page + place.
  *
  * Limits (else SVDP_ERR_UNSUPPORTED): page 32, 64, 128 or 256; dim 64, 128 or 256; R <= SVDP_MAX_REQUESTS;
- * pages * page, R * max_pages and max_pages * page below 2^31.  Values read from device memory that lie outside their
+ * T <= SVDP_MAX_ROWS; T * heads_q below 2^26; pages * page, R * max_pages and max_pages * page below 2^31.  Values read from device memory that lie outside their
  * range never lead outside a buffer: lengths are clamped to the table's width, a page id outside [0, pages) is
  * skipped with its tokens.                                                                                     */
 #define SVDP_MAX_NODES 64
 #define SVDP_MAX_REQUESTS 4096
+#define SVDP_MAX_ROWS (1 << 24)
 
 /* K and V of the cached tokens, all layers.  With e = 16 bytes / element size, V holds e tokens of a channel side by
  * side: what a lane of the matrix cores multiplies the weights of e tokens with is then one 16-byte load.        */

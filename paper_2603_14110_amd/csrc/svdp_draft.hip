@@ -59,7 +59,7 @@ svdp_status check_cache_memory(const svdp_kv_cache *c)
 svdp_status check_requests(int R, int T, int max_nodes)
 {
     if (R < 1 || T < 0 || max_nodes < 1) return SVDP_ERR_INVALID_ARG;
-    if (R > SVDP_MAX_REQUESTS || max_nodes > SVDP_MAX_NODES) return SVDP_ERR_UNSUPPORTED;
+    if (R > SVDP_MAX_REQUESTS || T > SVDP_MAX_ROWS || max_nodes > SVDP_MAX_NODES) return SVDP_ERR_UNSUPPORTED;
     return SVDP_OK;
 }
 svdp_status check_table(int R, int max_pages, int page)
@@ -170,7 +170,7 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     const int dt = cache->dtype, dim = cache->dim;
     if (layer < 0 || layer >= cache->layers || heads_q < 1 || heads_q % cache->heads != 0 || !std::isfinite(scale * LOG2E))
         return SVDP_ERR_INVALID_ARG;
-    if ((int64_t)T * heads_q >= INT_LIMIT) return SVDP_ERR_UNSUPPORTED;
+    if ((int64_t)T * heads_q >= 1 << 26) return SVDP_ERR_UNSUPPORTED;        // a wave each in the join: threads of a grid
     if (T == 0) return SVDP_OK;
     if (!q || !k || !v || !out || !table || !lens || !starts || !aligned16(q) || !aligned16(k) || !aligned16(v) ||
         !aligned16(out) || !aligned_to(table, 4) || !aligned_to(lens, 4) || !aligned_to(starts, 4) ||
@@ -240,7 +240,7 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
 
 size_t svdp_tree_accept_workspace_bytes(int32_t T, int32_t V, int32_t dtype)
 {
-    if (T < 0 || V < 1 || (dtype != SVDP_F32 && dtype != SVDP_BF16)) return 0;
+    if (T < 0 || T > SVDP_MAX_ROWS || V < 1 || (dtype != SVDP_F32 && dtype != SVDP_BF16)) return 0;
     return std::max(align_up((size_t)T * best_parts(T, V, dtype) * 8), ALIGN);
 }
 
@@ -316,6 +316,7 @@ svdp_status svdp_kv_commit(const svdp_kv_cache *cache, const void *k, int64_t k_
     if (st == SVDP_OK) st = check_cache_memory(cache);
     if (st != SVDP_OK) return st;
     if (T < 0) return SVDP_ERR_INVALID_ARG;
+    if (T > SVDP_MAX_ROWS) return SVDP_ERR_UNSUPPORTED;
     if (T == 0) return SVDP_OK;
     const int dt = cache->dtype;
     const int64_t row = (int64_t)cache->heads * cache->dim;

@@ -162,3 +162,14 @@ def test_oracle_commit_worked_example():
     k, v = np.ones((1, 2, 1, 64)), np.arange(128.0).reshape(1, 2, 1, 64) + 1
     draft.commit(K, V, k, v, [32 + 13, -1])
     assert K.sum() == 64 and (K[0, 1, 0, 13] == 1).all() and (V[0, 1, 0, 1, :, 5] == v[0, 0, 0]).all() and V.sum() == v[0, 0].sum()
+
+
+def test_rows_beyond_a_grid_are_refused(svdp):
+    most = 1 << 24
+    assert attn(svdp, T=most + 1) == UNSUPPORTED and attn(svdp, T=1 << 21, heads_q=32) == UNSUPPORTED
+    c = cache(svdp)
+    assert svdp.lib().svdp_kv_commit(ctypes.byref(c), P, 1 << 20, 1024, P, 1 << 20, 1024, P, most + 1, None) == UNSUPPORTED
+    assert svdp.lib().svdp_tree_accept(P, 100, 1, 100, P, P, P, 2, most + 1, 8, P, P, P, P, P, 1 << 40, None) == UNSUPPORTED
+    assert svdp.lib().svdp_tree_accept_workspace_bytes(most + 1, 100, 1) == 0
+    a = (2 * P, 4, 3 * P, 50, 64, 4 * P, 5 * P, 6 * P, 7 * P, None, 2, most + 1, 8 * P, 9 * P, 10 * P, 11 * P)
+    assert svdp.lib().svdp_kv_plan(*a, None) == UNSUPPORTED
