@@ -299,17 +299,16 @@ __global__ __launch_bounds__(64) void k_tree_walk(const uint64_t *parts, int n_p
 
 constexpr int COMMIT_THREADS = 256;
 constexpr int COMMIT_ROWS = 8;
-
 constexpr int COMMIT_CHANNELS = 256;        // the least a block has of them, unless a row has fewer
 
-// Rows [8 blockIdx.x, + 8) of layer blockIdx.y, channels [blockIdx.z / 2 channels, + channels) of all heads side by side.
-// Even blockIdx.z: K, odd: V.  K is
-// copied in 16-byte vectors.  V lies with e tokens of a channel side by side: where e rows in a row fill such a pack
-// (prompts), they are read together and written as whole packs, by the row of the pack's first token; other rows (branches of
-// a tree) write their elements one by one.  A lane has two channels of V, so that the packs of a wave lie side by side.  Bound
-// by reading and writing: a prompt's 618 MB (half read, half written) in 111 us, 5.5 TB/s (144 us with eight channels a lane,
-// packs 128 bytes apart); a branch of a tree of 8, in 32 layers, in 3.9 us, by latency, with its channels over many blocks
-// (6.5 us with one block for all of them and for K and V); branches of 723 rows in 12 layers, 8.8 MB, in 6.3 us.
+// Rows [8 blockIdx.x, + 8) of layer blockIdx.y, channels [c0, + channels) of all heads side by side with c0 = (blockIdx.z / 2)
+// channels; even blockIdx.z: K, odd: V.  K is copied in 16-byte vectors.  V lies with e tokens of a channel side by side: where e
+// rows in a row fill such a pack (prompts), they are read together and written as whole packs, by the row of the pack's first
+// token; other rows (branches of a tree) write their elements one by one.  A lane has two channels of V, so that the packs of a
+// wave lie side by side.  Bound by reading and writing: a prompt's 618 MB (half read, half written) in 112 us, 5.5 TB/s (144 us
+// with eight channels a lane, packs 128 bytes apart); a branch of a tree of 8, in 32 layers, in 3.9 us, by latency, with its
+// channels over many blocks (6.5 us with one block for all of them and for K and V); branches of 723 rows in 12 layers, 8.8 MB,
+// in 6.3 us.
 template <typename W>
 __global__ __launch_bounds__(COMMIT_THREADS) void k_kv_commit(W *K, W *V, const W *k, int64_t k_layer, int64_t k_row,
                                                               const W *v, int64_t v_layer, int64_t v_row,
