@@ -83,11 +83,13 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
             // them also holds up the reads from LDS.)
             int window = -64, window_ids = 0;
             bool window_whole = true;                            // no page of it is missing
+            const auto request_pages = [&](int step) {
+                window = (max(step - 1, s0) * TILES) >> per_page;                // the stage that is worked on as well
+                return A.table[(size_t)r * A.max_pages + max(min(window + (tid & 63), (S.tiles - 1) >> per_page), 0)];
+            };
             const auto see_pages = [&](int step) {
-                const int last_page = (S.tiles - 1) >> per_page;
-                if (min((step * TILES + TILES - 1) >> per_page, last_page) >= window + 64) {
-                    window = (max(step - 1, s0) * TILES) >> per_page;            // the stage that is worked on as well
-                    window_ids = here(A.table[(size_t)r * A.max_pages + min(window + (tid & 63), last_page)]);
+                if (min((step * TILES + TILES - 1) >> per_page, (S.tiles - 1) >> per_page) >= window + 64) {
+                    window_ids = here(request_pages(step));
                     window_whole = __all((uint32_t)window_ids < (uint32_t)A.pages);
                 }
             };
@@ -125,21 +127,29 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                 }
             };
 
-            // Q, and what the rows see of their tree, requested in front of the first stage and waited for behind it
+            // The first pages' ids, then Q and what the rows see of their tree, then the first stage, each requested before the one in
+            // front of it is waited for.
             const TreeScale scale(A.scale, X::SIGNS);
             uint4 q[KC], k[KC], v[DT][2];
+            uint64_t sees;
+            stage_barrier<0>();                                  // the last segment's stages and stores are done with
+            window_ids = request_pages(s0);                      // a segment of the tree's own tokens only: not looked at
             {
                 const int row = min(row0 + (here(lane) & 31), rows - 1), node = row / A.group, head = h * A.group + row - node * A.group;
                 const bf16 *from = static_cast<const bf16 *>(A.q) + (S.start + node) * A.q_stride + (int64_t)head * DIM + f * 8;
+                sees = A.tree != nullptr ? A.tree[S.start + node] : ~0ull >> (63 - node);
 #pragma unroll
                 for (int c = 0; c < KC; ++c) q[c] = load_raw(from + c * 16);
-                const uint64_t sees = A.tree != nullptr ? A.tree[S.start + node] : ~0ull >> (63 - node);
-                stage_barrier<0>();                              // the last segment's stages and stores are done with
-                if (f == 0) s_sees[wave * 32 + m] = sees;
             }
             int stage = 0;
-            if (s0 < s_end) fill(s0, 0);
-            else fill_own(0);
+            if (s0 < s_end) {
+                window_ids = here(window_ids);
+                window_whole = __all((uint32_t)window_ids < (uint32_t)A.pages);
+                fill(s0, 0);
+            } else {
+                fill_own(0);
+            }
+            if (f == 0) s_sees[wave * 32 + m] = sees;
 #pragma unroll
             for (int c = 0; c < KC; ++c) q[c] = scale.of(q[c]);
             // as in TreeWave: sum, shift, denominator (the lane half's part), and what a score has to exceed for the shift to move
@@ -167,7 +177,7 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                 if (step + 1 < s_end) fill(step + 1, stage ^ TW_STAGE);
                 else if (step + 1 < s1) fill_own(stage ^ TW_STAGE);
                 char *const lds = tw_smem + stage;
-                const int n_tiles = own_tokens ? (S.n + TA_TILE - 1) / TA_TILE : TILES;
+                const int n_tiles = own_tokens ? (S.n + TA_TILE - 1) / TA_TILE : min(TILES, S.tiles - step * TILES);
                 if (own_tokens) {                                // V into packs
                     int odd = 0;
                     for (int e = here(tid); e < n_tiles * 4 * DIM; e += TW_THREADS) {
@@ -186,10 +196,12 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                     }
                     finite = __syncthreads_or(odd) == 0;
                 } else if (!full) {                              // what lies behind the tokens in V must not be NaN
-                    for (int e = here(tid); e < V_AT / 16; e += TW_THREADS) {
-                        const int tile = e / (TILE_BYTES / 16), pack = e % (TILE_BYTES / 16) / DIM;
-                        uint4 *at = reinterpret_cast<uint4 *>(lds + V_AT) + e;
-                        *at = X::first(*at, count_of(tile) - pack * 8);
+                    for (int j = 0; j < n_tiles; ++j) {
+                        if (count_of(j) == TA_TILE) continue;
+                        for (int e = here(tid); e < TILE_BYTES / 16; e += TW_THREADS) {
+                            uint4 *at = reinterpret_cast<uint4 *>(lds + V_AT + j * TILE_BYTES) + e;
+                            *at = X::first(*at, count_of(j) - e / DIM * 8);
+                        }
                     }
                     __syncthreads();
                 }
