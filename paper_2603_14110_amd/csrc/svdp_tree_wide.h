@@ -10,8 +10,9 @@
 // What bounds it: a tile of 32 tokens is 528 cycles of a SIMD's matrix unit for each of its two waves, and about 600 of its
 // vector unit (16 exponentials and some 70 other instructions), side by side; what a stage costs besides (its barrier, addresses,
 // the first read of K) is why a stage is as large as LDS allows.  Trees of 64 with seven query heads a head over 20 000 to 32 768
-// tokens, 88 GFLOP: 128 us; a stage of 128 tokens takes 4.2 us, with the matrix units 63 % busy at a clock that sinks to 1.6 GHz
-// under them.  Some 14 us are not stages: 4 for the lengths, and a part of 133 KB that every block writes.
+// tokens, 88 GFLOP: 125 us; a stage of 128 tokens takes 4.2 us, with the matrix units 63 % busy at a clock that sinks to 1.6 GHz
+// under them.  Some 14 us are not stages: 2 for the lengths, 3 for the first pages, Q and K and V, and a part of 133 KB that every block
+// writes and that leaves the caches at the end.  A call of one stage takes 10 us.
 #pragma once
 
 #include "svdp_tree_attn.h"
