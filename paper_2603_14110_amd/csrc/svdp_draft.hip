@@ -109,9 +109,9 @@ AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, in
     const int dt = c->dtype, dim = c->dim, group = heads_q / c->heads;
     const int64_t rows = (int64_t)group * max_nodes, room = (int64_t)max_pages * c->page / TA_TILE, own = tiles(max_nodes, TA_TILE);
     AttnPlan p;
-    // More than 32 rows: over the waves, 32 each (36 rows, 135 MB: 31 us, where tiles of 64 rows over the waves' tokens took 34, and
-    // 10 us against 14 for 500 tokens).  At 32 rows: 28.6 us for one request of 30 000 tokens, 45 for 24 of 150, where
-    // k_tree_attn takes 25.4 and 24.5.
+    // More than 32 rows: over the waves, 32 each (eight requests of 4096 tokens, 135 MB: 36 rows 30.0 us, 64 rows 31.5, where
+    // k_tree_attn, with two row tiles after each other, takes 32.2 and 43.7).  At 32 rows k_tree_attn is ahead: 25.4 us for one
+    // request of 30 000 tokens and 24.5 for 24 of 150, where rows over the waves took 28.6 and 45.
     p.wide = dt == SVDP_BF16 && dim <= 128 && rows > 32;
     // Two row tiles of 16 read K and V once for 32 rows (8 requests of 4096 tokens, 135 MB: 28.5 us, one after the other 38.8); with
     // 256 channels a second one does not fit the registers.
