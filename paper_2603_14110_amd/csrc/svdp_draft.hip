@@ -134,6 +134,10 @@ AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, in
 constexpr int JOIN_WAVES = 512;
 constexpr int COMMIT_BLOCKS = 4096;       // K and V of few rows: fewer channels a block, until there are so many blocks
 
+// Bytes of a request's logits up to which one block reads them and walks, in one launch (125 KB: a call 8.6 us and 6.5 on the GPU,
+// in two launches 11.7 and 4.5 + 3.4; 250 KB: 9.2 and 9.3, in two 12.1 and 4.0 + 3.5, and by itself a call is 3 us slower).
+constexpr int64_t ACCEPT_SMALL = 128 << 10;
+
 // Parts that a row of logits is cut into: about a thousand blocks altogether, each of 8 to 32 KB.
 int best_parts(int T, int V, int dt)
 {
@@ -262,18 +266,21 @@ svdp_status svdp_tree_accept(const void *logits, int64_t stride, int32_t dtype, 
     st = check_ws(ws, ws_bytes, svdp_tree_accept_workspace_bytes(T, V, dtype));
     if (st != SVDP_OK) return st;
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    uint64_t *parts = static_cast<uint64_t *>(ws);
-    const int n_parts = best_parts(T, V, dtype);
-    if (T > 0)
-        on_type(dtype, [&](auto wt) {
-            using W = typename decltype(wt)::type;
-            // one vector more than the row has where it begins between two of them
-            const int per = tiles(tiles(V, Elem<W>::VEC) + 1, n_parts);
-            launch(k_logits_best<W>, dim3(T, n_parts), dim3(BEST_THREADS), 0, hs, static_cast<const W *>(logits), stride, V,
-                   per, parts);
-        });
-    launch(k_tree_walk, dim3(R + 1), dim3(64), 0, hs, parts, n_parts, tokens, tree, starts, R, T, max_nodes, keep, counts,
-           next, best);
+    const TreeWalk A{tokens, tree, starts, keep, counts, next, best, R, T, max_nodes};
+    on_type(dtype, [&](auto wt) {
+        using W = typename decltype(wt)::type;
+        const W *rows = static_cast<const W *>(logits);
+        if ((int64_t)max_nodes * V * bytes_of(dtype) <= ACCEPT_SMALL && T <= (int64_t)R * max_nodes) {
+            launch(k_tree_accept<W>, dim3(2 * R), dim3(SMALL_THREADS), 0, hs, rows, stride, V, A);
+            return;
+        }
+        uint64_t *parts = static_cast<uint64_t *>(ws);
+        const int n_parts = best_parts(T, V, dtype);
+        // one vector more than the row has where it begins between two of them
+        const int per = tiles(tiles(V, Elem<W>::VEC) + 1, n_parts);
+        launch(k_logits_best<W>, dim3(T, n_parts), dim3(BEST_THREADS), 0, hs, rows, stride, V, per, parts);
+        launch(k_tree_walk, dim3(R + 1), dim3(64), 0, hs, parts, n_parts, A);
+    });
     return hip_status(hipSuccess);
 }
 

@@ -172,29 +172,23 @@ __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v)
     return v;
 }
 
-// The largest logit of a part of a row.  A row is cut where 16-byte vectors begin, whatever its own alignment: part p has the
-// vectors [p per, (p + 1) per) counted from the aligned address at or before the row.  A lane keeps its best vector by the
-// largest of its values, a few operations for a vector, and looks for the place in it once, at the end.  Bound by reading:
-// 439 MB of bf16 logits in 77 us, 5.7 TB/s (90.7 us, by arithmetic, with an order and an index for every element); 8 rows of
-// 32 000 in 3.2 us, by the latency of one load and the launch.
-template <typename W>
-__global__ __launch_bounds__(BEST_THREADS) void k_logits_best(const W *logits, int64_t stride, int V, int per, uint64_t *parts)
+// The largest logit of a row's vectors [begin, end), of those that a lane takes (at, at + step, ...).  Vectors are counted from the
+// aligned address at or before the row, whatever its own alignment.  A lane keeps its best vector by the largest of its values, a few
+// operations for a vector, and looks for the place in it once, at the end.
+template <int AHEAD, typename W>
+__device__ __forceinline__ uint64_t best_of(const W *row, int V, int begin, int end, int at, int step)
 {
-    constexpr int VEC = Elem<W>::VEC, AHEAD = 4;
-    __shared__ uint64_t s_best[BEST_THREADS / 64];
-    const W *row = logits + (int64_t)blockIdx.x * stride;
+    constexpr int VEC = Elem<W>::VEC;
     const int skew = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / Elem<W>::BYTES);
-    const int vectors = (V + skew + VEC - 1) / VEC;
-    const int begin = blockIdx.y * per, end = min(begin + per, vectors);
     // vectors that lie in the row as a whole
     const int inner = max(begin, skew > 0 ? 1 : 0), outer = min(end, (V + skew) / VEC);
     uint4 kept = make_uint4(0, 0, 0, 0);
     uint32_t top = 0;                                       // order of the largest value, above 0 once there is one
     int place = 0;
-    for (int i0 = inner + threadIdx.x; i0 < outer; i0 += AHEAD * BEST_THREADS) {
+    for (int i0 = inner + at; i0 < outer; i0 += AHEAD * step) {
         uint4 in[AHEAD];
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) in[a] = load_raw(row + (min(i0 + a * BEST_THREADS, outer - 1) * VEC - skew));
+        for (int a = 0; a < AHEAD; ++a) in[a] = load_raw(row + (min(i0 + a * step, outer - 1) * VEC - skew));
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) {
             float v[VEC];
@@ -209,7 +203,7 @@ __global__ __launch_bounds__(BEST_THREADS) void k_logits_best(const W *logits, i
             const uint32_t o = nan ? 0xffffffffu : best_order(m);
             if (o > top) {
                 top = o;
-                place = min(i0 + a * BEST_THREADS, outer - 1);
+                place = min(i0 + a * step, outer - 1);
                 kept = in[a];
             }
         }
@@ -224,15 +218,31 @@ __global__ __launch_bounds__(BEST_THREADS) void k_logits_best(const W *logits, i
     }
     // the row's ends: the first and the last vector of the row, where they reach over it
     const auto edge = [&](int i) {
-        if (i < begin || i >= end || threadIdx.x >= VEC) return;
-        const int at = i * VEC - skew + (int)threadIdx.x;
-        if (at < 0 || at >= V) return;
-        const uint64_t key = best_key(to_f32(row[at]), at);
+        if (i < begin || i >= end || at >= VEC) return;
+        const int e = i * VEC - skew + at;
+        if (e < 0 || e >= V) return;
+        const uint64_t key = best_key(to_f32(row[e]), e);
         best = key > best ? key : best;
     };
     if (skew > 0) edge(0);
-    if ((V + skew) % VEC != 0) edge(vectors - 1);
-    best = wave_max_u64(best);
+    if ((V + skew) % VEC != 0) edge((V + skew) / VEC);
+    return wave_max_u64(best);
+}
+template <typename W>
+__device__ __forceinline__ int best_vectors(const W *row, int V)
+{
+    return (V + (int)((reinterpret_cast<uintptr_t>(row) & 15u) / Elem<W>::BYTES) + Elem<W>::VEC - 1) / Elem<W>::VEC;
+}
+
+// Part blockIdx.y of row blockIdx.x: `per` vectors.  Bound by reading: 439 MB of bf16 logits in 76 us, 5.8 TB/s (90.7 us, by
+// arithmetic, with an order and an index for every element); 8 rows of 32 000 in 3.2 us, by the latency of one load and the launch.
+template <typename W>
+__global__ __launch_bounds__(BEST_THREADS) void k_logits_best(const W *logits, int64_t stride, int V, int per, uint64_t *parts)
+{
+    __shared__ uint64_t s_best[BEST_THREADS / 64];
+    const W *row = logits + (int64_t)blockIdx.x * stride;
+    const int begin = blockIdx.y * per, end = min(begin + per, best_vectors(row, V));
+    uint64_t best = best_of<4>(row, V, begin, end, threadIdx.x, BEST_THREADS);
     if ((threadIdx.x & 63) == 0) s_best[threadIdx.x >> 6] = best;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -241,11 +251,40 @@ __global__ __launch_bounds__(BEST_THREADS) void k_logits_best(const W *logits, i
     }
 }
 
-// One wave a request, a lane a node: the rows' answers from their parts, then down the tree; the last block has the padding.
-// Bound by the latency of two loads after each other: 1.6 us for one tree of 8, 4.2 us for 32 trees and 10 parts a row.
-__global__ __launch_bounds__(64) void k_tree_walk(const uint64_t *parts, int n_parts, const int32_t *tokens, const uint64_t *tree,
-                                                  const int32_t *starts, int R, int T, int max_nodes, int32_t *keep,
-                                                  int32_t *counts, int32_t *next, int32_t *best)
+struct TreeWalk {
+    const int32_t *tokens;
+    const uint64_t *tree;
+    const int32_t *starts;
+    int32_t *keep, *counts, *next, *best;
+    int R, T, max_nodes;
+};
+// Down the tree of request r, n nodes from row a on, a lane each, by the whole wave; mine: the answer of the lane's node.
+__device__ __forceinline__ void walk_down(const TreeWalk &A, int r, int a, int n, int lane, int token, uint64_t sees, int mine)
+{
+    const bool node = lane < n;
+    const uint64_t up = sees & ((1ull << lane) - 1);
+    const int parent = node && up != 0 ? 63 - __clzll((long long)up) : -1;
+    int place = lane == 0 ? 0 : -1, count = n > 0 ? 1 : 0, at = 0;
+    while (count > 0) {                                     // at grows with every step
+        const int answered = __builtin_amdgcn_readlane(mine, at);
+        const uint64_t agree = __ballot(node && lane > at && parent == at && token == answered);
+        if (agree == 0) break;
+        at = __ffsll((unsigned long long)agree) - 1;
+        if (lane == at) place = count;
+        ++count;
+    }
+    const int following = __builtin_amdgcn_readlane(mine, at);
+    if (node) A.keep[a + lane] = place;
+    if (lane == 0) {
+        A.counts[r] = count;
+        A.next[r] = count > 0 ? following : -1;
+    }
+}
+__device__ __forceinline__ int best_index(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
+
+// One wave a request: the rows' answers from their parts, then down the tree; the last block has the padding.  Bound by the latency
+// of two loads after each other: 1.6 us for one tree of 8, 4.2 us for 32 trees and 10 parts a row.
+__global__ __launch_bounds__(64) void k_tree_walk(const uint64_t *parts, int n_parts, TreeWalk A)
 {
     const int r = blockIdx.x, lane = threadIdx.x;
     const auto answer = [&](int t) {
@@ -258,40 +297,64 @@ __global__ __launch_bounds__(64) void k_tree_walk(const uint64_t *parts, int n_p
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) k = o[i] > k ? o[i] : k;
         }
-        return (int)(0xffffffffu - (uint32_t)k);
+        return best_index(k);
     };
-    const int a = min(max(starts[r], 0), T), b = r < R ? min(max(starts[r + 1], a), T) : T;
-    const int n = r < R ? min(b - a, max_nodes) : 0;
-    const bool node = lane < n;
-    int mine = -1, token = -2, parent = -1;
-    if (node) {
-        const uint64_t before = (1ull << lane) - 1;
-        const uint64_t up = tree != nullptr ? tree[a + lane] & before : before;
-        token = tokens[a + lane];
+    const int a = min(max(A.starts[r], 0), A.T), b = r < A.R ? min(max(A.starts[r + 1], a), A.T) : A.T;
+    const int n = r < A.R ? min(b - a, A.max_nodes) : 0;
+    int mine = -1, token = -2;
+    uint64_t sees = 0;
+    if (lane < n) {
+        sees = A.tree != nullptr ? A.tree[a + lane] : ~0ull;
+        token = A.tokens[a + lane];
         mine = answer(a + lane);
-        best[a + lane] = mine;
-        parent = up != 0 ? 63 - __clzll((long long)up) : -1;
+        A.best[a + lane] = mine;
     }
-    if (r < R) {
-        int place = lane == 0 ? 0 : -1, count = n > 0 ? 1 : 0, at = 0;
-        while (count > 0) {                                 // at grows with every step
-            const int answered = __builtin_amdgcn_readlane(mine, at);
-            const uint64_t agree = __ballot(node && lane > at && parent == at && token == answered);
-            if (agree == 0) break;
-            at = __ffsll((unsigned long long)agree) - 1;
-            if (lane == at) place = count;
-            ++count;
-        }
-        const int following = __builtin_amdgcn_readlane(mine, at);
-        if (node) keep[a + lane] = place;
-        if (lane == 0) {
-            counts[r] = count;
-            next[r] = count > 0 ? following : -1;
-        }
-    }
+    if (r < A.R) walk_down(A, r, a, n, lane, token, sees, mine);
     for (int t = a + n + lane; t < b; t += 64) {            // rows that are no node
-        best[t] = answer(t);
-        keep[t] = -1;
+        A.best[t] = answer(t);
+        A.keep[t] = -1;
+    }
+}
+
+// Both in one launch, where a request's logits are few: a block has all rows of a request, as many of its waves as there are for
+// a row, and blocks R on have the padding, max_nodes rows each (T <= R max_nodes).  Bound by the latency of a block that reads by
+// itself: 8 rows of 8000 in 6.5 us, where the two launches take 4.5 + 3.4 and the host 3 us more; 500 KB a block take 15 us.
+constexpr int SMALL_THREADS = 1024, SMALL_WAVES = SMALL_THREADS / 64;
+template <typename W>
+__global__ __launch_bounds__(SMALL_THREADS) void k_tree_accept(const W *logits, int64_t stride, int V, TreeWalk A)
+{
+    __shared__ uint64_t s_best[64][SMALL_WAVES];
+    const int r = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int first = min(max(A.starts[min(r, A.R)], 0), A.T), a = r < A.R ? first : min(first + (r - A.R) * A.max_nodes, A.T);
+    const int b = r < A.R ? min(max(A.starts[r + 1], a), A.T) : min(a + A.max_nodes, A.T);
+    const int n = r < A.R ? min(b - a, A.max_nodes) : 0;
+    int token = -2;
+    uint64_t sees = 0;
+    if (wave == 0 && lane < n) {
+        sees = A.tree != nullptr ? A.tree[a + lane] : ~0ull;
+        token = A.tokens[a + lane];
+    }
+    bool nodes = true;                                      // the nodes first, then rows that are none
+    for (int t0 = a, rows = n; nodes || rows > 0; t0 += rows, rows = min(b - t0, 64), nodes = false) {
+        int share = SMALL_WAVES;                            // waves of a row: a power of two
+        while (share > 1 && share * rows > SMALL_WAVES) share >>= 1;
+        const int sub = wave & (share - 1);
+        for (int i = wave / share; i < rows; i += SMALL_WAVES / share) {
+            const W *row = logits + (int64_t)(t0 + i) * stride;
+            const uint64_t best = best_of<8>(row, V, 0, best_vectors(row, V), sub * 64 + lane, share * 64);
+            if (lane == 0) s_best[i][sub] = best;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            uint64_t k = 0;
+            if (lane < rows)
+                for (int w = 0; w < share; ++w) k = s_best[lane][w] > k ? s_best[lane][w] : k;
+            const int mine = lane < rows ? best_index(k) : -1;
+            if (lane < rows) A.best[t0 + lane] = mine;
+            if (nodes && r < A.R) walk_down(A, r, a, n, lane, token, sees, mine);
+            else if (lane < rows) A.keep[t0 + lane] = -1;
+        }
+        __syncthreads();
     }
 }
 

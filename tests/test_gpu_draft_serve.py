@@ -395,3 +395,33 @@ def test_plan_of_more_requests_than_threads(env, R, page, width, pages, rows, fr
     torch, binding, draft = env
     c = make_plan(R, R, page, width, pages, rows, free, padded=3)
     assert run_plan(torch, binding, c) == tuple(draft.plan(**c, rows=len(c["keep"])))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [701, 40003])
+def test_accept_of_few_and_of_many_logits(env, dtype, V):
+    """A request's logits read by one block, and by many: rows at any address, ties, infinities and NaN, padding behind the requests."""
+    torch, binding, draft = env
+    td, e = (torch.bfloat16, 8) if dtype == "bf16" else (torch.float32, 4)
+    inf, nan = float("inf"), float("nan")
+    g = torch.Generator(device="cuda").manual_seed(V)
+    for shift in range(e):
+        wide = torch.randn((24, V + 13), device="cuda", generator=g).to(td)
+        wide[:, :shift] = 1e9                                # neighbours that must not win
+        wide[:, shift + V:] = inf
+        x = wide[:, shift:shift + V]
+        x[0, [5, V // 2, V - 1]] = 50.0
+        x[1] = -inf
+        x[2, V - 1] = nan
+        x[3, 0] = nan
+        x[3, 7] = inf
+        x[4, [V - 2, V - 1]] = inf
+        x[5] = 0.0
+        x[5, 3] = -0.0
+        rows = x.float().cpu().numpy()
+        for starts in ([0, 8, 8, 15], [0, 1, 2, 3], [0, 0, 0, 0], [0, 8, 16, 24]):
+            tokens = [draft.best_token(rows[max(t - 1, 0)]) for t in range(24)]
+            got = run_accept(torch, binding, x, tokens, None, starts, max_nodes=8)
+            assert got == tuple(draft.accept(rows, tokens, None, starts))
+    best = got[3]
+    assert best[0] == 5 and best[1] == 0 and best[2] == V - 1 and best[3] == 0 and best[4] == V - 2 and best[5] == 0
