@@ -77,7 +77,7 @@ svdp_status check_ws(void *ws, size_t ws_bytes, size_t need)
 struct AttnPlan {
     bool wide;              // rows over the waves of a block (k_tree_attn_wide), or tokens (k_tree_attn)
     int nt;                 // row tiles of 16 in k_tree_attn
-    int block_bits, part_rows;
+    int block_bits, part_rows;      // part_rows 0: nothing is cut, no second launch
     int64_t steps, tasks;   // units of a request and head, and requests times heads times row tiles, at most
     size_t bytes;
 };
@@ -104,6 +104,10 @@ void on_kernel(const AttnPlan &p, int dt, int dim, F &&f)
         });
     });
 }
+// Units of a request and head up to which a block takes them all and there is nothing to join, if no block has two of them: one row,
+// 250 tokens: 9.0 us and a call 11.6, cut 7.5 + 3.4 and 14.6; 20 requests of 32 rows 13.4 us, cut 15.8 + 4.1; eight units 12.2 us, cut
+// 7.5 + 3.5.  Rows over the waves: 120 tokens 12.9 us, cut 9.6 + 4.3; 250 tokens 15.4, cut 9.5 + 4.9.
+constexpr int UNCUT = 4, UNCUT_WIDE = 2;
 AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, int max_nodes)
 {
     const int dt = c->dtype, dim = c->dim, group = heads_q / c->heads;
@@ -123,10 +127,11 @@ AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, in
         block_rows = Cut::ROWS;
         p.block_bits = Cut::BITS;
     });
-    p.part_rows = (int)std::min<int64_t>(rows, block_rows);
     p.steps = p.wide ? tiles(room, unit) + tiles(own, unit) : tiles(room + own, unit);
     p.tasks = (rows + block_rows - 1) / block_rows * c->heads * R;
-    p.bytes = align_up(((size_t)2 << p.block_bits) * p.part_rows * (dim + 2) * 4);
+    const bool uncut = p.steps <= 1 || (p.steps <= (p.wide ? UNCUT_WIDE : UNCUT) && p.tasks <= 1 << p.block_bits);
+    p.part_rows = uncut ? 0 : (int)std::min<int64_t>(rows, block_rows);
+    p.bytes = std::max(align_up(((size_t)2 << p.block_bits) * p.part_rows * (dim + 2) * 4), ALIGN);
     return p;
 }
 // Rows and heads from which the join has a wave for each, whatever the parts (768 of 24 requests: 4.2 us, with a block each 5.2; 256
@@ -220,7 +225,7 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const dim3 blocks(1 << plan.block_bits);
     bool granted = true;
-    // A request of one unit is never cut.  A row has at most blocks / heads parts and two more: up to eight, which a wave reads at
+    // A row has at most blocks / heads parts and two more: up to eight, which a wave reads at
     // once, or many rows, a wave each.
     const int items = T * heads_q;
     const bool shared = items < JOIN_WAVES && (1 << plan.block_bits) / cache->heads + 2 > 8;
@@ -235,7 +240,7 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
         } else {
             launch((k_tree_attn<W, DIM, Cut::ROWS / 16>), blocks, dim3(TA_THREADS), 0, hs, A);
         }
-        if (plan.steps <= 1) return;
+        if (plan.part_rows == 0) return;
         if (shared) launch((k_tree_join<W, DIM, Cut, true>), dim3(items), dim3(64 * tj_waves<true>()), 0, hs, J);
         else launch((k_tree_join<W, DIM, Cut, false>), dim3(tiles(items, tj_waves<false>())), dim3(64 * tj_waves<false>()), 0, hs, J);
     });

@@ -45,7 +45,7 @@ struct TreeJoinArgs {
     float *parts;                       // [2 << Cut::BITS] parts of part_rows (dim + 2) floats
     int room, heads, group, R, T;       // room: tokens that a request's row of the table can have
     uint16_t max_nodes;
-    uint16_t part_rows;                 // rows of a part: no more than a request has, nor a block
+    uint16_t part_rows;                 // rows of a part: no more than a request has, nor a block; 0: nothing is cut
 };
 static_assert(sizeof(TreeJoinArgs) == 64, "as many as are loaded ahead");
 struct TreeAttnArgs : TreeJoinArgs {
@@ -72,9 +72,9 @@ struct TreeCut {
 
 typedef const __attribute__((address_space(4))) int32_t *table_t;            // read through the scalar cache
 
-// One request's share: rows, tiles and units.
+// One request's share: rows, tiles, and units: as many as its steps for each head and row tile, or one where nothing is cut.
 struct TreeSpan {
-    int len, start, n, tiles, steps, row_tiles, units;
+    int len, start, n, tiles, steps, cuts, row_tiles, units;
 };
 template <typename Cut>
 __device__ __forceinline__ TreeSpan tree_span(const TreeJoinArgs &A, int len, int start, int n)
@@ -83,8 +83,9 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeJoinArgs &A, int len, in
     TreeSpan s{len, start, n};
     s.tiles = (s.len + TA_TILE - 1) / TA_TILE;
     s.steps = Cut::steps(s.tiles, s.n);
+    s.cuts = A.part_rows == 0 ? min(s.steps, 1) : s.steps;
     s.row_tiles = (s.n * A.group + ROWS - 1) / ROWS;
-    s.units = s.row_tiles * s.steps * A.heads;
+    s.units = s.row_tiles * s.cuts * A.heads;
     return s;
 }
 // 64 requests, a lane each: what there is of them, their units and the inclusive sums of these.  They are read once, all
@@ -461,9 +462,9 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
         if (S.units == 0) continue;
         const int r = chunk.first + l;
         const table_t table = (table_t)(uintptr_t)(A.table + (size_t)r * A.max_pages);
-        int task = rem / S.steps, s0 = rem - task * S.steps;
+        int task = rem / S.cuts, s0 = rem - task * S.cuts;
         for (; task < A.heads * S.row_tiles && u < u1; ++task, s0 = 0, first = false) {
-            const int s1 = min(S.steps, s0 + u1 - u);
+            const int s1 = A.part_rows == 0 ? S.steps : min(S.steps, s0 + u1 - u);
             const int h = task / S.row_tiles, row0 = (task - h * S.row_tiles) * ROWS, rows = S.n * A.group;
             const bool whole = s0 == 0 && s1 == S.steps;
 
@@ -707,7 +708,7 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
                 part[(size_t)A.part_rows * DIM + 2 * tid] = top;
                 part[(size_t)A.part_rows * DIM + 2 * tid + 1] = total_of(tid, finite_shift(top));
             }
-            u += s1 - s0;
+            u += A.part_rows == 0 ? 1 : s1 - s0;
         }
     }
 }

@@ -73,9 +73,9 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
         if (S.units == 0) continue;
         const int r = chunk.first + l;
         const int cached_steps = (S.tiles + TILES - 1) / TILES, per_page = A.page_bits - 5;
-        int task = rem / S.steps, s0 = rem - task * S.steps;
+        int task = rem / S.cuts, s0 = rem - task * S.cuts;
         for (; task < A.heads * S.row_tiles && u < u1; ++task, s0 = 0, first = false) {
-            const int s1 = min(S.steps, s0 + u1 - u), s_end = min(s1, cached_steps);
+            const int s1 = A.part_rows == 0 ? S.steps : min(S.steps, s0 + u1 - u), s_end = min(s1, cached_steps);
             const int h = task / S.row_tiles, rows = S.n * A.group, block_row0 = (task - h * S.row_tiles) * TW_ROWS;
             const int row0 = block_row0 + wave * 32;
             const bool whole = s0 == 0 && s1 == S.steps, active = row0 < rows;
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                     }
                 }
             }
-            u += s1 - s0;
+            u += A.part_rows == 0 ? 1 : s1 - s0;
         }
     }
 }

@@ -319,3 +319,19 @@ def test_few_rows_do_not_see_what_is_hidden(env, dtype, dim, group, bad):
     assert float((out3.float() - out.float()).abs()[blind].amax()) <= (2.0 ** -7 if dtype == "bf16" else 1e-5) * scale
     assert float((lse3 - lse).abs()[blind].amax()) <= 1e-5
     assert not bool(torch.isfinite(out3[t].float()).any())
+
+
+@pytest.mark.parametrize("tree", ["tree", None])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(map(str, s[:5])))
+def test_tables_wider_than_the_requests_are_long(env, shape, tree):
+    """Room for long requests, of which the host knows nothing but the table's width: what is short is cut all the same."""
+    torch, binding, draft = env
+    dtype, dim, heads, group, page, lens, nodes = shape
+    c = Attn(torch, binding, dtype=dtype, dim=dim, heads=heads, group=group, page=page, lens=lens, nodes=nodes, tree=tree, seed=len(lens) + dim)
+    narrow = c.call(binding)
+    wide = torch.full((c.d_table.shape[0], 4096 // page), 1 << 30, dtype=torch.int32, device="cuda")
+    wide[:, :c.d_table.shape[1]] = c.d_table
+    c.d_table = wide
+    out, lse = c.call(binding)
+    c.check(draft, out, lse)
+    assert float((out.float() - narrow[0].float()).abs().amax()) <= 2.0 ** -6 * float(out.float().abs().amax())
