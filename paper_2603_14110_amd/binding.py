@@ -473,12 +473,12 @@ def tree_attn(cache: KVCache, layer: int, q: torch.Tensor, k: torch.Tensor, v: t
     max_pages = table.shape[1]
     max_nodes = max(1, min(T, MAX_NODES)) if max_nodes is None else int(max_nodes)
     if out is None:
-        out = torch.empty((T, heads_q, dim), dtype=cache.dtype, device=q.device)
+        out = torch.empty_like(q)           # dense, as the heads of a row lie side by side
         out_at = out.data_ptr()
     else:
         out_at = _typed(out, cache.dtype, "out", (T, heads_q, dim))
     if want_lse and lse is None:
-        lse = torch.empty((T, heads_q), dtype=torch.float32, device=q.device)
+        lse = torch.empty(T, heads_q, dtype=torch.float32, device=q.device)
         lse_at = lse.data_ptr()
     else:
         lse_at = _typed(lse, torch.float32, "lse", (T, heads_q))
@@ -555,17 +555,17 @@ def kv_plan(table: torch.Tensor, ring: torch.Tensor, pool: torch.Tensor, lens: t
 
 def kv_commit(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """K and V of new rows, k, v [layers][T][heads][dim], into the cache at slots [T] (int64; negative: not stored)."""
-    shape = (cache.layers, slots.numel(), cache.heads, cache.dim)
-    for what, t in (("k", k), ("v", v)):
-        if (t.shape != shape or t.dtype != cache.dtype or not t.is_cuda or
-                (t.numel() and (t.stride(3) != 1 or (cache.heads > 1 and t.stride(2) != cache.dim)))):
-            raise SvdpError(f"{what}: expected {shape} of {cache.dtype} on the device, heads side by side, got {tuple(t.shape)} "
-                            f"{t.dtype}")
-    T, row = slots.numel(), cache.heads * cache.dim
-    # a dimension of one entry: its stride says nothing
-    steps = lambda t: (t.stride(0) if cache.layers > 1 else 0, t.stride(1) if T > 1 else row)
-    _check(lib().svdp_kv_commit(ctypes.byref(cache.c), k.data_ptr(), *steps(k), v.data_ptr(), *steps(v),
-                                _typed(slots, torch.int64, "slots"), T, _stream()), "svdp_kv_commit")
+    T, layers, heads, dim, dtype = slots.numel(), cache.layers, cache.heads, cache.dim, cache.dtype
+    shape, args = (layers, T, heads, dim), []
+    for t in (k, v):
+        if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
+            raise SvdpError(f"{'v' if t is v else 'k'}: expected {shape} of {dtype} on the device, got {tuple(t.shape)} {t.dtype}")
+        layer, row, head, one = t.stride()
+        if T and (one != 1 or (heads > 1 and head != dim)):
+            raise SvdpError(f"{'v' if t is v else 'k'}: the heads of a row have to lie side by side")
+        # a dimension of one entry: its stride says nothing
+        args += (t.data_ptr(), layer if layers > 1 else 0, row if T > 1 else heads * dim)
+    _check(lib().svdp_kv_commit(ctypes.byref(cache.c), *args, _typed(slots, torch.int64, "slots"), T, _stream()), "svdp_kv_commit")
 
 
 def version() -> str:
