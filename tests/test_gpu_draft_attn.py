@@ -335,3 +335,22 @@ def test_tables_wider_than_the_requests_are_long(env, shape, tree):
     out, lse = c.call(binding)
     c.check(draft, out, lse)
     assert float((out.float() - narrow[0].float()).abs().amax()) <= 2.0 ** -6 * float(out.float().abs().amax())
+
+
+@pytest.mark.parametrize("dtype,dim,group", [("bf16", 128, 2), ("bf16", 128, 5), ("bf16", 128, 9), ("bf16", 64, 9), ("bf16", 256, 2), ("f32", 64, 2), ("f32", 128, 5)])
+def test_cut_requests_with_padding_limits_and_missing_pages(env, dtype, dim, group):
+    """Tables with room for much more: work is cut into parts, of rows that are no node, pages that do not exist, requests of nothing."""
+    torch, binding, draft = env
+    c = Attn(torch, binding, dtype=dtype, dim=dim, heads=2, group=group, page=32, lens=[700, 20, 0, 1500, 0], nodes=[10, 4, 3, 6, 0], pad=5, seed=21)
+    for r, i, bad in ((0, 0, -1), (0, 21, c.cache.pages), (1, 0, -(1 << 31)), (3, 5, (1 << 31) - 1), (3, 6, 1 << 29)):
+        c.table[r][i] = bad
+    wide = torch.full((5, 128), 1 << 30, dtype=torch.int32, device="cuda")
+    wide[:, :c.d_table.shape[1]] = torch.tensor(c.table, dtype=torch.int32)
+    c.d_table = wide
+    T, hq = c.starts[-1] + 5, 2 * group
+    out = torch.full((T, hq, dim), 7.0, dtype=c.q.dtype, device="cuda")
+    lse = torch.full((T, hq), 7.0, device="cuda")
+    c.call(binding, out=out, lse=lse, max_nodes=6)
+    c.check(draft, out, lse, max_nodes=6)
+    for rows in (slice(6, 10), slice(c.starts[-1], T)):
+        assert bool((out[rows] == 7).all()) and bool((lse[rows] == 7).all())
