@@ -286,12 +286,12 @@ svdp_status svdp_ffn_step_glued(const svdp_layer *layer, const void *x_prev, con
  * Nodes come after their ancestors (node 0 first: the newest certain token).
  *
  * Pages.  A request's tokens lie in pages of `page` tokens: token i in page table[r][i / page], at i % page.
- * table: device [R][max_pages] int32; entries past a request's length are not read.  A slot is page id * page + place.
+ * table: device [R][max_pages] int32; entries past a request's length have no influence.  A slot is page id * page + place.
  *
- * Limits (else SVDP_ERR_UNSUPPORTED): page 32, 64, 128 or 256; dim 64, 128 or 256; R <= SVDP_MAX_REQUESTS;
- * T <= SVDP_MAX_ROWS; T * heads_q below 2^26; pages * page, R * max_pages and max_pages * page below 2^31.  Values read from device memory that lie outside their
- * range never lead outside a buffer: lengths are clamped to the table's width, a page id outside [0, pages) is
- * skipped with its tokens.                                                                                     */
+ * Limits (else SVDP_ERR_UNSUPPORTED): page 32, 64, 128 or 256; dim 64, 128 or 256; R <= SVDP_MAX_REQUESTS; T <=
+ * SVDP_MAX_ROWS; T * heads_q below 2^26; pages * page, R * max_pages and max_pages * page below 2^31.  Values read
+ * from device memory that lie outside their range never lead outside a buffer: lengths are clamped to the table's
+ * width, a page id outside [0, pages) is skipped with its tokens. */
 #define SVDP_MAX_NODES 64
 #define SVDP_MAX_REQUESTS 4096
 #define SVDP_MAX_ROWS (1 << 24)
@@ -307,11 +307,12 @@ typedef struct svdp_kv_cache {
 
 /* Attention of every row over its request's cached tokens 0 .. lens[r] and over the nodes that it sees:
  *   out[t][h] = sum_j softmax_j(scale q[t][h] . k_j[c]) v_j[c],  c = h / (heads_q / heads).
- * q: device rows of [heads_q][dim], q_stride elements apart; k, v: device rows of [heads][dim], the step's own tokens
- * (not in the cache), k_stride and v_stride elements apart; the three pointers 16-byte aligned, the strides whole
- * 16-byte vectors.  scale: finite, and times log2(e) too.  lens: device [R] int32.  out: device [T][heads_q][dim] in the
- * cache's type, rows of requests written (padding and nodes past max_nodes are not).  lse: device [T][heads_q] fp32, nullable: the natural logarithm
- * of the softmax's denominator (with its maximum), for joining with attention over other tokens.
+ * q: device rows of [heads_q][dim], q_stride elements apart; k, v: device rows of [heads][dim], the step's own
+ * tokens (not in the cache), k_stride and v_stride elements apart; the three pointers 16-byte aligned, the strides
+ * whole 16-byte vectors.  scale: finite, and times log2(e) too.  lens: device [R] int32.  out: device
+ * [T][heads_q][dim] in the cache's type, rows of requests written (padding and nodes past max_nodes are not).  lse:
+ * device [T][heads_q] fp32, nullable: the natural logarithm of the softmax's denominator (with its maximum), for
+ * joining with attention over other tokens.
  * A row that sees nothing: out 0, lse -inf; so too where every weight is zero (all scores -inf).  Tokens that a row
  * does not see have no influence on it, NaN and infinities included.  Scores, softmax and sums are fp32; the weights are
  * rounded to the cache's type for their product with V.
