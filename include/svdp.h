@@ -314,8 +314,8 @@ typedef struct svdp_kv_cache {
  * device [T][heads_q] fp32, nullable: the natural logarithm of the softmax's denominator (with its maximum), for
  * joining with attention over other tokens.
  * A row that sees nothing: out 0, lse -inf; so too where every weight is zero (all scores -inf).  Tokens that a row
- * does not see have no influence on it, NaN and infinities included.  Scores, softmax and sums are fp32; the weights are
- * rounded to the cache's type for their product with V.
+ * does not see have no influence on it, NaN and infinities included.  Scores, softmax and sums are fp32; for
+ * their product with V the weights of a bf16 cache are two bf16 terms each, within 2^-15.
  * ws: >= svdp_tree_attn_workspace_bytes() (0 for arguments it does not take).                                      */
 size_t svdp_tree_attn_workspace_bytes(const svdp_kv_cache *cache, int32_t heads_q, int32_t R, int32_t max_pages,
                                       int32_t max_nodes);

@@ -190,15 +190,29 @@ struct TreeTile<bf16, DIM> {
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ta_bf16x8, k), __builtin_bit_cast(ta_bf16x8, q), s, 0, 0, 0);
     }
-    typedef ta_bf16x8 Weights;                  // of a lane's 8 tokens: rounded once, for their product with V
+    // The weights of a lane's 8 tokens as two terms, hi + lo, each for its own product with V: within 2^-15 of the fp32 weight (one
+    // term: 2^-8, as much as the output's own rounding).  hi lies below the weight by half of its last place at the least, so that neither
+    // term of a weight is zero or negative: an infinity in V stays one.
+    struct Weights {
+        uint4 hi, lo;
+    };
     static __device__ __forceinline__ Weights pack_weights(const float (&p)[8])
     {
-        const ta_f32x8 w = {p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]};
-        return __builtin_convertvector(w, ta_bf16x8);
+        uint32_t hi[4];
+        ta_f32x8 rest;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t a = __builtin_elementwise_sub_sat(__float_as_uint(p[2 * i]), 0x8000u);
+            const uint32_t b = __builtin_elementwise_sub_sat(__float_as_uint(p[2 * i + 1]), 0x8000u);
+            hi[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);            // the upper halves of a and b
+            rest[2 * i] = p[2 * i] - __uint_as_float(a & 0xffff0000u);     // exact
+            rest[2 * i + 1] = p[2 * i + 1] - __uint_as_float(b & 0xffff0000u);
+        }
+        return {make_uint4(hi[0], hi[1], hi[2], hi[3]), __builtin_bit_cast(uint4, __builtin_convertvector(rest, ta_bf16x8))};
     }
     static __device__ __forceinline__ f32x4_t sum(const uint4 (&v)[1], const Weights &p, f32x4_t o)
     {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ta_bf16x8, v[0]), p, o, 0, 0, 0);
+        return score(v[0], p.hi, score(v[0], p.lo, o));
     }
     // each element: f(its bits in front of 16 zeros) as a new element
     template <typename F>

@@ -7,12 +7,12 @@
 // 16 (i / 8) + 8 f + i % 8, by the choice of K rows), which are the tokens that O^T += V^T P^T wants of that lane.
 // LDS: K rows of DIM channels, 16-byte chunk c of token i at slot c ^ swizzle(i), so that the tokens of an operand read lie in different
 // banks; V as in memory, of which 32 lanes read consecutive 512 bytes.
-// What bounds it: a tile of 32 tokens is 528 cycles of a SIMD's matrix unit for each of its two waves, and about 600 of its
-// vector unit (16 exponentials and some 70 other instructions), side by side; what a stage costs besides (its barrier, addresses,
-// the first read of K) is why a stage is as large as LDS allows.  Trees of 64 with seven query heads a head over 20 000 to 32 768
-// tokens, 88 GFLOP: 125 us; a stage of 128 tokens takes 4.2 us, with the matrix units 63 % busy at a clock that sinks to 1.6 GHz
-// under them.  Some 14 us are not stages: 2 for the lengths, 3 for the first pages, Q and K and V, and a part of 133 KB that every block
-// writes and that leaves the caches at the end.  A call of one stage takes 10 us.
+// What bounds it: a tile of 32 tokens is 792 cycles of a SIMD's matrix unit for each of its two waves (the weights' two terms have a
+// product with V each), and about 700 of its vector unit (16 exponentials and some 110 other instructions), side by side; what a
+// stage costs besides (its barrier, addresses, the first read of K) is why a stage is as large as LDS allows.  Trees of 64 with seven
+// query heads a head over 20 000 to 32 768 tokens, 88 GFLOP without the second terms: a call 165 to 175 us, with weights of one term 130.
+// Some 14 us are not stages: 2 for the lengths, 3 for the first pages, Q and K and V, and a part of 133 KB that every block writes
+// and that leaves the caches at the end.  A call of one stage takes 10 us.
 #pragma once
 
 #include "svdp_tree_attn.h"
@@ -266,20 +266,24 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                         for (int dt = 0; dt < DT; ++dt) o[dt] *= old;
                     }
                     float sum = 0.f;
-                    uint4 p[2];
+                    typename X::Weights p[2];
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         float e[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) e[i] = exp2_fast(z[8 * t + i]);
                         sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-                        p[t] = __builtin_bit_cast(uint4, X::pack_weights(e));
+                        p[t] = X::pack_weights(e);
                     }
                     total += sum;
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) o[dt] = mfma_32(v[dt][t], p[t], o[dt]);
+                        for (int dt = 0; dt < DT; ++dt) o[dt] = mfma_32(v[dt][t], p[t].lo, o[dt]);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) o[dt] = mfma_32(v[dt][t], p[t].hi, o[dt]);
                 }
                 if (finite) continue;
                 // infinities and NaN that a row sees (see TreeWave::add_special)
@@ -300,7 +304,7 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) seen[i] = (mask >> (8 * t + i)) & 1 ? 1.f : 0.f;
                                 const uint4 all = *reinterpret_cast<const uint4 *>(from + (2 * t * DIM + dt * 32) * 16);
-                                count = mfma_32(ones_of_kind<X>(all, kind), __builtin_bit_cast(uint4, X::pack_weights(seen)), count);
+                                count = mfma_32(ones_of_kind<X>(all, kind), X::pack_weights(seen).hi, count);
                             }
 #pragma unroll
                             for (int i = 0; i < 16; ++i) o[dt][i] += count[i] > 0.f ? value_of_kind(kind) : 0.f;
