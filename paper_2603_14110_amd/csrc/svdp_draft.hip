@@ -283,7 +283,7 @@ svdp_status svdp_tree_accept(const void *logits, int64_t stride, int32_t dtype, 
         const int n_parts = best_parts(T, V, dtype);
         // one vector more than the row has where it begins between two of them
         const int per = tiles(tiles(V, Elem<W>::VEC) + 1, n_parts);
-        launch(k_logits_best<W>, dim3(T, n_parts), dim3(BEST_THREADS), 0, hs, rows, stride, V, per, parts);
+        if (T > 0) launch(k_logits_best<W>, dim3(T, n_parts), dim3(BEST_THREADS), 0, hs, rows, stride, V, per, parts);
         launch(k_tree_walk, dim3(R + 1), dim3(64), 0, hs, parts, n_parts, A);
     });
     return hip_status(hipSuccess);

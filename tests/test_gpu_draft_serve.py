@@ -425,3 +425,28 @@ def test_accept_of_few_and_of_many_logits(env, dtype, V):
             assert got == tuple(draft.accept(rows, tokens, None, starts))
     best = got[3]
     assert best[0] == 5 and best[1] == 0 and best[2] == V - 1 and best[3] == 0 and best[4] == V - 2 and best[5] == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [333, 152064])
+@pytest.mark.parametrize("max_nodes", [None, 1, 64])
+def test_accept_of_no_rows(env, dtype, V, max_nodes):
+    """Requests without rows, whatever kernel their logits' number would ask for: lengths of zero and no next token."""
+    torch, binding, draft = env
+    logits = torch.empty((0, V), dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda")
+    got = run_accept(torch, binding, logits, [], None, [0, 0, 0, 0], max_nodes=max_nodes)
+    assert got == ([], [0, 0, 0], [-1, -1, -1], [])
+
+
+@pytest.mark.parametrize("V", [701, 40003])
+def test_accept_of_a_request_with_more_rows_than_nodes(env, V):
+    """Rows past the limit are answered and in no branch, in one launch (few logits) and in two; the requests behind have none."""
+    torch, binding, draft = env
+    logits = torch.randn((24, V), device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)).to(torch.bfloat16)
+    rows = logits.float().cpu().numpy()
+    tokens = [draft.best_token(rows[max(t - 1, 0)]) for t in range(24)]
+    tree = sum((words(parents(random.Random(k), 8)) for k in range(3)), [])
+    for t in (None, tree):
+        want = draft.accept(rows, tokens, t, [0, 8, 8, 8])
+        for starts in ([0, 24, 24, 24], [0, 17, 17, 17], [0, 9, 9, 9]):
+            assert run_accept(torch, binding, logits, tokens, t, starts, max_nodes=8) == tuple(want)
