@@ -143,6 +143,9 @@ constexpr int COMMIT_BLOCKS = 4096;       // K and V of few rows: fewer channels
 // in two launches 11.7 and 4.5 + 3.4; 250 KB: 9.2 and 9.3, in two 12.1 and 4.0 + 3.5, and by itself a call is 3 us slower).
 constexpr int64_t ACCEPT_SMALL = 128 << 10;
 
+constexpr int BEST_ROWS = 1 << 23;        // of a launch: its threads are counted in 32 bits
+static_assert((int64_t)BEST_ROWS * BEST_THREADS < (int64_t)1 << 32);
+
 // Parts that a row of logits is cut into: about a thousand blocks altogether, each of 8 to 32 KB.
 int best_parts(int T, int V, int dt)
 {
@@ -283,7 +286,9 @@ svdp_status svdp_tree_accept(const void *logits, int64_t stride, int32_t dtype, 
         const int n_parts = best_parts(T, V, dtype);
         // one vector more than the row has where it begins between two of them
         const int per = tiles(tiles(V, Elem<W>::VEC) + 1, n_parts);
-        if (T > 0) launch(k_logits_best<W>, dim3(T, n_parts), dim3(BEST_THREADS), 0, hs, rows, stride, V, per, parts);
+        for (int t = 0; t < T; t += BEST_ROWS)
+            launch(k_logits_best<W>, dim3(std::min(T - t, BEST_ROWS), n_parts), dim3(BEST_THREADS), 0, hs, rows + t * stride, stride, V, per,
+                   parts + (size_t)t * n_parts);
         launch(k_tree_walk, dim3(R + 1), dim3(64), 0, hs, parts, n_parts, A);
     });
     return hip_status(hipSuccess);

@@ -450,3 +450,15 @@ def test_accept_of_a_request_with_more_rows_than_nodes(env, V):
         want = draft.accept(rows, tokens, t, [0, 8, 8, 8])
         for starts in ([0, 24, 24, 24], [0, 17, 17, 17], [0, 9, 9, 9]):
             assert run_accept(torch, binding, logits, tokens, t, starts, max_nodes=8) == tuple(want)
+
+
+def test_accept_of_the_most_rows(env):
+    """As many rows as a call takes, all but 64 of them padding: more threads than one grid can have."""
+    torch, binding, draft = env
+    T, V = 1 << 24, 3
+    x = torch.randn((T, V), device="cuda", generator=torch.Generator(device="cuda").manual_seed(8))
+    best = torch.where(x == x.amax(1, keepdim=True), torch.arange(V, device="cuda", dtype=torch.int32), V).amin(1)
+    tokens = torch.cat([best[:1], best[:-1]])
+    keep, counts, following, got = binding.tree_accept(x, tokens, i32(torch, [0, 64]))
+    assert torch.equal(got, best) and counts.tolist() == [64] and following.tolist() == best[63:64].tolist()
+    assert keep[:64].tolist() == list(range(64)) and bool((keep[64:] == -1).all())
