@@ -131,7 +131,7 @@ AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, in
     p.tasks = (rows + block_rows - 1) / block_rows * c->heads * R;
     const bool uncut = p.steps <= 1 || (p.steps <= (p.wide ? UNCUT_WIDE : UNCUT) && p.tasks <= 1 << p.block_bits);
     p.part_rows = uncut ? 0 : (int)std::min<int64_t>(rows, block_rows);
-    p.bytes = std::max(align_up(((size_t)2 << p.block_bits) * p.part_rows * (dim + 2) * 4), ALIGN);
+    p.bytes = std::max(align_up(((size_t)2 << p.block_bits) * tree_part_floats(p.part_rows, dim) * 4), ALIGN);
     return p;
 }
 // Rows and heads from which the join has a wave for each, whatever the parts (768 of 24 requests: 4.2 us, with a block each 5.2; 256

@@ -42,7 +42,7 @@ struct TreeJoinArgs {
     const int32_t *lens, *starts;
     void *out;
     float *lse;
-    float *parts;                       // [2 << Cut::BITS] parts of part_rows (dim + 2) floats
+    float *parts;                       // [2 << Cut::BITS] parts of tree_part_floats(part_rows, dim)
     int room, heads, group, R, T;       // room: tokens that a request's row of the table can have
     uint16_t max_nodes;
     uint16_t part_rows;                 // rows of a part: no more than a request has, nor a block; 0: nothing is cut
@@ -168,10 +168,13 @@ __device__ __forceinline__ int tree_request(const TreeJoinArgs &A, int u, int la
     }
 }
 
-// A part's address: block b has two, of part_rows rows of DIM sums and behind them the rows' maxima and denominators.
+// Floats of a part: its rows' sums and behind them their maxima and denominators, up to whole 16 bytes, which it is written and read in.
+__host__ __device__ constexpr size_t tree_part_floats(int rows, int dim) { return ((size_t)rows * (dim + 2) + 3) & ~(size_t)3; }
+static_assert(tree_part_floats(1, 128) == 132 && tree_part_floats(7, 64) == 464 && tree_part_floats(256, 128) == 256 * 130);
+// A part's address: block b has two.
 __device__ __forceinline__ float *tree_part(const TreeJoinArgs &A, int b, int which, int dim)
 {
-    return A.parts + (size_t)(2 * b + which) * A.part_rows * (dim + 2);
+    return A.parts + (size_t)(2 * b + which) * tree_part_floats(A.part_rows, dim);
 }
 
 // ---- operands, by storage type --------------------------------------------------------------------------------------------

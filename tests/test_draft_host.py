@@ -173,3 +173,15 @@ def test_rows_beyond_a_grid_are_refused(svdp):
     assert svdp.lib().svdp_tree_accept_workspace_bytes(most + 1, 100, 1) == 0
     a = (2 * P, 4, 3 * P, 50, 64, 4 * P, 5 * P, 6 * P, 7 * P, None, 2, most + 1, 8 * P, 9 * P, 10 * P, 11 * P)
     assert svdp.lib().svdp_kv_plan(*a, None) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("dtype,dim,heads_q,nodes,parts", [(1, 128, 8, 1, 1024), (1, 128, 56, 1, 1024), (1, 64, 24, 5, 1024), (1, 128, 56, 3, 512),
+                                                           (1, 256, 8, 13, 512), (0, 64, 8, 7, 1024), (0, 64, 24, 9, 512), (1, 128, 56, 33, 512)])
+def test_parts_of_the_attention_begin_at_16_bytes(svdp, dtype, dim, heads_q, nodes, parts):
+    """Parts are written and read 16 bytes at a time: with odd numbers of rows, too, each of them is whole 16 bytes long."""
+    c = cache(svdp, dtype=dtype, dim=dim)
+    n = svdp.lib().svdp_tree_attn_workspace_bytes(ctypes.byref(c), heads_q, 8, 1000, nodes)
+    rows = min(nodes * heads_q // 8, 256 if nodes > 30 else 32 if parts == 512 and dim < 256 else 16)
+    least = rows * (dim + 2) * 4
+    assert rows % 2 == 1
+    assert n % (16 * parts) == 0 and least <= n // parts < least + 16
