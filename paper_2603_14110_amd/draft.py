@@ -103,6 +103,12 @@ class Decoder:
         binding.kv_commit(self.cache, k, v, slots)
         return refused
 
+    def release(self) -> None:
+        """Every request ends: all pages are free again.  What prefill() or step() stored before they raised is given back by it too."""
+        ends = torch.full_like(self.lens, -1)
+        none = torch.zeros(ends.numel() + 1, dtype=torch.int32, device=ends.device)
+        _, self.lens, self.pool, _ = binding.kv_plan(self.table, self.ring, self.pool, self.lens, ends, none, self.cache.page, rows=0)
+
     def prefill(self, prompts: List[List[int]]) -> None:
         """All but the last token of each prompt into the cache, up to 64 tokens of each request at a time."""
         done, ends = 0, [len(p) - 1 for p in prompts]
@@ -137,8 +143,17 @@ class Decoder:
     def generate(self, prompts: List[List[int]], new: int, nodes: int = 8,
                  draft: Callable[[Sequence[int], int], Tree] = lookup) -> Tuple[List[List[int]], int]:
         """``new`` tokens after each prompt (one for each of the cache's requests), and the number of steps that took.  draft
-        proposes up to nodes - 1 tokens from what a request has; nodes=1 decodes one by one."""
+        proposes up to nodes - 1 tokens from what a request has; nodes=1 decodes one by one.  All pages are free afterwards, after
+        an error too."""
         assert len(prompts) == self.lens.numel() and min(map(len, prompts)) > 0
+        if bool(self.lens.any()):
+            raise RuntimeError("the cache holds tokens of other requests: release() them first")
+        try:
+            return self._generate(prompts, new, nodes, draft)
+        finally:
+            self.release()
+
+    def _generate(self, prompts, new, nodes, draft):
         self.prefill(prompts)
         text, steps = [list(p) for p in prompts], 0
         live = [new > 0] * len(prompts)
@@ -151,9 +166,6 @@ class Decoder:
                 t += more
             steps += 1
             live = [on and len(t) < len(p) + new for on, t, p in zip(live, text, prompts)]
-        ends = torch.full_like(self.lens, -1)
-        none = torch.zeros(len(prompts) + 1, dtype=torch.int32, device=ends.device)
-        _, self.lens, self.pool, _ = binding.kv_plan(self.table, self.ring, self.pool, self.lens, ends, none, self.cache.page, rows=0)
         return [t[len(p):len(p) + new] for t, p in zip(text, prompts)], steps
 
 

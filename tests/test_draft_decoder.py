@@ -112,3 +112,43 @@ def test_bf16_decodes_and_too_few_pages_are_an_error():
     _all_free(decoder)
     with pytest.raises(RuntimeError, match="too few pages"):
         _decoder(pages=4).generate(PROMPTS, NEW)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fails", ["prompts", "steps", "draft"])
+def test_a_call_that_fails_leaves_nothing_behind(fails):
+    """Too few pages for the prompts or for what follows them, and a draft that raises: all pages are free again, and the next call's
+    tokens are those of a fresh decoder."""
+    short = [[9, 2, 9], [4], [8, 8, 1, 8]]
+    made = dict(bias=1e4, pages=7 if fails != "draft" else 24)
+    decoder = _decoder(**made)
+
+    def broken(history, nodes):
+        if len(history) > 10:
+            raise ValueError("no draft")
+        return [], []
+
+    if fails == "draft":
+        with pytest.raises(ValueError, match="no draft"):
+            decoder.generate(short, NEW, draft=broken)
+    else:
+        prompts = PROMPTS if fails == "steps" else [PROMPTS[2]] * 3          # 1 + 1 + 5 pages are there for those
+        with pytest.raises(RuntimeError, match="too few pages"):
+            decoder.generate(prompts, NEW)
+    _all_free(decoder)
+    out, _ = decoder.generate(short, 20, nodes=6)
+    fresh, _ = _decoder(**made).generate(short, 20, nodes=6)
+    assert out == fresh
+    _all_free(decoder)
+
+
+@pytest.mark.gpu
+def test_tokens_of_other_requests_are_not_taken_for_a_prompt():
+    decoder = _decoder(bias=1e4)
+    decoder.prefill(PROMPTS)
+    with pytest.raises(RuntimeError, match="release"):
+        decoder.generate(PROMPTS, 4)
+    assert decoder.lens.tolist() == [len(p) - 1 for p in PROMPTS]
+    decoder.release()
+    _all_free(decoder)
+    assert decoder.generate(PROMPTS, 4)[0] == _decoder(bias=1e4).generate(PROMPTS, 4)[0]
