@@ -41,6 +41,18 @@ def lookup(history: Sequence[int], nodes: int, branches: int = 3) -> Tree:
     return tokens, parents
 
 
+def cut(tree: Tree, levels: int) -> Tree:
+    """The first ``levels`` levels of a drafted tree."""
+    tokens, parents, depth, place = [], [], {-1: 0}, {-1: -1}
+    for j, (t, p) in enumerate(zip(*tree)):
+        depth[j] = depth[p] + 1
+        if depth[j] <= levels:
+            place[j] = len(tokens)
+            tokens.append(t)
+            parents.append(place[p])
+    return tokens, parents
+
+
 class Decoder:
     """Weights: per layer a binding.DeviceLayer, Wqkv [d][(heads_q + 2 heads) dim] and Wo [heads_q dim][d]; embed and
     head [V][d].  The cache has ``pages`` pages of ``page`` tokens for ``requests`` requests of up to ``max_len``."""
@@ -143,7 +155,8 @@ class Decoder:
     def generate(self, prompts: List[List[int]], new: int, nodes: int = 8,
                  draft: Callable[[Sequence[int], int], Tree] = lookup) -> Tuple[List[List[int]], int]:
         """``new`` tokens after each prompt (one for each of the cache's requests), and the number of steps that took.  draft
-        proposes up to nodes - 1 tokens from what a request has; nodes=1 decodes one by one.  All pages are free afterwards, after
+        proposes up to nodes - 1 tokens from what a request has (none are taken that would lead past ``new``, so a request never needs
+        room for more than its prompt and those); nodes=1 decodes one by one.  All pages are free afterwards, after
         an error too."""
         assert len(prompts) == self.lens.numel() and min(map(len, prompts)) > 0
         if bool(self.lens.any()):
@@ -159,8 +172,9 @@ class Decoder:
         live = [new > 0] * len(prompts)
         while any(live):
             trees = []
-            for t in text:
-                toks, parents = draft(t, nodes - 1) if nodes > 1 else ([], [])
+            for t, p in zip(text, prompts):
+                levels = len(p) + new - len(t) - 1          # a step's answers are one more than the drafts it keeps
+                toks, parents = cut(draft(t, nodes - 1), levels) if nodes > 1 and levels > 0 else ([], [])
                 trees.append(([t[-1]] + toks, [-1] + [p + 1 for p in parents]))
             for t, more in zip(text, self.step(trees, live)):
                 t += more

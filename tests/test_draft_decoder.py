@@ -152,3 +152,33 @@ def test_tokens_of_other_requests_are_not_taken_for_a_prompt():
     decoder.release()
     _all_free(decoder)
     assert decoder.generate(PROMPTS, 4)[0] == _decoder(bias=1e4).generate(PROMPTS, 4)[0]
+
+
+@pytest.mark.parametrize("tree,levels,want", [
+    (([], []), 3, ([], [])), (([5, 6, 7], [-1, 0, 1]), 2, ([5, 6], [-1, 0])), (([5, 6, 7], [-1, 0, 1]), 3, ([5, 6, 7], [-1, 0, 1])),
+    (([1, 2, 3, 4, 5, 6], [-1, 0, 1, -1, 3, 3]), 2, ([1, 2, 4, 5, 6], [-1, 0, -1, 2, 2])), (([1, 2, 3], [-1, 0, -1]), 1, ([1, 3], [-1, -1])),
+])
+def test_a_tree_is_cut_to_levels(tree, levels, want):
+    from paper_2603_14110_amd.draft import cut
+
+    assert cut(tree, levels) == want
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nodes", [2, 8, 12, 64])
+def test_drafts_need_no_more_room_than_the_text(nodes):
+    """Table and pool hold prompt and new tokens and nothing more, and every draft is right: the same tokens as one by one."""
+    prompts = [[(3 * i + r) % 300 for i in range(24)] for r in range(3)]
+    on, _ = _decoder(bias=1e4).generate(prompts, NEW + 64, nodes=1)        # on and on, past what is wanted
+    texts = {tuple(p): p + o for p, o in zip(prompts, on)}
+    decoder = _decoder(bias=1e4, pages=6, max_len=24 + NEW)
+    plain, _ = decoder.generate(prompts, NEW, nodes=1)
+    assert plain == [o[:NEW] for o in on]
+
+    def right(history, most):
+        more = texts[tuple(history[:24])][len(history):][:most]
+        return more, list(range(-1, len(more) - 1))
+
+    out, steps = decoder.generate(prompts, NEW, nodes=nodes, draft=right)
+    assert out == plain and steps == -(-NEW // nodes)
+    _all_free(decoder)
