@@ -348,7 +348,8 @@ svdp_status svdp_tree_accept(const void *logits, int64_t stride, int32_t dtype, 
  * lens_out [R] int32: the lengths after the step.  pool_out [2]: place and number of the free pages after it.
  * keep: device [T], the place of row t among its request's added tokens, -1 for a row that is not added (as
  * svdp_tree_accept writes it); NULL: row starts[r] + i has place i.  slots: device [T] 64-bit, the slot of each row, -1 where it has none.
- * table and ring are changed in place; pool_out and lens_out must not overlap the inputs.  Every other array is device int32.
+ * table and ring are changed in place; no array that is written (they, slots, lens_out, pool_out, refused) may overlap another
+ * one (else SVDP_ERR_INVALID_ARG).  Every other array is device int32.
  * A repeated call with the same inputs writes the same values.                                                        */
 svdp_status svdp_kv_plan(int32_t *table, int32_t max_pages, int32_t *ring, int32_t pages, int32_t page, const int32_t *pool,
                          const int32_t *lens, const int32_t *add, const int32_t *starts, const int32_t *keep, int32_t R,

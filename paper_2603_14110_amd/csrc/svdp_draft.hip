@@ -40,7 +40,7 @@ inline int tiles(int64_t n, int per) { return (int)((n + per - 1) / per); }
 bool overlap(const void *a, size_t an, const void *b, size_t bn)
 {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + bn && y < x + an;
+    return an > 0 && bn > 0 && x < y + bn && y < x + an;
 }
 
 svdp_status check_cache(const svdp_kv_cache *c)
@@ -308,13 +308,18 @@ svdp_status svdp_kv_plan(int32_t *table, int32_t max_pages, int32_t *ring, int32
     for (const void *p : words)
         if (p == nullptr || !aligned_to(p, 4)) return SVDP_ERR_INVALID_ARG;
     if (!aligned_to(keep, 4) || (T > 0 && slots == nullptr) || !aligned_to(slots, 8)) return SVDP_ERR_INVALID_ARG;
+    // blocks do not wait for each other: what one of them writes no other may read, nor write
     const size_t rows = (size_t)R * 4;
-    for (const void *o : {static_cast<const void *>(lens_out), static_cast<const void *>(refused)})
-        if (overlap(o, rows, lens, rows) || overlap(o, rows, add, rows) || overlap(o, rows, pool, 8) ||
-            overlap(o, rows, starts, rows + 4))
-            return SVDP_ERR_INVALID_ARG;
-    if (overlap(pool_out, 8, pool, 8) || overlap(pool_out, 8, lens, rows) || overlap(pool_out, 8, add, rows))
-        return SVDP_ERR_INVALID_ARG;
+    const struct {
+        const void *at;
+        size_t bytes;
+        bool written;
+    } arrays[] = {{slots, (size_t)T * 8, true}, {lens_out, rows, true}, {refused, rows, true}, {pool_out, 8, true},
+                  {table, rows * max_pages, true}, {ring, (size_t)pages * 4, true}, {pool, 8, false}, {lens, rows, false},
+                  {add, rows, false}, {starts, rows + 4, false}, {keep, keep != nullptr ? (size_t)T * 4 : 0, false}};
+    for (const auto &o : arrays)
+        for (const auto &i : arrays)
+            if (o.written && &o != &i && overlap(o.at, o.bytes, i.at, i.bytes)) return SVDP_ERR_INVALID_ARG;
     static_assert(SVDP_MAX_REQUESTS <= PLAN_EACH * PLAN_THREADS, "every request has a thread");
     const size_t lds = plan_lds(R);
     if (!grant_lds<k_kv_plan>(lds)) return SVDP_ERR_UNSUPPORTED;

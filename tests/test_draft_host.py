@@ -185,3 +185,22 @@ def test_parts_of_the_attention_begin_at_16_bytes(svdp, dtype, dim, heads_q, nod
     least = rows * (dim + 2) * 4
     assert rows % 2 == 1
     assert n % (16 * parts) == 0 and least <= n // parts < least + 16
+
+
+@pytest.mark.parametrize("keep", [None, 12])
+@pytest.mark.parametrize("name,at", [(o, i) for o in ("slots", "lens_out", "pool_out", "refused", "table", "ring")
+                                     for i in ("table", "ring", "pool", "lens", "add", "starts", "keep", "slots", "lens_out", "pool_out", "refused")
+                                     if o != i])
+def test_plan_writes_over_nothing_it_has(svdp, name, at, keep):
+    """Any two of its arrays of which one is written: from the same place on, and by the last eight bytes."""
+    a = dict(table=2, max_pages=4, ring=3, pages=50, page=64, pool=4, lens=5, add=6, starts=7, keep=keep, R=2, T=8,
+             slots=8, lens_out=9, pool_out=10, refused=11)
+    size = dict(table=32, ring=200, pool=8, lens=8, add=8, starts=12, keep=32, slots=64, lens_out=8, pool_out=8, refused=8)
+    if a[at] is None:
+        return
+    for back in (0, 8 - size[at]):
+        b = {k: v * P if k in size and v is not None else v for k, v in a.items()}
+        b[name] = b[at] - back
+        if b[name] % 8 and name == "slots":
+            continue
+        assert svdp.lib().svdp_kv_plan(*b.values(), None) == INVALID
