@@ -291,7 +291,7 @@ svdp_status svdp_ffn_step_glued(const svdp_layer *layer, const void *x_prev, con
  * Limits (else SVDP_ERR_UNSUPPORTED): page 32, 64, 128 or 256; dim 64, 128 or 256; R <= SVDP_MAX_REQUESTS; T <=
  * SVDP_MAX_ROWS; T * heads_q below 2^26; pages * page, R * max_pages and max_pages * page below 2^31.  Values read
  * from device memory that lie outside their range never lead outside a buffer: lengths are clamped to the table's
- * width, a page id outside [0, pages) is skipped with its tokens. */
+ * width, a page id outside [0, pages) is skipped with its tokens.  What a call writes must not overlap anything else it is given. */
 #define SVDP_MAX_NODES 64
 #define SVDP_MAX_REQUESTS 4096
 #define SVDP_MAX_ROWS (1 << 24)
@@ -343,8 +343,10 @@ svdp_status svdp_tree_accept(const void *logits, int64_t stride, int32_t dtype, 
  * ring[pages] from place pool[0] on (cyclic).  add[r] >= 0: request r, of lens[r] tokens, takes the pages that add[r] more need, in the
  * order of the requests, from the ring's front, and its new entries of `table` are written.  add[r] = -1: the
  * request ends, its pages go to the ring's end in the order of the requests and of its table row (they are free from
- * the next call on).  A request whose pages would not fit the table, or are not there after those of the requests before
- * it, is refused: refused[r] = 1 (else 0), its length stays, its rows get no slots (nor do those after it, unless they need no page).
+ * the next call on).  Refused (refused[r] = 1, else 0; its length stays, its rows get no slots) is a request
+ *  - whose tokens would not fit its row of the table: it asks for no pages, the requests after it are not touched by it;
+ *  - whose pages are not there after those of the requests before it: so is every request after it that needs a page, even
+ *    where there would be enough for that one.
  * lens_out [R] int32: the lengths after the step.  pool_out [2]: place and number of the free pages after it.
  * keep: device [T], the place of row t among its request's added tokens, -1 for a row that is not added (as
  * svdp_tree_accept writes it); NULL: row starts[r] + i has place i.  slots: device [T] 64-bit, the slot of each row, -1 where it has none.

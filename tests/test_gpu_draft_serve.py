@@ -462,3 +462,14 @@ def test_accept_of_the_most_rows(env):
     keep, counts, following, got = binding.tree_accept(x, tokens, i32(torch, [0, 64]))
     assert torch.equal(got, best) and counts.tolist() == [64] and following.tolist() == best[63:64].tolist()
     assert keep[:64].tolist() == list(range(64)) and bool((keep[64:] == -1).all())
+
+
+def test_plan_refuses_for_two_reasons(env):
+    """Too wide for the table: nobody else is touched.  Too few pages: nor does any later request get one."""
+    torch, binding, draft = env
+    c = dict(table=[[0, 1], [-1, -1], [-1, -1], [2, -1], [3, -1], [-1, -1]], ring=[4, 5, 6, 7, 8, 9, 10, 11], pool=[0, 3],
+             lens=[64, 0, 0, 10, 32, 0], add=[1, 64, 40, 5, 1, 0], starts=[0, 1, 65, 105, 110, 111, 111], keep=None, page=32)
+    want = draft.plan(**c, rows=111)
+    assert want[1] == [64, 64, 0, 15, 32, 0] and want[3] == [1, 0, 1, 0, 1, 0] and want[2] == [2, 1]
+    c["keep"] = []
+    assert run_plan(torch, binding, c, keep=False) == tuple(want)
