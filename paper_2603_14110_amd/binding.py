@@ -514,13 +514,14 @@ def tree_accept(logits: torch.Tensor, tokens: torch.Tensor, starts: torch.Tensor
     dt = SVDP_BF16 if logits.dtype == torch.bfloat16 else SVDP_F32
     max_nodes = max(1, min(T, MAX_NODES)) if max_nodes is None else int(max_nodes)
     nbytes = tree_accept_workspace_bytes(T, V, dt)
-    if ws is None:          # one allocation: the scratch in front of the outputs
-        at, keep, best, counts, following = torch.empty(
-            nbytes // 4 + 2 * T + 2 * max(R, 0), dtype=torch.int32, device=logits.device).split_with_sizes((nbytes // 4, T, T, max(R, 0), max(R, 0)))
-        at, room = at.data_ptr(), nbytes
+    # The scratch apart from the outputs, which a caller keeps; up to 2 KB in front of them: another allocation is 1 us of a call's 13.5.
+    near = nbytes // 4 if ws is None and nbytes <= 2048 else 0
+    scratch, keep, best, counts, following = torch.empty(near + 2 * T + 2 * max(R, 0), dtype=torch.int32, device=logits.device).split_with_sizes(
+        (near, T, T, max(R, 0), max(R, 0)))
+    if near:
+        at, room = scratch.data_ptr(), nbytes
     else:
-        keep, best, counts, following = torch.empty(2 * T + 2 * max(R, 0), dtype=torch.int32, device=logits.device).split(
-            (T, T, max(R, 0), max(R, 0)))
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=logits.device) if ws is None else ws
         at, room = _ptr(ws), ws.numel()
     _check(lib().svdp_tree_accept(
         logits.data_ptr(), logits.stride(0) if T > 1 else V, dt, V, _typed(tokens, torch.int32, "tokens", (T,)),

@@ -473,3 +473,14 @@ def test_plan_refuses_for_two_reasons(env):
     assert want[1] == [64, 64, 0, 15, 32, 0] and want[3] == [1, 0, 1, 0, 1, 0] and want[2] == [2, 1]
     c["keep"] = []
     assert run_plan(torch, binding, c, keep=False) == tuple(want)
+
+
+def test_accept_keeps_no_scratch_alive(env):
+    """What a caller keeps of the outputs holds the outputs' memory and not the call's scratch."""
+    torch, binding, draft = env
+    logits, tokens, tree, starts = make_accept(torch, 6, 4, 8, 152064, "bf16")
+    out = binding.tree_accept(logits, i32(torch, tokens), i32(torch, starts))
+    assert binding.tree_accept_workspace_bytes(len(tokens), 152064, binding.SVDP_BF16) > 2048
+    assert all(o.untyped_storage().nbytes() <= 4 * (2 * len(tokens) + 2 * 4) for o in out)
+    want = draft.accept(logits.float().cpu().numpy(), tokens, None, starts)
+    assert tuple(o.tolist() for o in out) == tuple(want)
