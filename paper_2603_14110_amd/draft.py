@@ -95,6 +95,8 @@ class Decoder:
         """Device tensors of one step's rows from (tokens, parents) of each request, roots among them (parent -1)."""
         tokens, masks, depth, starts = [], [], [], [0]
         for toks, parents in trees:
+            if len(toks) != len(parents) or any(not 0 <= t < self.embed.shape[0] for t in toks) or any(not -1 <= p < j for j, p in enumerate(parents)):
+                raise ValueError("a tree's tokens have to be of the vocabulary, its parents in front of their children")
             first = len(tokens)
             for j, p in enumerate(parents):
                 masks.append((masks[first + p] if p >= 0 else 0) | 1 << j)

@@ -182,3 +182,18 @@ def test_drafts_need_no_more_room_than_the_text(nodes):
     out, steps = decoder.generate(prompts, NEW, nodes=nodes, draft=right)
     assert out == plain and steps == -(-NEW // nodes)
     _all_free(decoder)
+
+
+@pytest.mark.parametrize("tree", [([300], [-1]), ([-1], [-1]), ([1, 2], [-1]), ([1, 2], [-1, 1]), ([1, 2], [-1, 2]), ([1, 2], [-1, -2])])
+def test_trees_are_looked_over_before_the_device_has_them(tree):
+    """A token outside the vocabulary would be read past the embedding's rows, by a kernel."""
+    import torch
+    from paper_2603_14110_amd.draft import Decoder
+
+    decoder = Decoder.__new__(Decoder)
+    decoder.embed, decoder.lens = torch.zeros(300, 8), torch.zeros(2, dtype=torch.int32)
+    good = ([299, 0, 5], [-1, 0, 0])
+    tokens, starts, masks, places, most = decoder._rows([good, ([], [])])
+    assert tokens.tolist() == good[0] and starts.tolist() == [0, 3, 3] and masks.tolist() == [1, 3, 5] and places.tolist() == [0, 1, 1] and most == 3
+    with pytest.raises(ValueError, match="vocabulary"):
+        decoder._rows([good, tree])
