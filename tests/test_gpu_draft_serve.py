@@ -484,3 +484,11 @@ def test_accept_keeps_no_scratch_alive(env):
     assert all(o.untyped_storage().nbytes() <= 4 * (2 * len(tokens) + 2 * 4) for o in out)
     want = draft.accept(logits.float().cpu().numpy(), tokens, None, starts)
     assert tuple(o.tolist() for o in out) == tuple(want)
+
+
+@pytest.mark.parametrize("R", [4064, 4095])
+def test_plan_at_the_end_of_the_memory_that_needs_no_grant(env, R):
+    """Sums of just below 64 KB, with what every block has besides above it."""
+    torch, binding, draft = env
+    c = make_plan(R, R, 32, 2, 9000, 30)
+    assert run_plan(torch, binding, c) == tuple(draft.plan(**c, rows=len(c["keep"])))
