@@ -215,7 +215,7 @@ struct TreeTile<bf16, DIM> {
     }
     static __device__ __forceinline__ f32x4_t sum(const uint4 (&v)[1], const Weights &p, f32x4_t o)
     {
-        return score(v[0], p.hi, score(v[0], p.lo, o));
+        return score(v[0], p.lo, score(v[0], p.hi, o));
     }
     // each element: f(its bits in front of 16 zeros) as a new element
     template <typename F>

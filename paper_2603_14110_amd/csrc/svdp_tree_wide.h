@@ -279,11 +279,11 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) o[dt] = mfma_32(v[dt][t], p[t].lo, o[dt]);
+                        for (int dt = 0; dt < DT; ++dt) o[dt] = mfma_32(v[dt][t], p[t].hi, o[dt]);
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) o[dt] = mfma_32(v[dt][t], p[t].hi, o[dt]);
+                        for (int dt = 0; dt < DT; ++dt) o[dt] = mfma_32(v[dt][t], p[t].lo, o[dt]);
                 }
                 if (finite) continue;
                 // infinities and NaN that a row sees (see TreeWave::add_special)
