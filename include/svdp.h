@@ -290,7 +290,8 @@ svdp_status svdp_ffn_step_glued(const svdp_layer *layer, const void *x_prev, con
  * table: device [R][max_pages] int32; entries past a request's length have no influence.  A slot is page id * page + place.
  *
  * Limits (else SVDP_ERR_UNSUPPORTED): page 32, 64, 128 or 256; dim 64, 128 or 256; R <= SVDP_MAX_REQUESTS; T <=
- * SVDP_MAX_ROWS; T * heads_q below 2^26; pages * page, R * max_pages and max_pages * page below 2^31.  Values read
+ * SVDP_MAX_ROWS; T * heads_q below 2^26; pages * page, R * max_pages and max_pages * page below 2^31; attention: R * heads *
+ * ceil(rows / 16) * (max_pages * page / 128 + 2) below 2^31, where rows = max_nodes * heads_q / heads (some more are taken).  Values read
  * from device memory that lie outside their range never lead outside a buffer: lengths are clamped to the table's
  * width, a page id outside [0, pages) is skipped with its tokens.  What a call writes must not overlap anything else it is given. */
 #define SVDP_MAX_NODES 64

@@ -105,19 +105,20 @@ void on_kernel(const AttnPlan &p, int dt, int dim, F &&f)
     });
 }
 // Units of a request and head up to which a block takes them all and there is nothing to join, if no block has two of them: one row,
-// 250 tokens: 9.0 us and a call 11.6, cut 7.5 + 3.4 and 14.6; 20 requests of 32 rows 13.4 us, cut 15.8 + 4.1; eight units 12.2 us, cut
-// 7.5 + 3.5.  Rows over the waves: 120 tokens 12.9 us, cut 9.6 + 4.3; 250 tokens 15.4, cut 9.5 + 4.9.
+// 250 tokens: 9.7 us and a call 12.3, cut 7.2 + 3.6 and 15.7; 20 requests of 32 rows 15.2 us, cut 17.4 + 4.4; seven units 14.1 us, cut
+// 7.6 + 3.7.  Rows over the waves, 120 tokens: 64 rows 14.0 us and a call 13.8, cut 10.6 + 3.5 and 15.0; 20 requests of 64 rows 15.2,
+// cut 19.6 + 7.1; 448 rows of one request, the other way round, 19.8 and 19.5, cut 14.8 + 4.0 and 17.6.
 constexpr int UNCUT = 4, UNCUT_WIDE = 2;
 AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, int max_nodes)
 {
     const int dt = c->dtype, dim = c->dim, group = heads_q / c->heads;
     const int64_t rows = (int64_t)group * max_nodes, room = (int64_t)max_pages * c->page / TA_TILE, own = tiles(max_nodes, TA_TILE);
     AttnPlan p;
-    // More than 32 rows: over the waves, 32 each (eight requests of 4096 tokens, 135 MB: 36 rows 30.0 us, 64 rows 31.5, where
-    // k_tree_attn, with two row tiles after each other, takes 32.2 and 43.7).  At 32 rows k_tree_attn is ahead: 25.4 us for one
-    // request of 30 000 tokens and 24.5 for 24 of 150, where rows over the waves took 28.6 and 45.
+    // More than 32 rows: over the waves, 32 each (eight requests of 4096 tokens, 135 MB: 36 and 64 rows 36 us, where k_tree_attn, with
+    // two row tiles after each other, takes 48).  At 32 rows k_tree_attn is ahead: 26.4 us for one request of 30 000 tokens and 13.4
+    // for 24 of 150, where rows over the waves took 32.0 and 16.6 + 4.4.
     p.wide = dt == SVDP_BF16 && dim <= 128 && rows > 32;
-    // Two row tiles of 16 read K and V once for 32 rows (8 requests of 4096 tokens, 135 MB: 28.5 us, one after the other 38.8); with
+    // Two row tiles of 16 read K and V once for 32 rows (8 requests of 4096 tokens, 135 MB: 29.6 us, one after the other 45.2); with
     // 256 channels a second one does not fit the registers.
     p.nt = rows <= 16 || dim == 256 ? 1 : 2;
     int unit, block_rows;
@@ -134,13 +135,16 @@ AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, in
     p.bytes = std::max(align_up(((size_t)2 << p.block_bits) * tree_part_floats(p.part_rows, dim) * 4), ALIGN);
     return p;
 }
-// Rows and heads from which the join has a wave for each, whatever the parts (768 of 24 requests: 4.2 us, with a block each 5.2; 256
-// of one request, with 32 parts: 8.2 us, with a block each 4.5).
+// Rows and heads from which the join has a wave for each, whatever the parts (12 288 of 24 requests: 7.1 us, with a block each 33.6; 256
+// of one request, with 32 parts: 7.4 us, with a block each 4.0; in between it depends on the parts: 512 with 32 of them 7.8 and 4.8, 2048
+// with few 4.6 and 5.4).
 constexpr int JOIN_WAVES = 512;
-constexpr int COMMIT_BLOCKS = 4096;       // K and V of few rows: fewer channels a block, until there are so many blocks
+// K and V of few rows: fewer channels a block, until there are so many blocks (five rows of 4096 channels in 32 layers: 6.6 us, with
+// one block for all channels 14.0; 500 rows of 1024 channels in 32 layers: 21.6 us, up to 16 384 blocks 23.4).
+constexpr int COMMIT_BLOCKS = 4096;
 
-// Bytes of a request's logits up to which one block reads them and walks, in one launch (125 KB: a call 8.6 us and 6.5 on the GPU,
-// in two launches 11.7 and 4.5 + 3.4; 250 KB: 9.2 and 9.3, in two 12.1 and 4.0 + 3.5, and by itself a call is 3 us slower).
+// Bytes of a request's logits up to which one block reads them and walks, in one launch (125 KB: a call 9.6 us and 6.1 on the GPU,
+// in two launches 12.4 and 3.3 + 1.6; 250 KB: 9.6 and 8.9, in two 12.3 and 3.3 + 1.7, so a caller who waits loses; 500 KB: 15.1, in two 12.2).
 constexpr int64_t ACCEPT_SMALL = 128 << 10;
 
 constexpr int BEST_ROWS = 1 << 23;        // of a launch: its threads are counted in 32 bits

@@ -22,7 +22,7 @@ inline size_t plan_lds(int R) { return ((size_t)4 * R + 1) * 4; }
 // its share of table rows and of slots, so that nothing waits for another block and nothing but the inputs is read: a new entry
 // of the table is taken from the ring again by the rows that lie in it.  Blocks for table rows and blocks for slots follow each
 // other in the grid.  What bounds it is the chain of loads (lengths, then the ring or the table), not bytes: 3.4 us for 8
-// requests, 7.0 us for 700 requests and 93 289 rows (7.8 us where a block does rows and then slots, 8.7 us with blocks of 256
+// requests, 7.2 us for 700 requests and 93 289 rows (7.8 us where a block does rows and then slots, 8.7 us with blocks of 256
 // threads, whose threads have three requests each).
 __global__ __launch_bounds__(PLAN_THREADS) void k_kv_plan(
     int32_t *table, int max_pages, int32_t *ring, int pages, int page_bits, const int32_t *pool, const int32_t *lens,
@@ -235,7 +235,7 @@ __device__ __forceinline__ int best_vectors(const W *row, int V)
 }
 
 // Part blockIdx.y of row blockIdx.x: `per` vectors.  Bound by reading: 439 MB of bf16 logits in 76 us, 5.8 TB/s (90.7 us, by
-// arithmetic, with an order and an index for every element); 8 rows of 32 000 in 3.2 us, by the latency of one load and the launch.
+// arithmetic, with an order and an index for every element); 8 rows of 32 000 in 3.4 us, by the latency of one load and the launch.
 template <typename W>
 __global__ __launch_bounds__(BEST_THREADS) void k_logits_best(const W *logits, int64_t stride, int V, int per, uint64_t *parts)
 {
@@ -283,7 +283,7 @@ __device__ __forceinline__ void walk_down(const TreeWalk &A, int r, int a, int n
 __device__ __forceinline__ int best_index(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
 
 // One wave a request: the rows' answers from their parts, then down the tree; the last block has the padding.  Bound by the latency
-// of two loads after each other: 1.6 us for one tree of 8, 4.2 us for 32 trees and 10 parts a row.
+// of two loads after each other: 2.1 us for one tree of 8, 5.1 us for 32 trees and 10 parts a row.
 __global__ __launch_bounds__(64) void k_tree_walk(const uint64_t *parts, int n_parts, TreeWalk A)
 {
     const int r = blockIdx.x, lane = threadIdx.x;
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(64) void k_tree_walk(const uint64_t *parts, int n_p
 
 // Both in one launch, where a request's logits are few: a block has all rows of a request, as many of its waves as there are for
 // a row, and blocks R on have the padding, max_nodes rows each (T <= R max_nodes).  Bound by the latency of a block that reads by
-// itself: 8 rows of 8000 in 6.5 us, where the two launches take 4.5 + 3.4 and the host 3 us more; 500 KB a block take 15 us.
+// itself: 8 rows of 8000 in 6.1 us, where the two launches take 3.3 + 1.6 and the host 3 us more; 500 KB a block take 15 us.
 constexpr int SMALL_THREADS = 1024, SMALL_WAVES = SMALL_THREADS / 64;
 template <typename W>
 __global__ __launch_bounds__(SMALL_THREADS) void k_tree_accept(const W *logits, int64_t stride, int V, TreeWalk A)
@@ -369,9 +369,9 @@ constexpr int COMMIT_CHANNELS = 256;        // the least a block has of them, un
 // rows in a row fill such a pack (prompts), they are read together and written as whole packs, by the row of the pack's first
 // token; other rows (branches of a tree) write their elements one by one.  A lane has two channels of V, so that the packs of a
 // wave lie side by side.  Bound by reading and writing: a prompt's 618 MB (half read, half written) in 112 us, 5.5 TB/s (144 us
-// with eight channels a lane, packs 128 bytes apart); a branch of a tree of 8, in 32 layers, in 3.9 us, by latency, with its
-// channels over many blocks (6.5 us with one block for all of them and for K and V); branches of 723 rows in 12 layers, 8.8 MB,
-// in 6.3 us.
+// with eight channels a lane, packs 128 bytes apart); a branch of a tree of 8, in 32 layers, in 4.0 us, by latency, with its
+// channels over many blocks (five rows of a branch 6.6 us, with one block for all channels 14.0); branches of 723 rows in 12 layers, 8.8 MB,
+// in 6.4 us.
 template <typename W>
 __global__ __launch_bounds__(COMMIT_THREADS) void k_kv_commit(W *K, W *V, const W *k, int64_t k_layer, int64_t k_row,
                                                               const W *v, int64_t v_layer, int64_t v_row,

@@ -16,9 +16,9 @@
 // has of a (request, head, row tile) goes to the output where it is the whole of it, and otherwise, as a sum with its maximum, to
 // the workspace, where k_tree_join puts the parts together.
 //
-// What bounds it: reading K and V.  24 requests of 3000 tokens, one row a head, bf16, 128 channels: 1180 MB in 197 us, 6.0 TB/s;
-// a ragged batch of 592 MB in 105 us; 32 rows over 30 000 tokens, 123 MB, in 25.6 us, of which some 5 go by before and behind the
-// reading.  One row over 780 tokens, 12.8 MB, takes 7.2 us, the latency of five loads after each other (lengths, page, K and V, parts).
+// What bounds it: reading K and V.  24 requests of 3000 tokens, one row a head, bf16, 128 channels: 1180 MB in 199 us, 5.9 TB/s;
+// a ragged batch of 592 MB in 106 us; 32 rows over 30 000 tokens, 123 MB, in 26.0 us, of which some 5 go by before and behind the
+// reading.  One row over 780 tokens, 12.8 MB, takes 7.6 us, the latency of five loads after each other (lengths, page, K and V, parts).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -445,9 +445,9 @@ constexpr int ta_waves(int element, int dim, int nt)
 {
     return nt * (dim / 4 + dim * element / 16) + 2 * dim * element / 8 <= 200 ? 2 : 1;
 }
-// One block a compute unit, so that there are few parts to join (32 rows over 30 000 tokens: 25.4 + 5.1 us; with 512 blocks
-// 25.9 + 6.6).  Two where the registers have room and the parts are small: their starts and ends overlap (a ragged batch
-// of eight requests, 592 MB: 105 us; with 256 blocks 110).
+// One block a compute unit, so that there are few parts to join (32 rows over 30 000 tokens: 25.9 + 4.2 us; with 512 blocks
+// 25.9 + 4.8).  Two where the registers have room and the parts are small: their starts and ends overlap (a ragged batch
+// of eight requests, 590 MB: 108.5 us; with 256 blocks 112).
 template <typename W, int DIM, int NT>
 using NarrowCut = TreeCut<16 * NT, TA_WAVES, NT == 1 && ta_waves(sizeof(W), DIM, NT) == 2 ? 9 : 8, false>;
 
@@ -732,7 +732,7 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
 
 // The parts of a row and head, where there are more than one: a wave each (SHARED false), or a block each, whose eight waves take
 // parts in turn (few rows with many parts).  Bound by latency, of the lengths and then of the parts, which other XCDs have written:
-// 2.9 us at the least; 4.2 us for 256 rows and heads with 32 parts each; 5740 rows and heads of wide blocks, 34 MB, in 8.8 us.
+// 2.8 us at the least; 4.0 us for 256 rows and heads with 32 parts each; 5740 rows and heads of wide blocks, 34 MB, in 8.7 us.
 template <bool SHARED>
 constexpr int tj_waves() { return SHARED ? 8 : 4; }
 template <typename W, int DIM, typename Cut, bool SHARED>

@@ -7,12 +7,14 @@
 // 16 (i / 8) + 8 f + i % 8, by the choice of K rows), which are the tokens that O^T += V^T P^T wants of that lane.
 // LDS: K rows of DIM channels, 16-byte chunk c of token i at slot c ^ swizzle(i), so that the tokens of an operand read lie in different
 // banks; V as in memory, of which 32 lanes read consecutive 512 bytes.
-// What bounds it: a tile of 32 tokens is 792 cycles of a SIMD's matrix unit for each of its two waves (the weights' two terms have a
-// product with V each), and about 700 of its vector unit (16 exponentials and some 110 other instructions), side by side; what a
-// stage costs besides (its barrier, addresses, the first read of K) is why a stage is as large as LDS allows.  Trees of 64 with seven
-// query heads a head over 20 000 to 32 768 tokens, 88 GFLOP without the second terms: a call 165 to 175 us, with weights of one term 130.
-// Some 14 us are not stages: 2 for the lengths, 3 for the first pages, Q and K and V, and a part of 133 KB that every block writes
-// and that leaves the caches at the end.  A call of one stage takes 10 us.
+// What bounds it: a tile of 32 tokens is 768 cycles of a SIMD's matrix unit for each of its two waves (the weights' two terms have a
+// product with V each) and about as many of its vector unit (16 exponentials, two terms, some 110 other instructions).  A wave's products and
+// its weights follow each other, so that the two waves of a SIMD run side by side only in part: by the counters the matrix unit is
+// busy 46 % of the time and the vector unit 48; the reads of LDS take 15 %, without bank conflicts.  Trees of 64 with seven query heads
+// a head over 27 000 to 32 768 tokens, 88 GFLOP without the second terms: 163 us (with weights of one term 127: 39 % and 41 %).  What a
+// stage costs besides (its barrier, addresses, the first read of K) is why a stage is as large as LDS allows, and some 14 us are
+// not stages: 2 for the lengths, 3 for the first pages, Q and K and V, and a part of 133 KB that every block writes and that leaves the
+// caches at the end.  A call of one stage of 64 rows takes 12 us.
 #pragma once
 
 #include "svdp_tree_attn.h"
