@@ -41,8 +41,15 @@ def lookup(history: Sequence[int], nodes: int, branches: int = 3) -> Tree:
     return tokens, parents
 
 
+def _look_over(tree: Tree, vocabulary: float = float("inf")) -> None:
+    tokens, parents = tree
+    if len(tokens) != len(parents) or any(not -1 <= p < j for j, p in enumerate(parents)) or any(not 0 <= t < vocabulary for t in tokens):
+        raise ValueError("a tree has tokens of the vocabulary and a parent for each, in front of it or -1")
+
+
 def cut(tree: Tree, levels: int) -> Tree:
     """The first ``levels`` levels of a drafted tree."""
+    _look_over(tree)
     tokens, parents, depth, place = [], [], {-1: 0}, {-1: -1}
     for j, (t, p) in enumerate(zip(*tree)):
         depth[j] = depth[p] + 1
@@ -95,8 +102,7 @@ class Decoder:
         """Device tensors of one step's rows from (tokens, parents) of each request, roots among them (parent -1)."""
         tokens, masks, depth, starts = [], [], [], [0]
         for toks, parents in trees:
-            if len(toks) != len(parents) or any(not 0 <= t < self.embed.shape[0] for t in toks) or any(not -1 <= p < j for j, p in enumerate(parents)):
-                raise ValueError("a tree's tokens have to be of the vocabulary, its parents in front of their children")
+            _look_over((toks, parents), self.embed.shape[0])
             first = len(tokens)
             for j, p in enumerate(parents):
                 masks.append((masks[first + p] if p >= 0 else 0) | 1 << j)

@@ -197,3 +197,11 @@ def test_trees_are_looked_over_before_the_device_has_them(tree):
     assert tokens.tolist() == good[0] and starts.tolist() == [0, 3, 3] and masks.tolist() == [1, 3, 5] and places.tolist() == [0, 1, 1] and most == 3
     with pytest.raises(ValueError, match="vocabulary"):
         decoder._rows([good, tree])
+
+
+@pytest.mark.parametrize("tree", [([1, 2], [-1]), ([1], [-1, 0]), ([1, 2], [-1, 1]), ([1, 2], [1, -1]), ([1, 2], [-1, -2])])
+def test_a_tree_that_is_none_is_not_cut(tree):
+    from paper_2603_14110_amd.draft import cut
+
+    with pytest.raises(ValueError, match="a tree"):
+        cut(tree, 5)
