@@ -58,7 +58,9 @@ typedef enum {
 
 typedef enum {
     SVDP_F32 = 0,  /* IEEE binary32 */
-    SVDP_BF16 = 1  /* bfloat16 bit patterns (upper 16 bits of a binary32) */
+    SVDP_BF16 = 1, /* bfloat16 bit patterns (upper 16 bits of a binary32) */
+    SVDP_E4M3 = 8  /* 8 bits, caches of K and V only: 1 sign, 4 exponent bits (bias 7), 3 bits of mantissa, no
+                      infinities, all ones NaN; times a power of two (see svdp_kv_cache)   */
 } svdp_dtype;
 
 /* Flags of svdp_layer.flags */
@@ -298,13 +300,15 @@ svdp_status svdp_ffn_step_glued(const svdp_layer *layer, const void *x_prev, con
 #define SVDP_MAX_REQUESTS 4096
 #define SVDP_MAX_ROWS (1 << 24)
 
-/* K and V of the cached tokens, all layers.  With e = 16 bytes / element size, V holds e tokens of a channel side by
+/* K and V of the cached tokens, all layers.  With e = 16 bytes / element size (8 in 8 bits too), V holds e tokens of a channel side by
  * side: what a lane of the matrix cores multiplies the weights of e tokens with is then one 16-byte load.        */
 typedef struct svdp_kv_cache {
     int32_t layers, pages, page, heads, dim;
-    int32_t dtype;         /* svdp_dtype of K and V, and of q, k, v and out           */
+    int32_t dtype;         /* svdp_dtype of K and V, and of q, k, v and out (SVDP_E4M3: those are bf16) */
     void *K;               /* [layers][pages][heads][page][dim], 16-byte aligned      */
     void *V;               /* [layers][pages][heads][page / e][dim][e], 16-byte aligned */
+    uint8_t *K_scale;      /* SVDP_E4M3 only, else not looked at: [layers][pages][heads][page], 16-byte aligned: each token's   */
+    uint8_t *V_scale;      /* head of K and of V is its codes times 2^(scale - 127), scale from 1 to 254                       */
 } svdp_kv_cache;
 
 /* Attention of every row over its request's cached tokens 0 .. lens[r] and over the nodes that it sees:
@@ -361,10 +365,59 @@ svdp_status svdp_kv_plan(int32_t *table, int32_t max_pages, int32_t *ring, int32
 
 /* K and V of new tokens into their slots, all layers: k, v: device, row t of layer l is [heads][dim] at
  * l * layer_stride + t * row_stride elements (whole 16-byte vectors, pointers 16-byte aligned).  slots: device [T]; a
- * slot outside [0, pages * page) is skipped, no two rows may have the same one.                                       */
+ * slot outside [0, pages * page) is skipped, no two rows may have the same one.  Rows are of the cache's type.
+ * SVDP_E4M3: rows are bf16.  Each token's head gets the least power of two 2^b, b >= -96, at which none of its elements is above
+ * 448 2^b, and its elements are divided by it and rounded to e4m3 (to the nearest, ties to even).  Infinities and NaN become NaN, and do
+ * not count for the power.                                                                                          */
 svdp_status svdp_kv_commit(const svdp_kv_cache *cache, const void *k, int64_t k_layer_stride, int64_t k_row_stride,
                            const void *v, int64_t v_layer_stride, int64_t v_row_stride, const int64_t *slots, int32_t T,
                            void *stream);
+
+/* The other way: row t of k and v, all layers, becomes K and V of slot slots[t]; zeros where that lies outside [0, pages * page).
+ * Strides and types as above (SVDP_E4M3: bf16, exact unless it is below bf16's range).  The same slot may be read
+ * by several rows; rows must not overlap each other or anything else.                                                */
+svdp_status svdp_kv_read(const svdp_kv_cache *cache, const int64_t *slots, int32_t T, void *k, int64_t k_layer_stride,
+                         int64_t k_row_stride, void *v, int64_t v_layer_stride, int64_t v_row_stride, void *stream);
+
+/* ---- around attention and logits ---- */
+
+/* Norms of the heads of q and k, and their rotation by the rows' positions:
+ *   y = x / sqrt(mean(x^2) + eps) * weight (SVDP_ROPE_NORM; weight NULL: 1),  then for i < rot / 2
+ *   (y_a, y_b) -> (y_a cos - y_b sin, y_b cos + y_a sin),  angle = places[t] * inv_freq[i],
+ * (a, b) = (i, rot / 2 + i), or (2 i, 2 i + 1) with SVDP_ROPE_INTERLEAVED; channels from rot on are not turned.
+ * q: device rows of [heads_q][dim], q_stride elements apart, k: of [heads][dim] (heads may be 0: no k), in `dtype`, SVDP_F32 or
+ * SVDP_BF16; q_out and k_out likewise.  In place (q_out = q with the same stride, k_out = k likewise) is fine; otherwise they
+ * overlap nothing.  Pointers 16-byte aligned, strides whole 16-byte vectors.  places: device [T] int32; inv_freq: device [rot / 2]
+ * fp32 (both may be NULL if rot is 0).  q_weight, k_weight: device [dim] fp32, with SVDP_ROPE_WEIGHT_EACH [heads][dim], 16-byte
+ * aligned, NULL for none.  dim 64, 128 or 256; rot a multiple of 8, up to dim.  Angles are taken in 64 bits, so that far positions lose
+ * nothing; all else is fp32, rounded once.                                                                          */
+enum { SVDP_ROPE_INTERLEAVED = 1u, SVDP_ROPE_NORM = 2u, SVDP_ROPE_WEIGHT_EACH = 4u };
+svdp_status svdp_qk_rope(int32_t dtype, int32_t dim, int32_t T, const void *q, int64_t q_stride, int32_t heads_q, const void *k,
+                         int64_t k_stride, int32_t heads, const int32_t *places, const float *inv_freq, int32_t rot, uint32_t flags,
+                         const float *q_weight, const float *k_weight, float eps, void *q_out, int64_t q_out_stride, void *k_out,
+                         int64_t k_out_stride, void *stream);
+
+/* A token for each row of logits, drawn with given random numbers.  logits: device rows of [V] in `dtype`, `stride` elements apart (aligned
+ * to their elements), V <= SVDP_MAX_VOCABULARY.  A row's tokens stand in order, largest logit first, lowest index first among
+ * equals, with weights w = 2^44 exp((x - x_first) / temperature) rounded to whole numbers.  Kept are the first tokens of the order: no more
+ * than top_k (0 or less: all); the fewest whose weight is at least top_p of the weight of those (1 or more, NaN: all);
+ * those with w >= min_p 2^44 (0 or less, NaN: all); always the first one.  Drawn is the first one at which the sum of
+ * the weights, in order, exceeds u times the kept tokens' sum: u in [0, 1), what lies outside counts as its nearest end.
+ * temperature 0 or less, or NaN: the first token.  A largest logit of +inf or NaN (NaN is above all): the lowest index that has
+ * it.  All logits -inf: -1.  Sums are whole numbers and exact, so that nothing depends on how the work is divided.
+ * u, temperature, top_p, min_p: device [T] fp32; top_k: device [T] int32; all but u may be NULL (1, all, all, all).
+ * answers [T] int32.  logp [T] fp32, nullable: logarithm of the drawn token's share of the kept weight (0 for a first token that is not
+ * drawn, -inf with -1).  ws: >= svdp_sample_workspace_bytes() (0 for arguments it does not take).                    */
+#define SVDP_MAX_VOCABULARY (1 << 19)
+size_t svdp_sample_workspace_bytes(int32_t T, int32_t V, int32_t dtype);
+svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32_t V, const float *u, const float *temperature,
+                        const int32_t *top_k, const float *top_p, const float *min_p, int32_t T, int32_t *answers, float *logp,
+                        void *ws, size_t ws_bytes, void *stream);
+
+/* The branch of each tree that agrees with given answers (drawn ones, e.g.): keep, counts and next as svdp_tree_accept forms them from its
+ * `best`, here answers [T] int32.  An answer of -1 agrees with no token from 0 on.                                  */
+svdp_status svdp_tree_walk(const int32_t *answers, const int32_t *tokens, const uint64_t *tree, const int32_t *starts, int32_t R,
+                           int32_t T, int32_t max_nodes, int32_t *keep, int32_t *counts, int32_t *next, void *stream);
 
 /* Static string for a status code.  Never NULL. */
 const char *svdp_status_string(svdp_status st);

@@ -17,12 +17,14 @@ import torch  # imported before the library so both share one HIP runtime
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsvdp.so")
 
-SVDP_F32, SVDP_BF16 = 0, 1
+SVDP_F32, SVDP_BF16, SVDP_E4M3 = 0, 1, 8
 FLAG_DRELU, FLAG_REVALIDATE, FLAG_ENGINE_VECTOR, FLAG_ENGINE_MATRIX = 1, 2, 4, 8
 MAX_BATCH = 8
 STATIC_SCRATCH_BYTES = 8 << 20
 MAX_NODES = 64
 MAX_REQUESTS = 4096
+MAX_VOCABULARY = 1 << 19
+ROPE_INTERLEAVED, ROPE_NORM, ROPE_WEIGHT_EACH = 1, 2, 4
 
 EXPORTS = [
     "svdp_workspace_bytes", "svdp_predict", "svdp_compact", "svdp_sparse_ffn", "svdp_dense_ffn",
@@ -31,7 +33,7 @@ EXPORTS = [
     "svdp_calib_stats_workspace_bytes", "svdp_calib_stats", "svdp_ffn_step_glued",
     "svdp_whiten_workspace_bytes", "svdp_whiten_factors",
     "svdp_tree_attn_workspace_bytes", "svdp_tree_attn", "svdp_tree_accept_workspace_bytes", "svdp_tree_accept",
-    "svdp_kv_plan", "svdp_kv_commit",
+    "svdp_kv_plan", "svdp_kv_commit", "svdp_kv_read", "svdp_qk_rope", "svdp_sample_workspace_bytes", "svdp_sample", "svdp_tree_walk",
 ]
 
 
@@ -52,6 +54,7 @@ class svdp_kv_cache(ctypes.Structure):
     _fields_ = [
         ("layers", ctypes.c_int32), ("pages", ctypes.c_int32), ("page", ctypes.c_int32), ("heads", ctypes.c_int32),
         ("dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p),
+        ("K_scale", ctypes.c_void_p), ("V_scale", ctypes.c_void_p),
     ]
 
 
@@ -118,6 +121,17 @@ def lib() -> ctypes.CDLL:
     L.svdp_kv_plan.restype = ctypes.c_int
     L.svdp_kv_commit.argtypes = [cp, vp, i64, i64, vp, i64, i64, vp, i32, vp]
     L.svdp_kv_commit.restype = ctypes.c_int
+    L.svdp_kv_read.argtypes = [cp, vp, i32, vp, i64, i64, vp, i64, i64, vp]
+    L.svdp_kv_read.restype = ctypes.c_int
+    L.svdp_qk_rope.argtypes = [i32, i32, i32, vp, i64, i32, vp, i64, i32, vp, vp, i32, ctypes.c_uint32, vp, vp, ctypes.c_float, vp, i64,
+                               vp, i64, vp]
+    L.svdp_qk_rope.restype = ctypes.c_int
+    L.svdp_sample_workspace_bytes.argtypes = [i32, i32, i32]
+    L.svdp_sample_workspace_bytes.restype = sz
+    L.svdp_sample.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    L.svdp_sample.restype = ctypes.c_int
+    L.svdp_tree_walk.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]
+    L.svdp_tree_walk.restype = ctypes.c_int
     _lib = L
     return L
 
@@ -390,31 +404,46 @@ def whiten_factors(W_gate: torch.Tensor, X: torch.Tensor, r: int):
 # ---- decoding with drafted tokens -----------------------------------------------------------------------------------
 
 
+_CACHE_TYPES = {torch.float32: SVDP_F32, torch.bfloat16: SVDP_BF16, torch.float8_e4m3fn: SVDP_E4M3}
+
+
 class KVCache:
     """K and V of the cached tokens of every layer, in pages: owns the tensors and the C struct that points at them.
 
-    K [layers][pages][heads][page][dim]; V [layers][pages][heads][page / e][dim][e], e = 8 (bfloat16) or 4 (float32)
-    tokens of a channel side by side."""
+    K [layers][pages][heads][page][dim]; V [layers][pages][heads][page / e][dim][e], e = 8 (bfloat16, float8_e4m3fn) or 4 (float32)
+    tokens of a channel side by side.  In 8 bits rows (q, k, v and outputs) are bfloat16, and each token's head of K and of V stands for its
+    elements times a power of two: K_scale, V_scale [layers][pages][heads][page] of float8_e8m0fnu."""
 
-    def __init__(self, K: torch.Tensor, V: torch.Tensor):
-        if K.dtype not in (torch.float32, torch.bfloat16) or V.dtype != K.dtype:
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, K_scale: Optional[torch.Tensor] = None, V_scale: Optional[torch.Tensor] = None):
+        if K.dtype not in _CACHE_TYPES or V.dtype != K.dtype:
             raise SvdpError(f"unsupported cache dtypes {K.dtype}, {V.dtype}")
         if K.dim() != 5 or not all(t.is_cuda and t.is_contiguous() for t in (K, V)):
             raise SvdpError("K, V: expected contiguous device tensors, K of five dimensions")
         self.layers, self.pages, self.heads, self.page, self.dim = K.shape
-        e = 16 // K.element_size()
+        coded = K.dtype == torch.float8_e4m3fn
+        e = 8 if coded else 16 // K.element_size()
         if tuple(V.shape) != (self.layers, self.pages, self.heads, self.page // e, self.dim, e):
             raise SvdpError(f"V: shape {tuple(V.shape)} does not go with K's {tuple(K.shape)}")
-        self.K, self.V, self.dtype = K, V, K.dtype
+        for t in (K_scale, V_scale):
+            if (t is not None) != coded:
+                raise SvdpError("K_scale, V_scale: both with a cache of float8_e4m3fn, none otherwise")
+            if coded and (t.dtype != torch.float8_e8m0fnu or t.shape != K.shape[:4] or not t.is_cuda or not t.is_contiguous()):
+                raise SvdpError(f"K_scale, V_scale: expected contiguous device tensors {tuple(K.shape[:4])} of float8_e8m0fnu, got {tuple(t.shape)} {t.dtype}")
+        if any(t is not None and t.device != K.device for t in (V, K_scale, V_scale)):
+            raise SvdpError("K, V and their scales: expected on one device")
+        self.K, self.V, self.K_scale, self.V_scale, self.dtype = K, V, K_scale, V_scale, K.dtype
+        self.rows = torch.bfloat16 if coded else K.dtype          # the type of q, k, v and outputs
         self._sizes = {}          # workspace bytes of the sizes asked for
-        self.c = svdp_kv_cache(self.layers, self.pages, self.page, self.heads, self.dim,
-                               SVDP_BF16 if K.dtype == torch.bfloat16 else SVDP_F32, K.data_ptr(), V.data_ptr())
+        self.c = svdp_kv_cache(self.layers, self.pages, self.page, self.heads, self.dim, _CACHE_TYPES[K.dtype], K.data_ptr(), V.data_ptr(),
+                               _ptr(K_scale), _ptr(V_scale))
 
     @classmethod
     def empty(cls, layers: int, pages: int, page: int, heads: int, dim: int, dtype=torch.bfloat16, device="cuda") -> "KVCache":
-        e = 16 // torch.empty(0, dtype=dtype).element_size()
+        coded = dtype == torch.float8_e4m3fn
+        e = 8 if coded else 16 // torch.empty(0, dtype=dtype).element_size()
+        scales = [torch.empty((layers, pages, heads, page), dtype=torch.float8_e8m0fnu, device=device) for _ in range(2 if coded else 0)]
         return cls(torch.empty((layers, pages, heads, page, dim), dtype=dtype, device=device),
-                   torch.empty((layers, pages, heads, page // e, dim, e), dtype=dtype, device=device))
+                   torch.empty((layers, pages, heads, page // e, dim, e), dtype=dtype, device=device), *scales)
 
 
 def _typed(t: Optional[torch.Tensor], dtype, what: str, shape=None) -> Optional[int]:
@@ -431,8 +460,8 @@ def _heads_rows(t: torch.Tensor, cache: KVCache, heads: int, what: str) -> int:
     """Stride of the rows [heads][dim] of q, k or v (a slice of a wider projection is fine)."""
     rows, _, dim = shape = t.shape
     row, head, one = t.stride()
-    if t.dtype != cache.dtype or not t.is_cuda or dim != cache.dim or shape[1] != heads:
-        raise SvdpError(f"{what}: expected [rows][{heads}][{cache.dim}] of {cache.dtype} on the device, got {tuple(shape)} {t.dtype}")
+    if t.dtype != cache.rows or not t.is_cuda or dim != cache.dim or shape[1] != heads:
+        raise SvdpError(f"{what}: expected [rows][{heads}][{cache.dim}] of {cache.rows} on the device, got {tuple(shape)} {t.dtype}")
     if rows and (one != 1 or (head != dim and heads > 1)):
         raise SvdpError(f"{what}: the heads of a row have to lie side by side")
     # one row: its stride says nothing
@@ -477,7 +506,7 @@ def tree_attn(cache: KVCache, layer: int, q: torch.Tensor, k: torch.Tensor, v: t
         out = torch.empty_like(q)           # dense, as the heads of a row lie side by side
         out_at = out.data_ptr()
     else:
-        out_at = _typed(out, cache.dtype, "out", (T, heads_q, dim))
+        out_at = _typed(out, cache.rows, "out", (T, heads_q, dim))
     if want_lse and lse is None:
         lse = torch.empty(T, heads_q, dtype=torch.float32, device=q.device)
         lse_at = lse.data_ptr()
@@ -555,9 +584,9 @@ def kv_plan(table: torch.Tensor, ring: torch.Tensor, pool: torch.Tensor, lens: t
     return slots, lens_out, pool_out, refused
 
 
-def kv_commit(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
-    """K and V of new rows, k, v [layers][T][heads][dim], into the cache at slots [T] (int64; negative: not stored)."""
-    T, layers, heads, dim, dtype = slots.numel(), cache.layers, cache.heads, cache.dim, cache.dtype
+def _kv_rows(cache: KVCache, T: int, k: torch.Tensor, v: torch.Tensor) -> list:
+    """Addresses and strides of rows k, v [layers][T][heads][dim]."""
+    layers, heads, dim, dtype = cache.layers, cache.heads, cache.dim, cache.rows
     shape, args = (layers, T, heads, dim), []
     for t in (k, v):
         if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
@@ -567,7 +596,138 @@ def kv_commit(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Ten
             raise SvdpError(f"{'v' if t is v else 'k'}: the heads of a row have to lie side by side")
         # a dimension of one entry: its stride says nothing
         args += (t.data_ptr(), layer if layers > 1 else 0, row if T > 1 else heads * dim)
+    return args
+
+
+def kv_commit(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """K and V of new rows, k, v [layers][T][heads][dim], into the cache at slots [T] (int64; negative: not stored).  A cache in 8 bits
+    takes bfloat16 rows and rounds them (see include/svdp.h)."""
+    T = slots.numel()
+    args = _kv_rows(cache, T, k, v)
     _check(lib().svdp_kv_commit(ctypes.byref(cache.c), *args, _typed(slots, torch.int64, "slots"), T, _stream()), "svdp_kv_commit")
+
+
+def kv_read(cache: KVCache, slots: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
+    """K and V of slots [T] (int64; zeros for one outside the cache) as rows k, v [layers][T][heads][dim], of every layer: what kv_commit
+    stored, in the cache's type (8 bits: bfloat16).  Returns (k, v)."""
+    T, shape = slots.numel(), (cache.layers, slots.numel(), cache.heads, cache.dim)
+    k = torch.empty(shape, dtype=cache.rows, device=slots.device) if k is None else k
+    v = torch.empty(shape, dtype=cache.rows, device=slots.device) if v is None else v
+    args = _kv_rows(cache, T, k, v)
+    _check(lib().svdp_kv_read(ctypes.byref(cache.c), _typed(slots, torch.int64, "slots"), T, *args, _stream()), "svdp_kv_read")
+    return k, v
+
+
+# ---- around attention and logits ------------------------------------------------------------------------------------
+
+
+def _head_stride(t: torch.Tensor, what: str) -> int:
+    """Stride of rows [T][heads][dim] whose heads lie side by side."""
+    if t.dim() != 3 or not t.is_cuda:
+        raise SvdpError(f"{what}: expected rows [T][heads][dim] on the device, got {tuple(t.shape)}")
+    T, heads, dim = t.shape
+    row, head, one = t.stride()
+    if T and (one != 1 or (heads > 1 and head != dim)):
+        raise SvdpError(f"{what}: the heads of a row have to lie side by side")
+    return row if T > 1 else heads * dim
+
+
+def qk_rope(q: torch.Tensor, k: torch.Tensor, places: torch.Tensor, inv_freq: torch.Tensor, q_weight: Optional[torch.Tensor] = None,
+            k_weight: Optional[torch.Tensor] = None, eps: Optional[float] = None, interleaved: bool = False,
+            q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """Norms of the heads of queries and keys (with eps; None: no norm) and their rotation by the rows' positions, in one pass.
+
+    q [T][heads_q][dim], k [T][heads][dim] of float32 or bfloat16 (rows may be slices of a wider projection); places [T] int32, inv_freq
+    [rot / 2] float32: the first rot channels are turned, pairs (i, rot / 2 + i), interleaved: (2 i, 2 i + 1).  q_weight, k_weight:
+    float32, [dim] for all heads, or both [heads][dim].  q_out = q and k_out = k work in place.  Returns (q_out, k_out)."""
+    qs, ks = _head_stride(q, "q"), _head_stride(k, "k")
+    T, heads_q, dim = q.shape
+    heads = k.shape[1]
+    if q.dtype not in (torch.float32, torch.bfloat16) or k.dtype is not q.dtype or k.shape[0] != T or k.shape[2] != dim:
+        raise SvdpError(f"svdp_qk_rope: q {tuple(q.shape)} {q.dtype} and k {tuple(k.shape)} {k.dtype} do not go together, or are of another type")
+    flags, weights = ROPE_INTERLEAVED if interleaved else 0, []
+    if eps is not None:
+        flags |= ROPE_NORM
+    elif q_weight is not None or k_weight is not None:
+        raise SvdpError("svdp_qk_rope: weights without a norm (eps)")
+    each = [w.dim() == 2 for w in (q_weight, k_weight) if w is not None]
+    if any(each):
+        if not all(each):
+            raise SvdpError("svdp_qk_rope: q_weight and k_weight have to be both [dim] or both [heads][dim]")
+        flags |= ROPE_WEIGHT_EACH
+    for w, n, what in ((q_weight, heads_q, "q_weight"), (k_weight, heads, "k_weight")):
+        weights.append(_typed(w, torch.float32, what, (n, dim) if flags & ROPE_WEIGHT_EACH else (dim,)))
+    if q_out is None:
+        q_out = torch.empty((T, heads_q, dim), dtype=q.dtype, device=q.device)
+        qo = heads_q * dim
+    else:
+        qo = _head_stride(q_out, "q_out")
+    if k_out is None:
+        k_out = torch.empty((T, heads, dim), dtype=q.dtype, device=q.device)
+        ko = heads * dim
+    else:
+        ko = _head_stride(k_out, "k_out")
+    if q_out.shape != q.shape or k_out.shape != k.shape or q_out.dtype is not q.dtype or k_out.dtype is not q.dtype:
+        raise SvdpError("svdp_qk_rope: q_out, k_out: expected the shapes and the type of q and k")
+    _check(lib().svdp_qk_rope(
+        SVDP_BF16 if q.dtype is torch.bfloat16 else SVDP_F32, dim, T, q.data_ptr(), qs, heads_q, k.data_ptr(), ks, heads,
+        _typed(places, torch.int32, "places", (T,)), _typed(inv_freq, torch.float32, "inv_freq"), 2 * inv_freq.numel(), flags, *weights,
+        0.0 if eps is None else eps, q_out.data_ptr(), qo, k_out.data_ptr(), ko, _stream()), "svdp_qk_rope")
+    return q_out, k_out
+
+
+@functools.lru_cache(maxsize=256)
+def sample_workspace_bytes(T: int, V: int, dtype: int) -> int:
+    n = int(lib().svdp_sample_workspace_bytes(T, V, dtype))
+    if n == 0:
+        raise SvdpError(f"svdp_sample: unsupported sizes T={T} V={V}")
+    return n
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, want_logp: bool = False,
+           ws: Optional[torch.Tensor] = None):
+    """A token for each row of logits [T][V] (rows may be strided; float32 or bfloat16) from random numbers u [T] in [0, 1).
+
+    temperature, top_p, min_p [T] float32 and top_k [T] int32, one entry a row (None: 1, all, all, all); temperature 0: the
+    first token.  The rules are in include/svdp.h.  Returns answers [T] int32 (and with want_logp the logarithms of their shares [T] float32)."""
+    if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or not logits.is_cuda or logits.stride(1) != 1:
+        raise SvdpError(f"logits: expected [T][V] of float32 or bfloat16 on the device, got {tuple(logits.shape)} {logits.dtype}")
+    T, V = logits.shape
+    dt, f32, rows = SVDP_BF16 if logits.dtype is torch.bfloat16 else SVDP_F32, torch.float32, (T,)
+    ws = torch.empty(sample_workspace_bytes(T, V, dt), dtype=torch.uint8, device=logits.device) if ws is None else ws
+    answers = torch.empty(T, dtype=torch.int32, device=logits.device)
+    logp = torch.empty(T, dtype=f32, device=logits.device) if want_logp else None
+    _check(lib().svdp_sample(
+        logits.data_ptr(), logits.stride(0) if T > 1 else V, dt, V, _typed(u, f32, "u", rows), _typed(temperature, f32, "temperature", rows),
+        _typed(top_k, torch.int32, "top_k", rows), _typed(top_p, f32, "top_p", rows), _typed(min_p, f32, "min_p", rows), T, answers.data_ptr(),
+        _ptr(logp), ws.data_ptr(), ws.numel(), _stream()), "svdp_sample")
+    return (answers, logp) if want_logp else answers
+
+
+def tree_walk(answers: torch.Tensor, tokens: torch.Tensor, starts: torch.Tensor, tree: Optional[torch.Tensor] = None,
+              max_nodes: Optional[int] = None):
+    """The branch of each drafted tree that agrees with given answers [T] (int32): tree_accept without its logits.
+    Returns (keep [T], counts [R], next [R]), all int32."""
+    T, R = answers.numel(), starts.numel() - 1
+    max_nodes = max(1, min(T, MAX_NODES)) if max_nodes is None else int(max_nodes)
+    keep, counts, following = torch.empty(T + 2 * max(R, 0), dtype=torch.int32, device=answers.device).split_with_sizes((T, max(R, 0), max(R, 0)))
+    i32 = torch.int32
+    _check(lib().svdp_tree_walk(_typed(answers, i32, "answers", (T,)), _typed(tokens, i32, "tokens", (T,)), _typed(tree, torch.int64, "tree", (T,)),
+                                _typed(starts, i32, "starts"), R, T, max_nodes, keep.data_ptr(), counts.data_ptr(), following.data_ptr(),
+                                _stream()), "svdp_tree_walk")
+    return keep, counts, following
+
+
+def tree_sample(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor, starts: torch.Tensor, tree: Optional[torch.Tensor] = None,
+                max_nodes: Optional[int] = None, want_logp: bool = False, **how):
+    """Acceptance of drafted tokens by drawn answers: sample() for every row (``how``: its temperature, top_k, top_p, min_p), then the
+    branch that agrees with them.  What is kept and what follows has the distribution of tokens drawn one after the other.
+    Returns (keep [T], counts [R], next [R], answers [T]) as tree_accept does (and logp [T] with want_logp)."""
+    got = sample(logits, u, want_logp=want_logp, **how)
+    answers = got[0] if want_logp else got
+    keep, counts, following = tree_walk(answers, tokens, starts, tree=tree, max_nodes=max_nodes)
+    return (keep, counts, following, answers) + ((got[1],) if want_logp else ())
 
 
 def version() -> str:

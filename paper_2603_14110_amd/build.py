@@ -9,8 +9,9 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "svdp.hip")
 DRAFT_SRC = os.path.join(HERE, "csrc", "svdp_draft.hip")
+SERVE_SRC = os.path.join(HERE, "csrc", "svdp_serve.hip")
 # every file the translation units include, and this one with the compiler's options: the library is rebuilt when any of them is newer
-DEPS = [os.path.abspath(__file__), SRC, DRAFT_SRC, os.path.join(os.path.dirname(HERE), "include", "svdp.h")] + sorted(glob.glob(os.path.join(HERE, "csrc", "*.h")))
+DEPS = [os.path.abspath(__file__), SRC, DRAFT_SRC, SERVE_SRC, os.path.join(os.path.dirname(HERE), "include", "svdp.h")] + sorted(glob.glob(os.path.join(HERE, "csrc", "*.h")))
 LIB = os.path.join(HERE, "libsvdp.so")
 # a matrix product that the device refused must not go unnoticed ([[nodiscard]])
 WARNINGS = ["-Wall", "-Wno-unused-function", "-Werror=unused-result"]
@@ -39,7 +40,7 @@ def build_lib(force: bool = True, verbose: bool = False) -> str:
     """Compile the C-ABI library.  Packed-fp32 instructions are disabled on purpose."""
     if not force and os.path.exists(LIB) and all(os.path.getmtime(LIB) >= os.path.getmtime(p) for p in DEPS):
         return LIB
-    _hipcc([SRC, DRAFT_SRC], LIB, verbose)
+    _hipcc([SRC, DRAFT_SRC, SERVE_SRC], LIB, verbose)
     return LIB
 
 

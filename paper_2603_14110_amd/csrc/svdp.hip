@@ -864,6 +864,6 @@ svdp_status svdp_whiten_factors(const void *W_gate, const void *X, int32_t d, in
     return whiten_impl<bf16>(W_gate, X, d, D, T, r, P, Q, sigma, sweeps, w, st);
 }
 
-const char *svdp_version(void) { return "0.6"; }
+const char *svdp_version(void) { return "0.7"; }
 
 }  // extern "C"

@@ -15,6 +15,22 @@ struct bf16 {
     uint16_t bits;
 };
 
+// e4m3 storage element: four bits of exponent, three behind the leading one, no infinities.  A cache of K and V in 8 bits holds these,
+// each token of a head with a power of two of its own that its elements are multiplied by, kept as a biased exponent (one byte).
+struct e4m3 {
+    uint8_t bits;
+};
+__device__ __forceinline__ float power_of(uint32_t biased) { return __uint_as_float(biased << 23); }
+// The type of rows (q, k, v, outputs) that goes with a storage type of the cache.
+template <typename W>
+struct RowOf {
+    using type = W;
+};
+template <>
+struct RowOf<e4m3> {
+    using type = bf16;
+};
+
 template <typename W>
 struct Elem;
 template <>
@@ -132,6 +148,15 @@ __device__ __forceinline__ float dot_raw(const uint4 &w, const uint4 &x, float a
     return acc;
 }
 
+// Eight e4m3 elements times a power of two as bf16: exact, as three bits behind the leading one fit into seven.
+__device__ __forceinline__ uint4 widen_e4m3(uint32_t a, uint32_t b, float by)
+{
+    return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, by, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, by, true)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, by, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, by, true)));
+}
+
 template <int CTRL>
 __device__ __forceinline__ float dpp_move(float v)
 {
@@ -197,6 +222,29 @@ __device__ __forceinline__ float group_sum(float v)
     if (LOG2 >= 4) v += dpp_move<0x140>(v);
     if (LOG2 >= 5) v = add_xor16(v);
     if (LOG2 >= 6) v = add_xor32(v);
+    return v;
+}
+
+// The largest value over aligned groups of 2^LOG2 consecutive lanes, in every lane of the group.
+__device__ __forceinline__ float max_xor16(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_xor32(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <int LOG2>
+__device__ __forceinline__ float group_max(float v)
+{
+    if (LOG2 >= 1) v = fmaxf(v, dpp_move<0xB1>(v));
+    if (LOG2 >= 2) v = fmaxf(v, dpp_move<0x4E>(v));
+    if (LOG2 >= 3) v = fmaxf(v, dpp_move<0x141>(v));
+    if (LOG2 >= 4) v = fmaxf(v, dpp_move<0x140>(v));
+    if (LOG2 >= 5) v = max_xor16(v);
+    if (LOG2 >= 6) v = max_xor32(v);
     return v;
 }
 

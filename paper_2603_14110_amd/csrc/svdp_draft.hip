@@ -6,6 +6,7 @@
 
 #include "svdp_draft_kernels.h"
 #include "svdp_host.h"
+#include "svdp_kv8.h"
 #include "svdp_tree_attn.h"
 #include "svdp_tree_wide.h"
 
@@ -30,7 +31,15 @@ auto on_type(int dt, F &&f)
     return dt == SVDP_F32 ? f(Type<float>{}) : f(Type<bf16>{});
 }
 
-inline int bytes_of(int dt) { return dt == SVDP_F32 ? 4 : 2; }
+// of the cache: its own types, or codes with powers of two
+template <typename F>
+auto on_cache_type(int dt, F &&f)
+{
+    return dt == SVDP_E4M3 ? f(Type<e4m3>{}) : on_type(dt, f);
+}
+
+inline int row_type(int dt) { return dt == SVDP_E4M3 ? SVDP_BF16 : dt; }             // of q, k, v and out
+inline int bytes_of(int dt) { return dt == SVDP_F32 ? 4 : dt == SVDP_BF16 ? 2 : 1; }
 inline bool aligned_to(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 inline bool whole_vectors(int64_t stride, int dt) { return stride % (16 / bytes_of(dt)) == 0; }
 inline bool good_page(int page) { return page == 32 || page == 64 || page == 128 || page == 256; }
@@ -46,7 +55,7 @@ bool overlap(const void *a, size_t an, const void *b, size_t bn)
 svdp_status check_cache(const svdp_kv_cache *c)
 {
     if (c == nullptr || c->layers < 1 || c->pages < 1 || c->heads < 1) return SVDP_ERR_INVALID_ARG;
-    if (c->dtype != SVDP_F32 && c->dtype != SVDP_BF16) return SVDP_ERR_UNSUPPORTED;
+    if (c->dtype != SVDP_F32 && c->dtype != SVDP_BF16 && c->dtype != SVDP_E4M3) return SVDP_ERR_UNSUPPORTED;
     if (!good_page(c->page) || (c->dim != 64 && c->dim != 128 && c->dim != 256)) return SVDP_ERR_UNSUPPORTED;
     if ((int64_t)c->pages * c->page >= INT_LIMIT || c->heads > 65535 || c->layers > 65535) return SVDP_ERR_UNSUPPORTED;
     return SVDP_OK;
@@ -54,6 +63,7 @@ svdp_status check_cache(const svdp_kv_cache *c)
 svdp_status check_cache_memory(const svdp_kv_cache *c)
 {
     if (!c->K || !c->V || !aligned16(c->K) || !aligned16(c->V)) return SVDP_ERR_INVALID_ARG;
+    if (c->dtype == SVDP_E4M3 && (!c->K_scale || !c->V_scale || !aligned16(c->K_scale) || !aligned16(c->V_scale))) return SVDP_ERR_INVALID_ARG;
     return SVDP_OK;
 }
 svdp_status check_requests(int R, int T, int max_nodes)
@@ -96,7 +106,7 @@ void on_kernel(const AttnPlan &p, int dt, int dim, F &&f)
         constexpr int DIM = decltype(dc)::value;
         if constexpr (DIM <= 128)
             if (p.wide) return f(Type<bf16>{}, dc, WideCut<DIM>{});
-        on_type(dt, [&](auto wt) {
+        on_cache_type(dt, [&](auto wt) {
             using W = typename decltype(wt)::type;
             if constexpr (DIM <= 128)
                 if (p.nt == 2) return f(wt, dc, NarrowCut<W, DIM, 2>{});
@@ -142,6 +152,32 @@ constexpr int JOIN_WAVES = 512;
 // K and V of few rows: fewer channels a block, until there are so many blocks (five rows of 4096 channels in 32 layers: 6.6 us, with
 // one block for all channels 14.0; 500 rows of 1024 channels in 32 layers: 21.6 us, up to 16 384 blocks 23.4).
 constexpr int COMMIT_BLOCKS = 4096;
+constexpr int KV_BLOCKS = 4096;
+
+// Rows of K and V, as a commit reads and a read writes them.
+svdp_status check_rows(const svdp_kv_cache *c, const int64_t *slots, int T, const void *k, int64_t k_layer, int64_t k_row, const void *v, int64_t v_layer,
+                       int64_t v_row)
+{
+    if (T < 0) return SVDP_ERR_INVALID_ARG;
+    if (T > SVDP_MAX_ROWS) return SVDP_ERR_UNSUPPORTED;
+    if (T == 0) return SVDP_OK;
+    const int rt = row_type(c->dtype);
+    const int64_t row = (int64_t)c->heads * c->dim;
+    if (!k || !v || !slots || !aligned16(k) || !aligned16(v) || !aligned_to(slots, 8) || k_row < row || v_row < row || k_layer < 0 || v_layer < 0 ||
+        !whole_vectors(k_row, rt) || !whole_vectors(v_row, rt) || !whole_vectors(k_layer, rt) || !whole_vectors(v_layer, rt))
+        return SVDP_ERR_INVALID_ARG;
+    return SVDP_OK;
+}
+KvArgs kv_args(const svdp_kv_cache *c, const int64_t *slots, int T, const void *k, int64_t k_layer, int64_t k_row, const void *v, int64_t v_layer,
+               int64_t v_row)
+{
+    // heads of a block: fewer, until there are so many blocks
+    int each = c->heads;
+    while (each > 1 && (int64_t)tiles(T, KV_ROWS) * c->layers * 2 * tiles(c->heads, each) < KV_BLOCKS) each = (each + 1) / 2;
+    return {c->K, c->V, c->K_scale, c->V_scale, const_cast<void *>(k), const_cast<void *>(v), k_layer, k_row, v_layer, v_row, slots, T, c->pages,
+            bits_of(c->page), c->heads, each};
+}
+dim3 kv_grid(const svdp_kv_cache *c, const KvArgs &A) { return dim3(tiles(A.T, KV_ROWS), c->layers, 2 * tiles(A.heads, A.heads_each)); }
 
 // Bytes of a request's logits up to which one block reads them and walks, in one launch (125 KB: a call 9.6 us and 6.1 on the GPU,
 // in two launches 12.4 and 3.3 + 1.6; 250 KB: 9.6 and 8.9, in two 12.3 and 3.3 + 1.7, so a caller who waits loses; 500 KB: 15.1, in two 12.2).
@@ -183,7 +219,7 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     if (st == SVDP_OK) st = check_requests(R, T, max_nodes);
     if (st == SVDP_OK) st = check_table(R, max_pages, cache->page);
     if (st != SVDP_OK) return st;
-    const int dt = cache->dtype, dim = cache->dim;
+    const int dt = cache->dtype, rt = row_type(dt), dim = cache->dim;
     if (layer < 0 || layer >= cache->layers || heads_q < 1 || heads_q % cache->heads != 0 || !std::isfinite(scale * LOG2E))
         return SVDP_ERR_INVALID_ARG;
     if ((int64_t)T * heads_q >= 1 << 26) return SVDP_ERR_UNSUPPORTED;        // a wave each in the join: threads of a grid
@@ -193,8 +229,8 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
         !aligned_to(tree, 8) || !aligned_to(lse, 4))
         return SVDP_ERR_INVALID_ARG;
     if (q_stride < (int64_t)heads_q * dim || k_stride < (int64_t)cache->heads * dim ||
-        v_stride < (int64_t)cache->heads * dim || !whole_vectors(q_stride, dt) || !whole_vectors(k_stride, dt) ||
-        !whole_vectors(v_stride, dt))
+        v_stride < (int64_t)cache->heads * dim || !whole_vectors(q_stride, rt) || !whole_vectors(k_stride, rt) ||
+        !whole_vectors(v_stride, rt))
         return SVDP_ERR_INVALID_ARG;
     const AttnPlan plan = attn_plan(cache, heads_q, R, max_pages, max_nodes);
     if (plan.steps * plan.tasks >= INT_LIMIT) return SVDP_ERR_UNSUPPORTED;
@@ -204,6 +240,10 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
     TreeAttnArgs A{};
     A.K = static_cast<const char *>(cache->K) + layer * layer_bytes;
     A.V = static_cast<const char *>(cache->V) + layer * layer_bytes;
+    if (dt == SVDP_E4M3) {
+        A.K_scale = cache->K_scale + layer * (layer_bytes / dim);
+        A.V_scale = cache->V_scale + layer * (layer_bytes / dim);
+    }
     A.q = q;
     A.k = k;
     A.v = v;
@@ -334,22 +374,36 @@ svdp_status svdp_kv_plan(int32_t *table, int32_t max_pages, int32_t *ring, int32
     return hip_status(hipSuccess);
 }
 
+svdp_status svdp_tree_walk(const int32_t *answers, const int32_t *tokens, const uint64_t *tree, const int32_t *starts, int32_t R, int32_t T,
+                           int32_t max_nodes, int32_t *keep, int32_t *counts, int32_t *next, void *stream)
+{
+    svdp_status st = check_requests(R, T, max_nodes);
+    if (st != SVDP_OK) return st;
+    if (!starts || !counts || !next || !aligned_to(starts, 4) || !aligned_to(counts, 4) || !aligned_to(next, 4)) return SVDP_ERR_INVALID_ARG;
+    if (T > 0 && (!answers || !tokens || !keep || !aligned_to(answers, 4) || !aligned_to(tokens, 4) || !aligned_to(tree, 8) || !aligned_to(keep, 4)))
+        return SVDP_ERR_INVALID_ARG;
+    const TreeWalk A{tokens, tree, starts, keep, counts, next, const_cast<int32_t *>(answers), R, T, max_nodes};
+    launch(k_tree_walk_given, dim3(R + 1), dim3(64), 0, static_cast<hipStream_t>(stream), A);
+    return hip_status(hipSuccess);
+}
+
 svdp_status svdp_kv_commit(const svdp_kv_cache *cache, const void *k, int64_t k_layer_stride, int64_t k_row_stride,
                            const void *v, int64_t v_layer_stride, int64_t v_row_stride, const int64_t *slots, int32_t T,
                            void *stream)
 {
     svdp_status st = check_cache(cache);
     if (st == SVDP_OK) st = check_cache_memory(cache);
-    if (st != SVDP_OK) return st;
-    if (T < 0) return SVDP_ERR_INVALID_ARG;
-    if (T > SVDP_MAX_ROWS) return SVDP_ERR_UNSUPPORTED;
-    if (T == 0) return SVDP_OK;
+    if (st == SVDP_OK) st = check_rows(cache, slots, T, k, k_layer_stride, k_row_stride, v, v_layer_stride, v_row_stride);
+    if (st != SVDP_OK || T == 0) return st;
     const int dt = cache->dtype;
+    if (dt == SVDP_E4M3) {
+        const KvArgs A = kv_args(cache, slots, T, k, k_layer_stride, k_row_stride, v, v_layer_stride, v_row_stride);
+        on_dim(cache->dim, [&](auto dc) {
+            launch(k_kv_commit8<decltype(dc)::value>, kv_grid(cache, A), dim3(KV_THREADS), 0, static_cast<hipStream_t>(stream), A);
+        });
+        return hip_status(hipSuccess);
+    }
     const int64_t row = (int64_t)cache->heads * cache->dim;
-    if (!k || !v || !slots || !aligned16(k) || !aligned16(v) || !aligned_to(slots, 8) || k_row_stride < row ||
-        v_row_stride < row || k_layer_stride < 0 || v_layer_stride < 0 || !whole_vectors(k_row_stride, dt) ||
-        !whole_vectors(v_row_stride, dt) || !whole_vectors(k_layer_stride, dt) || !whole_vectors(v_layer_stride, dt))
-        return SVDP_ERR_INVALID_ARG;
     const int groups = tiles(T, COMMIT_ROWS);
     int channels = (int)row;
     while (channels > COMMIT_CHANNELS && tiles(row, channels) < COMMIT_BLOCKS / (2 * (int64_t)groups * cache->layers))
@@ -362,6 +416,22 @@ svdp_status svdp_kv_commit(const svdp_kv_cache *cache, const void *k, int64_t k_
                v_row_stride, slots, T, cache->pages, bits_of(cache->page), cache->heads, bits_of(cache->dim), channels);
         return hip_status(hipSuccess);
     });
+}
+
+svdp_status svdp_kv_read(const svdp_kv_cache *cache, const int64_t *slots, int32_t T, void *k, int64_t k_layer_stride, int64_t k_row_stride, void *v,
+                         int64_t v_layer_stride, int64_t v_row_stride, void *stream)
+{
+    svdp_status st = check_cache(cache);
+    if (st == SVDP_OK) st = check_cache_memory(cache);
+    if (st == SVDP_OK) st = check_rows(cache, slots, T, k, k_layer_stride, k_row_stride, v, v_layer_stride, v_row_stride);
+    if (st != SVDP_OK || T == 0) return st;
+    const KvArgs A = kv_args(cache, slots, T, k, k_layer_stride, k_row_stride, v, v_layer_stride, v_row_stride);
+    on_cache_type(cache->dtype, [&](auto wt) {
+        on_dim(cache->dim, [&](auto dc) {
+            launch((k_kv_read<typename decltype(wt)::type, decltype(dc)::value>), kv_grid(cache, A), dim3(KV_THREADS), 0, static_cast<hipStream_t>(stream), A);
+        });
+    });
+    return hip_status(hipSuccess);
 }
 
 }  // extern "C"

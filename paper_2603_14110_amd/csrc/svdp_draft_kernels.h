@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "svdp_device.h"
+#include "svdp_order.h"
 
 namespace svdp {
 
@@ -152,26 +153,6 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_kv_plan(
 
 constexpr int BEST_THREADS = 256;
 
-// A word that grows with the value: NaN above all, -0 equal to 0; and one that then falls with the index.
-__device__ __forceinline__ uint32_t best_order(float v)
-{
-    const uint32_t u = __float_as_uint(v + 0.f);
-    return (u & 0x7fffffffu) > 0x7f800000u ? 0xffffffffu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
-}
-__device__ __forceinline__ uint64_t best_key(float v, uint32_t index)
-{
-    return ((uint64_t)best_order(v) << 32) | (0xffffffffu - index);
-}
-__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v)
-{
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) {
-        const uint64_t o = __shfl_xor((unsigned long long)v, m);
-        v = o > v ? o : v;
-    }
-    return v;
-}
-
 // The largest logit of a row's vectors [begin, end), of those that a lane takes (at, at + step, ...).  Vectors are counted from the
 // aligned address at or before the row, whatever its own alignment.  A lane keeps its best vector by the largest of its values, a few
 // operations for a vector, and looks for the place in it once, at the end.
@@ -280,7 +261,6 @@ __device__ __forceinline__ void walk_down(const TreeWalk &A, int r, int a, int n
         A.next[r] = count > 0 ? following : -1;
     }
 }
-__device__ __forceinline__ int best_index(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
 
 // One wave a request: the rows' answers from their parts, then down the tree; the last block has the padding.  Bound by the latency
 // of two loads after each other: 2.1 us for one tree of 8, 5.1 us for 32 trees and 10 parts a row.
@@ -314,6 +294,24 @@ __global__ __launch_bounds__(64) void k_tree_walk(const uint64_t *parts, int n_p
         A.best[t] = answer(t);
         A.keep[t] = -1;
     }
+}
+
+// The same way down for answers that are given, e.g. drawn: one wave a request, the last block has the padding.  Bound by the latency of
+// two loads after each other.
+__global__ __launch_bounds__(64) void k_tree_walk_given(TreeWalk A)
+{
+    const int r = blockIdx.x, lane = threadIdx.x;
+    const int a = min(max(A.starts[r], 0), A.T), b = r < A.R ? min(max(A.starts[r + 1], a), A.T) : A.T;
+    const int n = r < A.R ? min(b - a, A.max_nodes) : 0;
+    int mine = -1, token = -2;
+    uint64_t sees = 0;
+    if (lane < n) {
+        sees = A.tree != nullptr ? A.tree[a + lane] : ~0ull;
+        token = A.tokens[a + lane];
+        mine = A.best[a + lane];
+    }
+    if (r < A.R) walk_down(A, r, a, n, lane, token, sees, mine);
+    for (int t = a + n + lane; t < b; t += 64) A.keep[t] = -1;
 }
 
 // Both in one launch, where a request's logits are few: a block has all rows of a request, as many of its waves as there are for

@@ -1,0 +1,120 @@
+// C-ABI entry points of a decode step around attention and logits (see include/svdp.h): norms and rotation of heads, tokens from
+// logits.  Host-side validation and kernel launches; no allocation, no synchronisation, no state kept between calls.
+#include "../../include/svdp.h"
+
+#include <hip/hip_runtime.h>
+
+#include "svdp_host.h"
+#include "svdp_rope.h"
+#include "svdp_sample.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace {
+
+using namespace svdp;
+
+inline int bytes_of(int dt) { return dt == SVDP_F32 ? 4 : 2; }
+inline bool aligned_to(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+template <typename W, int DIM>
+void launch_rope(const RopeArgs &A, bool inter, bool norm, dim3 grid, hipStream_t hs)
+{
+    const auto with = [&](auto i, auto n) { launch((k_qk_rope<W, DIM, decltype(i)::value, decltype(n)::value>), grid, dim3(ROPE_THREADS), 0, hs, A); };
+    if (inter) norm ? with(std::true_type{}, std::true_type{}) : with(std::true_type{}, std::false_type{});
+    else norm ? with(std::false_type{}, std::true_type{}) : with(std::false_type{}, std::false_type{});
+}
+
+}  // namespace
+
+extern "C" {
+
+svdp_status svdp_qk_rope(int32_t dtype, int32_t dim, int32_t T, const void *q, int64_t q_stride, int32_t heads_q, const void *k, int64_t k_stride,
+                         int32_t heads, const int32_t *places, const float *inv_freq, int32_t rot, uint32_t flags, const float *q_weight,
+                         const float *k_weight, float eps, void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride, void *stream)
+{
+    if (T < 0 || heads_q < 1 || heads < 0 || rot < 0 || rot > dim) return SVDP_ERR_INVALID_ARG;
+    if ((flags & ~(uint32_t)(SVDP_ROPE_INTERLEAVED | SVDP_ROPE_NORM | SVDP_ROPE_WEIGHT_EACH)) != 0) return SVDP_ERR_INVALID_ARG;
+    if (dtype != SVDP_F32 && dtype != SVDP_BF16) return SVDP_ERR_UNSUPPORTED;
+    if ((dim != 64 && dim != 128 && dim != 256) || rot % 8 != 0 || heads_q > 65535 || heads > 65535 || T > SVDP_MAX_ROWS) return SVDP_ERR_UNSUPPORTED;
+    const bool norm = flags & SVDP_ROPE_NORM;
+    if (norm ? !(eps >= 0.f) || !std::isfinite(eps) : q_weight != nullptr || k_weight != nullptr || (flags & SVDP_ROPE_WEIGHT_EACH)) return SVDP_ERR_INVALID_ARG;
+    if (T == 0) return SVDP_OK;
+    const int vec = 16 / bytes_of(dtype);
+    const auto rows_ok = [&](const void *p, int64_t stride, int n) {
+        return p != nullptr && aligned16(p) && stride >= (int64_t)n * dim && stride % vec == 0 && stride < (int64_t)1 << 40;
+    };
+    if (!rows_ok(q, q_stride, heads_q) || !rows_ok(q_out, q_out_stride, heads_q)) return SVDP_ERR_INVALID_ARG;
+    if (heads > 0 && (!rows_ok(k, k_stride, heads) || !rows_ok(k_out, k_out_stride, heads))) return SVDP_ERR_INVALID_ARG;
+    if ((q == q_out && q_stride != q_out_stride) || (heads > 0 && k == k_out && k_stride != k_out_stride)) return SVDP_ERR_INVALID_ARG;
+    if ((rot > 0 && (!places || !inv_freq)) || !aligned_to(places, 4) || !aligned_to(inv_freq, 4) || !aligned16(q_weight) || !aligned16(k_weight))
+        return SVDP_ERR_INVALID_ARG;
+    RopeArgs A{};
+    A.q = q;
+    A.k = k;
+    A.q_out = q_out;
+    A.k_out = k_out;
+    A.q_stride = q_stride;
+    A.k_stride = k_stride;
+    A.q_out_stride = q_out_stride;
+    A.k_out_stride = k_out_stride;
+    A.places = places;
+    A.inv_freq = inv_freq;
+    A.q_weight = q_weight;
+    A.k_weight = k_weight;
+    A.T = T;
+    A.heads_q = heads_q;
+    A.heads = heads;
+    A.half = rot / 2;
+    A.q_each = A.k_each = flags & SVDP_ROPE_WEIGHT_EACH ? dim : 0;
+    A.eps = eps;
+    const int per = 512 / dim, rounds = (heads_q + heads + per - 1) / per;
+    A.each = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, (int64_t)T * rounds / 16384));
+    const int64_t waves = (int64_t)T * ((rounds + A.each - 1) / A.each), blocks = (waves + ROPE_WAVES - 1) / ROPE_WAVES;
+    if (blocks * ROPE_THREADS >= (int64_t)1 << 32) return SVDP_ERR_UNSUPPORTED;
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    const auto of = [&](auto dc) {
+        constexpr int DIM = decltype(dc)::value;
+        if (dtype == SVDP_F32) launch_rope<float, DIM>(A, flags & SVDP_ROPE_INTERLEAVED, norm, dim3((uint32_t)blocks), hs);
+        else launch_rope<bf16, DIM>(A, flags & SVDP_ROPE_INTERLEAVED, norm, dim3((uint32_t)blocks), hs);
+    };
+    if (dim == 64) of(std::integral_constant<int, 64>{});
+    else if (dim == 128) of(std::integral_constant<int, 128>{});
+    else of(std::integral_constant<int, 256>{});
+    return hip_status(hipSuccess);
+}
+
+size_t svdp_sample_workspace_bytes(int32_t T, int32_t V, int32_t dtype)
+{
+    if (T < 0 || T > SVDP_MAX_ROWS || V < 1 || V > SVDP_MAX_VOCABULARY || (dtype != SVDP_F32 && dtype != SVDP_BF16)) return 0;
+    return ALIGN;
+}
+
+svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32_t V, const float *u, const float *temperature, const int32_t *top_k,
+                        const float *top_p, const float *min_p, int32_t T, int32_t *answers, float *logp, void *ws, size_t ws_bytes, void *stream)
+{
+    static_assert(SAMPLE_MAX_V == SVDP_MAX_VOCABULARY);
+    if (T < 0 || V < 1 || stride < V) return SVDP_ERR_INVALID_ARG;
+    if (dtype != SVDP_F32 && dtype != SVDP_BF16) return SVDP_ERR_UNSUPPORTED;
+    if (T > SVDP_MAX_ROWS || V > SVDP_MAX_VOCABULARY) return SVDP_ERR_UNSUPPORTED;
+    if (T == 0) return SVDP_OK;
+    if (!logits || !u || !answers || !aligned_to(logits, bytes_of(dtype)) || !aligned_to(u, 4) || !aligned_to(temperature, 4) || !aligned_to(top_k, 4) ||
+        !aligned_to(top_p, 4) || !aligned_to(min_p, 4) || !aligned_to(answers, 4) || !aligned_to(logp, 4))
+        return SVDP_ERR_INVALID_ARG;
+    if (ws == nullptr || !aligned_to(ws, ALIGN) || ws_bytes < svdp_sample_workspace_bytes(T, V, dtype)) return SVDP_ERR_WORKSPACE;
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    constexpr int ROWS = 1 << 21;            // of a launch: its threads are counted in 32 bits
+    static_assert((int64_t)ROWS * SAMPLE_THREADS < (int64_t)1 << 32);
+    for (int t = 0; t < T; t += ROWS) {
+        const auto from = [&](auto *p) { return p != nullptr ? p + t : p; };
+        const SampleArgs A{static_cast<const char *>(logits) + (int64_t)t * stride * bytes_of(dtype), stride, from(u), from(temperature), from(top_k),
+                           from(top_p), from(min_p), from(answers), from(logp), V};
+        const dim3 grid(std::min(T - t, ROWS));
+        if (dtype == SVDP_F32) launch(k_sample<float>, grid, dim3(SAMPLE_THREADS), 0, hs, A);
+        else launch(k_sample<bf16>, grid, dim3(SAMPLE_THREADS), 0, hs, A);
+    }
+    return hip_status(hipSuccess);
+}
+
+}  // extern "C"

@@ -50,6 +50,7 @@ struct TreeJoinArgs {
 static_assert(sizeof(TreeJoinArgs) == 64, "as many as are loaded ahead");
 struct TreeAttnArgs : TreeJoinArgs {
     const void *K, *V;                  // of the layer
+    const uint8_t *K_scale, *V_scale;   // of a cache in 8 bits
     const void *q, *k, *v;
     int64_t q_stride, k_stride, v_stride;
     const uint64_t *tree;
@@ -185,8 +186,12 @@ struct TreeTile;
 
 template <int DIM>
 struct TreeTile<bf16, DIM> {
+    using Row = bf16;
+    static constexpr bool CODED = false;
     static constexpr uint32_t SIGNS = 0x80008000u;
     static constexpr int E = 8, KC = DIM / 32, VT = 1;
+    static __device__ __forceinline__ int channel(int c, int g) { return (4 * c + g) * E; }      // first of E, of Q and K, in product c
+    static __device__ __forceinline__ int v_channel(int dt, int m) { return 16 * dt + m; }       // of V, in product dt
     static __device__ __forceinline__ int key(int t, int m) { return (m >> 2) * 8 + (m & 3) + 4 * t; }
     static __device__ __forceinline__ int pack(int, int g) { return g; }          // of 8 tokens
     static __device__ __forceinline__ f32x4_t score(const uint4 &k, const uint4 &q, f32x4_t s)
@@ -242,8 +247,12 @@ struct TreeTile<bf16, DIM> {
 
 template <int DIM>
 struct TreeTile<float, DIM> {
+    using Row = float;
+    static constexpr bool CODED = false;
     static constexpr uint32_t SIGNS = 0x80000000u;
     static constexpr int E = 4, KC = DIM / 16, VT = 2;
+    static __device__ __forceinline__ int channel(int c, int g) { return (4 * c + g) * E; }
+    static __device__ __forceinline__ int v_channel(int dt, int m) { return 16 * dt + m; }
     static __device__ __forceinline__ int key(int t, int m) { return 16 * t + m; }
     static __device__ __forceinline__ int pack(int t, int g) { return 4 * t + g; } // of 4 tokens
     static __device__ __forceinline__ f32x4_t score(const uint4 &k, const uint4 &q, f32x4_t s)
@@ -293,16 +302,26 @@ struct TreeTile<float, DIM> {
     }
 };
 
-__device__ __forceinline__ float max_xor16(float v)
-{
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float max_xor32(float v)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
+// A cache in 8 bits: its elements become bf16 operands in registers, K's with the token's power of two (exact), V's without
+// (its eight tokens have one each: it goes to their weights).  A lane's 16 bytes are the operands of two products, so that the channels
+// that a product takes are others than in 16 bits.
+template <int DIM>
+struct TreeTile<e4m3, DIM> : TreeTile<bf16, DIM> {
+    static constexpr bool CODED = true;
+    static __device__ __forceinline__ int channel(int c, int g) { return (c >> 1) * 64 + g * 16 + (c & 1) * 8; }
+    static __device__ __forceinline__ int v_channel(int dt, int m) { return (dt >> 1) * 32 + 2 * m + (dt & 1); }
+    static __device__ __forceinline__ uint4 operand(const uint4 &raw, int half, float by)
+    {
+        return half == 0 ? widen_e4m3(raw.x, raw.y, by) : widen_e4m3(raw.z, raw.w, by);
+    }
+    // the first n of 8 tokens of two channels, zeros behind them
+    static __device__ __forceinline__ uint4 first_coded(const uint4 &v, int n)
+    {
+        const uint32_t a = n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1, b = n >= 8 ? ~0u : n <= 4 ? 0u : (1u << (8 * (n - 4))) - 1;
+        return make_uint4(v.x & a, v.y & b, v.z & a, v.w & b);
+    }
+};
+
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 // Scores are taken relative to a `shift` that follows their maximum, in base two: it moves only where a score exceeds it by more than
 // SLACK (then to the maximum), so that the sums are rarely brought down to a new one.  A weight is then below 2^SLACK, far from any
@@ -353,9 +372,9 @@ struct TreeWave {
     // the maximum that others compare theirs with: -inf for a row that has not seen anything
     __device__ __forceinline__ float top(int nt) const { return limit[nt] == -INFINITY ? -INFINITY : shift[nt]; }
 
-    // Scores in base two, relative to the shift -> weights.
-    template <int N>
-    __device__ __forceinline__ void weights(float (&z)[NT][8 * N], Weights (&w)[NT][N])
+    // Scores in base two, relative to the shift -> weights, each as by(i, weight) of the lane's token i for the product with V.
+    template <int N, typename By>
+    __device__ __forceinline__ void weights(float (&z)[NT][8 * N], Weights (&w)[NT][N], By &&by)
     {
         float top[NT];
         bool grew = false;
@@ -390,8 +409,15 @@ struct TreeWave {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) e[i] = exp2_fast(z[nt][8 * n + i]);
                 total[nt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = by(8 * n + i, e[i]);
                 w[nt][n] = X::pack_weights(e);
             }
+    }
+    template <int N>
+    __device__ __forceinline__ void weights(float (&z)[NT][8 * N], Weights (&w)[NT][N])
+    {
+        weights<N>(z, w, [](int, float e) { return e; });
     }
     // One V operand (16 channels) against the weights of all rows.
     template <int N>
@@ -449,12 +475,15 @@ constexpr int ta_waves(int element, int dim, int nt)
 // 25.9 + 4.8).  Two where the registers have room and the parts are small: their starts and ends overlap (a ragged batch
 // of eight requests, 590 MB: 108.5 us; with 256 blocks 112).
 template <typename W, int DIM, int NT>
-using NarrowCut = TreeCut<16 * NT, TA_WAVES, NT == 1 && ta_waves(sizeof(W), DIM, NT) == 2 ? 9 : 8, false>;
+constexpr int ta_waves_of() { return ta_waves(sizeof(typename RowOf<W>::type), DIM, NT); }
+template <typename W, int DIM, int NT>
+using NarrowCut = TreeCut<16 * NT, TA_WAVES, NT == 1 && ta_waves_of<W, DIM, NT>() == 2 ? 9 : 8, false>;
 
 template <typename W, int DIM, int NT>
-__global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tree_attn(TreeAttnArgs A)
+__global__ __launch_bounds__(TA_THREADS, (ta_waves_of<W, DIM, NT>())) void k_tree_attn(TreeAttnArgs A)
 {
     using X = TreeTile<W, DIM>;
+    using Row = typename X::Row;
     using Cut = NarrowCut<W, DIM, NT>;
     constexpr int ROWS = Cut::ROWS, E = X::E, KC = X::KC, VT = X::VT, DT = DIM / 16;
     constexpr int DC = DIM * NT <= 128 ? DIM : 128 / NT;       // channels that the waves' sums meet in LDS by: 32 KB
@@ -490,9 +519,9 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int row = min(row0 + 16 * nt + m, rows - 1), node = row / A.group, head = h * A.group + row - node * A.group;
-                const W *from = static_cast<const W *>(A.q) + (S.start + node) * A.q_stride + (int64_t)head * DIM + g * E;
+                const Row *from = static_cast<const Row *>(A.q) + (S.start + node) * A.q_stride + (int64_t)head * DIM;
 #pragma unroll
-                for (int c = 0; c < KC; ++c) q[c][nt] = load_raw(from + c * 4 * E);
+                for (int c = 0; c < KC; ++c) q[c][nt] = load_raw(from + X::channel(c, g));
             }
 
             // cached tokens: K of the next tile is requested when this one's has been used, and so is V
@@ -530,20 +559,27 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
             if (i >= i_end) {
                 scale_q();
             } else {
-                uint4 k[2][KC], v[DT][VT];
+                // what a lane holds of a tile: operands, or in 8 bits what they are made of
+                constexpr int KR = X::CODED ? KC / 2 : KC, VR = X::CODED ? DT / 2 : DT;
+                uint4 k[2][KR], v[VR][VT];
+                uint32_t k_by[2];
+                uint64_t v_by;
                 const auto load_k = [&](int64_t at) {
                     const W *from = static_cast<const W *>(A.K) + at;
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
+                    for (int t = 0; t < 2; ++t) {
 #pragma unroll
-                        for (int c = 0; c < KC; ++c) k[t][c] = load_raw(from + X::key(t, m) * DIM + (4 * c + g) * E);
+                        for (int c = 0; c < KR; ++c) k[t][c] = load_raw(from + X::key(t, m) * DIM + X::channel(X::CODED ? 2 * c : c, g));
+                        if constexpr (X::CODED) k_by[t] = A.K_scale[at / DIM + X::key(t, m)];
+                    }
                 };
                 const auto load_v = [&](int64_t at) {
                     const W *from = static_cast<const W *>(A.V) + at;
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt)
+                    for (int dt = 0; dt < VR; ++dt)
 #pragma unroll
-                        for (int t = 0; t < VT; ++t) v[dt][t] = load_raw(from + (X::pack(t, g) * DIM + dt * 16 + m) * E);
+                        for (int t = 0; t < VT; ++t) v[dt][t] = load_raw(from + (X::pack(t, g) * DIM + X::v_channel(X::CODED ? 2 * dt : dt, m)) * E);
+                    if constexpr (X::CODED) v_by = *reinterpret_cast<const uint64_t *>(A.V_scale + at / DIM + 8 * g);
                 };
                 id = page_of(i);
                 id_next = page_of(i + TA_WAVES);
@@ -556,22 +592,51 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
                     id_next = page_of(i + 2 * TA_WAVES);
                     const int64_t at = tile_at(min(i + TA_WAVES, S.tiles - 1), id);
                     float z[NT][8];
-                    scores(k, z);
+                    if constexpr (X::CODED) {
+                        uint4 wide[2][KC];
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int c = 0; c < KC; ++c) wide[t][c] = X::operand(k[t][c >> 1], c & 1, power_of(k_by[t]));
+                        scores(wide, z);
+                    } else {
+                        scores(k, z);
+                    }
                     if (i + TA_WAVES < i_end) load_k(at);
+                    float by[8];                                 // what V's tokens are multiplied by
+                    if constexpr (X::CODED) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) by[j] = power_of((uint32_t)(v_by >> (8 * j)) & 0xffu);
+                    }
                     if (count < TA_TILE) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
+                        for (int j = 0; j < 8; ++j) {
+                            const bool behind = X::key(j >> 2, 4 * g + (j & 3)) >= count;
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
-                                if (X::key(j >> 2, 4 * g + (j & 3)) >= count) z[nt][j] = -INFINITY;
+                                if (behind) z[nt][j] = -INFINITY;
+                            if (X::CODED && behind) by[j] = 0.f;
+                        }
 #pragma unroll
-                        for (int dt = 0; dt < DT; ++dt)
+                        for (int dt = 0; dt < VR; ++dt)
 #pragma unroll
-                            for (int t = 0; t < VT; ++t) v[dt][t] = X::first(v[dt][t], count - X::pack(t, g) * E);
+                            for (int t = 0; t < VT; ++t) {
+                                if constexpr (X::CODED) v[dt][t] = X::first_coded(v[dt][t], count - X::pack(t, g) * E);
+                                else v[dt][t] = X::first(v[dt][t], count - X::pack(t, g) * E);
+                            }
                     }
-                    mine.template weights<1>(z, p);
+                    if constexpr (X::CODED) {
+                        mine.template weights<1>(z, p, [&](int j, float e) { return e * by[j]; });
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) mine.add(dt, v[dt], p);
+                        for (int dt = 0; dt < DT; ++dt) {
+                            const uint4 wide[1] = {X::operand(v[dt >> 1][0], dt & 1, 1.f)};
+                            mine.add(dt, wide, p);
+                        }
+                    } else {
+                        mine.template weights<1>(z, p);
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) mine.add(dt, v[dt], p);
+                    }
                     if (i + TA_WAVES < i_end) load_v(at);
                 }
             }
@@ -581,16 +646,16 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
             for (; i < min(s1 * TA_WAVES, S.tiles + (S.n + TA_TILE - 1) / TA_TILE); i += TA_WAVES) {
                 const int g = here(lane) >> 4, m = here(lane) & 15;
                 const int node0 = (i - S.tiles) * TA_TILE;
-                const W *key = static_cast<const W *>(A.k) + (int64_t)h * DIM, *value = static_cast<const W *>(A.v) + (int64_t)h * DIM;
+                const Row *key = static_cast<const Row *>(A.k) + (int64_t)h * DIM, *value = static_cast<const Row *>(A.v) + (int64_t)h * DIM;
                 // K, what the rows see, and (where the registers have room) V, all requested before anything is waited for
-                constexpr bool EARLY = NT * DIM <= 128 && DIM * (int)sizeof(W) <= 256;
+                constexpr bool EARLY = NT * DIM <= 128 && DIM * (int)sizeof(Row) <= 256;
                 uint4 k[2][KC], v[DT][VT];
                 uint64_t sees[NT];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const W *from = key + (S.start + min(node0 + X::key(t, m), S.n - 1)) * A.k_stride + g * E;
+                    const Row *from = key + (S.start + min(node0 + X::key(t, m), S.n - 1)) * A.k_stride;
 #pragma unroll
-                    for (int c = 0; c < KC; ++c) k[t][c] = load_raw(from + c * 4 * E);
+                    for (int c = 0; c < KC; ++c) k[t][c] = load_raw(from + X::channel(c, g));
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
@@ -602,9 +667,9 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
 #pragma unroll
                     for (int t = 0; t < VT; ++t) {
                         const int node = node0 + X::pack(t, g) * E;
-                        W in[E];
+                        Row in[E];
 #pragma unroll
-                        for (int j = 0; j < E; ++j) in[j] = value[(S.start + min(node + j, S.n - 1)) * A.v_stride + dt * 16 + m];
+                        for (int j = 0; j < E; ++j) in[j] = value[(S.start + min(node + j, S.n - 1)) * A.v_stride + X::v_channel(dt, m)];
                         __builtin_memcpy(&to[t], in, 16);
                     }
                 };
@@ -686,8 +751,14 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
                 for (int dt = 0; dt < DC / 16; ++dt)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        const f32x4_t o = mine.o[d0 / 16 + dt][nt];
-                        *reinterpret_cast<float4 *>(&s_sum[wave][16 * nt + m][16 * dt + 4 * g]) =
+                        f32x4_t o = mine.o[d0 / 16 + dt][nt];
+                        int at = 16 * dt + 4 * g;
+                        if constexpr (X::CODED) {                // two products have every other channel: halves of both
+                            const f32x4_t a = mine.o[d0 / 16 + (dt & ~1)][nt], b = mine.o[d0 / 16 + (dt | 1)][nt];
+                            o = dt & 1 ? f32x4_t{a[2], b[2], a[3], b[3]} : f32x4_t{a[0], b[0], a[1], b[1]};
+                            at = 16 * (dt & ~1) + 8 * g + 4 * (dt & 1);
+                        }
+                        *reinterpret_cast<float4 *>(&s_sum[wave][16 * nt + m][at]) =
                             make_float4(o[0] * mine_by[nt], o[1] * mine_by[nt], o[2] * mine_by[nt], o[3] * mine_by[nt]);
                     }
                 __syncthreads();
@@ -708,12 +779,12 @@ __global__ __launch_bounds__(TA_THREADS, ta_waves(sizeof(W), DIM, NT)) void k_tr
                         const float by = total == 0.f ? 0.f : 1.f / total;
                         const int node = (row0 + row) / A.group, head = h * A.group + row0 + row - node * A.group;
                         const int64_t at = (int64_t)(S.start + node) * heads_q + head;
-                        W to[4];
+                        Row to[4];
                         from_f32(a.x * by, to);
                         from_f32(a.y * by, to + 1);
                         from_f32(a.z * by, to + 2);
                         from_f32(a.w * by, to + 3);
-                        __builtin_memcpy(__builtin_assume_aligned(static_cast<W *>(A.out) + at * DIM + d0 + c, sizeof(to)), to, sizeof(to));
+                        __builtin_memcpy(__builtin_assume_aligned(static_cast<Row *>(A.out) + at * DIM + d0 + c, sizeof(to)), to, sizeof(to));
                         if (d0 + c == 0 && A.lse != nullptr) A.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
                     } else {
                         *reinterpret_cast<float4 *>(part + (size_t)row * DIM + d0 + c) = a;
@@ -836,10 +907,11 @@ __global__ __launch_bounds__(64 * tj_waves<SHARED>()) void k_tree_join(TreeJoinA
     if (lane >= LANES) return;
     const int64_t at = (int64_t)t * heads_q + hq;
     const float by = total == 0.f ? 0.f : 1.f / total;
-    W to[4];
+    using Row = typename RowOf<W>::type;
+    Row to[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) from_f32(sum[i] * by, to + i);
-    __builtin_memcpy(__builtin_assume_aligned(static_cast<W *>(A.out) + at * DIM + c, sizeof(to)), to, sizeof(to));
+    __builtin_memcpy(__builtin_assume_aligned(static_cast<Row *>(A.out) + at * DIM + c, sizeof(to)), to, sizeof(to));
     if (lane == 0 && A.lse != nullptr) A.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
 }
 
