@@ -398,7 +398,7 @@ svdp_status svdp_qk_rope(int32_t dtype, int32_t dim, int32_t T, const void *q, i
                          int64_t k_out_stride, void *stream);
 
 /* A token for each row of logits, drawn with given random numbers.  logits: device rows of [V] in `dtype`, `stride` elements apart (aligned
- * to their elements), V <= SVDP_MAX_VOCABULARY.  A row's tokens stand in order, largest logit first, lowest index first among
+ * to their elements; 0: all draws from one row), V <= SVDP_MAX_VOCABULARY.  A row's tokens stand in order, largest logit first, lowest index first among
  * equals, with weights w = 2^44 exp((x - x_first) / temperature) rounded to whole numbers.  Kept are the first tokens of the order: no more
  * than top_k (0 or less: all); the fewest whose weight is at least top_p of the weight of those (1 or more, NaN: all);
  * those with w >= min_p 2^44 (0 or less, NaN: all); always the first one.  Drawn is the first one at which the sum of

@@ -34,10 +34,11 @@ svdp_status svdp_qk_rope(int32_t dtype, int32_t dim, int32_t T, const void *q, i
                          int32_t heads, const int32_t *places, const float *inv_freq, int32_t rot, uint32_t flags, const float *q_weight,
                          const float *k_weight, float eps, void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride, void *stream)
 {
-    if (T < 0 || heads_q < 1 || heads < 0 || rot < 0 || rot > dim) return SVDP_ERR_INVALID_ARG;
+    if (T < 0 || heads_q < 1 || heads < 0 || rot < 0) return SVDP_ERR_INVALID_ARG;
     if ((flags & ~(uint32_t)(SVDP_ROPE_INTERLEAVED | SVDP_ROPE_NORM | SVDP_ROPE_WEIGHT_EACH)) != 0) return SVDP_ERR_INVALID_ARG;
     if (dtype != SVDP_F32 && dtype != SVDP_BF16) return SVDP_ERR_UNSUPPORTED;
     if ((dim != 64 && dim != 128 && dim != 256) || rot % 8 != 0 || heads_q > 65535 || heads > 65535 || T > SVDP_MAX_ROWS) return SVDP_ERR_UNSUPPORTED;
+    if (rot > dim) return SVDP_ERR_INVALID_ARG;
     const bool norm = flags & SVDP_ROPE_NORM;
     if (norm ? !(eps >= 0.f) || !std::isfinite(eps) : q_weight != nullptr || k_weight != nullptr || (flags & SVDP_ROPE_WEIGHT_EACH)) return SVDP_ERR_INVALID_ARG;
     if (T == 0) return SVDP_OK;
@@ -95,7 +96,7 @@ svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32
                         const float *top_p, const float *min_p, int32_t T, int32_t *answers, float *logp, void *ws, size_t ws_bytes, void *stream)
 {
     static_assert(SAMPLE_MAX_V == SVDP_MAX_VOCABULARY);
-    if (T < 0 || V < 1 || stride < V) return SVDP_ERR_INVALID_ARG;
+    if (T < 0 || V < 1 || (stride != 0 && stride < V)) return SVDP_ERR_INVALID_ARG;
     if (dtype != SVDP_F32 && dtype != SVDP_BF16) return SVDP_ERR_UNSUPPORTED;
     if (T > SVDP_MAX_ROWS || V > SVDP_MAX_VOCABULARY) return SVDP_ERR_UNSUPPORTED;
     if (T == 0) return SVDP_OK;
