@@ -2,9 +2,10 @@
 
 A step takes, for each request, a tree of drafted tokens whose first node is the newest certain token.  It runs
 
-  binding.tree_attn    every layer's attention of the trees over the cache,
+  binding.qk_rope      norms and rotation of a layer's queries and keys (a decoder with inv_freq),
+  binding.tree_attn    every layer's attention of the trees over the cache (of the weights' type, or in 8 bits),
   binding.ffn_step     the layer's sparse FFN, up to ``rows`` tokens sharing one list of active neurons,
-  binding.tree_accept  the model's own answers and the branch that agrees with them,
+  binding.tree_accept  the model's own answers and the branch that agrees with them (or binding.tree_sample: answers drawn),
   binding.kv_plan      pages and slots for that branch (and pages back from requests that end),
   binding.kv_commit    K and V of that branch into the cache,
 
@@ -15,7 +16,7 @@ decoding one by one, up to rounding; more rows share the union of their lists, a
 """
 from __future__ import annotations
 
-from typing import Callable, List, Sequence, Tuple
+from typing import Callable, List, Optional, Sequence, Tuple
 
 import torch
 
@@ -62,14 +63,20 @@ def cut(tree: Tree, levels: int) -> Tree:
 
 class Decoder:
     """Weights: per layer a binding.DeviceLayer, Wqkv [d][(heads_q + 2 heads) dim] and Wo [heads_q dim][d]; embed and
-    head [V][d].  The cache has ``pages`` pages of ``page`` tokens for ``requests`` requests of up to ``max_len``."""
+    head [V][d].  The cache has ``pages`` pages of ``page`` tokens for ``requests`` requests of up to ``max_len``; cache_dtype: its
+    type, e.g. torch.float8_e4m3fn (default: the weights').  Positions are added to the embedding, or with inv_freq [rot / 2] turn queries
+    and keys; qk_norm: float32 weights ([layers][dim] for queries, for keys) of norms in front of that."""
 
     def __init__(self, ffn: List[binding.DeviceLayer], Wqkv: List[torch.Tensor], Wo: List[torch.Tensor], embed: torch.Tensor,
-                 head: torch.Tensor, heads_q: int, heads: int, dim: int, requests: int, pages: int, page: int = 64, max_len: int = 4096, rows: int = 8):
+                 head: torch.Tensor, heads_q: int, heads: int, dim: int, requests: int, pages: int, page: int = 64, max_len: int = 4096, rows: int = 8,
+                 cache_dtype=None, inv_freq: Optional[torch.Tensor] = None, qk_norm: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
         self.ffn, self.Wqkv, self.Wo, self.embed, self.head = ffn, Wqkv, Wo, embed, head
         self.heads_q, self.heads, self.dim, self.rows = heads_q, heads, dim, rows
         dev, i32 = embed.device, torch.int32
-        self.cache = binding.KVCache.empty(len(ffn), pages, page, heads, dim, dtype=embed.dtype, device=dev)
+        self.cache = binding.KVCache.empty(len(ffn), pages, page, heads, dim, dtype=embed.dtype if cache_dtype is None else cache_dtype, device=dev)
+        if inv_freq is None and qk_norm is not None:
+            raise ValueError("qk_norm goes with inv_freq")
+        self.inv_freq, self.qk_norm = inv_freq, qk_norm
         self.table = torch.zeros((requests, -(-max_len // page)), dtype=i32, device=dev)
         self.ring = torch.arange(pages, dtype=i32, device=dev)
         self.pool = torch.tensor([0, pages], dtype=i32, device=dev)
@@ -86,12 +93,19 @@ class Decoder:
     def forward(self, tokens, starts, tree, places, max_nodes: int):
         """logits [T][V], and K and V [layers][T][heads][dim] of rows that the cache does not have yet."""
         T, hq, h, dim, wt = tokens.numel(), self.heads_q, self.heads, self.dim, self.embed.dtype
-        x = self.embed[tokens].float() + self.where[places].float()
+        x = self.embed[tokens].float()
+        if self.inv_freq is None:
+            x = x + self.where[places].float()
         new = torch.empty((2, len(self.ffn), T, h, dim), dtype=wt, device=x.device)
         for l, layer in enumerate(self.ffn):
             qkv = (self._norm(x).to(wt) @ self.Wqkv[l]).view(T, hq + 2 * h, dim)
             q, k, v = qkv.split((hq, h, h), dim=1)
-            new[0, l], new[1, l] = k, v
+            if self.inv_freq is not None:
+                norm = dict(zip(("q_weight", "k_weight"), (w[l] for w in self.qk_norm)), eps=1e-6) if self.qk_norm is not None else {}
+                q, k = binding.qk_rope(q, k, places, self.inv_freq, k_out=new[0, l], **norm)
+            else:
+                new[0, l] = k
+            new[1, l] = v
             a = binding.tree_attn(self.cache, l, q, k, v, self.table, self.lens, starts, tree=tree, max_nodes=max_nodes)
             x = x + (a.view(T, hq * dim) @ self.Wo[l]).float()
             z = self._norm(x).to(wt)
@@ -140,12 +154,36 @@ class Decoder:
                 raise RuntimeError("the cache has too few pages for these prompts")
             done += binding.MAX_NODES
 
-    def step(self, trees: List[Tree], live: List[bool]) -> List[List[int]]:
+    def save(self):
+        """The cached tokens of all requests, to bring back with load(): (lengths, k, v [layers][tokens][heads][dim]).  All pages are free
+        afterwards."""
+        lens, page = self.lens.tolist(), self.cache.page
+        i = torch.cat([torch.arange(n, device=self.lens.device) for n in lens])
+        r = torch.repeat_interleave(torch.arange(len(lens), device=i.device), self.lens, output_size=sum(lens))
+        k, v = binding.kv_read(self.cache, self.table[r, i // page].long() * page + i % page)
+        self.release()
+        return lens, k, v
+
+    def load(self, saved) -> None:
+        """What save() gave, into pages of a decoder without tokens (of the same layers; its cache may be of another size)."""
+        lens, k, v = saved
+        if bool(self.lens.any()):
+            raise RuntimeError("the cache holds tokens of other requests: release() them first")
+        starts = torch.tensor([0] + lens, dtype=torch.int32, device=self.lens.device).cumsum(0, dtype=torch.int32)
+        if self._store(k, v, starts.diff(), starts, rows=sum(lens)).any():
+            self.release()
+            raise RuntimeError("the cache has too few pages for these requests")
+
+    def step(self, trees: List[Tree], live: List[bool], drawn: Optional[dict] = None) -> List[List[int]]:
         """One step; trees[r] starts with the newest certain token.  live[r] False: the request ends, its pages are free again.
+        drawn: settings of binding.sample as numbers, and ``generator`` of its random numbers; None: the largest logits.
         Returns the new certain tokens of each request, one at least."""
         tokens, starts, tree, places, most = self._rows([t if on else ([], []) for t, on in zip(trees, live)])
         logits, k, v = self.forward(tokens, starts, tree, places, most)
-        keep, counts, following, best = binding.tree_accept(logits, tokens, starts, tree=tree, max_nodes=most)
+        if drawn is None:
+            keep, counts, following, _ = binding.tree_accept(logits, tokens, starts, tree=tree, max_nodes=most)
+        else:
+            keep, counts, following, _ = self._drawn(logits, tokens, starts, tree, most, **drawn)
         add = torch.where(torch.tensor(live, device=counts.device), counts, -1)
         refused = self._store(k, v, add, starts, keep=keep)
         R, T = len(trees), tokens.numel()
@@ -160,21 +198,27 @@ class Decoder:
             out.append(branch + [following[r]] if live[r] else [])
         return out
 
-    def generate(self, prompts: List[List[int]], new: int, nodes: int = 8,
-                 draft: Callable[[Sequence[int], int], Tree] = lookup) -> Tuple[List[List[int]], int]:
+    @staticmethod
+    def _drawn(logits, tokens, starts, tree, most, generator=None, **how):
+        dev, T = logits.device, tokens.numel()
+        each = {n: torch.full((T,), v, dtype=torch.int32 if n == "top_k" else torch.float32, device=dev) for n, v in how.items()}
+        return binding.tree_sample(logits, torch.rand(T, device=dev, generator=generator), tokens, starts, tree=tree, max_nodes=most, **each)
+
+    def generate(self, prompts: List[List[int]], new: int, nodes: int = 8, draft: Callable[[Sequence[int], int], Tree] = lookup,
+                 drawn: Optional[dict] = None) -> Tuple[List[List[int]], int]:
         """``new`` tokens after each prompt (one for each of the cache's requests), and the number of steps that took.  draft
         proposes up to nodes - 1 tokens from what a request has (none are taken that would lead past ``new``, so a request never needs
-        room for more than its prompt and those); nodes=1 decodes one by one.  All pages are free afterwards, after
-        an error too."""
+        room for more than its prompt and those); nodes=1 decodes one by one.  drawn: as in step(), e.g. dict(temperature=0.8,
+        top_p=0.95).  All pages are free afterwards, after an error too."""
         assert len(prompts) == self.lens.numel() and min(map(len, prompts)) > 0
         if bool(self.lens.any()):
             raise RuntimeError("the cache holds tokens of other requests: release() them first")
         try:
-            return self._generate(prompts, new, nodes, draft)
+            return self._generate(prompts, new, nodes, draft, drawn)
         finally:
             self.release()
 
-    def _generate(self, prompts, new, nodes, draft):
+    def _generate(self, prompts, new, nodes, draft, drawn):
         self.prefill(prompts)
         text, steps = [list(p) for p in prompts], 0
         live = [new > 0] * len(prompts)
@@ -184,7 +228,7 @@ class Decoder:
                 levels = len(p) + new - len(t) - 1          # a step's answers are one more than the drafts it keeps
                 toks, parents = cut(draft(t, nodes - 1), levels) if nodes > 1 and levels > 0 else ([], [])
                 trees.append(([t[-1]] + toks, [-1] + [p + 1 for p in parents]))
-            for t, more in zip(text, self.step(trees, live)):
+            for t, more in zip(text, self.step(trees, live, drawn)):
                 t += more
             steps += 1
             live = [on and len(t) < len(p) + new for on, t, p in zip(live, text, prompts)]
@@ -218,6 +262,11 @@ def main() -> None:
     for nodes in (1, 8, 24):
         out, steps = decoder.generate(prompts, 100, nodes=nodes)
         print(f"trees of {nodes}: {steps} steps for 100 tokens of {len(prompts)} requests; the first of each: {[o[:3] for o in out]}")
+    inv_freq = (10000.0 ** (-torch.arange(0, 64, 2, device="cuda").double() / 64)).float()
+    weights = torch.ones((2, 64), device="cuda")
+    decoder = random_decoder(requests=len(prompts), pages=64, max_len=1024, cache_dtype=torch.float8_e4m3fn, inv_freq=inv_freq, qk_norm=(weights, weights))
+    out, steps = decoder.generate(prompts, 100, nodes=8, drawn=dict(temperature=0.8, top_k=50, top_p=0.95))
+    print(f"rotary positions, a cache in 8 bits, drawn tokens: {steps} steps; the first of each: {[o[:3] for o in out]}")
 
 
 if __name__ == "__main__":
