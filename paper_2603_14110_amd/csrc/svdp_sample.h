@@ -35,8 +35,16 @@ constexpr int SAMPLE_MAX_V = 1 << 19;
 
 // Bins of bf16 values, the largest first: magnitudes (bits without sign) from VALUE_LOW on, VALUE_SPAN of them; zero; then negative ones.
 constexpr int VALUE_LOW = (127 - 30) << 7, VALUE_HIGH = (127 + 8) << 7, VALUE_SPAN = VALUE_HIGH - VALUE_LOW;
-constexpr int VALUE_BINS = 2 * VALUE_SPAN + 1, VALUE_EACH = (VALUE_BINS + SAMPLE_THREADS - 1) / SAMPLE_THREADS;
+constexpr int VALUE_HALF = SAMPLE_THREADS / 2, VALUE_EACH = (VALUE_SPAN + VALUE_HALF - 1) / VALUE_HALF;      // threads of a sign; bins of a thread
+static_assert(VALUE_EACH * (VALUE_HALF - 1) >= VALUE_SPAN, "the last thread of the positive ones has zero");
 constexpr float VALUE_FAR = -256.f;                         // what lies at or below it has no bin
+// In LDS: counters of positive magnitudes, then of negative ones, each followed by one a lane for all that has no bin: lanes do
+// not meet there, whatever a row is filled up with.
+constexpr int VALUE_OTHER = 64, VALUE_SIDE = VALUE_SPAN + VALUE_OTHER;
+static_assert(4 * 2 * VALUE_SIDE < 65536, "addresses of counters are halves of a word");
+
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2_t __attribute__((ext_vector_type(2)));
 
 struct SampleArgs {
     const void *logits;
@@ -54,29 +62,45 @@ __device__ __forceinline__ float of_order(uint32_t o)
     return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
 
-// f(value, index) for the elements of a row that a thread has; vectors of 16 bytes but at the row's ends.
-template <typename W, typename F>
-__device__ __forceinline__ void each_logit(const W *row, int V, int tid, int threads, F &&f)
+// v(16 bytes, index of their first element) for a thread's share of a row, and f(value, index) for the elements at the row's ends that are
+// no whole vector.
+template <int AHEAD, typename W, typename Fv, typename F>
+__device__ __forceinline__ void each_vector(const W *row, int V, int tid, int threads, Fv &&v, F &&f)
 {
-    constexpr int VEC = Elem<W>::VEC, AHEAD = 4;
+    constexpr int VEC = Elem<W>::VEC;
     const int skew = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / Elem<W>::BYTES);
     const int head = min(skew > 0 ? VEC - skew : 0, V), vectors = (V - head) / VEC, tail = head + vectors * VEC;
-    for (int i0 = tid; i0 < vectors; i0 += AHEAD * threads) {
-        uint4 in[AHEAD];
+    // the next vectors are requested before these are looked at
+    uint4 in[AHEAD], next[AHEAD];
+    const auto request = [&](int i0, uint4 (&to)[AHEAD]) {
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) in[a] = load_raw(row + head + (int64_t)min(i0 + a * threads, vectors - 1) * VEC);
+        for (int a = 0; a < AHEAD; ++a) to[a] = load_raw(row + head + (int64_t)min(i0 + a * threads, vectors - 1) * VEC);
+    };
+    if (tid < vectors) request(tid, in);
+    for (int i0 = tid; i0 < vectors; i0 += AHEAD * threads) {
+        request(i0 + AHEAD * threads, next);
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) {
             const int i = i0 + a * threads;
-            if (i >= vectors) break;
-            float v[VEC];
-            widen(in[a], v, row);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) f(v[j], head + i * VEC + j);
+            if (i < vectors) v(in[a], head + i * VEC);
         }
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) in[a] = next[a];
     }
     if (tid < head) f(to_f32(row[tid]), tid);
     if (tail + tid < V) f(to_f32(row[tail + tid]), tail + tid);
+}
+// f(value, index) for a thread's share.
+template <int AHEAD, typename W, typename F>
+__device__ __forceinline__ void each_logit(const W *row, int V, int tid, int threads, F &&f)
+{
+    constexpr int VEC = Elem<W>::VEC;
+    each_vector<AHEAD>(row, V, tid, threads, [&](const uint4 &in, int i) {
+        float v[VEC];
+        widen(in, v, row);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) f(v[j], i + j);
+    }, f);
 }
 
 // 2^44 exp(z), rounded to a whole number, z = at / ln 2 <= 0 in 64 bits: 2^at by its Taylor series to the eleventh power around the nearest
@@ -107,7 +131,7 @@ struct SampleScale {
 
 struct SampleShared {
     union {
-        uint32_t values[SAMPLE_THREADS * VALUE_EACH];
+        uint32_t values[2 * VALUE_SIDE];
         struct {
             uint64_t bin_weight[SAMPLE_BINS];
             uint32_t bin_count[SAMPLE_BINS];
@@ -117,19 +141,44 @@ struct SampleShared {
     uint64_t wave_weight[SAMPLE_WAVES], wave_key[SAMPLE_WAVES];
     uint32_t wave_count[SAMPLE_WAVES], wave_low[SAMPLE_WAVES];
     // what the thread that a question leads to answers
-    uint64_t before_weight, weight, key;
+    uint64_t before_weight, key;
     uint32_t before_count, count, listed;
-    int bin, odd;
+    int bin;
+    struct {
+        uint64_t before_weight;
+        uint32_t before_count;
+        int thread;
+    } asked[3];                             // of three questions a row
 };
 
-__device__ __forceinline__ uint64_t wave_sums_u64(uint64_t v, int lane)
+// Inclusive sums over a wave, as wave_inclusive_scan.
+template <int CTRL, int ROW_MASK, int BANK_MASK>
+__device__ __forceinline__ uint64_t dpp_take_u64(uint64_t v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const uint64_t o = __shfl_up((unsigned long long)v, d);
-        v += lane >= d ? o : 0;
-    }
-    return v;
+    return (uint32_t)dpp_take<CTRL, ROW_MASK, BANK_MASK>((int)(uint32_t)v) | (uint64_t)(uint32_t)dpp_take<CTRL, ROW_MASK, BANK_MASK>((int)(v >> 32)) << 32;
+}
+__device__ __forceinline__ uint64_t wave_sums_u64(uint64_t v)
+{
+    uint64_t s = v + dpp_take_u64<0x111, 0xf, 0xf>(v);
+    s += dpp_take_u64<0x112, 0xf, 0xf>(v);
+    s += dpp_take_u64<0x113, 0xf, 0xf>(v);
+    s += dpp_take_u64<0x114, 0xf, 0xe>(s);
+    s += dpp_take_u64<0x118, 0xf, 0xc>(s);
+    s += dpp_take_u64<0x142, 0xa, 0xf>(s);
+    s += dpp_take_u64<0x143, 0xc, 0xf>(s);
+    return s;
+}
+__device__ __forceinline__ uint64_t lane_of_u64(uint64_t v, int lane)
+{
+    return (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32;
+}
+// a / b, of less than 2^31: the quotient in fp64 is at most one off, and put right.
+__device__ __forceinline__ uint32_t sample_quotient(uint64_t a, uint64_t b)
+{
+    uint32_t q = (uint32_t)((double)a / (double)b);
+    if ((uint64_t)q * b > a) --q;
+    if ((uint64_t)(q + 1) * b <= a) ++q;
+    return q;
 }
 // Sums over the threads before this one, and all of them.
 struct SampleSums {
@@ -139,20 +188,19 @@ struct SampleSums {
 __device__ __forceinline__ SampleSums sample_sums(SampleShared &s, uint64_t weight, uint32_t count, int tid)
 {
     const int lane = tid & 63, wave = tid >> 6;
-    const uint64_t w = wave_sums_u64(weight, lane);
+    const uint64_t w = wave_sums_u64(weight);
     const uint32_t c = (uint32_t)wave_inclusive_scan((int)count);
     if (lane == 63) {
         s.wave_weight[wave] = w;
         s.wave_count[wave] = c;
     }
     __syncthreads();
-    SampleSums r{w - weight, 0, c - count, 0};
-    for (int i = 0; i < SAMPLE_WAVES; ++i) {
-        r.before_weight += i < wave ? s.wave_weight[i] : 0;
-        r.before_count += i < wave ? s.wave_count[i] : 0;
-        r.weight += s.wave_weight[i];
-        r.count += s.wave_count[i];
-    }
+    // the waves' sums, a lane each
+    const uint64_t each_weight = lane < SAMPLE_WAVES ? s.wave_weight[lane] : 0, upto_weight = wave_sums_u64(each_weight);
+    const uint32_t each_count = lane < SAMPLE_WAVES ? s.wave_count[lane] : 0, upto_count = (uint32_t)wave_inclusive_scan((int)each_count);
+    const int at = __builtin_amdgcn_readfirstlane(wave);
+    const SampleSums r{w - weight + lane_of_u64(upto_weight - each_weight, at), lane_of_u64(upto_weight, 63),
+                       c - count + (uint32_t)__builtin_amdgcn_readlane((int)(upto_count - each_count), at), (uint32_t)__builtin_amdgcn_readlane((int)upto_count, 63)};
     __syncthreads();
     return r;
 }
@@ -165,6 +213,7 @@ __device__ __forceinline__ uint64_t sample_sum(SampleShared &s, uint64_t v, int 
 struct SampleHow {
     float temperature, top_p, min_p, u;
     int top_k;
+    bool first;                             // the first token of the order: nothing is drawn
     // weight that top_p asks for, of `kept`; at least one token's
     __device__ __forceinline__ uint64_t share(uint64_t kept) const
     {
@@ -180,40 +229,78 @@ struct SampleHow {
 };
 constexpr uint64_t SAMPLE_ONE = (uint64_t)1 << 44;
 
-// The index of the which-th element of a row (from 0) that is(value): waves take pieces of the row one after the other.
-template <typename W, typename F>
-__device__ __forceinline__ void sample_index(SampleShared &s, const W *row, int V, uint32_t which, int tid, F &&is, int32_t *answer)
+// Which elements of a vector have the value x (zero: of either sign; NaN: any NaN), as bits.
+template <typename W>
+__device__ __forceinline__ bool same_value(float v, float x)
 {
-    constexpr int VEC = Elem<W>::VEC, AHEAD = 4;
+    return v == x || (v != v && x != x);
+}
+__device__ __forceinline__ bool has_value(const uint4 &in, float x, const float *)
+{
+    const float4 v = as_float4(in);
+    return same_value<float>(v.x, x) || same_value<float>(v.y, x) || same_value<float>(v.z, x) || same_value<float>(v.w, x);
+}
+// The smallest of all halves' differences from x in bits: a half of zero is x.  NaN is compared one by one, the other sign of zero too.
+__device__ __forceinline__ bool has_value(const uint4 &in, float x, const bf16 *)
+{
+    if (!(x < 0.f || x > 0.f)) return true;
+    const uint32_t h = __float_as_uint(x) >> 16, both = h | h << 16;
+    const auto far = [&](uint32_t w) { return __builtin_bit_cast(u16x2_t, w ^ both); };
+    const u16x2_t a = __builtin_elementwise_min(far(in.x), far(in.y)), b = __builtin_elementwise_min(far(in.z), far(in.w));
+    const u16x2_t m = __builtin_elementwise_min(a, b);
+    return min(m[0], m[1]) == 0;
+}
+// The index of the which-th element (from 0) of value x: waves take pieces of the row one after the other.
+template <typename W>
+__device__ __forceinline__ void sample_index(SampleShared &s, const W *row, int V, uint32_t which, int tid, float x, int32_t *answer)
+{
+    constexpr int VEC = Elem<W>::VEC, AHEAD = 8;
     const int lane = tid & 63, wave = tid >> 6, skew = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / Elem<W>::BYTES);
     const int head = min(skew > 0 ? VEC - skew : 0, V), vectors = (V - head) / VEC, tail = head + vectors * VEC;
     const int piece = (vectors + SAMPLE_WAVES - 1) / SAMPLE_WAVES, begin = min(wave * piece, vectors), end = min(begin + piece, vectors);
     const bool first = wave == 0, last = wave == SAMPLE_WAVES - 1;
-    const auto is_head = [&] { return first && lane < head && is(to_f32(row[lane])); };
-    const auto is_tail = [&] { return last && tail + lane < V && is(to_f32(row[tail + lane])); };
+    const auto is_head = [&] { return first && lane < head && same_value<W>(to_f32(row[lane]), x); };
+    const auto is_tail = [&] { return last && tail + lane < V && same_value<W>(to_f32(row[tail + lane]), x); };
     const auto bits_of = [&](const uint4 &in) {
         float v[VEC];
         widen(in, v, row);
         uint32_t bits = 0;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) bits |= is(v[j]) ? 1u << j : 0u;
+        for (int j = 0; j < VEC; ++j) bits |= same_value<W>(v[j], x) ? 1u << j : 0u;
         return bits;
     };
-    int mine = 0;
-    for (int i0 = begin + lane; i0 < end; i0 += AHEAD * 64) {
+    int mine = 0, at = 0;                   // what a lane has, and the last place of them
+    for (int i0 = begin; i0 < end; i0 += AHEAD * 64) {
         uint4 in[AHEAD];
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) in[a] = load_raw(row + head + (int64_t)min(i0 + a * 64, end - 1) * VEC);
+        for (int a = 0; a < AHEAD; ++a) in[a] = load_raw(row + head + (int64_t)min(i0 + lane + a * 64, end - 1) * VEC);
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) mine += i0 + a * 64 < end ? __popc(bits_of(in[a])) : 0;
+        for (int a = 0; a < AHEAD; ++a)
+            if (__any(has_value(in[a], x, row))) {
+                const int i = i0 + lane + a * 64;
+                const uint32_t bits = i < end ? bits_of(in[a]) : 0;
+                mine += __popc(bits);
+                at = bits != 0 ? head + i * VEC + __ffs((int)bits) - 1 : at;
+            }
     }
-    mine += (is_head() ? 1 : 0) + (is_tail() ? 1 : 0);
+    if (is_head()) {
+        ++mine;
+        at = lane;
+    }
+    if (is_tail()) {
+        ++mine;
+        at = tail + lane;
+    }
     const int all = wave_inclusive_scan(mine);
     if (lane == 63) s.wave_count[wave] = (uint32_t)all;
     __syncthreads();
     uint32_t before = 0;
     for (int w = 0; w < wave; ++w) before += s.wave_count[w];
     if (which < before || which >= before + s.wave_count[wave]) return;
+    if (s.wave_count[wave] == 1) {
+        if (mine > 0) *answer = at;
+        return;
+    }
     uint32_t left = which - before;
     const uint64_t heads = __ballot(is_head());
     const auto nth = [](uint64_t set, uint32_t n) {
@@ -225,15 +312,22 @@ __device__ __forceinline__ void sample_index(SampleShared &s, const W *row, int 
         return;
     }
     left -= (uint32_t)__popcll(heads);
-    for (int i0 = begin; i0 < end; i0 += 64) {
-        const uint32_t bits = i0 + lane < end ? bits_of(load_raw(row + head + (int64_t)(i0 + lane) * VEC)) : 0;
-        if (__ballot(bits != 0) == 0) continue;
-        const int n = __popc(bits), upto = wave_inclusive_scan(n), sum = __builtin_amdgcn_readlane(upto, 63);
-        if (left < (uint32_t)sum) {
-            if ((int)left >= upto - n && (int)left < upto) *answer = head + (i0 + lane) * VEC + nth(bits, left - (uint32_t)(upto - n));
-            return;
+    for (int i0 = begin; i0 < end; i0 += AHEAD * 64) {
+        uint4 in[AHEAD];
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) in[a] = load_raw(row + head + (int64_t)min(i0 + lane + a * 64, end - 1) * VEC);
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            if (!__any(has_value(in[a], x, row))) continue;
+            const int i = i0 + lane + a * 64;
+            const uint32_t bits = i < end ? bits_of(in[a]) : 0;
+            const int n = __popc(bits), upto = wave_inclusive_scan(n), sum = __builtin_amdgcn_readlane(upto, 63);
+            if (left < (uint32_t)sum) {
+                if ((int)left >= upto - n && (int)left < upto) *answer = head + i * VEC + nth(bits, left - (uint32_t)(upto - n));
+                return;
+            }
+            left -= (uint32_t)sum;
         }
-        left -= (uint32_t)sum;
     }
     const uint64_t tails = __ballot(is_tail());
     if (lane == 0) *answer = tail + nth(tails, left);
@@ -241,107 +335,169 @@ __device__ __forceinline__ void sample_index(SampleShared &s, const W *row, int 
 
 // ---- bf16: one bin a value --------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ float value_of_bin(int b)
-{
-    const uint32_t bits = b < VALUE_SPAN ? VALUE_HIGH - 1 - b : b == VALUE_SPAN ? 0u : 0x8000u | (VALUE_LOW + b - VALUE_SPAN - 1);
-    return __uint_as_float(bits << 16);
-}
+// A thread's bins, the largest value first: the first half of the threads has the positive ones and, in its last thread, zero.
+struct ValueBins {
+    int bits, step, at, n;                  // of the first bin's value, from one to the next; its counter
+    bool zero;
+    __device__ __forceinline__ ValueBins(int tid)
+    {
+        const bool positive = tid < VALUE_HALF;
+        const int first = (positive ? tid : tid - VALUE_HALF) * VALUE_EACH;
+        step = positive ? -1 : 1;
+        zero = tid == VALUE_HALF - 1;
+        n = zero ? 1 : min(max(VALUE_SPAN - first, 0), VALUE_EACH);
+        bits = zero ? 0 : positive ? VALUE_HIGH - 1 - first : 0x8000 + VALUE_LOW + first;
+        at = positive ? VALUE_SPAN - 1 - first : VALUE_SIDE + first;
+    }
+    __device__ __forceinline__ float value(int j) const { return __uint_as_float((uint32_t)(bits + j * step) << 16); }
+    __device__ __forceinline__ uint32_t count(const SampleShared &s, int j, uint32_t zeros) const { return j >= n ? 0u : zero ? zeros : s.values[at + j * step]; }
+};
 // False: the row has to go the other way.
 __device__ __forceinline__ bool sample_by_value(SampleShared &s, const bf16 *row, int V, const SampleHow &how, int tid, int32_t *answer, float *logp)
 {
-#pragma unroll
-    for (int j = 0; j < VALUE_EACH; ++j) s.values[j * SAMPLE_THREADS + tid] = 0;
-    if (tid == 0) {
-        s.odd = 0;
-        s.bin = VALUE_BINS;
+    for (int i = tid; i < 2 * VALUE_SIDE; i += SAMPLE_THREADS) s.values[i] = 0;
+    if (tid == 0) s.count = 0;
+    __syncthreads();
+    // Two elements at a time, as halves of a word: magnitude from VALUE_LOW on (below it: a large number), up to the lane's own
+    // counter for others, plus one side for a sign.
+    const uint16_t other = (uint16_t)(VALUE_SPAN + (tid & (VALUE_OTHER - 1)));
+    const auto pair = [&](uint32_t w) {
+        const u16x2_t x = __builtin_bit_cast(u16x2_t, w);
+        const u16x2_t m = __builtin_elementwise_min((x & (uint16_t)0x7fff) - (uint16_t)VALUE_LOW, u16x2_t{other, other});
+        const uint32_t at = __builtin_bit_cast(uint32_t, (m + (x >> 15) * (uint16_t)VALUE_SIDE) << 2);
+        char *counters = reinterpret_cast<char *>(s.values);
+        atomicAdd(reinterpret_cast<uint32_t *>(counters + (at & 0xffffu)), 1u);
+        return reinterpret_cast<uint32_t *>(counters + (at >> 16));
+    };
+    each_vector<4>(row, V, tid, SAMPLE_THREADS, [&](const uint4 &in, int) {
+        atomicAdd(pair(in.x), 1u);
+        atomicAdd(pair(in.y), 1u);
+        atomicAdd(pair(in.z), 1u);
+        atomicAdd(pair(in.w), 1u);
+    }, [&](float x, int) { pair(__float_as_uint(x) >> 16); });
+    __syncthreads();
+    // Others: zeros are counted, values far below (-inf among them) have no weight; with any else (small: smaller than VALUE_LOW, but not zero;
+    // large or NaN) the row goes the other way.
+    const uint32_t others = tid < VALUE_OTHER ? s.values[VALUE_SPAN + tid] + s.values[VALUE_SIDE + VALUE_SPAN + tid] : 0;
+    uint32_t zeros = 0;
+    if (__syncthreads_or(others > 0)) {
+        u16x2_t small = {0xffff, 0xffff}, negative = {0, 0}, nonzero = {0, 0};
+        i16x2_t large = {0, 0};
+        uint32_t elements = 0;
+        const auto look = [&](uint32_t w) {
+            const u16x2_t x = __builtin_bit_cast(u16x2_t, w), m = x & (uint16_t)0x7fff;
+            small = __builtin_elementwise_min(small, m - (uint16_t)1);
+            nonzero += __builtin_elementwise_min(m, u16x2_t{1, 1});
+            large = __builtin_elementwise_max(large, __builtin_bit_cast(i16x2_t, x));
+            negative = __builtin_elementwise_max(negative, x);
+        };
+        each_vector<4>(row, V, tid, SAMPLE_THREADS, [&](const uint4 &in, int) {
+            look(in.x);
+            look(in.y);
+            look(in.z);
+            look(in.w);
+            elements += 8;
+        }, [&](float x, int) {
+            look(__float_as_uint(x) >> 16);
+            ++elements;                                      // and a half that is zero
+        });
+        const bool odd = min(small[0], small[1]) < VALUE_LOW - 1 || max(large[0], large[1]) >= VALUE_HIGH || max(negative[0], negative[1]) > 0xff80u;
+        zeros = (uint32_t)wave_inclusive_scan((int)(elements - nonzero[0] - nonzero[1]));
+        if ((tid & 63) == 63 && zeros > 0) atomicAdd(&s.count, zeros);
+        if (__syncthreads_or(odd)) return false;
+        zeros = s.count;
     }
-    __syncthreads();
-    bool odd = false;
-    each_logit(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
-        const uint32_t u = __float_as_uint(x), m = (u >> 16) & 0x7fffu;
-        const bool negative = u >> 31, binned = m - VALUE_LOW < (uint32_t)VALUE_SPAN;
-        const uint32_t b = negative ? m + (VALUE_SPAN + 1 - VALUE_LOW) : VALUE_HIGH - 1 - m;
-        if (binned || m == 0) atomicAdd(&s.values[m == 0 ? VALUE_SPAN : b], 1u);
-        else odd = odd || !negative || m < VALUE_LOW || m > 0x7f80u;            // else far below, or -inf
-    });
-    if (odd) s.odd = 1;
-    __syncthreads();
-    if (s.odd) return false;
-    uint32_t c[VALUE_EACH], count = 0;
-    int first = VALUE_BINS;
+    // the thread's bins: the largest value that there is, then the weights
+    const ValueBins bins(tid);
+    uint32_t count = 0;
+    int first = SAMPLE_THREADS * VALUE_EACH;
 #pragma unroll
     for (int j = VALUE_EACH - 1; j >= 0; --j) {
-        c[j] = s.values[tid * VALUE_EACH + j];
-        count += c[j];
-        first = c[j] > 0 ? tid * VALUE_EACH + j : first;
+        const uint32_t c = bins.count(s, j, zeros);
+        count += c;
+        first = c > 0 ? tid * VALUE_EACH + j : first;
     }
-    if (__any(count > 0)) {
-        const int lowest = __builtin_amdgcn_readlane(first, __ffsll((unsigned long long)__ballot(count > 0)) - 1);
-        if ((tid & 63) == 0) atomicMin(&s.bin, lowest);
-    }
+    const uint64_t some = __ballot(count > 0);
+    const int lowest = __builtin_amdgcn_readlane(first, some != 0 ? __ffsll((unsigned long long)some) - 1 : 0);       // by all lanes
+    if ((tid & 63) == 0) s.wave_low[tid >> 6] = (uint32_t)lowest;
     __syncthreads();
-    first = s.bin;
-    if (first == VALUE_BINS) return false;
-    const SampleScale scale(value_of_bin(first), how.temperature);
-    uint64_t w[VALUE_EACH], weight = 0;
-#pragma unroll
-    for (int j = 0; j < VALUE_EACH; ++j) {
-        w[j] = c[j] > 0 ? scale.of(value_of_bin(tid * VALUE_EACH + j)) : 0;
-        weight += w[j] * c[j];
+    first = (tid & 63) < SAMPLE_WAVES ? (int)s.wave_low[tid & 63] : SAMPLE_THREADS * VALUE_EACH;
+    const uint64_t where = __ballot(first < SAMPLE_THREADS * VALUE_EACH);           // waves' bins are in order
+    if (where == 0) return false;
+    first = __builtin_amdgcn_readlane(first, __ffsll((unsigned long long)where) - 1);
+    const float top = ValueBins(first / VALUE_EACH).value(first % VALUE_EACH);
+    if (how.first) {
+        if (tid == 0 && logp != nullptr) *logp = 0.f;
+        sample_index(s, row, V, 0, tid, top, answer);
+        return true;
+    }
+    const SampleScale scale(top, how.temperature);
+    uint64_t weight = 0;
+    if (some != 0) {
+#pragma unroll 1
+        for (int j = 0; j < VALUE_EACH; ++j) {
+            const uint32_t c = bins.count(s, j, zeros);
+            if (c > 0) weight += scale.of(bins.value(j)) * c;
+        }
     }
     const SampleSums sums = sample_sums(s, weight, count, tid);
     if (sums.count < (uint32_t)V && scale.live(VALUE_FAR)) return false;
-    // the bin that a question leads to: what is before it, and in it
-    const auto locate = [&](bool by_count, uint64_t need) {
+    // The bin that a question leads to: one thread has it among its own, and every wave looks for it there, a lane a bin.
+    struct Place {
+        float value;
+        uint64_t before_weight, weight;
+        uint32_t before_count;
+    };
+    const auto locate = [&](int question, bool by_count, uint64_t need) {
         const uint64_t lo = by_count ? sums.before_count : sums.before_weight, hi = lo + (by_count ? count : weight);
         if (lo < need && need <= hi) {
-            uint64_t bw = sums.before_weight;
-            uint32_t bc = sums.before_count;
-            bool found = false;
-#pragma unroll
-            for (int j = 0; j < VALUE_EACH; ++j) {
-                if (!found && need <= (by_count ? bc + c[j] : bw + w[j] * c[j])) {
-                    found = true;
-                    s.bin = tid * VALUE_EACH + j;
-                    s.before_weight = bw;
-                    s.before_count = bc;
-                    s.weight = w[j];
-                }
-                bw += w[j] * c[j];
-                bc += c[j];
-            }
+            s.asked[question].thread = tid;
+            s.asked[question].before_weight = sums.before_weight;
+            s.asked[question].before_count = sums.before_count;
         }
         __syncthreads();
+        const int lane = tid & 63;
+        const ValueBins its(__builtin_amdgcn_readfirstlane(s.asked[question].thread));
+        const float x = its.value(lane);
+        const uint32_t c = its.count(s, lane, zeros);
+        const uint64_t w = c > 0 ? scale.of(x) : 0;
+        const uint64_t upto_weight = s.asked[question].before_weight + wave_sums_u64(w * c);
+        const uint32_t upto_count = s.asked[question].before_count + (uint32_t)wave_inclusive_scan((int)c);
+        const int found = __ffsll((unsigned long long)__ballot(need <= (by_count ? upto_count : upto_weight))) - 1;
+        return Place{__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), found)), lane_of_u64(upto_weight - w * c, found), lane_of_u64(w, found),
+                     (uint32_t)__builtin_amdgcn_readlane((int)(upto_count - c), found)};
     };
     uint64_t kept = sums.weight;
     if (how.top_k > 0 && (uint32_t)how.top_k < sums.count) {
-        locate(true, (uint64_t)how.top_k);
-        kept = s.before_weight + (uint64_t)((uint32_t)how.top_k - s.before_count) * s.weight;
-        __syncthreads();
+        const Place p = locate(0, true, (uint64_t)how.top_k);
+        kept = p.before_weight + (uint64_t)((uint32_t)how.top_k - p.before_count) * p.weight;
     }
     if (how.top_p < 1.f) {
         const uint64_t need = how.share(kept);
         if (need <= SAMPLE_ONE) {
             kept = SAMPLE_ONE;
         } else {
-            locate(false, need);
-            kept = s.before_weight + (need - s.before_weight + s.weight - 1) / s.weight * s.weight;
-            __syncthreads();
+            const Place p = locate(1, false, need);
+            kept = p.before_weight + (uint64_t)(sample_quotient(need - p.before_weight - 1, p.weight) + 1) * p.weight;
         }
     }
     if (how.min_p > 0.f) {
         const uint64_t least = how.least();
         uint64_t sum = 0;
-#pragma unroll
-        for (int j = 0; j < VALUE_EACH; ++j) sum += w[j] >= least ? w[j] * c[j] : 0;
+#pragma unroll 1
+        for (int j = 0; j < VALUE_EACH; ++j) {
+            const uint32_t c = bins.count(s, j, zeros);
+            const uint64_t w = c > 0 ? scale.of(bins.value(j)) : 0;
+            sum += w >= least ? w * c : 0;
+        }
         kept = min(kept, sample_sum(s, sum, tid));
     }
     const uint64_t goal = how.goal(kept);
-    locate(false, goal + 1);
-    const float x = value_of_bin(s.bin);
-    const uint32_t which = (uint32_t)((goal - s.before_weight) / s.weight);
+    const Place p = locate(2, false, goal + 1);
+    const float x = p.value;
+    const uint32_t which = sample_quotient(goal - p.before_weight, p.weight);
     if (tid == 0 && logp != nullptr) *logp = (float)(((double)x - scale.top) / (double)how.temperature - log((double)kept / SAMPLE_UNIT));
-    sample_index(s, row, V, which, tid, [&](float v) { return v == x; }, answer);
+    sample_index(s, row, V, which, tid, x, answer);
     return true;
 }
 
@@ -351,22 +507,19 @@ template <typename W>
 __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, int V, const SampleHow &how, int tid, int32_t *answer, float *logp)
 {
     const int lane = tid & 63, wave = tid >> 6;
-    // the first token of the order, and the smallest finite logit
-    uint64_t best = 0;
-    uint32_t low = 0xffffffffu;
     __syncthreads();
-    each_logit(row, V, tid, SAMPLE_THREADS, [&](float x, int i) {
-        const uint64_t key = best_key(x, i);
-        best = key > best ? key : best;
-        const uint32_t o = (uint32_t)(key >> 32);
-        low = o > best_order(-INFINITY) && o < low ? o : low;
+    float top = -INFINITY, low = INFINITY;
+    bool nan = false;
+    each_logit<4>(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
+        top = fmaxf(top, x);
+        low = fminf(low, x);
+        nan = nan || x != x;
     });
-    best = wave_max_u64(best);
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, m));
+    top = group_max<6>(top);
+    low = -group_max<6>(-low);
     if (lane == 0) {
-        s.wave_key[wave] = best;
-        s.wave_low[wave] = low;
+        s.wave_low[wave] = __float_as_uint(low);
+        s.wave_count[wave] = __float_as_uint(top);
     }
     const auto clear = [&] {
 #pragma unroll
@@ -378,25 +531,24 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
     };
     clear();
     for (int w = 0; w < SAMPLE_WAVES; ++w) {
-        best = s.wave_key[w] > best ? s.wave_key[w] : best;
-        low = min(low, s.wave_low[w]);
+        top = fmaxf(top, __uint_as_float(s.wave_count[w]));
+        low = fminf(low, __uint_as_float(s.wave_low[w]));
     }
-    const uint32_t top_order = (uint32_t)(best >> 32);
-    const bool none = top_order == best_order(-INFINITY);
-    if (none || top_order >= best_order(INFINITY) || !(how.temperature > 0.f)) {
-        if (tid == 0) {
-            *answer = none ? -1 : best_index(best);
-            if (logp != nullptr) *logp = none ? -INFINITY : 0.f;
-        }
+    nan = __syncthreads_or(nan);
+    const bool none = !nan && top == -INFINITY;
+    if (nan || none || top == INFINITY || how.first) {
+        if (tid == 0 && logp != nullptr) *logp = none ? -INFINITY : 0.f;
+        if (none && tid == 0) *answer = -1;
+        if (!none) sample_index(s, row, V, 0, tid, nan ? NAN : top, answer);
         return;
     }
-    const float top = of_order(top_order);
     const SampleScale scale(top, how.temperature);
     // Bins over the values that have a weight, or over all if these lie closer.
-    const float range = fminf(scale.zero, top - of_order(low)), per = range > 0.f ? fminf(SAMPLE_BINS / range, 3e38f) : 0.f;
-    const auto bin_of = [&](float x) { return (int)fminf((top - x) * per, SAMPLE_BINS - 1.f); };
+    const float range = fminf(scale.zero, top - low), per = range > 0.f ? fminf(SAMPLE_BINS / range, 3e38f) : 0.f;
+    const auto place_of = [&](float x) { return fminf((top - x) * per, SAMPLE_BINS - 1.f); };
+    const auto bin_of = [&](float x) { return (int)place_of(x); };
     const bool counted = how.top_k > 0 && how.top_k < V;
-    each_logit(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
+    each_logit<4>(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
         if (counted) atomicAdd(&s.bin_count[bin_of(x)], 1u);
         if (scale.live(x)) atomicAdd(reinterpret_cast<unsigned long long *>(&s.bin_weight[bin_of(x)]), (unsigned long long)scale.of(x));
     });
@@ -451,11 +603,13 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
         if (tid == 0) s.listed = 0;
         find(sums, w, c, weight, count, by_count, need);
         const int bin = s.bin;
+        const float from = (float)bin, to = from + 1.f;
         uint64_t before_weight = s.before_weight;
         uint32_t before_count = s.before_count;
         uint32_t lo = 0xffffffffu, hi = 0;
-        each_logit(row, V, tid, SAMPLE_THREADS, [&](float x, int i) {
-            if (bin_of(x) != bin) return;
+        each_logit<4>(row, V, tid, SAMPLE_THREADS, [&](float x, int i) {
+            const float place = place_of(x);
+            if (place < from || place >= to) return;
             const uint64_t key = best_key(x, i);
             lo = min(lo, (uint32_t)(key >> 32));
             hi = max(hi, (uint32_t)(key >> 32));
@@ -506,7 +660,7 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
         while (lo < hi) {
             const int shift = max(0, 32 - __clz(hi - lo) - 12);
             clear();
-            each_logit(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
+            each_logit<4>(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
                 const uint32_t o = best_order(x);
                 if (o < lo || o > hi || bin_of(x) != bin) return;
                 atomicAdd(&s.bin_count[(hi - o) >> shift], 1u);
@@ -527,7 +681,7 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
             __syncthreads();
         }
         const uint64_t each = scale.of(of_order(hi));
-        const uint64_t tokens = by_count ? need - before_count : (need - before_weight + each - 1) / each;
+        const uint64_t tokens = by_count ? need - before_count : sample_quotient(need - before_weight - 1, each) + 1;
         return Place{before_weight + tokens * each, hi, -1, (uint32_t)(tokens - 1)};
     };
 
@@ -539,8 +693,11 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
     }
     if (how.min_p > 0.f) {
         const uint64_t least = how.least();
+        // no weight behind that is so large: ln(2^44 / (least - 1/2)) and some more
+        const float reach = (31.3f - logf((float)least)) * 1.001f * how.temperature;
         uint64_t sum = 0;
-        each_logit(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
+        each_logit<4>(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
+            if (top - x > reach) return;
             const uint64_t w = scale.of(x);
             sum += w >= least ? w : 0;
         });
@@ -551,22 +708,33 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
         if (logp != nullptr) *logp = (float)(((double)of_order(p.order) - (double)top) / (double)how.temperature - log((double)kept / SAMPLE_UNIT));
         if (p.index >= 0) *answer = p.index;
     }
-    if (p.index < 0) sample_index(s, row, V, p.which, tid, [&](float v) { return best_order(v) == p.order; }, answer);
+    if (p.index < 0) sample_index(s, row, V, p.which, tid, of_order(p.order), answer);
 }
 
-// One block a row.
-template <typename W>
-__global__ __launch_bounds__(SAMPLE_THREADS) void k_sample(SampleArgs A)
+// One block a row.  WAYS: by value, and by range where that does not do (one launch); by value only, and SAMPLE_LATER for such a row;
+// by range only, the rows that were left.
+constexpr int SAMPLE_LATER = -2;
+enum class SampleWays { ALL, VALUE, LEFT };
+template <typename W, SampleWays WAYS>
+__device__ __forceinline__ void sample_row(SampleShared &s, const SampleArgs &A)
+{
+    const int tid = threadIdx.x, t = blockIdx.x;
+    if (WAYS == SampleWays::LEFT && A.answers[t] != SAMPLE_LATER) return;
+    const W *row = static_cast<const W *>(A.logits) + (int64_t)t * A.stride;
+    const float temperature = A.temperature != nullptr ? A.temperature[t] : 1.f;
+    const SampleHow how{temperature, A.top_p != nullptr ? A.top_p[t] : 1.f, A.min_p != nullptr ? A.min_p[t] : 0.f, A.u[t], A.top_k != nullptr ? A.top_k[t] : 0,
+                        !(temperature > 0.f)};
+    float *logp = A.logp != nullptr ? A.logp + t : nullptr;
+    if constexpr (sizeof(W) == 2 && WAYS != SampleWays::LEFT)
+        if (sample_by_value(s, row, A.V, how, tid, A.answers + t, logp)) return;
+    if constexpr (WAYS != SampleWays::VALUE) sample_by_range(s, row, A.V, how, tid, A.answers + t, logp);
+    else if (tid == 0) A.answers[t] = SAMPLE_LATER;
+}
+template <typename W, SampleWays WAYS>
+__global__ __launch_bounds__(SAMPLE_THREADS, WAYS == SampleWays::VALUE ? 8 : 4) void k_sample(SampleArgs A)
 {
     __shared__ SampleShared s;
-    const int tid = threadIdx.x, t = blockIdx.x;
-    const W *row = static_cast<const W *>(A.logits) + (int64_t)t * A.stride;
-    const SampleHow how{A.temperature != nullptr ? A.temperature[t] : 1.f, A.top_p != nullptr ? A.top_p[t] : 1.f, A.min_p != nullptr ? A.min_p[t] : 0.f, A.u[t],
-                        A.top_k != nullptr ? A.top_k[t] : 0};
-    float *logp = A.logp != nullptr ? A.logp + t : nullptr;
-    if constexpr (sizeof(W) == 2)
-        if (how.temperature > 0.f && sample_by_value(s, row, A.V, how, tid, A.answers + t, logp)) return;
-    sample_by_range(s, row, A.V, how, tid, A.answers + t, logp);
+    sample_row<W, WAYS>(s, A);
 }
 
 }  // namespace svdp

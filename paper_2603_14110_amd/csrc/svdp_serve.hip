@@ -26,6 +26,8 @@ void launch_rope(const RopeArgs &A, bool inter, bool norm, dim3 grid, hipStream_
     else norm ? with(std::false_type{}, std::true_type{}) : with(std::false_type{}, std::false_type{});
 }
 
+constexpr int SAMPLE_ONE_LAUNCH = 256;
+
 }  // namespace
 
 extern "C" {
@@ -112,8 +114,15 @@ svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32
         const SampleArgs A{static_cast<const char *>(logits) + (int64_t)t * stride * bytes_of(dtype), stride, from(u), from(temperature), from(top_k),
                            from(top_p), from(min_p), from(answers), from(logp), V};
         const dim3 grid(std::min(T - t, ROWS));
-        if (dtype == SVDP_F32) launch(k_sample<float>, grid, dim3(SAMPLE_THREADS), 0, hs, A);
-        else launch(k_sample<bf16>, grid, dim3(SAMPLE_THREADS), 0, hs, A);
+        const auto with = [&](auto kernel) { launch(kernel, grid, dim3(SAMPLE_THREADS), 0, hs, A); };
+        if (dtype == SVDP_F32) {
+            with(k_sample<float, SampleWays::ALL>);
+        } else if (T <= SAMPLE_ONE_LAUNCH) {
+            with(k_sample<bf16, SampleWays::ALL>);
+        } else {
+            with(k_sample<bf16, SampleWays::VALUE>);
+            with(k_sample<bf16, SampleWays::LEFT>);
+        }
     }
     return hip_status(hipSuccess);
 }
