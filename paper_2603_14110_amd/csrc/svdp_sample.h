@@ -21,26 +21,30 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "svdp_device.h"
 #include "svdp_order.h"
 
 namespace svdp {
 
+constexpr int SAMPLE_MAX_V = 1 << 19;
 constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = SAMPLE_THREADS / 64;
 constexpr int SAMPLE_EACH = 4, SAMPLE_BINS = SAMPLE_THREADS * SAMPLE_EACH;
 constexpr int SAMPLE_LIST = 768;                            // elements of a bin that are ordered by comparing all with all
 constexpr double SAMPLE_UNIT = 17592186044416.0;            // 2^44
 constexpr float SAMPLE_ZERO = 31.5f;                        // (top - x) / temperature from which weights are 0: 45 ln 2 = 31.19
-constexpr int SAMPLE_MAX_V = 1 << 19;
 
 // Bins of bf16 values, the largest first: magnitudes (bits without sign) from VALUE_LOW on, VALUE_SPAN of them; zero; then negative ones.
 constexpr int VALUE_LOW = (127 - 30) << 7, VALUE_HIGH = (127 + 8) << 7, VALUE_SPAN = VALUE_HIGH - VALUE_LOW;
-constexpr int VALUE_HALF = SAMPLE_THREADS / 2, VALUE_EACH = (VALUE_SPAN + VALUE_HALF - 1) / VALUE_HALF;      // threads of a sign; bins of a thread
-static_assert(VALUE_EACH * (VALUE_HALF - 1) >= VALUE_SPAN, "the last thread of the positive ones has zero");
 constexpr float VALUE_FAR = -256.f;                         // what lies at or below it has no bin
 // In LDS: counters of positive magnitudes, then of negative ones, each followed by one a lane for all that has no bin: lanes do
 // not meet there, whatever a row is filled up with.
+// A counter's lower bits are the count; the upper ones are the sum of the places of what was counted, in pieces of the row: where the
+// count is one, the piece that has the element.
 constexpr int VALUE_OTHER = 64, VALUE_SIDE = VALUE_SPAN + VALUE_OTHER;
+constexpr int VALUE_COUNT = 20, VALUE_PIECE = 16;           // bits of the count; 16-byte vectors of a piece
+static_assert(SAMPLE_MAX_V < 1 << VALUE_COUNT && SAMPLE_MAX_V / 8 / VALUE_PIECE <= 1 << (32 - VALUE_COUNT));
 static_assert(4 * 2 * VALUE_SIDE < 65536, "addresses of counters are halves of a word");
 
 typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
@@ -129,27 +133,36 @@ struct SampleScale {
     __device__ __forceinline__ uint64_t of(float x) const { return live(x) ? sample_weight(((double)x - top) * per) : 0; }
 };
 
-struct SampleShared {
-    union {
-        uint32_t values[2 * VALUE_SIDE];
-        struct {
-            uint64_t bin_weight[SAMPLE_BINS];
-            uint32_t bin_count[SAMPLE_BINS];
-            uint64_t list[SAMPLE_LIST], list_weight[SAMPLE_LIST];
-        };
-    };
-    uint64_t wave_weight[SAMPLE_WAVES], wave_key[SAMPLE_WAVES];
-    uint32_t wave_count[SAMPLE_WAVES], wave_low[SAMPLE_WAVES];
-    // what the thread that a question leads to answers
-    uint64_t before_weight, key;
-    uint32_t before_count, count, listed;
-    int bin;
+// What the threads of a row share.
+template <int THREADS>
+struct SampleWaveSums {
+    static constexpr int WAVES = THREADS / 64;
+    uint64_t weight[WAVES];
+    uint32_t count[WAVES], low[WAVES];
+};
+template <int THREADS>
+struct SampleValues {
+    uint32_t values[2 * VALUE_SIDE];
+    SampleWaveSums<THREADS> waves;
+    uint32_t zeros;
+    // where a question leads to, of three a row: the thread, and what is before its bins
     struct {
         uint64_t before_weight;
         uint32_t before_count;
         int thread;
-    } asked[3];                             // of three questions a row
+    } asked[3];
 };
+struct SampleBins {
+    uint64_t weight[SAMPLE_BINS];
+    uint32_t count[SAMPLE_BINS];
+    uint64_t list[SAMPLE_LIST], list_weight[SAMPLE_LIST];
+    SampleWaveSums<SAMPLE_THREADS> waves;
+    // what the thread that a question leads to answers
+    uint64_t before_weight, key;
+    uint32_t before_count, listed;
+    int bin;
+};
+static_assert(sizeof(SampleBins) <= 64 << 10 && 4 * sizeof(SampleValues<512>) <= 160 << 10);
 
 // Inclusive sums over a wave, as wave_inclusive_scan.
 template <int CTRL, int ROW_MASK, int BANK_MASK>
@@ -185,26 +198,29 @@ struct SampleSums {
     uint64_t before_weight, weight;
     uint32_t before_count, count;
 };
-__device__ __forceinline__ SampleSums sample_sums(SampleShared &s, uint64_t weight, uint32_t count, int tid)
+template <int THREADS>
+__device__ __forceinline__ SampleSums sample_sums(SampleWaveSums<THREADS> &s, uint64_t weight, uint32_t count, int tid)
 {
+    constexpr int WAVES = THREADS / 64;
     const int lane = tid & 63, wave = tid >> 6;
     const uint64_t w = wave_sums_u64(weight);
     const uint32_t c = (uint32_t)wave_inclusive_scan((int)count);
     if (lane == 63) {
-        s.wave_weight[wave] = w;
-        s.wave_count[wave] = c;
+        s.weight[wave] = w;
+        s.count[wave] = c;
     }
     __syncthreads();
     // the waves' sums, a lane each
-    const uint64_t each_weight = lane < SAMPLE_WAVES ? s.wave_weight[lane] : 0, upto_weight = wave_sums_u64(each_weight);
-    const uint32_t each_count = lane < SAMPLE_WAVES ? s.wave_count[lane] : 0, upto_count = (uint32_t)wave_inclusive_scan((int)each_count);
+    const uint64_t each_weight = lane < WAVES ? s.weight[lane] : 0, upto_weight = wave_sums_u64(each_weight);
+    const uint32_t each_count = lane < WAVES ? s.count[lane] : 0, upto_count = (uint32_t)wave_inclusive_scan((int)each_count);
     const int at = __builtin_amdgcn_readfirstlane(wave);
     const SampleSums r{w - weight + lane_of_u64(upto_weight - each_weight, at), lane_of_u64(upto_weight, 63),
                        c - count + (uint32_t)__builtin_amdgcn_readlane((int)(upto_count - each_count), at), (uint32_t)__builtin_amdgcn_readlane((int)upto_count, 63)};
     __syncthreads();
     return r;
 }
-__device__ __forceinline__ uint64_t sample_sum(SampleShared &s, uint64_t v, int tid)
+template <int THREADS>
+__device__ __forceinline__ uint64_t sample_sum(SampleWaveSums<THREADS> &s, uint64_t v, int tid)
 {
     return sample_sums(s, v, 0, tid).weight;
 }
@@ -251,14 +267,14 @@ __device__ __forceinline__ bool has_value(const uint4 &in, float x, const bf16 *
     return min(m[0], m[1]) == 0;
 }
 // The index of the which-th element (from 0) of value x: waves take pieces of the row one after the other.
-template <typename W>
-__device__ __forceinline__ void sample_index(SampleShared &s, const W *row, int V, uint32_t which, int tid, float x, int32_t *answer)
+template <int THREADS, typename W>
+__device__ __forceinline__ void sample_index(SampleWaveSums<THREADS> &s, const W *row, int V, uint32_t which, int tid, float x, int32_t *answer)
 {
-    constexpr int VEC = Elem<W>::VEC, AHEAD = 8;
+    constexpr int VEC = Elem<W>::VEC, AHEAD = 8, WAVES = THREADS / 64;
     const int lane = tid & 63, wave = tid >> 6, skew = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / Elem<W>::BYTES);
     const int head = min(skew > 0 ? VEC - skew : 0, V), vectors = (V - head) / VEC, tail = head + vectors * VEC;
-    const int piece = (vectors + SAMPLE_WAVES - 1) / SAMPLE_WAVES, begin = min(wave * piece, vectors), end = min(begin + piece, vectors);
-    const bool first = wave == 0, last = wave == SAMPLE_WAVES - 1;
+    const int piece = (vectors + WAVES - 1) / WAVES, begin = min(wave * piece, vectors), end = min(begin + piece, vectors);
+    const bool first = wave == 0, last = wave == WAVES - 1;
     const auto is_head = [&] { return first && lane < head && same_value<W>(to_f32(row[lane]), x); };
     const auto is_tail = [&] { return last && tail + lane < V && same_value<W>(to_f32(row[tail + lane]), x); };
     const auto bits_of = [&](const uint4 &in) {
@@ -292,12 +308,12 @@ __device__ __forceinline__ void sample_index(SampleShared &s, const W *row, int 
         at = tail + lane;
     }
     const int all = wave_inclusive_scan(mine);
-    if (lane == 63) s.wave_count[wave] = (uint32_t)all;
+    if (lane == 63) s.count[wave] = (uint32_t)all;
     __syncthreads();
     uint32_t before = 0;
-    for (int w = 0; w < wave; ++w) before += s.wave_count[w];
-    if (which < before || which >= before + s.wave_count[wave]) return;
-    if (s.wave_count[wave] == 1) {
+    for (int w = 0; w < wave; ++w) before += s.count[w];
+    if (which < before || which >= before + s.count[wave]) return;
+    if (s.count[wave] == 1) {
         if (mine > 0) *answer = at;
         return;
     }
@@ -333,52 +349,85 @@ __device__ __forceinline__ void sample_index(SampleShared &s, const W *row, int 
     if (lane == 0) *answer = tail + nth(tails, left);
 }
 
+// The index of the only element of value x, which lies in a piece of VALUE_PIECE vectors or at the end of the row beside it: by one wave.
+__device__ __forceinline__ void sample_index_in(const bf16 *row, int V, int piece, int lane, float x, int32_t *answer)
+{
+    const int skew = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / 2), head = min(skew > 0 ? 8 - skew : 0, V), vectors = (V - head) / 8, tail = head + vectors * 8;
+    const int i = piece * VALUE_PIECE + lane;
+    if (lane < VALUE_PIECE && i < vectors) {
+        float v[8];
+        widen(load_raw(row + head + (int64_t)i * 8), v, row);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (v[j] == x) *answer = head + i * 8 + j;
+    }
+    if (lane < head && to_f32(row[lane]) == x) *answer = lane;
+    if (tail + lane < V && to_f32(row[tail + lane]) == x) *answer = tail + lane;
+}
+
 // ---- bf16: one bin a value --------------------------------------------------------------------------------------------------
 
 // A thread's bins, the largest value first: the first half of the threads has the positive ones and, in its last thread, zero.
+template <int THREADS>
 struct ValueBins {
+    static constexpr int HALF = THREADS / 2, EACH = (VALUE_SPAN + HALF - 2) / (HALF - 1);     // threads of a sign; bins of a thread, below 64
+    static_assert(EACH * (HALF - 1) >= VALUE_SPAN && EACH < 64, "the last thread of the positive ones has zero");
     int bits, step, at, n;                  // of the first bin's value, from one to the next; its counter
     bool zero;
     __device__ __forceinline__ ValueBins(int tid)
     {
-        const bool positive = tid < VALUE_HALF;
-        const int first = (positive ? tid : tid - VALUE_HALF) * VALUE_EACH;
+        const bool positive = tid < HALF;
+        const int first = (positive ? tid : tid - HALF) * EACH;
         step = positive ? -1 : 1;
-        zero = tid == VALUE_HALF - 1;
-        n = zero ? 1 : min(max(VALUE_SPAN - first, 0), VALUE_EACH);
+        zero = tid == HALF - 1;
+        n = zero ? 1 : min(max(VALUE_SPAN - first, 0), EACH);
         bits = zero ? 0 : positive ? VALUE_HIGH - 1 - first : 0x8000 + VALUE_LOW + first;
         at = positive ? VALUE_SPAN - 1 - first : VALUE_SIDE + first;
     }
     __device__ __forceinline__ float value(int j) const { return __uint_as_float((uint32_t)(bits + j * step) << 16); }
-    __device__ __forceinline__ uint32_t count(const SampleShared &s, int j, uint32_t zeros) const { return j >= n ? 0u : zero ? zeros : s.values[at + j * step]; }
+    __device__ __forceinline__ uint32_t count(const SampleValues<THREADS> &s, int j, uint32_t zeros) const
+    {
+        return j >= n ? 0u : zero ? zeros : s.values[at + j * step] & ((1u << VALUE_COUNT) - 1);
+    }
+    // the piece of an element that is the only one of its value; -1: not known
+    __device__ __forceinline__ int piece(const SampleValues<THREADS> &s, int j) const
+    {
+        const uint32_t c = zero ? 0u : s.values[at + j * step];
+        return (c & ((1u << VALUE_COUNT) - 1)) == 1 ? (int)(c >> VALUE_COUNT) : -1;
+    }
 };
 // False: the row has to go the other way.
-__device__ __forceinline__ bool sample_by_value(SampleShared &s, const bf16 *row, int V, const SampleHow &how, int tid, int32_t *answer, float *logp)
+template <int THREADS>
+__device__ __forceinline__ bool sample_by_value(SampleValues<THREADS> &s, const bf16 *row, int V, const SampleHow &how, int tid, int32_t *answer, float *logp)
 {
-    for (int i = tid; i < 2 * VALUE_SIDE; i += SAMPLE_THREADS) s.values[i] = 0;
-    if (tid == 0) s.count = 0;
+    using Bins = ValueBins<THREADS>;
+    constexpr int EACH = Bins::EACH;
+    for (int i = tid; i < 2 * VALUE_SIDE; i += THREADS) s.values[i] = 0;
+    if (tid == 0) s.zeros = 0;
     __syncthreads();
     // Two elements at a time, as halves of a word: magnitude from VALUE_LOW on (below it: a large number), up to the lane's own
     // counter for others, plus one side for a sign.
     const uint16_t other = (uint16_t)(VALUE_SPAN + (tid & (VALUE_OTHER - 1)));
-    const auto pair = [&](uint32_t w) {
+    const auto pair = [&](uint32_t w, uint32_t one) {
         const u16x2_t x = __builtin_bit_cast(u16x2_t, w);
         const u16x2_t m = __builtin_elementwise_min((x & (uint16_t)0x7fff) - (uint16_t)VALUE_LOW, u16x2_t{other, other});
         const uint32_t at = __builtin_bit_cast(uint32_t, (m + (x >> 15) * (uint16_t)VALUE_SIDE) << 2);
         char *counters = reinterpret_cast<char *>(s.values);
-        atomicAdd(reinterpret_cast<uint32_t *>(counters + (at & 0xffffu)), 1u);
+        atomicAdd(reinterpret_cast<uint32_t *>(counters + (at & 0xffffu)), one);
         return reinterpret_cast<uint32_t *>(counters + (at >> 16));
     };
-    each_vector<4>(row, V, tid, SAMPLE_THREADS, [&](const uint4 &in, int) {
-        atomicAdd(pair(in.x), 1u);
-        atomicAdd(pair(in.y), 1u);
-        atomicAdd(pair(in.z), 1u);
-        atomicAdd(pair(in.w), 1u);
-    }, [&](float x, int) { pair(__float_as_uint(x) >> 16); });
+    each_vector<4>(row, V, tid, THREADS, [&](const uint4 &in, int i) {
+        // i begins at the row's head, less than a vector: that leaves the quotient by vectors alone
+        const uint32_t one = 1u + ((uint32_t)(i / 8 / VALUE_PIECE) << VALUE_COUNT);
+        atomicAdd(pair(in.x, one), one);
+        atomicAdd(pair(in.y, one), one);
+        atomicAdd(pair(in.z, one), one);
+        atomicAdd(pair(in.w, one), one);
+    }, [&](float x, int) { pair(__float_as_uint(x) >> 16, 1u); });
     __syncthreads();
     // Others: zeros are counted, values far below (-inf among them) have no weight; with any else (small: smaller than VALUE_LOW, but not zero;
     // large or NaN) the row goes the other way.
-    const uint32_t others = tid < VALUE_OTHER ? s.values[VALUE_SPAN + tid] + s.values[VALUE_SIDE + VALUE_SPAN + tid] : 0;
+    const uint32_t others = tid < VALUE_OTHER ? s.values[VALUE_SPAN + tid] | s.values[VALUE_SIDE + VALUE_SPAN + tid] : 0;
     uint32_t zeros = 0;
     if (__syncthreads_or(others > 0)) {
         u16x2_t small = {0xffff, 0xffff}, negative = {0, 0}, nonzero = {0, 0};
@@ -391,7 +440,7 @@ __device__ __forceinline__ bool sample_by_value(SampleShared &s, const bf16 *row
             large = __builtin_elementwise_max(large, __builtin_bit_cast(i16x2_t, x));
             negative = __builtin_elementwise_max(negative, x);
         };
-        each_vector<4>(row, V, tid, SAMPLE_THREADS, [&](const uint4 &in, int) {
+        each_vector<4>(row, V, tid, THREADS, [&](const uint4 &in, int) {
             look(in.x);
             look(in.y);
             look(in.z);
@@ -403,50 +452,56 @@ __device__ __forceinline__ bool sample_by_value(SampleShared &s, const bf16 *row
         });
         const bool odd = min(small[0], small[1]) < VALUE_LOW - 1 || max(large[0], large[1]) >= VALUE_HIGH || max(negative[0], negative[1]) > 0xff80u;
         zeros = (uint32_t)wave_inclusive_scan((int)(elements - nonzero[0] - nonzero[1]));
-        if ((tid & 63) == 63 && zeros > 0) atomicAdd(&s.count, zeros);
+        if ((tid & 63) == 63 && zeros > 0) atomicAdd(&s.zeros, zeros);
         if (__syncthreads_or(odd)) return false;
-        zeros = s.count;
+        zeros = s.zeros;
     }
     // the thread's bins: the largest value that there is, then the weights
-    const ValueBins bins(tid);
+    const Bins bins(tid);
     uint32_t count = 0;
-    int first = SAMPLE_THREADS * VALUE_EACH;
+    int first = THREADS * EACH;
 #pragma unroll
-    for (int j = VALUE_EACH - 1; j >= 0; --j) {
+    for (int j = EACH - 1; j >= 0; --j) {
         const uint32_t c = bins.count(s, j, zeros);
         count += c;
-        first = c > 0 ? tid * VALUE_EACH + j : first;
+        first = c > 0 ? tid * EACH + j : first;
     }
     const uint64_t some = __ballot(count > 0);
     const int lowest = __builtin_amdgcn_readlane(first, some != 0 ? __ffsll((unsigned long long)some) - 1 : 0);       // by all lanes
-    if ((tid & 63) == 0) s.wave_low[tid >> 6] = (uint32_t)lowest;
+    if ((tid & 63) == 0) s.waves.low[tid >> 6] = (uint32_t)lowest;
     __syncthreads();
-    first = (tid & 63) < SAMPLE_WAVES ? (int)s.wave_low[tid & 63] : SAMPLE_THREADS * VALUE_EACH;
-    const uint64_t where = __ballot(first < SAMPLE_THREADS * VALUE_EACH);           // waves' bins are in order
+    first = (tid & 63) < THREADS / 64 ? (int)s.waves.low[tid & 63] : THREADS * EACH;
+    const uint64_t where = __ballot(first < THREADS * EACH);           // waves' bins are in order
     if (where == 0) return false;
     first = __builtin_amdgcn_readlane(first, __ffsll((unsigned long long)where) - 1);
-    const float top = ValueBins(first / VALUE_EACH).value(first % VALUE_EACH);
+    const Bins top_bins(first / EACH);
+    const float top = top_bins.value(first % EACH);
+    const auto answer_with = [&](float x, uint32_t which, int piece) {
+        if (piece < 0) sample_index(s.waves, row, V, which, tid, x, answer);
+        else if (tid < 64) sample_index_in(row, V, piece, tid, x, answer);
+    };
     if (how.first) {
         if (tid == 0 && logp != nullptr) *logp = 0.f;
-        sample_index(s, row, V, 0, tid, top, answer);
+        answer_with(top, 0, __builtin_amdgcn_readfirstlane(top_bins.piece(s, first % EACH)));
         return true;
     }
     const SampleScale scale(top, how.temperature);
     uint64_t weight = 0;
     if (some != 0) {
 #pragma unroll 1
-        for (int j = 0; j < VALUE_EACH; ++j) {
+        for (int j = 0; j < EACH; ++j) {
             const uint32_t c = bins.count(s, j, zeros);
             if (c > 0) weight += scale.of(bins.value(j)) * c;
         }
     }
-    const SampleSums sums = sample_sums(s, weight, count, tid);
+    const SampleSums sums = sample_sums(s.waves, weight, count, tid);
     if (sums.count < (uint32_t)V && scale.live(VALUE_FAR)) return false;
     // The bin that a question leads to: one thread has it among its own, and every wave looks for it there, a lane a bin.
     struct Place {
         float value;
         uint64_t before_weight, weight;
         uint32_t before_count;
+        int piece;
     };
     const auto locate = [&](int question, bool by_count, uint64_t need) {
         const uint64_t lo = by_count ? sums.before_count : sums.before_weight, hi = lo + (by_count ? count : weight);
@@ -457,7 +512,7 @@ __device__ __forceinline__ bool sample_by_value(SampleShared &s, const bf16 *row
         }
         __syncthreads();
         const int lane = tid & 63;
-        const ValueBins its(__builtin_amdgcn_readfirstlane(s.asked[question].thread));
+        const Bins its(__builtin_amdgcn_readfirstlane(s.asked[question].thread));
         const float x = its.value(lane);
         const uint32_t c = its.count(s, lane, zeros);
         const uint64_t w = c > 0 ? scale.of(x) : 0;
@@ -465,7 +520,7 @@ __device__ __forceinline__ bool sample_by_value(SampleShared &s, const bf16 *row
         const uint32_t upto_count = s.asked[question].before_count + (uint32_t)wave_inclusive_scan((int)c);
         const int found = __ffsll((unsigned long long)__ballot(need <= (by_count ? upto_count : upto_weight))) - 1;
         return Place{__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), found)), lane_of_u64(upto_weight - w * c, found), lane_of_u64(w, found),
-                     (uint32_t)__builtin_amdgcn_readlane((int)(upto_count - c), found)};
+                     (uint32_t)__builtin_amdgcn_readlane((int)(upto_count - c), found), __builtin_amdgcn_readfirstlane(its.piece(s, found))};
     };
     uint64_t kept = sums.weight;
     if (how.top_k > 0 && (uint32_t)how.top_k < sums.count) {
@@ -485,26 +540,26 @@ __device__ __forceinline__ bool sample_by_value(SampleShared &s, const bf16 *row
         const uint64_t least = how.least();
         uint64_t sum = 0;
 #pragma unroll 1
-        for (int j = 0; j < VALUE_EACH; ++j) {
+        for (int j = 0; j < EACH; ++j) {
             const uint32_t c = bins.count(s, j, zeros);
             const uint64_t w = c > 0 ? scale.of(bins.value(j)) : 0;
             sum += w >= least ? w * c : 0;
         }
-        kept = min(kept, sample_sum(s, sum, tid));
+        kept = min(kept, sample_sum(s.waves, sum, tid));
     }
     const uint64_t goal = how.goal(kept);
     const Place p = locate(2, false, goal + 1);
     const float x = p.value;
     const uint32_t which = sample_quotient(goal - p.before_weight, p.weight);
     if (tid == 0 && logp != nullptr) *logp = (float)(((double)x - scale.top) / (double)how.temperature - log((double)kept / SAMPLE_UNIT));
-    sample_index(s, row, V, which, tid, x, answer);
+    answer_with(x, which, p.piece);
     return true;
 }
 
 // ---- any values -------------------------------------------------------------------------------------------------------------
 
 template <typename W>
-__device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, int V, const SampleHow &how, int tid, int32_t *answer, float *logp)
+__device__ __forceinline__ void sample_by_range(SampleBins &s, const W *row, int V, const SampleHow &how, int tid, int32_t *answer, float *logp)
 {
     const int lane = tid & 63, wave = tid >> 6;
     __syncthreads();
@@ -518,28 +573,28 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
     top = group_max<6>(top);
     low = -group_max<6>(-low);
     if (lane == 0) {
-        s.wave_low[wave] = __float_as_uint(low);
-        s.wave_count[wave] = __float_as_uint(top);
+        s.waves.low[wave] = __float_as_uint(low);
+        s.waves.count[wave] = __float_as_uint(top);
     }
     const auto clear = [&] {
 #pragma unroll
         for (int j = 0; j < SAMPLE_EACH; ++j) {
-            s.bin_weight[j * SAMPLE_THREADS + tid] = 0;
-            s.bin_count[j * SAMPLE_THREADS + tid] = 0;
+            s.weight[j * SAMPLE_THREADS + tid] = 0;
+            s.count[j * SAMPLE_THREADS + tid] = 0;
         }
         __syncthreads();
     };
     clear();
     for (int w = 0; w < SAMPLE_WAVES; ++w) {
-        top = fmaxf(top, __uint_as_float(s.wave_count[w]));
-        low = fminf(low, __uint_as_float(s.wave_low[w]));
+        top = fmaxf(top, __uint_as_float(s.waves.count[w]));
+        low = fminf(low, __uint_as_float(s.waves.low[w]));
     }
     nan = __syncthreads_or(nan);
     const bool none = !nan && top == -INFINITY;
     if (nan || none || top == INFINITY || how.first) {
         if (tid == 0 && logp != nullptr) *logp = none ? -INFINITY : 0.f;
         if (none && tid == 0) *answer = -1;
-        if (!none) sample_index(s, row, V, 0, tid, nan ? NAN : top, answer);
+        if (!none) sample_index(s.waves, row, V, 0, tid, nan ? NAN : top, answer);
         return;
     }
     const SampleScale scale(top, how.temperature);
@@ -549,8 +604,8 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
     const auto bin_of = [&](float x) { return (int)place_of(x); };
     const bool counted = how.top_k > 0 && how.top_k < V;
     each_logit<4>(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
-        if (counted) atomicAdd(&s.bin_count[bin_of(x)], 1u);
-        if (scale.live(x)) atomicAdd(reinterpret_cast<unsigned long long *>(&s.bin_weight[bin_of(x)]), (unsigned long long)scale.of(x));
+        if (counted) atomicAdd(&s.count[bin_of(x)], 1u);
+        if (scale.live(x)) atomicAdd(reinterpret_cast<unsigned long long *>(&s.weight[bin_of(x)]), (unsigned long long)scale.of(x));
     });
     __syncthreads();
 
@@ -583,14 +638,14 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
         count = 0;
 #pragma unroll
         for (int j = 0; j < SAMPLE_EACH; ++j) {
-            w[j] = s.bin_weight[tid * SAMPLE_EACH + j];
-            c[j] = s.bin_count[tid * SAMPLE_EACH + j];
+            w[j] = s.weight[tid * SAMPLE_EACH + j];
+            c[j] = s.count[tid * SAMPLE_EACH + j];
             weight += w[j];
             count += c[j];
         }
     };
     read(w, c, weight, count);
-    const SampleSums sums = sample_sums(s, weight, count, tid);
+    const SampleSums sums = sample_sums(s.waves, weight, count, tid);
 
     // The token that a question leads to: weight up to it and with it, and its key (order, and index in reverse); by_index: the index is needed.
     struct Place {
@@ -648,13 +703,13 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
             hi = max(hi, (uint32_t)__shfl_xor((int)hi, m));
         }
         if (lane == 0) {
-            s.wave_low[wave] = lo;
-            s.wave_count[wave] = hi;
+            s.waves.low[wave] = lo;
+            s.waves.count[wave] = hi;
         }
         __syncthreads();
         for (int i = 0; i < SAMPLE_WAVES; ++i) {
-            lo = min(lo, s.wave_low[i]);
-            hi = max(hi, s.wave_count[i]);
+            lo = min(lo, s.waves.low[i]);
+            hi = max(hi, s.waves.count[i]);
         }
         __syncthreads();
         while (lo < hi) {
@@ -663,14 +718,14 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
             each_logit<4>(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
                 const uint32_t o = best_order(x);
                 if (o < lo || o > hi || bin_of(x) != bin) return;
-                atomicAdd(&s.bin_count[(hi - o) >> shift], 1u);
-                if (scale.live(x)) atomicAdd(reinterpret_cast<unsigned long long *>(&s.bin_weight[(hi - o) >> shift]), (unsigned long long)scale.of(x));
+                atomicAdd(&s.count[(hi - o) >> shift], 1u);
+                if (scale.live(x)) atomicAdd(reinterpret_cast<unsigned long long *>(&s.weight[(hi - o) >> shift]), (unsigned long long)scale.of(x));
             });
             __syncthreads();
             uint64_t w[SAMPLE_EACH], weight;
             uint32_t c[SAMPLE_EACH], count;
             read(w, c, weight, count);
-            SampleSums inner = sample_sums(s, weight, count, tid);
+            SampleSums inner = sample_sums(s.waves, weight, count, tid);
             inner.before_weight += before_weight;
             inner.before_count += before_count;
             find(inner, w, c, weight, count, by_count, need);
@@ -701,23 +756,33 @@ __device__ __forceinline__ void sample_by_range(SampleShared &s, const W *row, i
             const uint64_t w = scale.of(x);
             sum += w >= least ? w : 0;
         });
-        kept = min(kept, sample_sum(s, sum, tid));
+        kept = min(kept, sample_sum(s.waves, sum, tid));
     }
     const Place p = locate(false, how.goal(kept) + 1);
     if (tid == 0) {
         if (logp != nullptr) *logp = (float)(((double)of_order(p.order) - (double)top) / (double)how.temperature - log((double)kept / SAMPLE_UNIT));
         if (p.index >= 0) *answer = p.index;
     }
-    if (p.index < 0) sample_index(s, row, V, p.which, tid, of_order(p.order), answer);
+    if (p.index < 0) sample_index(s.waves, row, V, p.which, tid, of_order(p.order), answer);
 }
 
 // One block a row.  WAYS: by value, and by range where that does not do (one launch); by value only, and SAMPLE_LATER for such a row;
 // by range only, the rows that were left.
 constexpr int SAMPLE_LATER = -2;
 enum class SampleWays { ALL, VALUE, LEFT };
+constexpr int VALUE_THREADS = 512;
 template <typename W, SampleWays WAYS>
-__device__ __forceinline__ void sample_row(SampleShared &s, const SampleArgs &A)
+constexpr int sample_threads() { return WAYS == SampleWays::VALUE ? VALUE_THREADS : SAMPLE_THREADS; }
+template <typename W, SampleWays WAYS>
+__global__ __launch_bounds__((sample_threads<W, WAYS>()), WAYS == SampleWays::VALUE ? 8 : 4) void k_sample(SampleArgs A)
 {
+    constexpr int THREADS = sample_threads<W, WAYS>();
+    constexpr bool BY_VALUE = sizeof(W) == 2 && WAYS != SampleWays::LEFT, BY_RANGE = WAYS != SampleWays::VALUE;
+    union Shared {
+        SampleValues<BY_VALUE ? THREADS : 64> values;
+        SampleBins bins;
+    };
+    __shared__ std::conditional_t<BY_VALUE && BY_RANGE, Shared, std::conditional_t<BY_VALUE, SampleValues<THREADS>, SampleBins>> s;
     const int tid = threadIdx.x, t = blockIdx.x;
     if (WAYS == SampleWays::LEFT && A.answers[t] != SAMPLE_LATER) return;
     const W *row = static_cast<const W *>(A.logits) + (int64_t)t * A.stride;
@@ -725,16 +790,13 @@ __device__ __forceinline__ void sample_row(SampleShared &s, const SampleArgs &A)
     const SampleHow how{temperature, A.top_p != nullptr ? A.top_p[t] : 1.f, A.min_p != nullptr ? A.min_p[t] : 0.f, A.u[t], A.top_k != nullptr ? A.top_k[t] : 0,
                         !(temperature > 0.f)};
     float *logp = A.logp != nullptr ? A.logp + t : nullptr;
-    if constexpr (sizeof(W) == 2 && WAYS != SampleWays::LEFT)
-        if (sample_by_value(s, row, A.V, how, tid, A.answers + t, logp)) return;
-    if constexpr (WAYS != SampleWays::VALUE) sample_by_range(s, row, A.V, how, tid, A.answers + t, logp);
-    else if (tid == 0) A.answers[t] = SAMPLE_LATER;
-}
-template <typename W, SampleWays WAYS>
-__global__ __launch_bounds__(SAMPLE_THREADS, WAYS == SampleWays::VALUE ? 8 : 4) void k_sample(SampleArgs A)
-{
-    __shared__ SampleShared s;
-    sample_row<W, WAYS>(s, A);
+    if constexpr (BY_VALUE && BY_RANGE) {
+        if (!sample_by_value<THREADS>(s.values, row, A.V, how, tid, A.answers + t, logp)) sample_by_range(s.bins, row, A.V, how, tid, A.answers + t, logp);
+    } else if constexpr (BY_VALUE) {
+        if (!sample_by_value<THREADS>(s, row, A.V, how, tid, A.answers + t, logp) && tid == 0) A.answers[t] = SAMPLE_LATER;
+    } else {
+        sample_by_range(s, row, A.V, how, tid, A.answers + t, logp);
+    }
 }
 
 }  // namespace svdp

@@ -114,14 +114,14 @@ svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32
         const SampleArgs A{static_cast<const char *>(logits) + (int64_t)t * stride * bytes_of(dtype), stride, from(u), from(temperature), from(top_k),
                            from(top_p), from(min_p), from(answers), from(logp), V};
         const dim3 grid(std::min(T - t, ROWS));
-        const auto with = [&](auto kernel) { launch(kernel, grid, dim3(SAMPLE_THREADS), 0, hs, A); };
+        const auto with = [&](auto kernel, int threads) { launch(kernel, grid, dim3(threads), 0, hs, A); };
         if (dtype == SVDP_F32) {
-            with(k_sample<float, SampleWays::ALL>);
+            with(k_sample<float, SampleWays::ALL>, SAMPLE_THREADS);
         } else if (T <= SAMPLE_ONE_LAUNCH) {
-            with(k_sample<bf16, SampleWays::ALL>);
+            with(k_sample<bf16, SampleWays::ALL>, SAMPLE_THREADS);
         } else {
-            with(k_sample<bf16, SampleWays::VALUE>);
-            with(k_sample<bf16, SampleWays::LEFT>);
+            with(k_sample<bf16, SampleWays::VALUE>, VALUE_THREADS);
+            with(k_sample<bf16, SampleWays::LEFT>, SAMPLE_THREADS);
         }
     }
     return hip_status(hipSuccess);
