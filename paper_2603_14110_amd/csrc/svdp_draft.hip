@@ -105,7 +105,7 @@ void on_kernel(const AttnPlan &p, int dt, int dim, F &&f)
     on_dim(dim, [&](auto dc) {
         constexpr int DIM = decltype(dc)::value;
         if constexpr (DIM <= 128)
-            if (p.wide) return f(Type<bf16>{}, dc, WideCut<DIM>{});
+            if (p.wide) return dt == SVDP_E4M3 ? f(Type<e4m3>{}, dc, WideCut<DIM>{}) : f(Type<bf16>{}, dc, WideCut<DIM>{});
         on_cache_type(dt, [&](auto wt) {
             using W = typename decltype(wt)::type;
             if constexpr (DIM <= 128)
@@ -127,7 +127,7 @@ AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, in
     // More than 32 rows: over the waves, 32 each (eight requests of 4096 tokens, 135 MB: 36 and 64 rows 36 us, where k_tree_attn, with
     // two row tiles after each other, takes 48).  At 32 rows k_tree_attn is ahead: 26.4 us for one request of 30 000 tokens and 13.4
     // for 24 of 150, where rows over the waves took 32.0 and 16.6 + 4.4.
-    p.wide = dt == SVDP_BF16 && dim <= 128 && rows > 32;
+    p.wide = dt != SVDP_F32 && dim <= 128 && rows > 32;
     // Two row tiles of 16 read K and V once for 32 rows (8 requests of 4096 tokens, 135 MB: 29.6 us, one after the other 45.2); with
     // 256 channels a second one does not fit the registers.
     p.nt = rows <= 16 || dim == 256 ? 1 : 2;
@@ -281,9 +281,9 @@ svdp_status svdp_tree_attn(const svdp_kv_cache *cache, int32_t layer, const void
         using Cut = decltype(cut);
         constexpr int DIM = decltype(dc)::value;
         if constexpr (Cut::ROWS == TW_ROWS) {
-            granted = grant_lds<k_tree_attn_wide<DIM>>(TW_LDS);
+            granted = grant_lds<k_tree_attn_wide<W, DIM>>(TW_LDS);
             if (!granted) return;
-            launch(k_tree_attn_wide<DIM>, blocks, dim3(TW_THREADS), TW_LDS, hs, A);
+            launch((k_tree_attn_wide<W, DIM>), blocks, dim3(TW_THREADS), TW_LDS, hs, A);
         } else {
             launch((k_tree_attn<W, DIM, Cut::ROWS / 16>), blocks, dim3(TA_THREADS), 0, hs, A);
         }

@@ -37,10 +37,16 @@ __device__ __forceinline__ f32x16_t mfma_32(const uint4 &a, const uint4 &b, cons
 __device__ __forceinline__ int tw_token(int at) { return (at >> 4) * 16 + ((at >> 2) & 1) * 8 + ((at >> 3) & 1) * 4 + (at & 3); }
 __device__ __forceinline__ int tw_swizzle(int token, int dim) { return dim == 64 ? token & 7 : token & 15; }
 
-template <int DIM>
+// A cache in 8 bits: its tiles come into LDS as they are, in two stages of 32 KB, and the block makes bf16 operands of one of them
+// (K and V with their tokens' powers of two, exact) in the 64 KB that the products read, between two barriers.  The tree's own tokens,
+// bf16 as ever, come straight to those 64 KB.
+constexpr int TW_CODED = TW_STAGE / 2, TW_SCALES = 512;         // bytes of a stage: codes; scales of K and of V
+
+template <typename W, int DIM>
 __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_tree_attn_wide(TreeAttnArgs A)
 {
     using X = TreeTile<bf16, DIM>;
+    constexpr bool CODED = sizeof(W) == 1;
     constexpr int TILES = tw_tiles<DIM>(), KC = DIM / 16, DT = DIM / 32, CHUNKS = DIM / 8;
     using Cut = WideCut<DIM>;
     constexpr int TILE_BYTES = TA_TILE * DIM * 2, V_AT = TW_STAGE / 2;
@@ -48,9 +54,11 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
     // a stage of the tree's tokens: K where it always is; V as it comes, then in packs (finite elements), and as it is in packs
     constexpr int OWN_RAW = V_AT, OWN_PACKS = V_AT + TW_STAGE / 4, OWN_ALL = TW_STAGE / 4;
     extern __shared__ __align__(16) char tw_smem[];
+    __shared__ __align__(16) uint8_t s_scales[CODED ? 2 : 1][CODED ? TW_SCALES : 16];     // of a stage's tokens: K's, then V's
     __shared__ uint64_t s_sees[TW_WAVES * 32];                   // what a row sees of its tree
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), f = lane >> 5, m = lane & 31;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t *)tw_smem;
+    const uint32_t scales0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t *)&s_scales[0][0]);
 
     TreeChunk<Cut> chunk;
     const int units = tree_units(A, lane, chunk);
@@ -99,7 +107,36 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
             const auto page_of = [&](int tile) {
                 return __builtin_amdgcn_readlane(window_ids, (min(tile, S.tiles - 1) >> per_page) - window);
             };
+            // codes of a stage: rows of K as they lie, packs of V as they lie; a wave brings 2 KB of each, and one of them the scales
+            const auto fill_coded = [&](int step, int stage) {
+                see_pages(step);
+                const int lane = here(tid) & 63, which = stage == 0 ? 0 : 1;
+                const uint32_t to = lds0 + TW_STAGE + which * TW_CODED;
+                const auto token_at = [&](int tile, int id) {        // the first one of a tile
+                    const int64_t page = (int64_t)((uint32_t)id < (uint32_t)A.pages ? id : 0) * A.heads + h;
+                    return ((page << per_page) + (tile & ((1 << per_page) - 1))) * TA_TILE;
+                };
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int piece = (wave * 2 + i) * 64, per = TA_TILE * DIM / 16;           // pieces of 16 bytes; of a tile
+                    const int tile = min(step * TILES + piece / per, S.tiles - 1);
+                    const int64_t at = token_at(tile, page_of(tile)) * DIM + (piece % per + lane) * 16;
+                    load_to_lds(static_cast<const char *>(A.K) + at, to + piece * 16);
+                    load_to_lds(static_cast<const char *>(A.V) + at, to + TW_CODED / 2 + piece * 16);
+                }
+                // 32 scales of a tile are eight words, a stage's 64 at the most: wave 0 brings K's, wave 1 V's
+                static_assert(TILES * 8 <= 64);
+                if (wave < 2) {
+                    const int tile = min(step * TILES + min(lane / 8, TILES - 1), S.tiles - 1);
+                    const uint8_t *from = (wave == 0 ? A.K_scale : A.V_scale) + token_at(tile, __shfl(window_ids, (tile >> per_page) - window)) + (lane & 7) * 4;
+                    load_words_to_lds(from, scales0 + which * TW_SCALES + wave * (TW_SCALES / 2));
+                }
+            };
             const auto fill = [&](int step, int stage) {
+                if constexpr (CODED) {
+                    fill_coded(step, stage);
+                    return;
+                }
                 see_pages(step);
                 const int tile = min(step * TILES + fill_tile, S.tiles - 1), id = page_of(tile);
                 const int64_t page = (int64_t)((uint32_t)id < (uint32_t)A.pages ? id : 0) * A.heads + h;
@@ -144,6 +181,40 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
 #pragma unroll
                 for (int c = 0; c < KC; ++c) q[c] = load_raw(from + c * 16);
             }
+            // codes of a stage into operands, where a stage of 16 bits would have been filled
+            const auto widen_stage = [&](int stage) {
+                const int which = stage == 0 ? 0 : 1;
+                const char *from = tw_smem + TW_STAGE + which * TW_CODED;
+                for (int p = here(tid); p < TILES * TA_TILE * DIM / 16; p += TW_THREADS) {
+                    constexpr int PER = DIM / 16;                // pieces of 16 channels of a token
+                    const int token = p / PER, piece = p % PER, in_tile = token & (TA_TILE - 1);
+                    const uint4 raw = *reinterpret_cast<const uint4 *>(from + p * 16);
+                    const float by = power_of(s_scales[which][token]);
+                    char *to = tw_smem + token * DIM * 2;
+                    *reinterpret_cast<uint4 *>(to + (((2 * piece) ^ tw_swizzle(in_tile, DIM)) * 16)) = widen_e4m3(raw.x, raw.y, by);
+                    *reinterpret_cast<uint4 *>(to + (((2 * piece + 1) ^ tw_swizzle(in_tile, DIM)) * 16)) = widen_e4m3(raw.z, raw.w, by);
+                }
+                for (int p = here(tid); p < TILES * TA_TILE * DIM / 16; p += TW_THREADS) {
+                    const int pack = p / (DIM / 2);              // two channels of eight tokens
+                    const uint4 raw = *reinterpret_cast<const uint4 *>(from + TW_CODED / 2 + p * 16);
+                    const uint2 scales = *reinterpret_cast<const uint2 *>(&s_scales[which][TW_SCALES / 2 + pack * 8]);
+                    const auto eight = [&](uint32_t a, uint32_t b) {
+                        ta_f32x8 x;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t w = i == 0 ? a : b, s = i == 0 ? scales.x : scales.y;
+                            const auto low = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), high = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+                            x[4 * i] = low[0] * power_of(s & 0xffu);
+                            x[4 * i + 1] = low[1] * power_of((s >> 8) & 0xffu);
+                            x[4 * i + 2] = high[0] * power_of((s >> 16) & 0xffu);
+                            x[4 * i + 3] = high[1] * power_of(s >> 24);
+                        }
+                        return __builtin_bit_cast(uint4, __builtin_convertvector(x, ta_bf16x8));
+                    };
+                    *reinterpret_cast<uint4 *>(tw_smem + V_AT + p * 32) = eight(raw.x, raw.y);
+                    *reinterpret_cast<uint4 *>(tw_smem + V_AT + p * 32 + 16) = eight(raw.z, raw.w);
+                }
+            };
             int stage = 0;
             if (s0 < s_end) {
                 window_ids = here(window_ids);
@@ -177,9 +248,20 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                     }
                 }
                 const auto count_of = [&](int j) { return (int)(counts >> (8 * j)) & 0xff; };
-                if (step + 1 < s_end) fill(step + 1, stage ^ TW_STAGE);
-                else if (step + 1 < s1) fill_own(stage ^ TW_STAGE);
-                char *const lds = tw_smem + stage;
+                if constexpr (CODED) {
+                    if (!own_tokens) {
+                        widen_stage(stage);
+                        if (step + 1 < s_end) fill(step + 1, stage ^ TW_STAGE);
+                        lds_barrier();
+                    } else if (step > s0) {                      // the operands' memory is free only now
+                        fill_own(0);
+                        stage_barrier<0>();
+                    }
+                } else {
+                    if (step + 1 < s_end) fill(step + 1, stage ^ TW_STAGE);
+                    else if (step + 1 < s1) fill_own(stage ^ TW_STAGE);
+                }
+                char *const lds = tw_smem + (CODED ? 0 : stage);
                 const int n_tiles = own_tokens ? (S.n + TA_TILE - 1) / TA_TILE : min(TILES, S.tiles - step * TILES);
                 if (own_tokens) {                                // V into packs
                     int odd = 0;
