@@ -38,8 +38,6 @@ __device__ __forceinline__ uint32_t kv8_codes(float a, float b, float c, float d
     const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, low, true);
 }
-__device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 struct KvArgs {
     void *K, *V;
@@ -93,8 +91,8 @@ struct KvRows {
 };
 
 // Rows [8 blockIdx.x, + 8) of layer blockIdx.y, heads [z / 2 heads_each, + heads_each); even z: K, odd z: V.
-// K: dim / 8 lanes a head, eight channels each.  V: a wave a head; where a pack's eight tokens are rows of the step (prompts) it reads them all, and
-// writes 16 bytes a lane; a token on its own is written byte by byte.
+// K: dim / 8 lanes a head, eight channels each.  V: where a pack's eight tokens are rows of the step (prompts), a wave takes them all; a token
+// on its own is written byte by byte.
 template <int DIM>
 __global__ __launch_bounds__(KV_THREADS) void k_kv_commit8(KvArgs A)
 {
@@ -131,54 +129,69 @@ __global__ __launch_bounds__(KV_THREADS) void k_kv_commit8(KvArgs A)
         return;
     }
     const bf16 *v = static_cast<const bf16 *>(A.v) + layer * A.v_layer + t0 * A.v_row + (int64_t)h0 * DIM;
-    // C channels of a row, quantised; all lanes get the exponent
-    const auto read = [&](int64_t row, int h, float (&x)[C]) {
-        bf16 in[C];
-        __builtin_memcpy(in, __builtin_assume_aligned(v + row * A.v_row + (int64_t)h * DIM + lane * C, sizeof(in)), sizeof(in));
+    // Whole packs: a quarter of the wave has two of the tokens, a lane eight of 128 channels (two heads of 64, or 256 twice), in 16-byte loads;
+    // the quarters then exchange words of two channels and two tokens, so that a lane has all tokens of two channels.
+    constexpr int SIDE = DIM == 64 ? 2 : 1, PIECES = DIM == 256 ? 2 : 1;      // heads, pieces of 128 channels
+    const int g = lane >> 4, c8 = (lane & 15) * 8, side = c8 / DIM, groups = (hn + SIDE - 1) / SIDE;
+    for (int i = wave; i < s.whole * groups; i += KV_WAVES) {
+        const int job = i / groups, h = (i - job * groups) * SIDE + side, row = s.rows[job], channel = c8 - side * DIM;
+        const bf16 *from = v + (int64_t)(row + 2 * g) * A.v_row + (int64_t)min(h, hn - 1) * DIM + channel;
+        uint4 raw[2][PIECES];
 #pragma unroll
-        for (int c = 0; c < C; ++c) x[c] = to_f32(in[c]);
-    };
-    const auto quantise = [&](float (&x)[C]) {
-        float top = 0.f;
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int c = 0; c < C; ++c) top = fmaxf(top, kv8_magnitude(x[c]));
-        const uint32_t by = kv8_exponent(group_max<6>(top));
-        const float inverse = kv8_inverse(by);
+            for (int p = 0; p < PIECES; ++p) raw[t][p] = load_raw(from + t * A.v_row + p * 128);
+        float x[2][PIECES][8];
+        uint32_t by[2];
 #pragma unroll
-        for (int c = 0; c < C; ++c) x[c] = kv8_finite(x[c]) * inverse;
-        return by;
-    };
-    for (int i = wave; i < s.whole * hn; i += KV_WAVES) {
-        const int job = i / hn, h = i - job * hn, row = s.rows[job];
-        float x[E][C];
-        uint32_t by[E];
+        for (int t = 0; t < 2; ++t) {
+            float top = 0.f;
 #pragma unroll
-        for (int t = 0; t < E; ++t) read(row + t, h, x[t]);
+            for (int p = 0; p < PIECES; ++p) {
+                widen(raw[t][p], x[t][p], (const bf16 *)nullptr);
 #pragma unroll
-        for (int t = 0; t < E; ++t) by[t] = quantise(x[t]);
-        uint32_t out[C][2];
+                for (int j = 0; j < 8; ++j) top = fmaxf(top, kv8_magnitude(x[t][p][j]));
+            }
+            by[t] = kv8_exponent(group_max<DIM == 64 ? 3 : 4>(top));
+            const float inverse = kv8_inverse(by[t]);
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+            for (int p = 0; p < PIECES; ++p)
 #pragma unroll
-            for (int w = 0; w < 2; ++w) out[c][w] = kv8_codes(x[4 * w][c], x[4 * w + 1][c], x[4 * w + 2][c], x[4 * w + 3][c]);
-        const int64_t token = token_of(s.slot(row), h0 + h);
-        uint8_t *to = static_cast<uint8_t *>(A.V) + token * DIM + lane * C * E;              // token is the pack's first
-        __builtin_memcpy(__builtin_assume_aligned(to, C == 1 ? 8 : 16), out, sizeof(out));
-        if (lane == 0) {
-            const uint32_t low = by[0] | by[1] << 8 | by[2] << 16 | by[3] << 24, high = by[4] | by[5] << 8 | by[6] << 16 | by[7] << 24;
-            *reinterpret_cast<uint2 *>(A.V_scale + token) = make_uint2(low, high);
+                for (int j = 0; j < 8; ++j) x[t][p][j] = kv8_finite(x[t][p][j]) * inverse;
         }
+        const int64_t token = token_of(s.slot(row), h0 + min(h, hn - 1));                    // the pack's first
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[q] = kv8_codes(x[0][p][2 * q], x[1][p][2 * q], x[0][p][2 * q + 1], x[1][p][2 * q + 1]);
+            const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+            const auto front = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), back = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+            // words of tokens 0 and 1, 2 and 3, 4 and 5, 6 and 7 of channels 2 g and 2 g + 1 of the lane's eight
+            const uint4 out = make_uint4(__builtin_amdgcn_perm(front[1], front[0], 0x05040100u), __builtin_amdgcn_perm(back[1], back[0], 0x05040100u),
+                                         __builtin_amdgcn_perm(front[1], front[0], 0x07060302u), __builtin_amdgcn_perm(back[1], back[0], 0x07060302u));
+            if (h < hn) *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(A.V) + token * DIM + (channel + p * 128 + 2 * g) * E) = out;
+        }
+        if (h < hn && channel == 0) *reinterpret_cast<uint16_t *>(A.V_scale + token + 2 * g) = (uint16_t)(by[0] | by[1] << 8);
     }
+    // tokens on their own: C channels a lane
     for (int i = wave; i < s.alone * hn; i += KV_WAVES) {
         const int job = i / hn, h = i - job * hn, row = s.rows[KV_ROWS - 1 - job];
-        float x[C];
-        read(row, h, x);
-        const uint32_t by = quantise(x);
+        bf16 in[C];
+        __builtin_memcpy(in, __builtin_assume_aligned(v + row * A.v_row + (int64_t)h * DIM + lane * C, sizeof(in)), sizeof(in));
+        float x[C], top = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            x[c] = to_f32(in[c]);
+            top = fmaxf(top, kv8_magnitude(x[c]));
+        }
+        const uint32_t by = kv8_exponent(group_max<6>(top));
+        const float inverse = kv8_inverse(by);
         const int64_t token = token_of(s.slot(row), h0 + h);
         const int in_pack = (int)(token & (E - 1));
         uint8_t *to = static_cast<uint8_t *>(A.V) + (token - in_pack) * DIM + in_pack;
 #pragma unroll
-        for (int c = 0; c < C; ++c) to[(lane * C + c) * E] = (uint8_t)kv8_codes(x[c], 0.f, 0.f, 0.f);
+        for (int c = 0; c < C; ++c) to[(lane * C + c) * E] = (uint8_t)kv8_codes(kv8_finite(x[c]) * inverse, 0.f, 0.f, 0.f);
         if (lane == 0) A.V_scale[token] = (uint8_t)by;
     }
 }

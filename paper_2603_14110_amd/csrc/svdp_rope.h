@@ -2,7 +2,7 @@
 //   y = x / sqrt(mean(x^2) + eps) * weight,   (a, b) -> (a cos - b sin, b cos + a sin),   angle = position * inv_freq[i]
 // for the pairs (a, b) of the first 2 half channels: i and half + i, or (INTER) 2 i and 2 i + 1.  Channels behind them are not turned.
 //
-// A head is dim / 8 lanes with four pairs each, so that both elements of a pair are in a lane, and a wave has 512 / dim heads of one row at
+// A head is dim / 2 P lanes with P pairs each, so that both elements of a pair are in a lane, and a wave has 128 P / dim heads of one row at
 // a time; its angles are computed once.  An angle is taken in turns in 64 bits, of which the whole ones are dropped: positions of a
 // million lose nothing.  All else is fp32, rounded once.
 #pragma once
@@ -25,70 +25,76 @@ struct RopeArgs {
     int64_t q_stride, k_stride, q_out_stride, k_out_stride;
     int T, heads_q, heads, half;
     int q_each, k_each;                     // floats from one head's weights to the next one's
-    int each;                               // rounds of a wave (512 / dim heads each)
+    int each;                               // rounds of a wave (128 P / dim heads each)
     float eps;
 };
 
-template <typename W>
-__device__ __forceinline__ void load_four(const W *p, float (&x)[4])
+template <int N, typename W>
+__device__ __forceinline__ void load_some(const W *p, float (&x)[N])
 {
-    W in[4];
-    __builtin_memcpy(in, __builtin_assume_aligned(p, sizeof(in)), sizeof(in));
+    W in[N];
+    __builtin_memcpy(in, __builtin_assume_aligned(p, sizeof(in) < 16 ? sizeof(in) : 16), sizeof(in));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = to_f32(in[j]);
+    for (int j = 0; j < N; ++j) x[j] = to_f32(in[j]);
 }
-template <typename W>
-__device__ __forceinline__ void store_four(W *p, const float (&x)[4])
+template <int N, typename W>
+__device__ __forceinline__ void store_some(W *p, const float (&x)[N])
 {
-    W out[4];
+    W out[N];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) from_f32(x[j], out + j);
-    __builtin_memcpy(__builtin_assume_aligned(p, sizeof(out)), out, sizeof(out));
+    for (int j = 0; j < N; ++j) from_f32(x[j], out + j);
+    __builtin_memcpy(__builtin_assume_aligned(p, sizeof(out) < 16 ? sizeof(out) : 16), out, sizeof(out));
 }
 
-template <typename W, int DIM, bool INTER, bool NORM>
+template <typename W, int DIM, int P, bool INTER, bool NORM>
 __global__ __launch_bounds__(ROPE_THREADS) void k_qk_rope(RopeArgs A)
 {
-    constexpr int LANES = DIM / 8, LOG2 = DIM == 64 ? 3 : DIM == 128 ? 4 : 5, HEADS = 64 / LANES;
+    constexpr int LANES = DIM / 2 / P, LOG2 = LANES == 4 ? 2 : LANES == 8 ? 3 : LANES == 16 ? 4 : 5, HEADS = 64 / LANES;
+    static_assert(LANES == 1 << LOG2);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = A.heads_q + A.heads;
     const int rounds = (heads + HEADS - 1) / HEADS, parts = (rounds + A.each - 1) / A.each;
     const int64_t job = (int64_t)blockIdx.x * ROPE_WAVES + wave;
     const int t = (int)(job / parts);
     if (t >= A.T) return;
     const int h0 = (int)(job - (int64_t)t * parts) * A.each * HEADS, h1 = min(h0 + A.each * HEADS, heads);
-    const int i0 = (lane % LANES) * 4, rot = 2 * A.half;
+    const int i0 = (lane % LANES) * P, rot = 2 * A.half;
     const bool turned = i0 < A.half;
-    // the lane's channels: two times four
-    const int at0 = !turned ? rot + 2 * (i0 - A.half) : INTER ? 2 * i0 : i0, at1 = turned && !INTER ? A.half + i0 : at0 + 4;
-    float sin[4], cos[4];
+    // the lane's channels: two times P
+    const int at0 = !turned ? rot + 2 * (i0 - A.half) : INTER ? 2 * i0 : i0, at1 = turned && !INTER ? A.half + i0 : at0 + P;
+    float sin[P], cos[P];
     if (turned) {
         const double place = A.places[t];
+        float freq[P];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const double turns = place * ((double)A.inv_freq[i0 + j] * 0.15915494309189533577);
+        for (int j = 0; j < P; ++j) freq[j] = A.inv_freq[i0 + j];
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const double turns = place * ((double)freq[j] * 0.15915494309189533577);
             sincospif(2.f * (float)(turns - rint(turns)), &sin[j], &cos[j]);
         }
     }
     for (int h = h0; h < h1; h += HEADS) {
         const int mine = h + lane / LANES, head = min(mine, heads - 1), of_k = head >= A.heads_q, local = of_k ? head - A.heads_q : head;
         const W *from = static_cast<const W *>(of_k ? A.k : A.q) + t * (of_k ? A.k_stride : A.q_stride) + (int64_t)local * DIM;
-        float x[2][4];
-        load_four(from + at0, x[0]);
-        load_four(from + at1, x[1]);
+        float x[2][P];
+        load_some(from + at0, x[0]);
+        load_some(from + at1, x[1]);
         if constexpr (NORM) {
             const float *weight = of_k ? A.k_weight : A.q_weight;
             float square = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) square += x[0][j] * x[0][j] + x[1][j] * x[1][j];
+            for (int j = 0; j < P; ++j) square += x[0][j] * x[0][j] + x[1][j] * x[1][j];
             const float by = 1.f / sqrtf(group_sum<LOG2>(square) * (1.f / DIM) + A.eps);
-            float w[2][4] = {{1.f, 1.f, 1.f, 1.f}, {1.f, 1.f, 1.f, 1.f}};
+            float w[2][P];
+#pragma unroll
+            for (int j = 0; j < P; ++j) w[0][j] = w[1][j] = 1.f;
             if (weight != nullptr) {
                 weight += (int64_t)local * (of_k ? A.k_each : A.q_each);
-                load_four(weight + at0, w[0]);
-                load_four(weight + at1, w[1]);
+                load_some(weight + at0, w[0]);
+                load_some(weight + at1, w[1]);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < P; ++j) {
                 x[0][j] = x[0][j] * by * w[0][j];
                 x[1][j] = x[1][j] * by * w[1][j];
             }
@@ -100,19 +106,20 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_qk_rope(RopeArgs A)
                 a = y;
             };
             if constexpr (INTER) {
-                turn(x[0][0], x[0][1], cos[0], sin[0]);
-                turn(x[0][2], x[0][3], cos[1], sin[1]);
-                turn(x[1][0], x[1][1], cos[2], sin[2]);
-                turn(x[1][2], x[1][3], cos[3], sin[3]);
+#pragma unroll
+                for (int j = 0; j < P / 2; ++j) {
+                    turn(x[0][2 * j], x[0][2 * j + 1], cos[j], sin[j]);
+                    turn(x[1][2 * j], x[1][2 * j + 1], cos[P / 2 + j], sin[P / 2 + j]);
+                }
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) turn(x[0][j], x[1][j], cos[j], sin[j]);
+                for (int j = 0; j < P; ++j) turn(x[0][j], x[1][j], cos[j], sin[j]);
             }
         }
         if (mine >= h1) continue;
         W *to = static_cast<W *>(of_k ? A.k_out : A.q_out) + t * (of_k ? A.k_out_stride : A.q_out_stride) + (int64_t)local * DIM;
-        store_four(to + at0, x[0]);
-        store_four(to + at1, x[1]);
+        store_some(to + at0, x[0]);
+        store_some(to + at1, x[1]);
     }
 }
 

@@ -18,12 +18,24 @@ using namespace svdp;
 inline int bytes_of(int dt) { return dt == SVDP_F32 ? 4 : 2; }
 inline bool aligned_to(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
-template <typename W, int DIM>
-void launch_rope(const RopeArgs &A, bool inter, bool norm, dim3 grid, hipStream_t hs)
+template <bool B>
+using Flag = std::integral_constant<bool, B>;
+template <typename F>
+void on_flag(bool b, F &&f)
 {
-    const auto with = [&](auto i, auto n) { launch((k_qk_rope<W, DIM, decltype(i)::value, decltype(n)::value>), grid, dim3(ROPE_THREADS), 0, hs, A); };
-    if (inter) norm ? with(std::true_type{}, std::true_type{}) : with(std::true_type{}, std::false_type{});
-    else norm ? with(std::false_type{}, std::true_type{}) : with(std::false_type{}, std::false_type{});
+    if (b) f(Flag<true>{});
+    else f(Flag<false>{});
+}
+template <typename W, int DIM>
+void launch_rope(const RopeArgs &A, bool eight, bool inter, bool norm, dim3 grid, hipStream_t hs)
+{
+    on_flag(eight, [&](auto e) {
+        on_flag(inter, [&](auto i) {
+            on_flag(norm, [&](auto n) {
+                launch((k_qk_rope<W, DIM, decltype(e)::value ? 8 : 4, decltype(i)::value, decltype(n)::value>), grid, dim3(ROPE_THREADS), 0, hs, A);
+            });
+        });
+    });
 }
 
 constexpr int SAMPLE_ONE_LAUNCH = 256;
@@ -72,15 +84,16 @@ svdp_status svdp_qk_rope(int32_t dtype, int32_t dim, int32_t T, const void *q, i
     A.half = rot / 2;
     A.q_each = A.k_each = flags & SVDP_ROPE_WEIGHT_EACH ? dim : 0;
     A.eps = eps;
-    const int per = 512 / dim, rounds = (heads_q + heads + per - 1) / per;
+    const bool eight = rot % 16 == 0;
+    const int per = (eight ? 1024 : 512) / dim, rounds = (heads_q + heads + per - 1) / per;
     A.each = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, (int64_t)T * rounds / 16384));
     const int64_t waves = (int64_t)T * ((rounds + A.each - 1) / A.each), blocks = (waves + ROPE_WAVES - 1) / ROPE_WAVES;
     if (blocks * ROPE_THREADS >= (int64_t)1 << 32) return SVDP_ERR_UNSUPPORTED;
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const auto of = [&](auto dc) {
         constexpr int DIM = decltype(dc)::value;
-        if (dtype == SVDP_F32) launch_rope<float, DIM>(A, flags & SVDP_ROPE_INTERLEAVED, norm, dim3((uint32_t)blocks), hs);
-        else launch_rope<bf16, DIM>(A, flags & SVDP_ROPE_INTERLEAVED, norm, dim3((uint32_t)blocks), hs);
+        if (dtype == SVDP_F32) launch_rope<float, DIM>(A, eight, flags & SVDP_ROPE_INTERLEAVED, norm, dim3((uint32_t)blocks), hs);
+        else launch_rope<bf16, DIM>(A, eight, flags & SVDP_ROPE_INTERLEAVED, norm, dim3((uint32_t)blocks), hs);
     };
     if (dim == 64) of(std::integral_constant<int, 64>{});
     else if (dim == 128) of(std::integral_constant<int, 128>{});
