@@ -407,12 +407,11 @@ svdp_status svdp_qk_rope(int32_t dtype, int32_t dim, int32_t T, const void *q, i
  * it.  All logits -inf: -1.  Sums are whole numbers and exact, so that nothing depends on how the work is divided.
  * u, temperature, top_p, min_p: device [T] fp32; top_k: device [T] int32; all but u may be NULL (1, all, all, all).
  * answers [T] int32.  logp [T] fp32, nullable: logarithm of the drawn token's share of the kept weight (0 for a first token that is not
- * drawn, -inf with -1).  ws: >= svdp_sample_workspace_bytes() (0 for arguments it does not take).                    */
+ * drawn, -inf with -1).  No scratch memory is needed.                                                              */
 #define SVDP_MAX_VOCABULARY (1 << 19)
-size_t svdp_sample_workspace_bytes(int32_t T, int32_t V, int32_t dtype);
 svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32_t V, const float *u, const float *temperature,
                         const int32_t *top_k, const float *top_p, const float *min_p, int32_t T, int32_t *answers, float *logp,
-                        void *ws, size_t ws_bytes, void *stream);
+                        void *stream);
 
 /* The branch of each tree that agrees with given answers (drawn ones, e.g.): keep, counts and next as svdp_tree_accept forms them from its
  * `best`, here answers [T] int32.  An answer of -1 agrees with no token from 0 on.                                  */

@@ -33,7 +33,7 @@ EXPORTS = [
     "svdp_calib_stats_workspace_bytes", "svdp_calib_stats", "svdp_ffn_step_glued",
     "svdp_whiten_workspace_bytes", "svdp_whiten_factors",
     "svdp_tree_attn_workspace_bytes", "svdp_tree_attn", "svdp_tree_accept_workspace_bytes", "svdp_tree_accept",
-    "svdp_kv_plan", "svdp_kv_commit", "svdp_kv_read", "svdp_qk_rope", "svdp_sample_workspace_bytes", "svdp_sample", "svdp_tree_walk",
+    "svdp_kv_plan", "svdp_kv_commit", "svdp_kv_read", "svdp_qk_rope", "svdp_sample", "svdp_tree_walk",
 ]
 
 
@@ -126,9 +126,7 @@ def lib() -> ctypes.CDLL:
     L.svdp_qk_rope.argtypes = [i32, i32, i32, vp, i64, i32, vp, i64, i32, vp, vp, i32, ctypes.c_uint32, vp, vp, ctypes.c_float, vp, i64,
                                vp, i64, vp]
     L.svdp_qk_rope.restype = ctypes.c_int
-    L.svdp_sample_workspace_bytes.argtypes = [i32, i32, i32]
-    L.svdp_sample_workspace_bytes.restype = sz
-    L.svdp_sample.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    L.svdp_sample.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     L.svdp_sample.restype = ctypes.c_int
     L.svdp_tree_walk.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]
     L.svdp_tree_walk.restype = ctypes.c_int
@@ -641,52 +639,41 @@ def qk_rope(q: torch.Tensor, k: torch.Tensor, places: torch.Tensor, inv_freq: to
     [rot / 2] float32: the first rot channels are turned, pairs (i, rot / 2 + i), interleaved: (2 i, 2 i + 1).  q_weight, k_weight:
     float32, [dim] for all heads, or both [heads][dim].  q_out = q and k_out = k work in place.  Returns (q_out, k_out)."""
     qs, ks = _head_stride(q, "q"), _head_stride(k, "k")
-    T, heads_q, dim = q.shape
-    heads = k.shape[1]
-    if q.dtype not in (torch.float32, torch.bfloat16) or k.dtype is not q.dtype or k.shape[0] != T or k.shape[2] != dim:
-        raise SvdpError(f"svdp_qk_rope: q {tuple(q.shape)} {q.dtype} and k {tuple(k.shape)} {k.dtype} do not go together, or are of another type")
-    flags, weights = ROPE_INTERLEAVED if interleaved else 0, []
-    if eps is not None:
-        flags |= ROPE_NORM
-    elif q_weight is not None or k_weight is not None:
-        raise SvdpError("svdp_qk_rope: weights without a norm (eps)")
-    each = [w.dim() == 2 for w in (q_weight, k_weight) if w is not None]
-    if any(each):
-        if not all(each):
-            raise SvdpError("svdp_qk_rope: q_weight and k_weight have to be both [dim] or both [heads][dim]")
-        flags |= ROPE_WEIGHT_EACH
-    for w, n, what in ((q_weight, heads_q, "q_weight"), (k_weight, heads, "k_weight")):
-        weights.append(_typed(w, torch.float32, what, (n, dim) if flags & ROPE_WEIGHT_EACH else (dim,)))
+    shape_q, shape_k, dtype, f32 = q.shape, k.shape, q.dtype, torch.float32
+    T, heads_q, dim = shape_q
+    heads = shape_k[1]
+    if (dtype is not torch.bfloat16 and dtype is not f32) or k.dtype is not dtype or shape_k[0] != T or shape_k[2] != dim:
+        raise SvdpError(f"svdp_qk_rope: q {tuple(shape_q)} {dtype} and k {tuple(shape_k)} {k.dtype} do not go together, or are of another type")
+    flags = (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_NORM if eps is not None else 0)
+    wq = wk = None
+    if q_weight is not None or k_weight is not None:
+        each = [w.dim() == 2 for w in (q_weight, k_weight) if w is not None]
+        if eps is None or any(each) != all(each):
+            raise SvdpError("svdp_qk_rope: weights go with a norm (eps), and are both [dim] or both [heads][dim]")
+        flags |= ROPE_WEIGHT_EACH if each[0] else 0
+        wq = _typed(q_weight, f32, "q_weight", (heads_q, dim) if each[0] else (dim,))
+        wk = _typed(k_weight, f32, "k_weight", (heads, dim) if each[0] else (dim,))
     if q_out is None:
-        q_out = torch.empty((T, heads_q, dim), dtype=q.dtype, device=q.device)
-        qo = heads_q * dim
+        q_out, qo = torch.empty(shape_q, dtype=dtype, device=q.device), heads_q * dim
+    elif q_out.shape != shape_q or q_out.dtype is not dtype:
+        raise SvdpError("svdp_qk_rope: q_out: expected the shape and the type of q")
     else:
         qo = _head_stride(q_out, "q_out")
     if k_out is None:
-        k_out = torch.empty((T, heads, dim), dtype=q.dtype, device=q.device)
-        ko = heads * dim
+        k_out, ko = torch.empty(shape_k, dtype=dtype, device=q.device), heads * dim
+    elif k_out.shape != shape_k or k_out.dtype is not dtype:
+        raise SvdpError("svdp_qk_rope: k_out: expected the shape and the type of k")
     else:
         ko = _head_stride(k_out, "k_out")
-    if q_out.shape != q.shape or k_out.shape != k.shape or q_out.dtype is not q.dtype or k_out.dtype is not q.dtype:
-        raise SvdpError("svdp_qk_rope: q_out, k_out: expected the shapes and the type of q and k")
     _check(lib().svdp_qk_rope(
-        SVDP_BF16 if q.dtype is torch.bfloat16 else SVDP_F32, dim, T, q.data_ptr(), qs, heads_q, k.data_ptr(), ks, heads,
-        _typed(places, torch.int32, "places", (T,)), _typed(inv_freq, torch.float32, "inv_freq"), 2 * inv_freq.numel(), flags, *weights,
+        SVDP_BF16 if dtype is torch.bfloat16 else SVDP_F32, dim, T, q.data_ptr(), qs, heads_q, k.data_ptr(), ks, heads,
+        _typed(places, torch.int32, "places", (T,)), _typed(inv_freq, f32, "inv_freq"), 2 * inv_freq.numel(), flags, wq, wk,
         0.0 if eps is None else eps, q_out.data_ptr(), qo, k_out.data_ptr(), ko, _stream()), "svdp_qk_rope")
     return q_out, k_out
 
 
-@functools.lru_cache(maxsize=256)
-def sample_workspace_bytes(T: int, V: int, dtype: int) -> int:
-    n = int(lib().svdp_sample_workspace_bytes(T, V, dtype))
-    if n == 0:
-        raise SvdpError(f"svdp_sample: unsupported sizes T={T} V={V}")
-    return n
-
-
 def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
-           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, want_logp: bool = False,
-           ws: Optional[torch.Tensor] = None):
+           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, want_logp: bool = False):
     """A token for each row of logits [T][V] (rows may be strided; float32 or bfloat16) from random numbers u [T] in [0, 1).
 
     temperature, top_p, min_p [T] float32 and top_k [T] int32, one entry a row (None: 1, all, all, all); temperature 0: the
@@ -695,13 +682,12 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
         raise SvdpError(f"logits: expected [T][V] of float32 or bfloat16 on the device, got {tuple(logits.shape)} {logits.dtype}")
     T, V = logits.shape
     dt, f32, rows = SVDP_BF16 if logits.dtype is torch.bfloat16 else SVDP_F32, torch.float32, (T,)
-    ws = torch.empty(sample_workspace_bytes(T, V, dt), dtype=torch.uint8, device=logits.device) if ws is None else ws
     answers = torch.empty(T, dtype=torch.int32, device=logits.device)
     logp = torch.empty(T, dtype=f32, device=logits.device) if want_logp else None
     _check(lib().svdp_sample(
         logits.data_ptr(), logits.stride(0) if T > 1 else V, dt, V, _typed(u, f32, "u", rows), _typed(temperature, f32, "temperature", rows),
         _typed(top_k, torch.int32, "top_k", rows), _typed(top_p, f32, "top_p", rows), _typed(min_p, f32, "min_p", rows), T, answers.data_ptr(),
-        _ptr(logp), ws.data_ptr(), ws.numel(), _stream()), "svdp_sample")
+        _ptr(logp), _stream()), "svdp_sample")
     return (answers, logp) if want_logp else answers
 
 

@@ -259,11 +259,6 @@ __device__ __forceinline__ void load_to_lds(const void *src, uint32_t at)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(src) : "m0", "memory");
 }
-// The same of 64 lanes x 4 bytes, to [at, at + 256).
-__device__ __forceinline__ void load_words_to_lds(const void *src, uint32_t at)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(at), "v"(src) : "m0", "memory");
-}
 #pragma clang diagnostic pop
 
 // Every wave's LDS reads and writes are done, in all waves of the block; loads stay on their way.

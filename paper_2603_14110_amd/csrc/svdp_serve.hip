@@ -29,16 +29,24 @@ void on_flag(bool b, F &&f)
 template <typename W, int DIM>
 void launch_rope(const RopeArgs &A, bool eight, bool inter, bool norm, dim3 grid, hipStream_t hs)
 {
-    on_flag(eight, [&](auto e) {
-        on_flag(inter, [&](auto i) {
-            on_flag(norm, [&](auto n) {
-                launch((k_qk_rope<W, DIM, decltype(e)::value ? 8 : 4, decltype(i)::value, decltype(n)::value>), grid, dim3(ROPE_THREADS), 0, hs, A);
-            });
+    on_flag(inter, [&](auto i) {
+        on_flag(norm, [&](auto n) {
+            constexpr bool INTER = decltype(i)::value, NORM = decltype(n)::value;
+            if constexpr (sizeof(W) == 2)
+                if (eight) return launch(k_qk_rope<W, DIM, 8, INTER, NORM>, grid, dim3(ROPE_THREADS), 0, hs, A);
+            launch(k_qk_rope<W, DIM, 4, INTER, NORM>, grid, dim3(ROPE_THREADS), 0, hs, A);
         });
     });
 }
 
+// Rows of bf16 up to which one launch does all, a block of 1024 threads for each compute unit: 256 of 152 064 logits 33.2 us, in two launches
+// 39.4, 256 of 32 000 19.2 and 21.6.  Beyond, blocks of 512 threads that do not carry the other way's registers, and a launch for
+// the rows they left: 400 rows 50.0 us, in one launch 51.8; 768 rows 69.9 and 83.4, of 32 000 logits 34.6 and 49.0.
 constexpr int SAMPLE_ONE_LAUNCH = 256;
+// Heads (of all rows) from which a lane of bf16 has eight pairs, in 16-byte accesses: 16 384 rows of 40 heads 71.0 us, with four pairs
+// 74.5; 1024 of them 8.4 and 9.4.  Few heads are bound by the chain of a wave, which four pairs shorten: one row of 64 heads 3.0 us,
+// with eight 3.65.  In fp32 four are 16 bytes already (16 384 rows of 6 heads of 64: 12.5 us, with eight 16.9).
+constexpr int64_t ROPE_EIGHT = 16384;
 
 }  // namespace
 
@@ -84,7 +92,7 @@ svdp_status svdp_qk_rope(int32_t dtype, int32_t dim, int32_t T, const void *q, i
     A.half = rot / 2;
     A.q_each = A.k_each = flags & SVDP_ROPE_WEIGHT_EACH ? dim : 0;
     A.eps = eps;
-    const bool eight = rot % 16 == 0;
+    const bool eight = dtype == SVDP_BF16 && rot % 16 == 0 && (int64_t)T * (heads_q + heads) >= ROPE_EIGHT;
     const int per = (eight ? 1024 : 512) / dim, rounds = (heads_q + heads + per - 1) / per;
     A.each = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, (int64_t)T * rounds / 16384));
     const int64_t waves = (int64_t)T * ((rounds + A.each - 1) / A.each), blocks = (waves + ROPE_WAVES - 1) / ROPE_WAVES;
@@ -101,14 +109,8 @@ svdp_status svdp_qk_rope(int32_t dtype, int32_t dim, int32_t T, const void *q, i
     return hip_status(hipSuccess);
 }
 
-size_t svdp_sample_workspace_bytes(int32_t T, int32_t V, int32_t dtype)
-{
-    if (T < 0 || T > SVDP_MAX_ROWS || V < 1 || V > SVDP_MAX_VOCABULARY || (dtype != SVDP_F32 && dtype != SVDP_BF16)) return 0;
-    return ALIGN;
-}
-
 svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32_t V, const float *u, const float *temperature, const int32_t *top_k,
-                        const float *top_p, const float *min_p, int32_t T, int32_t *answers, float *logp, void *ws, size_t ws_bytes, void *stream)
+                        const float *top_p, const float *min_p, int32_t T, int32_t *answers, float *logp, void *stream)
 {
     static_assert(SAMPLE_MAX_V == SVDP_MAX_VOCABULARY);
     if (T < 0 || V < 1 || (stride != 0 && stride < V)) return SVDP_ERR_INVALID_ARG;
@@ -118,7 +120,6 @@ svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32
     if (!logits || !u || !answers || !aligned_to(logits, bytes_of(dtype)) || !aligned_to(u, 4) || !aligned_to(temperature, 4) || !aligned_to(top_k, 4) ||
         !aligned_to(top_p, 4) || !aligned_to(min_p, 4) || !aligned_to(answers, 4) || !aligned_to(logp, 4))
         return SVDP_ERR_INVALID_ARG;
-    if (ws == nullptr || !aligned_to(ws, ALIGN) || ws_bytes < svdp_sample_workspace_bytes(T, V, dtype)) return SVDP_ERR_WORKSPACE;
     hipStream_t hs = static_cast<hipStream_t>(stream);
     constexpr int ROWS = 1 << 21;            // of a launch: its threads are counted in 32 bits
     static_assert((int64_t)ROWS * SAMPLE_THREADS < (int64_t)1 << 32);
@@ -126,8 +127,7 @@ svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32
         const auto from = [&](auto *p) { return p != nullptr ? p + t : p; };
         const SampleArgs A{static_cast<const char *>(logits) + (int64_t)t * stride * bytes_of(dtype), stride, from(u), from(temperature), from(top_k),
                            from(top_p), from(min_p), from(answers), from(logp), V};
-        const dim3 grid(std::min(T - t, ROWS));
-        const auto with = [&](auto kernel, int threads) { launch(kernel, grid, dim3(threads), 0, hs, A); };
+        const auto with = [&](auto kernel, int threads) { launch(kernel, dim3(std::min(T - t, ROWS)), dim3(threads), 0, hs, A); };
         if (dtype == SVDP_F32) {
             with(k_sample<float, SampleWays::ALL>, SAMPLE_THREADS);
         } else if (T <= SAMPLE_ONE_LAUNCH) {

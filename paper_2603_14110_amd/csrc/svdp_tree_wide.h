@@ -40,7 +40,7 @@ __device__ __forceinline__ int tw_swizzle(int token, int dim) { return dim == 64
 // A cache in 8 bits: its tiles come into LDS as they are, in two stages of 32 KB, and the block makes bf16 operands of one of them
 // (K and V with their tokens' powers of two, exact) in the 64 KB that the products read, between two barriers.  The tree's own tokens,
 // bf16 as ever, come straight to those 64 KB.
-constexpr int TW_CODED = TW_STAGE / 2, TW_SCALES = 512;         // bytes of a stage: codes; scales of K and of V
+constexpr int TW_CODED = TW_STAGE / 2, TW_SCALES = 1024;        // bytes of a stage: codes; scales of K and of V, and what a load fills besides
 
 template <typename W, int DIM>
 __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_tree_attn_wide(TreeAttnArgs A)
@@ -54,7 +54,7 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
     // a stage of the tree's tokens: K where it always is; V as it comes, then in packs (finite elements), and as it is in packs
     constexpr int OWN_RAW = V_AT, OWN_PACKS = V_AT + TW_STAGE / 4, OWN_ALL = TW_STAGE / 4;
     extern __shared__ __align__(16) char tw_smem[];
-    __shared__ __align__(16) uint8_t s_scales[CODED ? 2 : 1][CODED ? TW_SCALES : 16];     // of a stage's tokens: K's, then V's
+    __shared__ __align__(16) uint8_t s_scales[CODED ? 2 : 1][CODED ? TW_SCALES : 16];     // of a stage's tokens: K's, behind them V's
     __shared__ uint64_t s_sees[TW_WAVES * 32];                   // what a row sees of its tree
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), f = lane >> 5, m = lane & 31;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t *)tw_smem;
@@ -124,12 +124,11 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                     load_to_lds(static_cast<const char *>(A.K) + at, to + piece * 16);
                     load_to_lds(static_cast<const char *>(A.V) + at, to + TW_CODED / 2 + piece * 16);
                 }
-                // 32 scales of a tile are eight words, a stage's 64 at the most: wave 0 brings K's, wave 1 V's
-                static_assert(TILES * 8 <= 64);
-                if (wave < 2) {
-                    const int tile = min(step * TILES + min(lane / 8, TILES - 1), S.tiles - 1);
-                    const uint8_t *from = (wave == 0 ? A.K_scale : A.V_scale) + token_at(tile, __shfl(window_ids, (tile >> per_page) - window)) + (lane & 7) * 4;
-                    load_words_to_lds(from, scales0 + which * TW_SCALES + wave * (TW_SCALES / 2));
+                // 32 scales of a tile are two times 16 bytes: wave 0 brings all K's, behind them V's (lanes past them the last ones again)
+                if (wave == 0) {
+                    const int piece = min(lane, 4 * TILES - 1), of_v = piece >= 2 * TILES, tile = min(step * TILES + (piece >> 1) % TILES, S.tiles - 1);
+                    load_to_lds((of_v ? A.V_scale : A.K_scale) + token_at(tile, __shfl(window_ids, (tile >> per_page) - window)) + (piece & 1) * 16,
+                                scales0 + which * TW_SCALES);
                 }
             };
             const auto fill = [&](int step, int stage) {
@@ -197,7 +196,7 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                 for (int p = here(tid); p < TILES * TA_TILE * DIM / 16; p += TW_THREADS) {
                     const int pack = p / (DIM / 2);              // two channels of eight tokens
                     const uint4 raw = *reinterpret_cast<const uint4 *>(from + TW_CODED / 2 + p * 16);
-                    const uint2 scales = *reinterpret_cast<const uint2 *>(&s_scales[which][TW_SCALES / 2 + pack * 8]);
+                    const uint2 scales = *reinterpret_cast<const uint2 *>(&s_scales[which][TILES * TA_TILE + pack * 8]);
                     const auto eight = [&](uint32_t a, uint32_t b) {
                         ta_f32x8 x;
 #pragma unroll

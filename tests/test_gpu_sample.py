@@ -164,10 +164,9 @@ def test_no_rows_repeats_streams_and_graphs(env):
     how = dict(temperature=f32(torch, [0.9] * 30), top_p=f32(torch, [0.8] * 30), want_logp=True)
     u = torch.rand(30, device="cuda")
     graph, out = torch.cuda.CUDAGraph(), None
-    ws = torch.empty(binding.sample_workspace_bytes(30, 5000, binding.SVDP_BF16), dtype=torch.uint8, device="cuda")
     torch.cuda.synchronize()
     with torch.cuda.graph(graph):
-        out = binding.sample(x, u, ws=ws, **how)
+        out = binding.sample(x, u, **how)
     side = torch.cuda.Stream()
     for step in range(4):
         u.uniform_()
@@ -224,7 +223,7 @@ def test_binding_refuses_what_does_not_go_together(env):
     x, u = torch.randn((4, 100), device="cuda"), torch.rand(4, device="cuda")
     binding.sample(x, u)
     for bad in (dict(logits=x.half()), dict(logits=x.t()), dict(logits=x[0]), dict(u=u[:2]), dict(u=u.double()), dict(temperature=u[:1]), dict(top_k=u),
-                dict(top_p=u.bfloat16()), dict(min_p=u.cpu()), dict(ws=torch.empty(8, dtype=torch.uint8, device="cuda")),
+                dict(top_p=u.bfloat16()), dict(min_p=u.cpu()),
                 dict(logits=torch.empty((4, (1 << 19) + 1), device="cuda"))):
         with pytest.raises(binding.SvdpError):
             binding.sample(**{**dict(logits=x, u=u), **bad})
@@ -232,3 +231,20 @@ def test_binding_refuses_what_does_not_go_together(env):
     for a, b, c in ((i32.long(), i32, i32[:2]), (i32, i32[:3], i32[:2]), (i32, i32, i32[:2].long())):
         with pytest.raises(binding.SvdpError):
             binding.tree_walk(a, b, c)
+
+
+@pytest.mark.parametrize("T", [256, 257, 700])
+def test_many_rows_of_every_kind(env, T):
+    """More rows than there are compute units: rows with values that have no bin, masked ones and ordinary ones between each other."""
+    torch, binding, serve, _ = env
+    rng, inf = np.random.default_rng(T), float("inf")
+    x = torch.randn((T, 1201), device="cuda", generator=torch.Generator(device="cuda").manual_seed(T)).mul_(3).bfloat16()
+    x[::7] *= 1e-20                                              # below the smallest bin
+    x[3::11, ::2] = -inf
+    x[5::13, 17] = 300.0
+    x[6::17] = -inf
+    x[8::19, 40:50] = 0.0
+    x[2::23, 9] = float("nan")
+    x[4::29] -= 270.0                                            # all far below, and near to each other
+    u = [float(v) for v in rng.random(T, dtype=np.float32)]
+    check(torch, binding, serve, x, u, [SETTINGS[i % len(SETTINGS)] for i in range(T)])

@@ -92,20 +92,12 @@ def test_rotation_checks_its_arguments(svdp, over, status):
     (dict(T=0), OK), (dict(T=-1), INVALID), (dict(T=(1 << 24) + 1), UNSUPPORTED), (dict(V=0), INVALID), (dict(V=(1 << 19) + 1, stride=1 << 20), UNSUPPORTED),
     (dict(stride=99), INVALID), (dict(dtype=8), UNSUPPORTED), (dict(logits=None), INVALID), (dict(u=None), INVALID), (dict(answers=None), INVALID),
     (dict(logits=P + 1), INVALID), (dict(u=P + 2), INVALID), (dict(temperature=P + 1), INVALID), (dict(top_k=P + 2), INVALID), (dict(top_p=P + 3), INVALID),
-    (dict(min_p=P + 1), INVALID), (dict(answers=P + 2), INVALID), (dict(logp=P + 2), INVALID), (dict(ws=None), WORKSPACE), (dict(ws=P + 128), WORKSPACE),
-    (dict(ws_bytes=8), WORKSPACE),
+    (dict(min_p=P + 1), INVALID), (dict(answers=P + 2), INVALID), (dict(logp=P + 2), INVALID),
 ])
 def test_sampling_checks_its_arguments(svdp, over, status):
-    a = dict(logits=P, stride=100, dtype=1, V=100, u=P, temperature=None, top_k=None, top_p=None, min_p=None, T=8, answers=P, logp=None, ws=P,
-             ws_bytes=1 << 30)
+    a = dict(logits=P, stride=100, dtype=1, V=100, u=P, temperature=None, top_k=None, top_p=None, min_p=None, T=8, answers=P, logp=None)
     a.update(over)
     assert svdp.lib().svdp_sample(*a.values(), None) == status
-
-
-def test_sampling_workspace(svdp):
-    f = svdp.lib().svdp_sample_workspace_bytes
-    assert f(1, 32000, 1) % 256 == 0 and f(0, 1, 0) > 0 and f(2048, 1 << 19, 0) > 0
-    assert f(-1, 10, 1) == 0 and f(1, 0, 1) == 0 and f(1, (1 << 19) + 1, 1) == 0 and f(1, 10, 8) == 0 and f((1 << 24) + 1, 10, 1) == 0
 
 
 @pytest.mark.parametrize("over,status", [
