@@ -31,6 +31,7 @@ namespace svdp {
 constexpr int SAMPLE_MAX_V = 1 << 19;
 constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = SAMPLE_THREADS / 64;
 constexpr int SAMPLE_EACH = 4, SAMPLE_BINS = SAMPLE_THREADS * SAMPLE_EACH;
+constexpr int SAMPLE_TABLE = SAMPLE_BINS / 2;
 constexpr int SAMPLE_LIST = 768;                            // elements of a bin that are ordered by comparing all with all
 constexpr double SAMPLE_UNIT = 17592186044416.0;            // 2^44
 constexpr float SAMPLE_ZERO = 31.5f;                        // (top - x) / temperature from which weights are 0: 45 ln 2 = 31.19
@@ -153,6 +154,7 @@ struct SampleValues {
     } asked[3];
 };
 struct SampleBins {
+    double table[SAMPLE_TABLE];             // weights, not rounded, in the middle of every two bins
     uint64_t weight[SAMPLE_BINS];
     uint32_t count[SAMPLE_BINS];
     uint64_t list[SAMPLE_LIST], list_weight[SAMPLE_LIST];
@@ -162,7 +164,7 @@ struct SampleBins {
     uint32_t before_count, listed;
     int bin;
 };
-static_assert(sizeof(SampleBins) <= 64 << 10 && 4 * sizeof(SampleValues<512>) <= 160 << 10);
+static_assert(2 * sizeof(SampleBins) <= LDS_MAX && 4 * sizeof(SampleValues<512>) <= LDS_MAX);
 
 // Inclusive sums over a wave, as wave_inclusive_scan.
 template <int CTRL, int ROW_MASK, int BANK_MASK>
@@ -597,15 +599,39 @@ __device__ __forceinline__ void sample_by_range(SampleBins &s, const W *row, int
         if (!none) sample_index(s.waves, row, V, 0, tid, nan ? NAN : top, answer);
         return;
     }
-    const SampleScale scale(top, how.temperature);
-    // Bins over the values that have a weight, or over all if these lie closer.
-    const float range = fminf(scale.zero, top - low), per = range > 0.f ? fminf(SAMPLE_BINS / range, 3e38f) : 0.f;
-    const auto place_of = [&](float x) { return fminf((top - x) * per, SAMPLE_BINS - 1.f); };
-    const auto bin_of = [&](float x) { return (int)place_of(x); };
+    // Bins over the values that have a weight, or over all if these lie closer; every two of them have an entry of the table, from which a
+    // weight is no further away than z = 0.0077: 2^44 exp(z) by five more terms of the series, within 2^-50 of its value.  All in 64 bits;
+    // an infinite temperature has one bin.
+    const bool flat = how.temperature == INFINITY;
+    const double zero = (double)SAMPLE_ZERO * (double)how.temperature, range = flat ? 0.0 : fmin(zero, ((double)top - (double)low) * (1.0 + 0x1p-20));
+    const double per = range > 0.0 ? SAMPLE_TABLE / range : 0.0, step = flat ? 0.0 : range / SAMPLE_TABLE / (double)how.temperature;
+    for (int i = tid; i < SAMPLE_TABLE; i += SAMPLE_THREADS) s.table[i] = SAMPLE_UNIT * exp(-(i + 0.5) * step);
+    const double c1 = -step, c2 = step * step / 2, c3 = c2 * c1 / 3, c4 = c3 * c1 / 4, c5 = c4 * c1 / 5;
+    struct Spot {
+        int bin;
+        uint64_t weight;
+    };
+    const auto spot_of = [&](float x) {
+        const double away = (double)top - (double)x, y = away * per;
+        if (!(away < zero)) return Spot{SAMPLE_BINS - 1, 0};
+        const int i = min((int)y, SAMPLE_TABLE - 1);
+        const double d = __builtin_amdgcn_fract(y) - 0.5;
+        const double p = fma(fma(fma(fma(fma(c5, d, c4), d, c3), d, c2), d, c1), d, 1.0);
+        // the sum with 2^52 rounds to whole numbers, which are its lower bits
+        const uint64_t bits = (uint64_t)__double_as_longlong(fma(s.table[i], p, 4503599627370496.0));
+        return Spot{2 * i + (d >= 0.0 ? 1 : 0), bits & (((uint64_t)1 << 52) - 1)};
+    };
+    const auto bin_of = [&](float x) {
+        const double away = (double)top - (double)x;
+        return away < zero ? min((int)(away * (2 * per)), SAMPLE_BINS - 1) : SAMPLE_BINS - 1;
+    };
+    const auto weight_of = [&](float x) { return spot_of(x).weight; };
+    __syncthreads();
     const bool counted = how.top_k > 0 && how.top_k < V;
     each_logit<4>(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
-        if (counted) atomicAdd(&s.count[bin_of(x)], 1u);
-        if (scale.live(x)) atomicAdd(reinterpret_cast<unsigned long long *>(&s.weight[bin_of(x)]), (unsigned long long)scale.of(x));
+        const Spot p = spot_of(x);
+        if (counted) atomicAdd(&s.count[p.bin], 1u);
+        if (p.weight > 0) atomicAdd(reinterpret_cast<unsigned long long *>(&s.weight[p.bin]), (unsigned long long)p.weight);
     });
     __syncthreads();
 
@@ -658,20 +684,24 @@ __device__ __forceinline__ void sample_by_range(SampleBins &s, const W *row, int
         if (tid == 0) s.listed = 0;
         find(sums, w, c, weight, count, by_count, need);
         const int bin = s.bin;
-        const float from = (float)bin, to = from + 1.f;
         uint64_t before_weight = s.before_weight;
         uint32_t before_count = s.before_count;
+        // in fp32, and with more than its error on both sides, what lies in the bin: all others are not looked at in 64 bits
+        const float slack = 1e-6f * (fabsf(top) + (float)range);
+        const double wide = 0.5 / per;
+        const bool bounded = per > 0.0 && slack < 1e30f;
+        const float from = bounded && bin < SAMPLE_BINS - 1 ? (float)((double)top - (bin + 1) * wide) - slack : -INFINITY;
+        const float to = bounded ? (float)((double)top - bin * wide) + slack : INFINITY;
         uint32_t lo = 0xffffffffu, hi = 0;
         each_logit<4>(row, V, tid, SAMPLE_THREADS, [&](float x, int i) {
-            const float place = place_of(x);
-            if (place < from || place >= to) return;
+            if (x < from || x > to || bin_of(x) != bin) return;
             const uint64_t key = best_key(x, i);
             lo = min(lo, (uint32_t)(key >> 32));
             hi = max(hi, (uint32_t)(key >> 32));
             const uint32_t at = atomicAdd(&s.listed, 1u);
             if (at < SAMPLE_LIST) {
                 s.list[at] = key;
-                s.list_weight[at] = scale.of(x);
+                s.list_weight[at] = weight_of(x);
             }
         });
         __syncthreads();
@@ -719,7 +749,8 @@ __device__ __forceinline__ void sample_by_range(SampleBins &s, const W *row, int
                 const uint32_t o = best_order(x);
                 if (o < lo || o > hi || bin_of(x) != bin) return;
                 atomicAdd(&s.count[(hi - o) >> shift], 1u);
-                if (scale.live(x)) atomicAdd(reinterpret_cast<unsigned long long *>(&s.weight[(hi - o) >> shift]), (unsigned long long)scale.of(x));
+                const uint64_t w = weight_of(x);
+                if (w > 0) atomicAdd(reinterpret_cast<unsigned long long *>(&s.weight[(hi - o) >> shift]), (unsigned long long)w);
             });
             __syncthreads();
             uint64_t w[SAMPLE_EACH], weight;
@@ -735,7 +766,7 @@ __device__ __forceinline__ void sample_by_range(SampleBins &s, const W *row, int
             lo = max(lo, hi - min(hi, (1u << shift) - 1));
             __syncthreads();
         }
-        const uint64_t each = scale.of(of_order(hi));
+        const uint64_t each = weight_of(of_order(hi));
         const uint64_t tokens = by_count ? need - before_count : sample_quotient(need - before_weight - 1, each) + 1;
         return Place{before_weight + tokens * each, hi, -1, (uint32_t)(tokens - 1)};
     };
@@ -753,7 +784,7 @@ __device__ __forceinline__ void sample_by_range(SampleBins &s, const W *row, int
         uint64_t sum = 0;
         each_logit<4>(row, V, tid, SAMPLE_THREADS, [&](float x, int) {
             if (top - x > reach) return;
-            const uint64_t w = scale.of(x);
+            const uint64_t w = weight_of(x);
             sum += w >= least ? w : 0;
         });
         kept = min(kept, sample_sum(s.waves, sum, tid));
@@ -774,15 +805,19 @@ constexpr int VALUE_THREADS = 512;
 template <typename W, SampleWays WAYS>
 constexpr int sample_threads() { return WAYS == SampleWays::VALUE ? VALUE_THREADS : SAMPLE_THREADS; }
 template <typename W, SampleWays WAYS>
+constexpr size_t sample_lds()
+{
+    constexpr size_t values = sizeof(W) == 2 && WAYS != SampleWays::LEFT ? sizeof(SampleValues<sample_threads<W, WAYS>()>) : 0;
+    return WAYS != SampleWays::VALUE && sizeof(SampleBins) > values ? sizeof(SampleBins) : values;
+}
+template <typename W, SampleWays WAYS>
 __global__ __launch_bounds__((sample_threads<W, WAYS>()), WAYS == SampleWays::VALUE ? 8 : 4) void k_sample(SampleArgs A)
 {
     constexpr int THREADS = sample_threads<W, WAYS>();
     constexpr bool BY_VALUE = sizeof(W) == 2 && WAYS != SampleWays::LEFT, BY_RANGE = WAYS != SampleWays::VALUE;
-    union Shared {
-        SampleValues<BY_VALUE ? THREADS : 64> values;
-        SampleBins bins;
-    };
-    __shared__ std::conditional_t<BY_VALUE && BY_RANGE, Shared, std::conditional_t<BY_VALUE, SampleValues<THREADS>, SampleBins>> s;
+    extern __shared__ __align__(16) char sample_smem[];
+    auto &values = *reinterpret_cast<SampleValues<BY_VALUE ? THREADS : 64> *>(sample_smem);
+    auto &bins = *reinterpret_cast<SampleBins *>(sample_smem);
     const int tid = threadIdx.x, t = blockIdx.x;
     if (WAYS == SampleWays::LEFT && A.answers[t] != SAMPLE_LATER) return;
     const W *row = static_cast<const W *>(A.logits) + (int64_t)t * A.stride;
@@ -791,11 +826,11 @@ __global__ __launch_bounds__((sample_threads<W, WAYS>()), WAYS == SampleWays::VA
                         !(temperature > 0.f)};
     float *logp = A.logp != nullptr ? A.logp + t : nullptr;
     if constexpr (BY_VALUE && BY_RANGE) {
-        if (!sample_by_value<THREADS>(s.values, row, A.V, how, tid, A.answers + t, logp)) sample_by_range(s.bins, row, A.V, how, tid, A.answers + t, logp);
+        if (!sample_by_value<THREADS>(values, row, A.V, how, tid, A.answers + t, logp)) sample_by_range(bins, row, A.V, how, tid, A.answers + t, logp);
     } else if constexpr (BY_VALUE) {
-        if (!sample_by_value<THREADS>(s, row, A.V, how, tid, A.answers + t, logp) && tid == 0) A.answers[t] = SAMPLE_LATER;
+        if (!sample_by_value<THREADS>(values, row, A.V, how, tid, A.answers + t, logp) && tid == 0) A.answers[t] = SAMPLE_LATER;
     } else {
-        sample_by_range(s, row, A.V, how, tid, A.answers + t, logp);
+        sample_by_range(bins, row, A.V, how, tid, A.answers + t, logp);
     }
 }
 

@@ -18,6 +18,8 @@ using namespace svdp;
 inline int bytes_of(int dt) { return dt == SVDP_F32 ? 4 : 2; }
 inline bool aligned_to(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+template <SampleWays WAYS>
+using Ways = std::integral_constant<SampleWays, WAYS>;
 template <bool B>
 using Flag = std::integral_constant<bool, B>;
 template <typename F>
@@ -123,21 +125,28 @@ svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32
     hipStream_t hs = static_cast<hipStream_t>(stream);
     constexpr int ROWS = 1 << 21;            // of a launch: its threads are counted in 32 bits
     static_assert((int64_t)ROWS * SAMPLE_THREADS < (int64_t)1 << 32);
+    bool granted = true;
     for (int t = 0; t < T; t += ROWS) {
         const auto from = [&](auto *p) { return p != nullptr ? p + t : p; };
         const SampleArgs A{static_cast<const char *>(logits) + (int64_t)t * stride * bytes_of(dtype), stride, from(u), from(temperature), from(top_k),
                            from(top_p), from(min_p), from(answers), from(logp), V};
-        const auto with = [&](auto kernel, int threads) { launch(kernel, dim3(std::min(T - t, ROWS)), dim3(threads), 0, hs, A); };
+        const auto with = [&](auto wt, auto ways) {
+            using W = decltype(wt);
+            constexpr SampleWays WAYS = decltype(ways)::value;
+            constexpr size_t LDS = sample_lds<W, WAYS>();
+            granted = granted && grant_lds<k_sample<W, WAYS>>(LDS);
+            if (granted) launch(k_sample<W, WAYS>, dim3(std::min(T - t, ROWS)), dim3(sample_threads<W, WAYS>()), LDS, hs, A);
+        };
         if (dtype == SVDP_F32) {
-            with(k_sample<float, SampleWays::ALL>, SAMPLE_THREADS);
+            with(float{}, Ways<SampleWays::ALL>{});
         } else if (T <= SAMPLE_ONE_LAUNCH) {
-            with(k_sample<bf16, SampleWays::ALL>, SAMPLE_THREADS);
+            with(bf16{}, Ways<SampleWays::ALL>{});
         } else {
-            with(k_sample<bf16, SampleWays::VALUE>, VALUE_THREADS);
-            with(k_sample<bf16, SampleWays::LEFT>, SAMPLE_THREADS);
+            with(bf16{}, Ways<SampleWays::VALUE>{});
+            with(bf16{}, Ways<SampleWays::LEFT>{});
         }
     }
-    return hip_status(hipSuccess);
+    return granted ? hip_status(hipSuccess) : SVDP_ERR_UNSUPPORTED;
 }
 
 }  // extern "C"
