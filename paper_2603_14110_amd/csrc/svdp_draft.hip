@@ -127,7 +127,9 @@ AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, in
     // More than 32 rows: over the waves, 32 each (eight requests of 4096 tokens, 135 MB: 36 and 64 rows 36 us, where k_tree_attn, with
     // two row tiles after each other, takes 48).  At 32 rows k_tree_attn is ahead: 26.4 us for one request of 30 000 tokens and 13.4
     // for 24 of 150, where rows over the waves took 32.0 and 16.6 + 4.4.
-    p.wide = dt != SVDP_F32 && dim <= 128 && rows > 32;
+    // An 8-bit cache: more than 64, as reading K and V once more costs half (eight requests of 4096 tokens: 36 rows 32.6 us, over the
+    // waves 44.3; 64 rows 38.0 and 46.3; 100 rows 51.1 and 48.5; 24 requests of 150 tokens and 98 rows 25.3 and 20.4).
+    p.wide = dim <= 128 && (dt == SVDP_BF16 ? rows > 32 : dt == SVDP_E4M3 && rows > 64);
     // Two row tiles of 16 read K and V once for 32 rows (8 requests of 4096 tokens, 135 MB: 29.6 us, one after the other 45.2); with
     // 256 channels a second one does not fit the registers.
     p.nt = rows <= 16 || dim == 256 ? 1 : 2;
@@ -152,7 +154,9 @@ constexpr int JOIN_WAVES = 512;
 // K and V of few rows: fewer channels a block, until there are so many blocks (five rows of 4096 channels in 32 layers: 6.6 us, with
 // one block for all channels 14.0; 500 rows of 1024 channels in 32 layers: 21.6 us, up to 16 384 blocks 23.4).
 constexpr int COMMIT_BLOCKS = 4096;
-constexpr int KV_BLOCKS = 4096;
+// Heads of a block that writes or reads 8-bit rows (reads any): fewer, until there are so many blocks (a row of 32 heads in 32 layers stored
+// in 3.6 us, up to 4096 blocks 4.5; 40 rows of 8 heads 6.3 and 7.3; five rows of 32 heads 5.2, with all heads in a block 18.9).
+constexpr int KV_BLOCKS = 1024;
 
 // Rows of K and V, as a commit reads and a read writes them.
 svdp_status check_rows(const svdp_kv_cache *c, const int64_t *slots, int T, const void *k, int64_t k_layer, int64_t k_row, const void *v, int64_t v_layer,
