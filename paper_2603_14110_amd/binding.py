@@ -608,6 +608,7 @@ def kv_commit(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Ten
 def kv_read(cache: KVCache, slots: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
     """K and V of slots [T] (int64; zeros for one outside the cache) as rows k, v [layers][T][heads][dim], of every layer: what kv_commit
     stored, in the cache's type (8 bits: bfloat16).  Returns (k, v)."""
+    _here(cache.K, "svdp_kv_read")
     T, shape = slots.numel(), (cache.layers, slots.numel(), cache.heads, cache.dim)
     k = torch.empty(shape, dtype=cache.rows, device=slots.device) if k is None else k
     v = torch.empty(shape, dtype=cache.rows, device=slots.device) if v is None else v
@@ -617,6 +618,13 @@ def kv_read(cache: KVCache, slots: torch.Tensor, k: Optional[torch.Tensor] = Non
 
 
 # ---- around attention and logits ------------------------------------------------------------------------------------
+
+
+def _here(t: torch.Tensor, what: str) -> None:
+    """Kernels go to the current device's stream: what they work on has to lie there."""
+    now = torch.cuda.current_device() if _current_device is None else _current_device()
+    if t.get_device() != now:
+        raise SvdpError(f"{what}: its tensors are on {t.device}, the current device is cuda:{now}")
 
 
 def _head_stride(t: torch.Tensor, what: str) -> int:
@@ -639,6 +647,7 @@ def qk_rope(q: torch.Tensor, k: torch.Tensor, places: torch.Tensor, inv_freq: to
     [rot / 2] float32: the first rot channels are turned, pairs (i, rot / 2 + i), interleaved: (2 i, 2 i + 1).  q_weight, k_weight:
     float32, [dim] for all heads, or both [heads][dim].  q_out = q and k_out = k work in place.  Returns (q_out, k_out)."""
     qs, ks = _head_stride(q, "q"), _head_stride(k, "k")
+    _here(q, "svdp_qk_rope")
     shape_q, shape_k, dtype, f32 = q.shape, k.shape, q.dtype, torch.float32
     T, heads_q, dim = shape_q
     heads = shape_k[1]
@@ -680,6 +689,7 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
     first token.  The rules are in include/svdp.h.  Returns answers [T] int32 (and with want_logp the logarithms of their shares [T] float32)."""
     if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or not logits.is_cuda or logits.stride(1) != 1:
         raise SvdpError(f"logits: expected [T][V] of float32 or bfloat16 on the device, got {tuple(logits.shape)} {logits.dtype}")
+    _here(logits, "svdp_sample")
     T, V = logits.shape
     dt, f32, rows = SVDP_BF16 if logits.dtype is torch.bfloat16 else SVDP_F32, torch.float32, (T,)
     answers = torch.empty(T, dtype=torch.int32, device=logits.device)
@@ -695,6 +705,7 @@ def tree_walk(answers: torch.Tensor, tokens: torch.Tensor, starts: torch.Tensor,
               max_nodes: Optional[int] = None):
     """The branch of each drafted tree that agrees with given answers [T] (int32): tree_accept without its logits.
     Returns (keep [T], counts [R], next [R]), all int32."""
+    _here(answers, "svdp_tree_walk")
     T, R = answers.numel(), starts.numel() - 1
     max_nodes = max(1, min(T, MAX_NODES)) if max_nodes is None else int(max_nodes)
     keep, counts, following = torch.empty(T + 2 * max(R, 0), dtype=torch.int32, device=answers.device).split_with_sizes((T, max(R, 0), max(R, 0)))

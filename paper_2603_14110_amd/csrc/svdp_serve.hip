@@ -125,7 +125,12 @@ svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32
     hipStream_t hs = static_cast<hipStream_t>(stream);
     constexpr int ROWS = 1 << 21;            // of a launch: its threads are counted in 32 bits
     static_assert((int64_t)ROWS * SAMPLE_THREADS < (int64_t)1 << 32);
-    bool granted = true;
+    // before anything is enqueued (the kernel by value alone needs no grant)
+    if (!(dtype == SVDP_F32 ? grant_lds<k_sample<float, SampleWays::ALL>>(sample_lds<float, SampleWays::ALL>())
+          : T <= SAMPLE_ONE_LAUNCH ? grant_lds<k_sample<bf16, SampleWays::ALL>>(sample_lds<bf16, SampleWays::ALL>())
+                                   : grant_lds<k_sample<bf16, SampleWays::LEFT>>(sample_lds<bf16, SampleWays::LEFT>())))
+        return SVDP_ERR_UNSUPPORTED;
+    static_assert(sample_lds<bf16, SampleWays::VALUE>() <= LDS_DEFAULT);
     for (int t = 0; t < T; t += ROWS) {
         const auto from = [&](auto *p) { return p != nullptr ? p + t : p; };
         const SampleArgs A{static_cast<const char *>(logits) + (int64_t)t * stride * bytes_of(dtype), stride, from(u), from(temperature), from(top_k),
@@ -133,9 +138,7 @@ svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32
         const auto with = [&](auto wt, auto ways) {
             using W = decltype(wt);
             constexpr SampleWays WAYS = decltype(ways)::value;
-            constexpr size_t LDS = sample_lds<W, WAYS>();
-            granted = granted && grant_lds<k_sample<W, WAYS>>(LDS);
-            if (granted) launch(k_sample<W, WAYS>, dim3(std::min(T - t, ROWS)), dim3(sample_threads<W, WAYS>()), LDS, hs, A);
+            launch(k_sample<W, WAYS>, dim3(std::min(T - t, ROWS)), dim3(sample_threads<W, WAYS>()), sample_lds<W, WAYS>(), hs, A);
         };
         if (dtype == SVDP_F32) {
             with(float{}, Ways<SampleWays::ALL>{});
@@ -146,7 +149,7 @@ svdp_status svdp_sample(const void *logits, int64_t stride, int32_t dtype, int32
             with(bf16{}, Ways<SampleWays::LEFT>{});
         }
     }
-    return granted ? hip_status(hipSuccess) : SVDP_ERR_UNSUPPORTED;
+    return hip_status(hipSuccess);
 }
 
 }  // extern "C"

@@ -248,3 +248,30 @@ def test_many_rows_of_every_kind(env, T):
     x[4::29] -= 270.0                                            # all far below, and near to each other
     u = [float(v) for v in rng.random(T, dtype=np.float32)]
     check(torch, binding, serve, x, u, [SETTINGS[i % len(SETTINGS)] for i in range(T)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_rows_than_a_launch_takes(env, dtype):
+    torch, binding, serve, _ = env
+    T = (1 << 21) + 7
+    x = torch.tensor([[0.0, 1.0], [3.0, -1.0]], device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32).repeat(T // 2 + 1, 1)[:T]
+    u = torch.rand(T, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    answers = binding.sample(x, u)
+    share = x.double().softmax(1).amax(1)                        # of the larger one, which comes first in the order
+    clear = (u.double() - share).abs() > 1e-6
+    first = x.float().argmax(1).int()
+    assert torch.equal(answers[clear], torch.where(u.double() < share, first, 1 - first)[clear]) and int((~clear).sum()) < 100
+
+
+def test_tensors_of_another_device_are_refused(env, monkeypatch):
+    """Kernels go to the current device's stream."""
+    torch, binding, serve, _ = env
+    x, u = torch.randn((2, 50), device="cuda"), torch.rand(2, device="cuda")
+    cache = binding.KVCache.empty(1, 1, 32, 1, 64)
+    i32 = torch.zeros(2, dtype=torch.int32, device="cuda")
+    q = torch.zeros((2, 1, 64), device="cuda")
+    monkeypatch.setattr(binding, "_current_device", lambda: 1)
+    for call in (lambda: binding.sample(x, u), lambda: binding.tree_walk(i32, i32, i32), lambda: binding.kv_read(cache, i32.long()),
+                 lambda: binding.qk_rope(q, q, i32, torch.ones(4, device="cuda"))):
+        with pytest.raises(binding.SvdpError, match="current device"):
+            call()

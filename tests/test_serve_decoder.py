@@ -131,6 +131,10 @@ def test_requests_that_leave_and_come_back(dtype):
         with pytest.raises(RuntimeError, match="other requests"):
             decoder.load(saved)
         decoder.release()
+    nothing = a.save() if not bool(a.lens.any()) else None               # requests without tokens
+    assert nothing[0] == [0] * len(PROMPTS) and nothing[1].shape[1] == 0
+    a.load(nothing)
+    _all_free(a)
     small = _decoder(pages=3, **how)
     with pytest.raises(RuntimeError, match="too few pages"):
         small.load(saved)
