@@ -4,6 +4,10 @@
 // the least whole number with max |x| <= 448 2^b, 448 being the largest e4m3 number.  A power of two costs no precision beside any other
 // scale (at most one of the fifteen binades at the lower end), makes x / 2^b and code 2^b exact, and is one byte.
 // Infinities and NaN become NaN and do not count for the maximum.
+//
+// What bounds both: reading and writing.  A prompt of 2357 tokens, 32 layers of 8 heads of 128, 465 MB, stored in 87 us, 5.3 TB/s (111 us
+// with a wave that has two channels a lane of every token, in 4-byte loads and with a maximum over 64 lanes each); 3400 tokens of the
+// same, 892 MB, read in 162 us, 5.5 TB/s.  A branch of five rows in 32 layers of 32 heads: 5.4 us; 77 tokens read: 4.9 us, by latency.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -304,7 +304,8 @@ struct TreeTile<float, DIM> {
 
 // A cache in 8 bits: its elements become bf16 operands in registers, K's with the token's power of two (exact), V's without
 // (its eight tokens have one each: it goes to their weights).  A lane's 16 bytes are the operands of two products, so that the channels
-// that a product takes are others than in 16 bits.
+// that a product takes are others than in 16 bits.  24 requests of 500 to 16 384 tokens, four query heads a head, 210 MB: 42 to 49 us,
+// 4.3 to 5.0 TB/s, of which some 5 us go by before and behind the reading; half of what 16 bits take.
 template <int DIM>
 struct TreeTile<e4m3, DIM> : TreeTile<bf16, DIM> {
     static constexpr bool CODED = true;
