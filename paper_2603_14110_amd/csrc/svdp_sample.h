@@ -835,7 +835,9 @@ __global__ __launch_bounds__((sample_threads<W, WAYS>()), WAYS == SampleWays::VA
                         !(temperature > 0.f)};
     float *logp = A.logp != nullptr ? A.logp + t : nullptr;
     if constexpr (BY_VALUE && BY_RANGE) {
-        if (!sample_by_value<THREADS>(values, row, A.V, how, tid, A.answers + t, logp)) sample_by_range(bins, row, A.V, how, tid, A.answers + t, logp);
+        if (sample_by_value<THREADS>(values, row, A.V, how, tid, A.answers + t, logp)) return;
+        __syncthreads();                    // the bins lie where other waves may still read why the row goes this way
+        sample_by_range(bins, row, A.V, how, tid, A.answers + t, logp);
     } else if constexpr (BY_VALUE) {
         if (!sample_by_value<THREADS>(values, row, A.V, how, tid, A.answers + t, logp) && tid == 0) A.answers[t] = SAMPLE_LATER;
     } else {
