@@ -154,7 +154,7 @@ template <int THREADS>
 struct SampleValues {
     uint32_t values[2 * VALUE_SIDE];
     SampleWaveSums<THREADS> waves;
-    uint32_t zeros;
+    uint32_t zeros, others, odd;
     // where a question leads to, of three a row: the thread, and what is before its bins
     struct {
         uint64_t before_weight;
@@ -414,15 +414,18 @@ __device__ __forceinline__ bool sample_by_value(SampleValues<THREADS> &s, const 
     using Bins = ValueBins<THREADS>;
     constexpr int EACH = Bins::EACH;
     for (int i = tid; i < 2 * VALUE_SIDE; i += THREADS) s.values[i] = 0;
-    if (tid == 0) s.zeros = 0;
+    if (tid == 0) s.zeros = s.others = s.odd = 0;
     __syncthreads();
-    // Two elements at a time, as halves of a word: magnitude from VALUE_LOW on (below it: a large number), up to the lane's own
-    // counter for others, plus one side for a sign.
-    const uint16_t other = (uint16_t)(VALUE_SPAN + (tid & (VALUE_OTHER - 1)));
+    // Two elements at a time, as halves of a word, in two bytes a bin until the last step: magnitude from VALUE_LOW on (below it: a large
+    // number; doubled, an element has lost its sign), up to the lane's own counter for others, plus one side for a sign.
+    const uint16_t other = (uint16_t)(2 * (VALUE_SPAN + (tid & (VALUE_OTHER - 1))));
+    // Factors that the compiler does not know stay factors: a product and a sum in one instruction.
+    u16x2_t two = {2, 2}, side = {2 * VALUE_SIDE, 2 * VALUE_SIDE};
+    asm("" : "+v"(two), "+v"(side));
     const auto pair = [&](uint32_t w, uint32_t one) {
         const u16x2_t x = __builtin_bit_cast(u16x2_t, w);
-        const u16x2_t m = __builtin_elementwise_min((x & (uint16_t)0x7fff) - (uint16_t)VALUE_LOW, u16x2_t{other, other});
-        const uint32_t at = __builtin_bit_cast(uint32_t, (m + (x >> 15) * (uint16_t)VALUE_SIDE) << 2);
+        const u16x2_t m = __builtin_elementwise_min(x * two - (uint16_t)(2 * VALUE_LOW), u16x2_t{other, other});
+        const uint32_t at = __builtin_bit_cast(uint32_t, (x >> 15) * side + m) << 1;
         char *counters = reinterpret_cast<char *>(s.values);
         atomicAdd(reinterpret_cast<uint32_t *>(counters + (at & 0xffffu)), one);
         return reinterpret_cast<uint32_t *>(counters + (at >> 16));
@@ -438,9 +441,10 @@ __device__ __forceinline__ bool sample_by_value(SampleValues<THREADS> &s, const 
     __syncthreads();
     // Others: zeros are counted, values far below (-inf among them) have no weight; with any else (small: smaller than VALUE_LOW, but not zero;
     // large or NaN) the row goes the other way.
-    const uint32_t others = tid < VALUE_OTHER ? s.values[VALUE_SPAN + tid] | s.values[VALUE_SIDE + VALUE_SPAN + tid] : 0;
+    if (tid < VALUE_OTHER && (s.values[VALUE_SPAN + tid] | s.values[VALUE_SIDE + VALUE_SPAN + tid]) != 0) s.others = 1;
+    __syncthreads();
     uint32_t zeros = 0;
-    if (__syncthreads_or(others > 0)) {
+    if (s.others != 0) {
         u16x2_t small = {0xffff, 0xffff}, negative = {0, 0}, nonzero = {0, 0};
         i16x2_t large = {0, 0};
         uint32_t elements = 0;
@@ -464,7 +468,9 @@ __device__ __forceinline__ bool sample_by_value(SampleValues<THREADS> &s, const 
         const bool odd = min(small[0], small[1]) < VALUE_LOW - 1 || max(large[0], large[1]) >= VALUE_HIGH || max(negative[0], negative[1]) > 0xff80u;
         zeros = (uint32_t)wave_inclusive_scan((int)(elements - nonzero[0] - nonzero[1]));
         if ((tid & 63) == 63 && zeros > 0) atomicAdd(&s.zeros, zeros);
-        if (__syncthreads_or(odd)) return false;
+        if (odd) s.odd = 1;
+        __syncthreads();
+        if (s.odd != 0) return false;
         zeros = s.zeros;
     }
     // the thread's bins: the largest value that there is, then the weights
