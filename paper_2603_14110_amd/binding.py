@@ -444,22 +444,25 @@ class KVCache:
                    torch.empty((layers, pages, heads, page // e, dim, e), dtype=dtype, device=device), *scales)
 
 
-def _typed(t: Optional[torch.Tensor], dtype, what: str, shape=None) -> Optional[int]:
-    """Address of a contiguous device tensor of one type (and shape); None stays None."""
+def _typed(t: Optional[torch.Tensor], dtype, what: str, shape=None, on: Optional[int] = None) -> Optional[int]:
+    """Address of a contiguous device tensor of one type (and shape; on: of that device); None stays None."""
     if t is None:
         return None
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or (shape is not None and t.shape != shape):
+    if (t.dtype is not dtype or not (t.is_cuda if on is None else t.get_device() == on) or not t.is_contiguous()
+            or (shape is not None and t.shape != shape)):
         raise SvdpError(f"{what}: expected a contiguous device tensor of {dtype}"
-                        f"{'' if shape is None else ' ' + str(tuple(shape))}, got {tuple(t.shape)} {t.dtype}")
+                        f"{'' if shape is None else ' ' + str(tuple(shape))}, got {tuple(t.shape)} {t.dtype}"
+                        f"{'' if on is None else f' on {t.device}, the current device being cuda:{on}'}")
     return t.data_ptr()
 
 
-def _heads_rows(t: torch.Tensor, cache: KVCache, heads: int, what: str) -> int:
+def _heads_rows(t: torch.Tensor, cache: KVCache, heads: int, what: str, on: Optional[int] = None) -> int:
     """Stride of the rows [heads][dim] of q, k or v (a slice of a wider projection is fine)."""
     rows, _, dim = shape = t.shape
     row, head, one = t.stride()
-    if t.dtype != cache.rows or not t.is_cuda or dim != cache.dim or shape[1] != heads:
-        raise SvdpError(f"{what}: expected [rows][{heads}][{cache.dim}] of {cache.rows} on the device, got {tuple(shape)} {t.dtype}")
+    if t.dtype != cache.rows or not (t.is_cuda if on is None else t.get_device() == on) or dim != cache.dim or shape[1] != heads:
+        raise SvdpError(f"{what}: expected [rows][{heads}][{cache.dim}] of {cache.rows} on the device, got {tuple(shape)} {t.dtype}"
+                        f"{'' if on is None else f' on {t.device}, the current device being cuda:{on}'}")
     if rows and (one != 1 or (head != dim and heads > 1)):
         raise SvdpError(f"{what}: the heads of a row have to lie side by side")
     # one row: its stride says nothing
@@ -491,34 +494,35 @@ def tree_attn(cache: KVCache, layer: int, q: torch.Tensor, k: torch.Tensor, v: t
     Returns out [T][heads_q][dim] (and lse [T][heads_q] fp32 with want_lse)."""
     if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
         raise SvdpError("svdp_tree_attn: q, k, v are rows of heads of channels")
+    on = _here(cache.K, "svdp_tree_attn") if cache.K_scale is not None else None
     T, heads_q, dim = q.shape
     R = lens.numel()
     if k.shape[0] != T or v.shape[0] != T or table.dim() != 2 or table.shape[0] != R or starts.numel() != R + 1:
         raise SvdpError(f"svdp_tree_attn: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, table "
                         f"{tuple(table.shape)}, lens [{R}] and starts [{starts.numel()}] do not go together")
-    qs, ks, vs = (_heads_rows(q, cache, heads_q, "q"), _heads_rows(k, cache, cache.heads, "k"),
-                  _heads_rows(v, cache, cache.heads, "v"))
+    qs, ks, vs = (_heads_rows(q, cache, heads_q, "q", on), _heads_rows(k, cache, cache.heads, "k", on),
+                  _heads_rows(v, cache, cache.heads, "v", on))
     max_pages = table.shape[1]
     max_nodes = max(1, min(T, MAX_NODES)) if max_nodes is None else int(max_nodes)
     if out is None:
         out = torch.empty_like(q)           # dense, as the heads of a row lie side by side
         out_at = out.data_ptr()
     else:
-        out_at = _typed(out, cache.rows, "out", (T, heads_q, dim))
+        out_at = _typed(out, cache.rows, "out", (T, heads_q, dim), on)
     if want_lse and lse is None:
         lse = torch.empty(T, heads_q, dtype=torch.float32, device=q.device)
         lse_at = lse.data_ptr()
     else:
-        lse_at = _typed(lse, torch.float32, "lse", (T, heads_q))
+        lse_at = _typed(lse, torch.float32, "lse", (T, heads_q), on)
     if ws is None:
         ws = torch.empty(tree_attn_workspace_bytes(cache, heads_q, R, max_pages, max_nodes), dtype=torch.uint8, device=q.device)
-    elif not (ws.is_cuda and ws.is_contiguous()):
+    elif not (ws.is_contiguous() and (ws.is_cuda if on is None else ws.get_device() == on)):
         raise SvdpError("ws: expected a contiguous device tensor")
     i32 = torch.int32
     _check(lib().svdp_tree_attn(
         ctypes.byref(cache.c), layer, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
-        _typed(tree, torch.int64, "tree", (T,)), _typed(table, i32, "table"), max_pages, _typed(lens, i32, "lens"),
-        _typed(starts, i32, "starts"), R, T, max_nodes, heads_q, dim ** -0.5 if scale is None else scale, out_at, lse_at,
+        _typed(tree, torch.int64, "tree", (T,), on), _typed(table, i32, "table", None, on), max_pages, _typed(lens, i32, "lens", None, on),
+        _typed(starts, i32, "starts", None, on), R, T, max_nodes, heads_q, dim ** -0.5 if scale is None else scale, out_at, lse_at,
         ws.data_ptr(), ws.numel(), _stream()), "svdp_tree_attn")
     return (out, lse) if want_lse else out
 
@@ -582,13 +586,14 @@ def kv_plan(table: torch.Tensor, ring: torch.Tensor, pool: torch.Tensor, lens: t
     return slots, lens_out, pool_out, refused
 
 
-def _kv_rows(cache: KVCache, T: int, k: torch.Tensor, v: torch.Tensor) -> list:
+def _kv_rows(cache: KVCache, T: int, k: torch.Tensor, v: torch.Tensor, on: Optional[int] = None) -> list:
     """Addresses and strides of rows k, v [layers][T][heads][dim]."""
     layers, heads, dim, dtype = cache.layers, cache.heads, cache.dim, cache.rows
     shape, args = (layers, T, heads, dim), []
     for t in (k, v):
-        if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
-            raise SvdpError(f"{'v' if t is v else 'k'}: expected {shape} of {dtype} on the device, got {tuple(t.shape)} {t.dtype}")
+        if t.shape != shape or t.dtype is not dtype or not (t.is_cuda if on is None else t.get_device() == on):
+            raise SvdpError(f"{'v' if t is v else 'k'}: expected {shape} of {dtype} on the device, got {tuple(t.shape)} {t.dtype}"
+                            f"{'' if on is None else f' on {t.device}, the current device being cuda:{on}'}")
         layer, row, head, one = t.stride()
         if T and (one != 1 or (heads > 1 and head != dim)):
             raise SvdpError(f"{'v' if t is v else 'k'}: the heads of a row have to lie side by side")
@@ -600,37 +605,39 @@ def _kv_rows(cache: KVCache, T: int, k: torch.Tensor, v: torch.Tensor) -> list:
 def kv_commit(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """K and V of new rows, k, v [layers][T][heads][dim], into the cache at slots [T] (int64; negative: not stored).  A cache in 8 bits
     takes bfloat16 rows and rounds them (see include/svdp.h)."""
+    on = _here(cache.K, "svdp_kv_commit") if cache.K_scale is not None else None
     T = slots.numel()
-    args = _kv_rows(cache, T, k, v)
-    _check(lib().svdp_kv_commit(ctypes.byref(cache.c), *args, _typed(slots, torch.int64, "slots"), T, _stream()), "svdp_kv_commit")
+    args = _kv_rows(cache, T, k, v, on)
+    _check(lib().svdp_kv_commit(ctypes.byref(cache.c), *args, _typed(slots, torch.int64, "slots", None, on), T, _stream()), "svdp_kv_commit")
 
 
 def kv_read(cache: KVCache, slots: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
     """K and V of slots [T] (int64; zeros for one outside the cache) as rows k, v [layers][T][heads][dim], of every layer: what kv_commit
     stored, in the cache's type (8 bits: bfloat16).  Returns (k, v)."""
-    _here(cache.K, "svdp_kv_read")
+    on = _here(cache.K, "svdp_kv_read")
     T, shape = slots.numel(), (cache.layers, slots.numel(), cache.heads, cache.dim)
-    k = torch.empty(shape, dtype=cache.rows, device=slots.device) if k is None else k
-    v = torch.empty(shape, dtype=cache.rows, device=slots.device) if v is None else v
-    args = _kv_rows(cache, T, k, v)
-    _check(lib().svdp_kv_read(ctypes.byref(cache.c), _typed(slots, torch.int64, "slots"), T, *args, _stream()), "svdp_kv_read")
+    k = torch.empty(shape, dtype=cache.rows, device=cache.K.device) if k is None else k
+    v = torch.empty(shape, dtype=cache.rows, device=cache.K.device) if v is None else v
+    args = _kv_rows(cache, T, k, v, on)
+    _check(lib().svdp_kv_read(ctypes.byref(cache.c), _typed(slots, torch.int64, "slots", None, on), T, *args, _stream()), "svdp_kv_read")
     return k, v
 
 
 # ---- around attention and logits ------------------------------------------------------------------------------------
 
 
-def _here(t: torch.Tensor, what: str) -> None:
-    """Kernels go to the current device's stream: what they work on has to lie there."""
+def _here(t: torch.Tensor, what: str) -> int:
+    """The current device, to whose stream kernels go: what they work on has to lie there."""
     now = torch.cuda.current_device() if _current_device is None else _current_device()
     if t.get_device() != now:
-        raise SvdpError(f"{what}: its tensors are on {t.device}, the current device is cuda:{now}")
+        raise SvdpError(f"{what}: its tensors are on {t.device}, the current device being cuda:{now}")
+    return now
 
 
-def _head_stride(t: torch.Tensor, what: str) -> int:
+def _head_stride(t: torch.Tensor, what: str, on: int) -> int:
     """Stride of rows [T][heads][dim] whose heads lie side by side."""
-    if t.dim() != 3 or not t.is_cuda:
-        raise SvdpError(f"{what}: expected rows [T][heads][dim] on the device, got {tuple(t.shape)}")
+    if t.dim() != 3 or t.get_device() != on:
+        raise SvdpError(f"{what}: expected rows [T][heads][dim] on the device, got {tuple(t.shape)} on {t.device}, the current device being cuda:{on}")
     T, heads, dim = t.shape
     row, head, one = t.stride()
     if T and (one != 1 or (heads > 1 and head != dim)):
@@ -646,8 +653,8 @@ def qk_rope(q: torch.Tensor, k: torch.Tensor, places: torch.Tensor, inv_freq: to
     q [T][heads_q][dim], k [T][heads][dim] of float32 or bfloat16 (rows may be slices of a wider projection); places [T] int32, inv_freq
     [rot / 2] float32: the first rot channels are turned, pairs (i, rot / 2 + i), interleaved: (2 i, 2 i + 1).  q_weight, k_weight:
     float32, [dim] for all heads, or both [heads][dim].  q_out = q and k_out = k work in place.  Returns (q_out, k_out)."""
-    qs, ks = _head_stride(q, "q"), _head_stride(k, "k")
-    _here(q, "svdp_qk_rope")
+    on = torch.cuda.current_device() if _current_device is None else _current_device()
+    qs, ks = _head_stride(q, "q", on), _head_stride(k, "k", on)
     shape_q, shape_k, dtype, f32 = q.shape, k.shape, q.dtype, torch.float32
     T, heads_q, dim = shape_q
     heads = shape_k[1]
@@ -660,23 +667,23 @@ def qk_rope(q: torch.Tensor, k: torch.Tensor, places: torch.Tensor, inv_freq: to
         if eps is None or any(each) != all(each):
             raise SvdpError("svdp_qk_rope: weights go with a norm (eps), and are both [dim] or both [heads][dim]")
         flags |= ROPE_WEIGHT_EACH if each[0] else 0
-        wq = _typed(q_weight, f32, "q_weight", (heads_q, dim) if each[0] else (dim,))
-        wk = _typed(k_weight, f32, "k_weight", (heads, dim) if each[0] else (dim,))
+        wq = _typed(q_weight, f32, "q_weight", (heads_q, dim) if each[0] else (dim,), on)
+        wk = _typed(k_weight, f32, "k_weight", (heads, dim) if each[0] else (dim,), on)
     if q_out is None:
         q_out, qo = torch.empty(shape_q, dtype=dtype, device=q.device), heads_q * dim
     elif q_out.shape != shape_q or q_out.dtype is not dtype:
         raise SvdpError("svdp_qk_rope: q_out: expected the shape and the type of q")
     else:
-        qo = _head_stride(q_out, "q_out")
+        qo = _head_stride(q_out, "q_out", on)
     if k_out is None:
         k_out, ko = torch.empty(shape_k, dtype=dtype, device=q.device), heads * dim
     elif k_out.shape != shape_k or k_out.dtype is not dtype:
         raise SvdpError("svdp_qk_rope: k_out: expected the shape and the type of k")
     else:
-        ko = _head_stride(k_out, "k_out")
+        ko = _head_stride(k_out, "k_out", on)
     _check(lib().svdp_qk_rope(
         SVDP_BF16 if dtype is torch.bfloat16 else SVDP_F32, dim, T, q.data_ptr(), qs, heads_q, k.data_ptr(), ks, heads,
-        _typed(places, torch.int32, "places", (T,)), _typed(inv_freq, f32, "inv_freq"), 2 * inv_freq.numel(), flags, wq, wk,
+        _typed(places, torch.int32, "places", (T,), on), _typed(inv_freq, f32, "inv_freq", None, on), 2 * inv_freq.numel(), flags, wq, wk,
         0.0 if eps is None else eps, q_out.data_ptr(), qo, k_out.data_ptr(), ko, _stream()), "svdp_qk_rope")
     return q_out, k_out
 
@@ -689,14 +696,14 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
     first token.  The rules are in include/svdp.h.  Returns answers [T] int32 (and with want_logp the logarithms of their shares [T] float32)."""
     if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or not logits.is_cuda or logits.stride(1) != 1:
         raise SvdpError(f"logits: expected [T][V] of float32 or bfloat16 on the device, got {tuple(logits.shape)} {logits.dtype}")
-    _here(logits, "svdp_sample")
+    on = _here(logits, "svdp_sample")
     T, V = logits.shape
     dt, f32, rows = SVDP_BF16 if logits.dtype is torch.bfloat16 else SVDP_F32, torch.float32, (T,)
     answers = torch.empty(T, dtype=torch.int32, device=logits.device)
     logp = torch.empty(T, dtype=f32, device=logits.device) if want_logp else None
     _check(lib().svdp_sample(
-        logits.data_ptr(), logits.stride(0) if T > 1 else V, dt, V, _typed(u, f32, "u", rows), _typed(temperature, f32, "temperature", rows),
-        _typed(top_k, torch.int32, "top_k", rows), _typed(top_p, f32, "top_p", rows), _typed(min_p, f32, "min_p", rows), T, answers.data_ptr(),
+        logits.data_ptr(), logits.stride(0) if T > 1 else V, dt, V, _typed(u, f32, "u", rows, on), _typed(temperature, f32, "temperature", rows, on),
+        _typed(top_k, torch.int32, "top_k", rows, on), _typed(top_p, f32, "top_p", rows, on), _typed(min_p, f32, "min_p", rows, on), T, answers.data_ptr(),
         _ptr(logp), _stream()), "svdp_sample")
     return (answers, logp) if want_logp else answers
 
@@ -705,13 +712,13 @@ def tree_walk(answers: torch.Tensor, tokens: torch.Tensor, starts: torch.Tensor,
               max_nodes: Optional[int] = None):
     """The branch of each drafted tree that agrees with given answers [T] (int32): tree_accept without its logits.
     Returns (keep [T], counts [R], next [R]), all int32."""
-    _here(answers, "svdp_tree_walk")
+    on = _here(answers, "svdp_tree_walk")
     T, R = answers.numel(), starts.numel() - 1
     max_nodes = max(1, min(T, MAX_NODES)) if max_nodes is None else int(max_nodes)
     keep, counts, following = torch.empty(T + 2 * max(R, 0), dtype=torch.int32, device=answers.device).split_with_sizes((T, max(R, 0), max(R, 0)))
     i32 = torch.int32
-    _check(lib().svdp_tree_walk(_typed(answers, i32, "answers", (T,)), _typed(tokens, i32, "tokens", (T,)), _typed(tree, torch.int64, "tree", (T,)),
-                                _typed(starts, i32, "starts"), R, T, max_nodes, keep.data_ptr(), counts.data_ptr(), following.data_ptr(),
+    _check(lib().svdp_tree_walk(_typed(answers, i32, "answers", (T,), on), _typed(tokens, i32, "tokens", (T,), on),
+                                _typed(tree, torch.int64, "tree", (T,), on), _typed(starts, i32, "starts", None, on), R, T, max_nodes, keep.data_ptr(), counts.data_ptr(), following.data_ptr(),
                                 _stream()), "svdp_tree_walk")
     return keep, counts, following
 

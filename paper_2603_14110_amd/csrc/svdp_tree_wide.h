@@ -40,7 +40,7 @@ __device__ __forceinline__ int tw_swizzle(int token, int dim) { return dim == 64
 // A cache in 8 bits: its tiles come into LDS as they are, in two stages of 32 KB, and the block makes bf16 operands of one of them
 // (K and V with their tokens' powers of two, exact) in the 64 KB that the products read, between two barriers.  The tree's own tokens,
 // bf16 as ever, come straight to those 64 KB.  Made by each wave in registers, the operands would cost every wave what the block does once.
-// Trees of 64 over 20 000 to 32 768 tokens, seven query heads a head: 166 us in a profile and a call 151, where the rows' tiles one after
+// Trees of 64 over 20 000 to 32 768 tokens, seven query heads a head: 166 to 179 us in a profile and a call 153, where the rows' tiles one after
 // the other, 32 at a time, take 226; the matrix unit is busy 37 % of the time, the vector unit 51.
 constexpr int TW_CODED = TW_STAGE / 2, TW_SCALES = 1024;        // bytes of a stage: codes; scales of K and of V, and what a load fills besides
 

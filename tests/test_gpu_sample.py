@@ -271,7 +271,10 @@ def test_tensors_of_another_device_are_refused(env, monkeypatch):
     i32 = torch.zeros(2, dtype=torch.int32, device="cuda")
     q = torch.zeros((2, 1, 64), device="cuda")
     monkeypatch.setattr(binding, "_current_device", lambda: 1)
+    coded = binding.KVCache.empty(1, 1, 32, 1, 64, dtype=torch.float8_e4m3fn)
+    h, slots = q.bfloat16(), torch.zeros(2, dtype=torch.int64, device="cuda")
     for call in (lambda: binding.sample(x, u), lambda: binding.tree_walk(i32, i32, i32), lambda: binding.kv_read(cache, i32.long()),
-                 lambda: binding.qk_rope(q, q, i32, torch.ones(4, device="cuda"))):
+                 lambda: binding.qk_rope(q, q, i32, torch.ones(4, device="cuda")), lambda: binding.kv_commit(coded, h[None], h[None], slots),
+                 lambda: binding.tree_attn(coded, 0, h, h, h, i32[None], i32[:1], i32)):
         with pytest.raises(binding.SvdpError, match="current device"):
             call()
