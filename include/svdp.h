@@ -308,7 +308,8 @@ typedef struct svdp_kv_cache {
     void *K;               /* [layers][pages][heads][page][dim], 16-byte aligned      */
     void *V;               /* [layers][pages][heads][page / e][dim][e], 16-byte aligned */
     uint8_t *K_scale;      /* SVDP_E4M3 only, else not looked at: [layers][pages][heads][page], 16-byte aligned: each token's   */
-    uint8_t *V_scale;      /* head of K and of V is its codes times 2^(scale - 127), scale from 1 to 254                       */
+    uint8_t *V_scale;      /* head of K and of V is its codes times 2^(scale - 127), scale from 1 to 254, as bf16: exact from  */
+                           /* 2^-126 on up to bf16's largest number; infinite beyond it, and below 2^-126 it may lose bits     */
 } svdp_kv_cache;
 
 /* Attention of every row over its request's cached tokens 0 .. lens[r] and over the nodes that it sees:

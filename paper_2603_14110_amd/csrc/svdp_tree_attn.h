@@ -302,10 +302,13 @@ struct TreeTile<float, DIM> {
     }
 };
 
-// A cache in 8 bits: its elements become bf16 operands in registers, K's with the token's power of two (exact), V's without
-// (its eight tokens have one each: it goes to their weights).  A lane's 16 bytes are the operands of two products, so that the channels
-// that a product takes are others than in 16 bits.  24 requests of 500 to 16 384 tokens, four query heads a head, 210 MB: 42 to 49 us,
-// 4.3 to 5.0 TB/s, of which some 5 us go by before and behind the reading; half of what 16 bits take.
+// A cache in 8 bits: its elements become bf16 operands in registers, with their tokens' powers of two: K's (one token a lane) in the
+// conversion, V's (eight tokens in an operand, one power each) as fp32, which is rounded to bf16, exactly.  Multiplied into the weights
+// instead, which are up to 2^SLACK, powers near either end of fp32's range would make them infinite or cost them their second terms.  That was
+// no faster either: eight requests of 4096 tokens, 32 rows 27.4 us against 26.5, 64 rows 40.6 against 38.6.
+// A lane's 16 bytes are the operands of two products, so that the channels that a product takes are others than in 16 bits.
+// 24 requests of 500 to 16 384 tokens, four query heads a head, 210 MB: 42 to 49 us, 4.3 to 5.0 TB/s, of which some 5 us go by before and
+// behind the reading; half of what 16 bits take.
 template <int DIM>
 struct TreeTile<e4m3, DIM> : TreeTile<bf16, DIM> {
     static constexpr bool CODED = true;
@@ -314,6 +317,27 @@ struct TreeTile<e4m3, DIM> : TreeTile<bf16, DIM> {
     static __device__ __forceinline__ uint4 operand(const uint4 &raw, int half, float by)
     {
         return half == 0 ? widen_e4m3(raw.x, raw.y, by) : widen_e4m3(raw.z, raw.w, by);
+    }
+    // the first n of eight tokens' powers, 2^0 behind them
+    static __device__ __forceinline__ uint64_t first_powers(uint64_t by, int n)
+    {
+        const uint64_t keep = n >= 8 ? ~0ull : n <= 0 ? 0ull : (1ull << (8 * n)) - 1;
+        return (by & keep) | (0x7f7f7f7f7f7f7f7full & ~keep);
+    }
+    // eight tokens of a channel, each with its own power
+    static __device__ __forceinline__ uint4 decoded(uint32_t a, uint32_t b, uint64_t by)
+    {
+        ta_f32x8 x;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t w = i == 0 ? a : b, s = (uint32_t)(by >> (32 * i));
+            const auto low = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), high = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+            x[4 * i] = low[0] * power_of(s & 0xffu);
+            x[4 * i + 1] = low[1] * power_of((s >> 8) & 0xffu);
+            x[4 * i + 2] = high[0] * power_of((s >> 16) & 0xffu);
+            x[4 * i + 3] = high[1] * power_of(s >> 24);
+        }
+        return __builtin_bit_cast(uint4, __builtin_convertvector(x, ta_bf16x8));
     }
     // the first n of 8 tokens of two channels, zeros behind them
     static __device__ __forceinline__ uint4 first_coded(const uint4 &v, int n)
@@ -325,8 +349,8 @@ struct TreeTile<e4m3, DIM> : TreeTile<bf16, DIM> {
 
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 // Scores are taken relative to a `shift` that follows their maximum, in base two: it moves only where a score exceeds it by more than
-// SLACK (then to the maximum), so that the sums are rarely brought down to a new one.  A weight is then below 2^SLACK, far from any
-// limit of fp32 (nor of bf16, which has the same exponents).
+// SLACK (then to the maximum), so that the sums are rarely brought down to a new one.  A weight is then at most 2^SLACK, far from any
+// limit of fp32 (and of bf16, which has the same exponents).
 constexpr float SLACK = 8.f;
 // -inf (nothing but zero weights so far) must not make -inf - -inf
 __device__ __forceinline__ float finite_shift(float shift) { return shift == -INFINITY ? 0.f : shift; }
@@ -373,9 +397,9 @@ struct TreeWave {
     // the maximum that others compare theirs with: -inf for a row that has not seen anything
     __device__ __forceinline__ float top(int nt) const { return limit[nt] == -INFINITY ? -INFINITY : shift[nt]; }
 
-    // Scores in base two, relative to the shift -> weights, each as by(i, weight) of the lane's token i for the product with V.
-    template <int N, typename By>
-    __device__ __forceinline__ void weights(float (&z)[NT][8 * N], Weights (&w)[NT][N], By &&by)
+    // Scores in base two, relative to the shift -> weights.
+    template <int N>
+    __device__ __forceinline__ void weights(float (&z)[NT][8 * N], Weights (&w)[NT][N])
     {
         float top[NT];
         bool grew = false;
@@ -410,15 +434,8 @@ struct TreeWave {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) e[i] = exp2_fast(z[nt][8 * n + i]);
                 total[nt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-#pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = by(8 * n + i, e[i]);
                 w[nt][n] = X::pack_weights(e);
             }
-    }
-    template <int N>
-    __device__ __forceinline__ void weights(float (&z)[NT][8 * N], Weights (&w)[NT][N])
-    {
-        weights<N>(z, w, [](int, float e) { return e; });
     }
     // One V operand (16 channels) against the weights of all rows.
     template <int N>
@@ -604,11 +621,6 @@ __global__ __launch_bounds__(TA_THREADS, (ta_waves_of<W, DIM, NT>())) void k_tre
                         scores(k, z);
                     }
                     if (i + TA_WAVES < i_end) load_k(at);
-                    float by[8];                                 // what V's tokens are multiplied by
-                    if constexpr (X::CODED) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) by[j] = power_of((uint32_t)(v_by >> (8 * j)) & 0xffu);
-                    }
                     if (count < TA_TILE) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
@@ -616,8 +628,8 @@ __global__ __launch_bounds__(TA_THREADS, (ta_waves_of<W, DIM, NT>())) void k_tre
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
                                 if (behind) z[nt][j] = -INFINITY;
-                            if (X::CODED && behind) by[j] = 0.f;
                         }
+                        if constexpr (X::CODED) v_by = X::first_powers(v_by, count - 8 * g);
 #pragma unroll
                         for (int dt = 0; dt < VR; ++dt)
 #pragma unroll
@@ -626,17 +638,15 @@ __global__ __launch_bounds__(TA_THREADS, (ta_waves_of<W, DIM, NT>())) void k_tre
                                 else v[dt][t] = X::first(v[dt][t], count - X::pack(t, g) * E);
                             }
                     }
-                    if constexpr (X::CODED) {
-                        mine.template weights<1>(z, p, [&](int j, float e) { return e * by[j]; });
+                    mine.template weights<1>(z, p);
 #pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) {
-                            const uint4 wide[1] = {X::operand(v[dt >> 1][0], dt & 1, 1.f)};
+                    for (int dt = 0; dt < DT; ++dt) {
+                        if constexpr (X::CODED) {
+                            const uint4 &raw = v[dt >> 1][0], wide[1] = {dt & 1 ? X::decoded(raw.z, raw.w, v_by) : X::decoded(raw.x, raw.y, v_by)};
                             mine.add(dt, wide, p);
+                        } else {
+                            mine.add(dt, v[dt], p);
                         }
-                    } else {
-                        mine.template weights<1>(z, p);
-#pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) mine.add(dt, v[dt], p);
                     }
                     if (i + TA_WAVES < i_end) load_v(at);
                 }

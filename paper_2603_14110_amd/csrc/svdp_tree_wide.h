@@ -198,22 +198,9 @@ __global__ __launch_bounds__(TW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2
                 for (int p = here(tid); p < TILES * TA_TILE * DIM / 16; p += TW_THREADS) {
                     const int pack = p / (DIM / 2);              // two channels of eight tokens
                     const uint4 raw = *reinterpret_cast<const uint4 *>(from + TW_CODED / 2 + p * 16);
-                    const uint2 scales = *reinterpret_cast<const uint2 *>(&s_scales[which][TILES * TA_TILE + pack * 8]);
-                    const auto eight = [&](uint32_t a, uint32_t b) {
-                        ta_f32x8 x;
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const uint32_t w = i == 0 ? a : b, s = i == 0 ? scales.x : scales.y;
-                            const auto low = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), high = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-                            x[4 * i] = low[0] * power_of(s & 0xffu);
-                            x[4 * i + 1] = low[1] * power_of((s >> 8) & 0xffu);
-                            x[4 * i + 2] = high[0] * power_of((s >> 16) & 0xffu);
-                            x[4 * i + 3] = high[1] * power_of(s >> 24);
-                        }
-                        return __builtin_bit_cast(uint4, __builtin_convertvector(x, ta_bf16x8));
-                    };
-                    *reinterpret_cast<uint4 *>(tw_smem + V_AT + p * 32) = eight(raw.x, raw.y);
-                    *reinterpret_cast<uint4 *>(tw_smem + V_AT + p * 32 + 16) = eight(raw.z, raw.w);
+                    const uint64_t scales = *reinterpret_cast<const uint64_t *>(&s_scales[which][TILES * TA_TILE + pack * 8]);
+                    *reinterpret_cast<uint4 *>(tw_smem + V_AT + p * 32) = TreeTile<e4m3, DIM>::decoded(raw.x, raw.y, scales);
+                    *reinterpret_cast<uint4 *>(tw_smem + V_AT + p * 32 + 16) = TreeTile<e4m3, DIM>::decoded(raw.z, raw.w, scales);
                 }
             };
             int stage = 0;
