@@ -368,14 +368,14 @@ svdp_status svdp_kv_plan(int32_t *table, int32_t max_pages, int32_t *ring, int32
  * l * layer_stride + t * row_stride elements (whole 16-byte vectors, pointers 16-byte aligned).  slots: device [T]; a
  * slot outside [0, pages * page) is skipped, no two rows may have the same one.  Rows are of the cache's type.
  * SVDP_E4M3: rows are bf16.  Each token's head gets the least power of two 2^b, b >= -96, at which none of its elements is above
- * 448 2^b, and its elements are divided by it and rounded to e4m3 (to the nearest, ties to even).  Infinities and NaN become NaN, and do
- * not count for the power.                                                                                          */
+ * 448 2^b, and its elements are divided by it and rounded to e4m3 (to the nearest, ties to even; where b is 120 to no more than 240, so
+ * that every element is a finite bf16 number again).  Infinities and NaN become NaN, and do not count for the power.  */
 svdp_status svdp_kv_commit(const svdp_kv_cache *cache, const void *k, int64_t k_layer_stride, int64_t k_row_stride,
                            const void *v, int64_t v_layer_stride, int64_t v_row_stride, const int64_t *slots, int32_t T,
                            void *stream);
 
 /* The other way: row t of k and v, all layers, becomes K and V of slot slots[t]; zeros where that lies outside [0, pages * page).
- * Strides and types as above (SVDP_E4M3: bf16, exact unless it is below bf16's range).  The same slot may be read
+ * Strides and types as above (SVDP_E4M3: bf16, exact for all that svdp_kv_commit writes).  The same slot may be read
  * by several rows; rows must not overlap each other or anything else.                                                */
 svdp_status svdp_kv_read(const svdp_kv_cache *cache, const int64_t *slots, int32_t T, void *k, int64_t k_layer_stride,
                          int64_t k_row_stride, void *v, int64_t v_layer_stride, int64_t v_row_stride, void *stream);

@@ -10,6 +10,7 @@ import numpy as np
 
 E4M3_MAX = 448.0
 LEAST = -96          # of the powers of two of an 8-bit cache
+MOST, MOST_CODE = 120, 240.0        # the largest one, of bf16's largest numbers, and its largest code: 256 2^120 is no bf16 number
 
 
 def e4m3_values() -> np.ndarray:
@@ -38,7 +39,8 @@ def quantise(x: np.ndarray):
     by = np.full(top.shape, LEAST, dtype=np.int64)
     while (top > E4M3_MAX * 2.0 ** by).any():
         by = np.where(top > E4M3_MAX * 2.0 ** by, by + 1, by)
-    return e4m3(x / (2.0 ** by)[..., None]), by
+    y = x / (2.0 ** by)[..., None]
+    return e4m3(np.where((by[..., None] == MOST) & np.isfinite(x), np.clip(y, -MOST_CODE, MOST_CODE), y)), by
 
 
 def commit(K, V, K_by, V_by, k, v, slots) -> None:

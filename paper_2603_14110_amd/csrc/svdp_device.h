@@ -148,7 +148,7 @@ __device__ __forceinline__ float dot_raw(const uint4 &w, const uint4 &x, float a
     return acc;
 }
 
-// Eight e4m3 elements times a power of two as bf16: exact, as three bits behind the leading one fit into seven.
+// Eight e4m3 elements times a power of two as bf16: exact in bf16's normal range, as three bits behind the leading one fit into seven.
 __device__ __forceinline__ uint4 widen_e4m3(uint32_t a, uint32_t b, float by)
 {
     return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, by, false)),

@@ -3,7 +3,8 @@
 // The dim elements x of a token's head become codes x / 2^b, rounded to e4m3 (to the nearest, ties to even), where b >= KV8_LEAST is
 // the least whole number with max |x| <= 448 2^b, 448 being the largest e4m3 number.  A power of two costs no precision beside any other
 // scale (at most one of the fifteen binades at the lower end), makes x / 2^b and code 2^b exact, and is one byte.
-// Infinities and NaN become NaN and do not count for the maximum.
+// Infinities and NaN become NaN and do not count for the maximum.  At the largest power, 2^120, codes end at 240 instead of 448: from 256 2^120
+// on there is no bf16 number, and what was finite would come back infinite; 255 2^120, the largest one, is off by less than half a step.
 //
 // What bounds both: reading and writing.  A prompt of 2357 tokens, 32 layers of 8 heads of 128, 465 MB, stored in 87 us, 5.3 TB/s (111 us
 // with a wave that has two channels a lane of every token, in 4-byte loads and with a maximum over 64 lanes each); 3400 tokens of the
@@ -20,6 +21,8 @@ namespace svdp {
 constexpr int KV_THREADS = 256, KV_WAVES = KV_THREADS / 64;
 constexpr int KV_ROWS = 8;                 // rows of a block: a pack's tokens at the most
 constexpr int KV8_LEAST = -96;
+constexpr uint32_t KV8_MOST = 120 + 127;   // as it is kept
+constexpr float KV8_MOST_CODE = 240.f;
 
 // Biased exponent (b + 127) for the largest magnitude of a token's head.
 __device__ __forceinline__ uint32_t kv8_exponent(float top)
@@ -36,6 +39,18 @@ __device__ __forceinline__ float kv8_magnitude(float x)
     return u < 0x7f800000u ? __uint_as_float(u) : 0.f;
 }
 __device__ __forceinline__ float kv8_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? NAN : x; }
+// What is rounded to codes: x times 2^-b.
+template <int N>
+__device__ __forceinline__ void kv8_scale(float (&x)[N], uint32_t biased)
+{
+    const float by = kv8_inverse(biased);
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = kv8_finite(x[j]) * by;
+    if (biased == KV8_MOST) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = fabsf(x[j]) > KV8_MOST_CODE ? copysignf(KV8_MOST_CODE, x[j]) : x[j];      // NaN stays
+    }
+}
 // Four codes in a word.
 __device__ __forceinline__ uint32_t kv8_codes(float a, float b, float c, float d)
 {
@@ -121,9 +136,7 @@ __global__ __launch_bounds__(KV_THREADS) void k_kv_commit8(KvArgs A)
 #pragma unroll
             for (int j = 0; j < 8; ++j) top = fmaxf(top, kv8_magnitude(x[j]));
             const uint32_t by = kv8_exponent(group_max<LOG2>(top));
-            const float inverse = kv8_inverse(by);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = kv8_finite(x[j]) * inverse;
+            kv8_scale(x, by);
             const int64_t slot = s.slot(row);
             if (i0 >= items || slot < 0) continue;
             const int64_t token = token_of(slot, h0 + h);
@@ -157,11 +170,8 @@ __global__ __launch_bounds__(KV_THREADS) void k_kv_commit8(KvArgs A)
                 for (int j = 0; j < 8; ++j) top = fmaxf(top, kv8_magnitude(x[t][p][j]));
             }
             by[t] = kv8_exponent(group_max<DIM == 64 ? 3 : 4>(top));
-            const float inverse = kv8_inverse(by[t]);
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[t][p][j] = kv8_finite(x[t][p][j]) * inverse;
+            for (int p = 0; p < PIECES; ++p) kv8_scale(x[t][p], by[t]);
         }
         const int64_t token = token_of(s.slot(row), h0 + min(h, hn - 1));                    // the pack's first
 #pragma unroll
@@ -190,18 +200,18 @@ __global__ __launch_bounds__(KV_THREADS) void k_kv_commit8(KvArgs A)
             top = fmaxf(top, kv8_magnitude(x[c]));
         }
         const uint32_t by = kv8_exponent(group_max<6>(top));
-        const float inverse = kv8_inverse(by);
+        kv8_scale(x, by);
         const int64_t token = token_of(s.slot(row), h0 + h);
         const int in_pack = (int)(token & (E - 1));
         uint8_t *to = static_cast<uint8_t *>(A.V) + (token - in_pack) * DIM + in_pack;
 #pragma unroll
-        for (int c = 0; c < C; ++c) to[(lane * C + c) * E] = (uint8_t)kv8_codes(kv8_finite(x[c]) * inverse, 0.f, 0.f, 0.f);
+        for (int c = 0; c < C; ++c) to[(lane * C + c) * E] = (uint8_t)kv8_codes(x[c], 0.f, 0.f, 0.f);
         if (lane == 0) A.V_scale[token] = (uint8_t)by;
     }
 }
 
-// The same rows, the other way: K and V of slots as rows of the cache's type (8 bits: bf16, rounded once, exact as a rule).  Rows without a slot
-// become zeros.
+// The same rows, the other way: K and V of slots as rows of the cache's type (8 bits: bf16, exact for all that the commit writes).  Rows without a
+// slot become zeros.
 template <typename W, int DIM>
 __global__ __launch_bounds__(KV_THREADS) void k_kv_read(KvArgs A)
 {

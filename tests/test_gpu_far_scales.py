@@ -112,3 +112,50 @@ def test_powers_far_apart(env, dim, group, page, nodes, lens):
     scale = c.dim ** -0.5
     out, lse = c.call(binding)
     check(c, draft, out, lse, scale)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_the_largest_numbers_stay_finite(env, dim):
+    """Every bf16 number from 2^126 on, of either sign: what was finite is read back finite and within half a step of e4m3, and stored again it is the
+    same; in whole packs, and for tokens on their own."""
+    torch, binding, _, serve = env
+    T = 24
+    rng = np.random.default_rng(dim)
+    bits = np.concatenate([np.arange(0x7e80, 0x7f80), rng.integers(0x7e80, 0x7f80, T * dim)])[:T * dim]
+    bits[::3] |= 0x8000
+    x = torch.from_numpy(rng.permutation(bits).astype(np.uint16).view(np.int16)).view(torch.bfloat16).view(1, T, 1, dim).cuda()
+    x[0, 0, 0, 0], x[0, 0, 0, 1], x[0, 0, 0, 2] = float("nan"), float("inf"), 3.3895313892515355e38
+    want, by = serve.quantise(decoded(x))
+    assert by.max() == 120
+    for slots in (list(range(8, 8 + T)), [2 * i for i in range(T)]):
+        cache = binding.KVCache.empty(1, 2, 32, 1, dim, dtype=torch.float8_e4m3fn)
+        d_slots = torch.tensor(slots, dtype=torch.int64, device="cuda")
+        binding.kv_commit(cache, x, x, d_slots)
+        first = binding.kv_read(cache, d_slots)
+        binding.kv_commit(cache, *first, d_slots)
+        for rows in (first, binding.kv_read(cache, d_slots)):
+            for t in rows:
+                got = decoded(t)
+                assert np.array_equal(got, want * 2.0 ** by[..., None].astype(float), equal_nan=True)
+                fin = np.isfinite(decoded(x))
+                assert np.array_equal(np.isfinite(got), fin)
+                assert (np.abs(got - decoded(x))[fin] <= 2.0 ** -4 * np.abs(decoded(x))[fin]).all()
+
+
+def test_read_of_every_scale_and_code(env):
+    """What the header says of an element: exact from 2^-126 on, infinite past bf16's largest number, below 2^-126 no further off than that."""
+    torch, binding, _, serve = env
+    cache = binding.KVCache.empty(1, 1, 256, 2, 256, dtype=torch.float8_e4m3fn)
+    every = torch.arange(256, device="cuda", dtype=torch.uint8)
+    cache.K.view(torch.uint8).copy_(every)
+    cache.V.view(torch.uint8).copy_(every[:, None])
+    for t in (cache.K_scale, cache.V_scale):
+        t.view(torch.uint8).copy_(every)
+    value = serve.e4m3_values() * 2.0 ** (np.arange(256)[:, None] - 127.0)
+    for slots in (list(range(1, 255)), list(range(254, 0, -1))):         # packs, and tokens on their own
+        for rows in binding.kv_read(cache, torch.tensor(slots, dtype=torch.int64, device="cuda")):
+            got, want = decoded(rows)[0], np.repeat(value[slots][:, None], 2, 1)
+            normal = np.abs(want) >= 2.0 ** -126
+            assert np.array_equal(got[normal], np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)[normal])
+            assert np.array_equal(np.isnan(got), np.isnan(want))
+            assert (np.abs(got - want)[np.abs(want) < 2.0 ** -126] <= 2.0 ** -126).all()

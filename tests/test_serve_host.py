@@ -174,3 +174,13 @@ def test_rotation_keeps_lengths_and_depends_on_distance_only():
         assert np.allclose(np.linalg.norm(y, axis=-1), np.linalg.norm(x, axis=-1)) and np.array_equal(y[..., 32:], x[..., 32:])
         near, far = serve.rope(x, [3, 10], f, interleaved=inter), serve.rope(x, [1003, 1010], f, interleaved=inter)
         assert np.allclose((near[0] * near[1]).sum(-1), (far[0] * far[1]).sum(-1))
+
+
+def test_quantised_rows_are_finite_in_bf16():
+    """At the largest power, 2^120, codes end at 240: 256 2^120 is no bf16 number any more.  255 2^120, the largest one, is off by less than half a step."""
+    x = np.array([255.0, 248.0, 247.0, 232.0, -255.0, 1.0, 100.0, 240.0]) * 2.0 ** 120
+    codes, by = serve.quantise(x)
+    assert by == 120 and codes.tolist() == [240.0, 240.0, 240.0, 224.0, -240.0, 1.0, 96.0, 240.0]
+    assert (np.abs(codes * 2.0 ** 120 - x) <= 2.0 ** -4 * np.abs(x)).all()
+    codes, by = serve.quantise(np.array([224.0, 223.0, 112.0]) * 2.0 ** 120)
+    assert by == 119 and codes.tolist() == [448.0, 448.0, 224.0]
