@@ -376,7 +376,8 @@ svdp_status svdp_kv_commit(const svdp_kv_cache *cache, const void *k, int64_t k_
 
 /* The other way: row t of k and v, all layers, becomes K and V of slot slots[t]; zeros where that lies outside [0, pages * page).
  * Strides and types as above (SVDP_E4M3: bf16, exact for all that svdp_kv_commit writes).  The same slot may be read
- * by several rows; rows must not overlap each other or anything else.                                                */
+ * by several rows; rows must not overlap each other or anything else (refused where rows of K meet, rows of V, or rows of
+ * both whose strides are the same).                                                                                  */
 svdp_status svdp_kv_read(const svdp_kv_cache *cache, const int64_t *slots, int32_t T, void *k, int64_t k_layer_stride,
                          int64_t k_row_stride, void *v, int64_t v_layer_stride, int64_t v_row_stride, void *stream);
 

@@ -613,7 +613,7 @@ def kv_commit(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Ten
 
 def kv_read(cache: KVCache, slots: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
     """K and V of slots [T] (int64; zeros for one outside the cache) as rows k, v [layers][T][heads][dim], of every layer: what kv_commit
-    stored, in the cache's type (8 bits: bfloat16).  Returns (k, v)."""
+    stored, in the cache's type (8 bits: bfloat16).  k and v may be slices of something wider; rows that overlap are refused.  Returns (k, v)."""
     on = _here(cache.K, "svdp_kv_read")
     T, shape = slots.numel(), (cache.layers, slots.numel(), cache.heads, cache.dim)
     k = torch.empty(shape, dtype=cache.rows, device=cache.K.device) if k is None else k

@@ -172,6 +172,36 @@ svdp_status check_rows(const svdp_kv_cache *c, const int64_t *slots, int T, cons
         return SVDP_ERR_INVALID_ARG;
     return SVDP_OK;
 }
+// Rows of `row` elements at l * layer + t * step, l < layers, t < T, step >= row.  Whether one of them and one of the same rows moved by `apart`
+// elements have an element in common (apart 0: two different rows).  For each difference of layers only the two nearest of rows can.
+bool rows_meet(int64_t apart, int layers, int T, int64_t layer, int64_t step, int64_t row)
+{
+    if (layers == 1) layer = 0;
+    if (T == 1) step = row;
+    const int64_t far = apart < 0 ? -apart : apart;
+    // one layer after the other, and between two rows of the one there is room for one of the other
+    if ((layers == 1 || layer >= (T - 1) * step + far + row) && (apart == 0 || (far >= row && far + row <= step))) return false;
+    for (int l = apart == 0 ? 1 : 1 - layers; l < layers; ++l) {
+        const int64_t at = apart + l * layer, t = at / step;                // rows at - t step + (-1, 0, 1) step apart
+        for (int64_t i = t - 1; i <= t + 1; ++i)
+            if (i > -T && i < T && at - i * step > -row && at - i * step < row) return true;
+    }
+    return false;
+}
+// What is written: no row may overlap another one.  K's rows and V's are compared where their strides are the same, else their first ones.
+bool rows_apart(const svdp_kv_cache *c, int T, const void *k, int64_t k_layer, int64_t k_row, const void *v, int64_t v_layer, int64_t v_row)
+{
+    const int64_t row = (int64_t)c->heads * c->dim, apart = ((intptr_t)v - (intptr_t)k) / bytes_of(row_type(c->dtype));
+    constexpr int64_t MOST = (int64_t)1 << 46;                              // elements: more than any memory has; what follows stays in range
+    if (std::max(k_layer, v_layer) >= MOST / c->layers && c->layers > 1) return false;
+    if (std::max(k_row, v_row) >= MOST / T && T > 1) return false;
+    if (rows_meet(0, c->layers, T, k_layer, k_row, row) || rows_meet(0, c->layers, T, v_layer, v_row, row)) return false;
+    if (apart > -row && apart < row) return false;
+    const auto extent = [&](int64_t layer, int64_t step) { return (c->layers > 1 ? (c->layers - 1) * layer : 0) + (T > 1 ? (T - 1) * step : 0) + row; };
+    if (apart >= extent(k_layer, k_row) || -apart >= extent(v_layer, v_row)) return true;
+    const bool alike = (c->layers == 1 || k_layer == v_layer) && (T == 1 || k_row == v_row);
+    return !alike || !rows_meet(apart, c->layers, T, k_layer, k_row, row);
+}
 KvArgs kv_args(const svdp_kv_cache *c, const int64_t *slots, int T, const void *k, int64_t k_layer, int64_t k_row, const void *v, int64_t v_layer,
                int64_t v_row)
 {
@@ -429,6 +459,7 @@ svdp_status svdp_kv_read(const svdp_kv_cache *cache, const int64_t *slots, int32
     if (st == SVDP_OK) st = check_cache_memory(cache);
     if (st == SVDP_OK) st = check_rows(cache, slots, T, k, k_layer_stride, k_row_stride, v, v_layer_stride, v_row_stride);
     if (st != SVDP_OK || T == 0) return st;
+    if (!rows_apart(cache, T, k, k_layer_stride, k_row_stride, v, v_layer_stride, v_row_stride)) return SVDP_ERR_INVALID_ARG;
     const KvArgs A = kv_args(cache, slots, T, k, k_layer_stride, k_row_stride, v, v_layer_stride, v_row_stride);
     on_cache_type(cache->dtype, [&](auto wt) {
         on_dim(cache->dim, [&](auto dc) {

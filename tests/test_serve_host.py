@@ -184,3 +184,40 @@ def test_quantised_rows_are_finite_in_bf16():
     assert (np.abs(codes * 2.0 ** 120 - x) <= 2.0 ** -4 * np.abs(x)).all()
     codes, by = serve.quantise(np.array([224.0, 223.0, 112.0]) * 2.0 ** 120)
     assert by == 119 and codes.tolist() == [448.0, 448.0, 224.0]
+
+
+def _rows_meet(at_k, at_v, layers, T, k, v, row):
+    """By looking at every element."""
+    where = [at + l * s[0] + t * s[1] for at, s in ((at_k, k), (at_v, v)) for l in range(layers) for t in range(T)]
+    return len({w + i for w in where for i in range(row)}) < len(where) * row
+
+
+def test_read_refuses_rows_that_overlap(svdp):
+    """A read writes its rows: layers on top of each other, one buffer for K and V, rows that run into each other's gaps.  Where K's strides are V's every
+    such call is refused; with other strides where their first rows meet, or K's or V's rows each other.  What does not overlap is
+    not refused (asked only where no GPU is there to follow the addresses)."""
+    import torch
+
+    rng, row, unit = np.random.default_rng(6), 128, 64
+    refused = taken = 0
+    for _ in range(3000):
+        layers, T = int(rng.integers(1, 5)), int(rng.integers(1, 5))
+        strides = lambda: (unit * int(rng.choice([0, 1, 2, 3, 4, 6, 8, 16, 20])), row + unit * int(rng.choice([0, 1, 2, 4, 6, 14])))
+        k, alike = strides(), rng.random() < 0.7
+        v = k if alike else strides()
+        apart = unit * int(rng.choice([0, 1, 2, 3, 4, 8, 10, 100, -1, -2, -4, -40]))
+        c = cache8(svdp, layers=layers, heads=2, dim=64, dtype=1)
+        call = lambda: svdp.lib().svdp_kv_read(ctypes.byref(c), P, T, 1 << 20, k[0], k[1], (1 << 20) + 2 * apart, v[0], v[1], None)
+        itself = _rows_meet(0, 1 << 30, layers, T, k, v, row)
+        meet = _rows_meet(0, apart, layers, T, k, v, row)
+        if itself or abs(apart) < row or (alike and meet):
+            assert call() == INVALID, (layers, T, k, v, apart)
+            refused += 1
+        elif not meet and not torch.cuda.is_available():
+            assert call() != INVALID, (layers, T, k, v, apart)
+            taken += 1
+    assert refused > 500 and (taken > 100 or torch.cuda.is_available())
+    for over in (dict(kl=1 << 46), dict(vl=1 << 62), dict(kr=1 << 45), dict(vr=1 << 62)):
+        a = {**dict(kl=1 << 20, kr=1024, vl=1 << 20, vr=1024), **over}
+        assert svdp.lib().svdp_kv_read(ctypes.byref(cache8(svdp)), P, 3, P, a["kl"], a["kr"], 1 << 40, a["vl"], a["vr"], None) == INVALID
+
