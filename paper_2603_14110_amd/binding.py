@@ -444,25 +444,32 @@ class KVCache:
                    torch.empty((layers, pages, heads, page // e, dim, e), dtype=dtype, device=device), *scales)
 
 
-def _typed(t: Optional[torch.Tensor], dtype, what: str, shape=None, on: Optional[int] = None) -> Optional[int]:
-    """Address of a contiguous device tensor of one type (and shape; on: of that device); None stays None."""
+def _here(t: torch.Tensor, what: str) -> int:
+    """The current device, to whose stream kernels go: what they work on has to lie there."""
+    now = torch.cuda.current_device() if _current_device is None else _current_device()
+    if t.get_device() != now:
+        raise SvdpError(f"{what}: its tensors are on {t.device}, the current device being cuda:{now}")
+    return now
+
+
+def _typed(t: Optional[torch.Tensor], dtype, what: str, shape, on: int) -> Optional[int]:
+    """Address of a contiguous tensor of one type (and shape) on one device; None stays None."""
     if t is None:
         return None
-    if (t.dtype is not dtype or not (t.is_cuda if on is None else t.get_device() == on) or not t.is_contiguous()
-            or (shape is not None and t.shape != shape)):
+    if t.dtype is not dtype or t.get_device() != on or not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise SvdpError(f"{what}: expected a contiguous device tensor of {dtype}"
-                        f"{'' if shape is None else ' ' + str(tuple(shape))}, got {tuple(t.shape)} {t.dtype}"
-                        f"{'' if on is None else f' on {t.device}, the current device being cuda:{on}'}")
+                        f"{'' if shape is None else ' ' + str(tuple(shape))}, got {tuple(t.shape)} {t.dtype} on {t.device}, "
+                        f"the current device being cuda:{on}")
     return t.data_ptr()
 
 
-def _heads_rows(t: torch.Tensor, cache: KVCache, heads: int, what: str, on: Optional[int] = None) -> int:
+def _heads_rows(t: torch.Tensor, cache: KVCache, heads: int, what: str, on: int) -> int:
     """Stride of the rows [heads][dim] of q, k or v (a slice of a wider projection is fine)."""
     rows, _, dim = shape = t.shape
     row, head, one = t.stride()
-    if t.dtype != cache.rows or not (t.is_cuda if on is None else t.get_device() == on) or dim != cache.dim or shape[1] != heads:
-        raise SvdpError(f"{what}: expected [rows][{heads}][{cache.dim}] of {cache.rows} on the device, got {tuple(shape)} {t.dtype}"
-                        f"{'' if on is None else f' on {t.device}, the current device being cuda:{on}'}")
+    if t.dtype != cache.rows or t.get_device() != on or dim != cache.dim or shape[1] != heads:
+        raise SvdpError(f"{what}: expected [rows][{heads}][{cache.dim}] of {cache.rows} on the device, got {tuple(shape)} {t.dtype} on {t.device}, "
+                        f"the current device being cuda:{on}")
     if rows and (one != 1 or (head != dim and heads > 1)):
         raise SvdpError(f"{what}: the heads of a row have to lie side by side")
     # one row: its stride says nothing
@@ -494,7 +501,7 @@ def tree_attn(cache: KVCache, layer: int, q: torch.Tensor, k: torch.Tensor, v: t
     Returns out [T][heads_q][dim] (and lse [T][heads_q] fp32 with want_lse)."""
     if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
         raise SvdpError("svdp_tree_attn: q, k, v are rows of heads of channels")
-    on = _here(cache.K, "svdp_tree_attn") if cache.K_scale is not None else None
+    on = _here(cache.K, "svdp_tree_attn")
     T, heads_q, dim = q.shape
     R = lens.numel()
     if k.shape[0] != T or v.shape[0] != T or table.dim() != 2 or table.shape[0] != R or starts.numel() != R + 1:
@@ -516,8 +523,8 @@ def tree_attn(cache: KVCache, layer: int, q: torch.Tensor, k: torch.Tensor, v: t
         lse_at = _typed(lse, torch.float32, "lse", (T, heads_q), on)
     if ws is None:
         ws = torch.empty(tree_attn_workspace_bytes(cache, heads_q, R, max_pages, max_nodes), dtype=torch.uint8, device=q.device)
-    elif not (ws.is_contiguous() and (ws.is_cuda if on is None else ws.get_device() == on)):
-        raise SvdpError("ws: expected a contiguous device tensor")
+    elif not ws.is_contiguous() or ws.get_device() != on:
+        raise SvdpError(f"ws: expected a contiguous tensor on the current device, cuda:{on}")
     i32 = torch.int32
     _check(lib().svdp_tree_attn(
         ctypes.byref(cache.c), layer, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
@@ -541,6 +548,7 @@ def tree_accept(logits: torch.Tensor, tokens: torch.Tensor, starts: torch.Tensor
     tree [T] int64 or None (chains).  Returns (keep [T], counts [R], next [R], best [T]), all int32."""
     if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or not logits.is_cuda or logits.stride(1) != 1:
         raise SvdpError(f"logits: expected [T][V] of float32 or bfloat16 on the device, got {tuple(logits.shape)} {logits.dtype}")
+    on = _here(logits, "svdp_tree_accept")
     T, V = logits.shape
     R = starts.numel() - 1
     dt = SVDP_BF16 if logits.dtype == torch.bfloat16 else SVDP_F32
@@ -554,10 +562,11 @@ def tree_accept(logits: torch.Tensor, tokens: torch.Tensor, starts: torch.Tensor
         at, room = scratch.data_ptr(), nbytes
     else:
         ws = torch.empty(nbytes, dtype=torch.uint8, device=logits.device) if ws is None else ws
+        _here(ws, "svdp_tree_accept")
         at, room = _ptr(ws), ws.numel()
     _check(lib().svdp_tree_accept(
-        logits.data_ptr(), logits.stride(0) if T > 1 else V, dt, V, _typed(tokens, torch.int32, "tokens", (T,)),
-        _typed(tree, torch.int64, "tree", (T,)), _typed(starts, torch.int32, "starts"), R, T, max_nodes, keep.data_ptr(),
+        logits.data_ptr(), logits.stride(0) if T > 1 else V, dt, V, _typed(tokens, torch.int32, "tokens", (T,), on),
+        _typed(tree, torch.int64, "tree", (T,), on), _typed(starts, torch.int32, "starts", None, on), R, T, max_nodes, keep.data_ptr(),
         counts.data_ptr(), following.data_ptr(), best.data_ptr(), at, room, _stream()), "svdp_tree_accept")
     return keep, counts, following, best
 
@@ -569,6 +578,7 @@ def kv_plan(table: torch.Tensor, ring: torch.Tensor, pool: torch.Tensor, lens: t
     table [R][max_pages] and ring [pages] are changed in place; pool [2], lens, add [R], starts [R + 1], keep [T] are read,
     all int32.  keep: as tree_accept returns it; None: every row is kept, ``rows`` of them.
     Returns (slots [T] int64, lens [R], pool [2], refused [R])."""
+    on = _here(lens, "svdp_kv_plan")
     R = lens.numel()
     if table.dim() != 2 or table.shape[0] != R or add.numel() != R or starts.numel() != R + 1 or pool.numel() != 2:
         raise SvdpError(f"svdp_kv_plan: table {tuple(table.shape)}, lens [{R}], add [{add.numel()}], starts [{starts.numel()}] "
@@ -580,20 +590,21 @@ def kv_plan(table: torch.Tensor, ring: torch.Tensor, pool: torch.Tensor, lens: t
     lens_out, refused, pool_out = torch.empty(2 * R + 2, dtype=torch.int32, device=lens.device).split_with_sizes((R, R, 2))
     i32 = torch.int32
     _check(lib().svdp_kv_plan(
-        _typed(table, i32, "table"), table.shape[1], _typed(ring, i32, "ring"), ring.numel(), int(page), _typed(pool, i32, "pool"),
-        _typed(lens, i32, "lens"), _typed(add, i32, "add"), _typed(starts, i32, "starts"), _typed(keep, i32, "keep"), R, T,
+        _typed(table, i32, "table", None, on), table.shape[1], _typed(ring, i32, "ring", None, on), ring.numel(), int(page),
+        _typed(pool, i32, "pool", None, on), _typed(lens, i32, "lens", None, on), _typed(add, i32, "add", None, on),
+        _typed(starts, i32, "starts", None, on), _typed(keep, i32, "keep", None, on), R, T,
         slots.data_ptr(), lens_out.data_ptr(), pool_out.data_ptr(), refused.data_ptr(), _stream()), "svdp_kv_plan")
     return slots, lens_out, pool_out, refused
 
 
-def _kv_rows(cache: KVCache, T: int, k: torch.Tensor, v: torch.Tensor, on: Optional[int] = None) -> list:
+def _kv_rows(cache: KVCache, T: int, k: torch.Tensor, v: torch.Tensor, on: int) -> list:
     """Addresses and strides of rows k, v [layers][T][heads][dim]."""
     layers, heads, dim, dtype = cache.layers, cache.heads, cache.dim, cache.rows
     shape, args = (layers, T, heads, dim), []
     for t in (k, v):
-        if t.shape != shape or t.dtype is not dtype or not (t.is_cuda if on is None else t.get_device() == on):
-            raise SvdpError(f"{'v' if t is v else 'k'}: expected {shape} of {dtype} on the device, got {tuple(t.shape)} {t.dtype}"
-                            f"{'' if on is None else f' on {t.device}, the current device being cuda:{on}'}")
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != on:
+            raise SvdpError(f"{'v' if t is v else 'k'}: expected {shape} of {dtype} on the device, got {tuple(t.shape)} {t.dtype} on {t.device}, "
+                            f"the current device being cuda:{on}")
         layer, row, head, one = t.stride()
         if T and (one != 1 or (heads > 1 and head != dim)):
             raise SvdpError(f"{'v' if t is v else 'k'}: the heads of a row have to lie side by side")
@@ -605,7 +616,7 @@ def _kv_rows(cache: KVCache, T: int, k: torch.Tensor, v: torch.Tensor, on: Optio
 def kv_commit(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """K and V of new rows, k, v [layers][T][heads][dim], into the cache at slots [T] (int64; negative: not stored).  A cache in 8 bits
     takes bfloat16 rows and rounds them (see include/svdp.h)."""
-    on = _here(cache.K, "svdp_kv_commit") if cache.K_scale is not None else None
+    on = _here(cache.K, "svdp_kv_commit")
     T = slots.numel()
     args = _kv_rows(cache, T, k, v, on)
     _check(lib().svdp_kv_commit(ctypes.byref(cache.c), *args, _typed(slots, torch.int64, "slots", None, on), T, _stream()), "svdp_kv_commit")
@@ -624,14 +635,6 @@ def kv_read(cache: KVCache, slots: torch.Tensor, k: Optional[torch.Tensor] = Non
 
 
 # ---- around attention and logits ------------------------------------------------------------------------------------
-
-
-def _here(t: torch.Tensor, what: str) -> int:
-    """The current device, to whose stream kernels go: what they work on has to lie there."""
-    now = torch.cuda.current_device() if _current_device is None else _current_device()
-    if t.get_device() != now:
-        raise SvdpError(f"{what}: its tensors are on {t.device}, the current device being cuda:{now}")
-    return now
 
 
 def _head_stride(t: torch.Tensor, what: str, on: int) -> int:
