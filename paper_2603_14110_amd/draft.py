@@ -167,6 +167,11 @@ class Decoder:
     def load(self, saved) -> None:
         """What save() gave, into pages of a decoder without tokens (of the same layers; its cache may be of another size)."""
         lens, k, v = saved
+        c, shape = self.cache, (self.cache.layers, sum(lens), self.heads, self.dim)
+        if (len(lens) != self.lens.numel() or any(n < 0 for n in lens)
+                or any(t.shape != shape or t.dtype is not c.rows or t.device != c.K.device for t in (k, v))):
+            raise ValueError(f"a length for each request and K and V {shape} of {c.rows} on {c.K.device} go with this decoder, "
+                             f"got {len(lens)} lengths, {tuple(k.shape)} {k.dtype} on {k.device} and {tuple(v.shape)} {v.dtype} on {v.device}")
         if bool(self.lens.any()):
             raise RuntimeError("the cache holds tokens of other requests: release() them first")
         starts = torch.tensor([0] + lens, dtype=torch.int32, device=self.lens.device).cumsum(0, dtype=torch.int32)
