@@ -127,8 +127,8 @@ AttnPlan attn_plan(const svdp_kv_cache *c, int heads_q, int R, int max_pages, in
     // More than 32 rows: over the waves, 32 each (eight requests of 4096 tokens, 135 MB: 36 and 64 rows 36 us, where k_tree_attn, with
     // two row tiles after each other, takes 48).  At 32 rows k_tree_attn is ahead: 26.4 us for one request of 30 000 tokens and 13.4
     // for 24 of 150, where rows over the waves took 32.0 and 16.6 + 4.4.
-    // An 8-bit cache: more than 64, as reading K and V once more costs half (eight requests of 4096 tokens: 36 rows 32.6 us, over the
-    // waves 44.3; 64 rows 38.0 and 46.3; 100 rows 51.1 and 48.5; 24 requests of 150 tokens and 98 rows 25.3 and 20.4).
+    // An 8-bit cache: more than 64, as reading K and V once more costs half (eight requests of 4096 tokens: 36 rows 31.5 us, over the
+    // waves 44.3; 64 rows 36.1 and 45.8; 100 rows 47.8 and 48.0; 128 rows 56.3 and 49.9; 24 requests of 150 tokens and 98 rows 25.0 and 20.2).
     p.wide = dim <= 128 && (dt == SVDP_BF16 ? rows > 32 : dt == SVDP_E4M3 && rows > 64);
     // Two row tiles of 16 read K and V once for 32 rows (8 requests of 4096 tokens, 135 MB: 29.6 us, one after the other 45.2); with
     // 256 channels a second one does not fit the registers.

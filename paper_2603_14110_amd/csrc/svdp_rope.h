@@ -6,8 +6,8 @@
 // a time; its angles are computed once.  An angle is taken in turns in 64 bits, of which the whole ones are dropped: positions of a
 // million lose nothing.  All else is fp32, rounded once.
 //
-// What bounds it: reading and writing.  19 001 rows of 40 heads of 128 in bf16, 389 MB, in 79 us, 4.9 TB/s (a copy reaches 5.1); one row of 64
-// heads in 3.2 us, by the latency of position, angles and row.
+// What bounds it: reading and writing.  19 001 rows of 40 heads of 128 in bf16, 389 MB, in 79 us, 4.9 TB/s (a copy of 1 GiB reaches 5.1, rows read
+// back from a cache 5.5); one row of 64 heads in 3.2 us, by the latency of position, angles and row.
 #pragma once
 
 #include <hip/hip_runtime.h>

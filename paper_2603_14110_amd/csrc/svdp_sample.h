@@ -19,8 +19,10 @@
 //    the bin is divided by their keys' bits.
 //
 // What bounds it.  bf16, 769 rows of 152 064, 234 MB: 72 us (and 4.6 for the launch that looks after left rows), where reading takes 46: vector
-// units 59 % of the time (10 instructions for two elements, and half of all for the bins' weights and the questions), LDS 42 %; a row whose
-// token's value is not the only one of its kind is read once more.  8 rows of 32 000: 13 us, by the latency of one block's passes.
+// units 59 % of the time (10 instructions for two elements, and half of all for the bins' weights and the questions), LDS 42 %, of which two
+// thirds are bank conflicts of the counters (10.5 of 15.0 million cycles); a row whose token's value is not the only one of its kind is read
+// once more, and so is one with zeros or masked logits (-inf, or the type's lowest value), whose others are looked at: 769 rows of 152 064
+// 70 -> 97 us, one of them 18.9 -> 26.5, 8 rows of 32 000 16.6 -> 18.6.  8 rows of 32 000: 13 us, by the latency of one block's passes.
 // fp32: weights and additions of 64 bits in LDS.  One row of 32 000, by one compute unit: 19 us (with a series of 11 terms and no table 21.7,
 // of which the weights' pass took 9.5, each question 3, the maximum 3); 256 rows of 152 064: 111 us, where reading takes 30.  Tried and
 // dropped: bins over the front of the values only, all others just summed up (more registers than there are: 31 us for one row of 32 000);

@@ -10,7 +10,7 @@
 // What bounds it: a tile of 32 tokens is 768 cycles of a SIMD's matrix unit for each of its two waves (the weights' two terms have a
 // product with V each) and about as many of its vector unit (16 exponentials, two terms, some 110 other instructions).  A wave's products and
 // its weights follow each other, so that the two waves of a SIMD run side by side only in part: by the counters the matrix unit is
-// busy 46 % of the time and the vector unit 48; the reads of LDS take 15 %, without bank conflicts.  Trees of 64 with seven query heads
+// busy 46 % of the time and the vector unit 48; the reads of LDS take 15 %, without bank conflicts (in 16 bits; 8 bits below).  Trees of 64 with seven query heads
 // a head over 27 000 to 32 768 tokens, 88 GFLOP without the second terms: 163 us (with weights of one term 127: 39 % and 41 %).  What a
 // stage costs besides (its barrier, addresses, the first read of K) is why a stage is as large as LDS allows, and some 14 us are
 // not stages: 2 for the lengths, 3 for the first pages, Q and K and V, and a part of 133 KB that every block writes and that leaves the
@@ -40,8 +40,9 @@ __device__ __forceinline__ int tw_swizzle(int token, int dim) { return dim == 64
 // A cache in 8 bits: its tiles come into LDS as they are, in two stages of 32 KB, and the block makes bf16 operands of one of them
 // (K and V with their tokens' powers of two, exact) in the 64 KB that the products read, between two barriers.  The tree's own tokens,
 // bf16 as ever, come straight to those 64 KB.  Made by each wave in registers, the operands would cost every wave what the block does once.
-// Trees of 64 over 20 000 to 32 768 tokens, seven query heads a head: 166 to 179 us in a profile and a call 153, where the rows' tiles one after
-// the other, 32 at a time, take 226; the matrix unit is busy 37 % of the time, the vector unit 51.
+// Trees of 64 over 20 000 to 32 768 tokens, seven query heads a head: 163 to 179 us in a profile and a call 149 to 157, where the rows' tiles one
+// after the other, 32 at a time, take 205; the matrix unit is busy 37 % of the time, the vector unit 51.  Of the cycles of LDS 17 % are bank
+// conflicts: the operands are written in pieces of 16 bytes that lie 32 bytes apart from lane to lane.
 constexpr int TW_CODED = TW_STAGE / 2, TW_SCALES = 1024;        // bytes of a stage: codes; scales of K and of V, and what a load fills besides
 
 template <typename W, int DIM>
