@@ -389,7 +389,7 @@ svdp_status svdp_kv_read(const svdp_kv_cache *cache, const int64_t *slots, int32
  * (a, b) = (i, rot / 2 + i), or (2 i, 2 i + 1) with SVDP_ROPE_INTERLEAVED; channels from rot on are not turned.
  * q: device rows of [heads_q][dim], q_stride elements apart, k: of [heads][dim] (heads may be 0: no k), in `dtype`, SVDP_F32 or
  * SVDP_BF16; q_out and k_out likewise.  In place (q_out = q with the same stride, k_out = k likewise) is fine; otherwise they
- * overlap nothing.  Pointers 16-byte aligned, strides whole 16-byte vectors.  places: device [T] int32; inv_freq: device [rot / 2]
+ * overlap nothing (refused where rows of the same stride meet).  Pointers 16-byte aligned, strides whole 16-byte vectors.  places: device [T] int32; inv_freq: device [rot / 2]
  * fp32 (both may be NULL if rot is 0).  q_weight, k_weight: device [dim] fp32, with SVDP_ROPE_WEIGHT_EACH [heads][dim], 16-byte
  * aligned, NULL for none.  dim 64, 128 or 256; rot a multiple of 8, up to dim.  Angles are taken in 64 bits, so that far positions lose
  * nothing; all else is fp32, rounded once.                                                                          */

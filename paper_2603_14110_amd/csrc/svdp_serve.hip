@@ -18,6 +18,16 @@ using namespace svdp;
 inline int bytes_of(int dt) { return dt == SVDP_F32 ? 4 : 2; }
 inline bool aligned_to(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+// T rows of `written` elements, and T rows of `other` elements: whether one of the first has an element in common with one of the second.
+// Looked at where both have the same stride.
+bool rows_meet(int T, const void *a, int64_t a_stride, int64_t written, const void *b, int64_t b_stride, int64_t other, int bytes)
+{
+    if (T > 1 && a_stride != b_stride) return false;
+    const int64_t by = ((intptr_t)b - (intptr_t)a) / bytes, last = written - 1 - by;         // b's rows are at by + i a_stride of a's, |i| < T
+    int64_t i = 0;                                                                           // the largest i that does not lie behind the row
+    if (T > 1) i = std::min<int64_t>(last >= 0 ? last / a_stride : -((-last + a_stride - 1) / a_stride), T - 1);
+    return i > -T && by + i * a_stride < written && by + i * a_stride > -other;
+}
 template <SampleWays WAYS>
 using Ways = std::integral_constant<SampleWays, WAYS>;
 template <bool B>
@@ -73,6 +83,13 @@ svdp_status svdp_qk_rope(int32_t dtype, int32_t dim, int32_t T, const void *q, i
     if (!rows_ok(q, q_stride, heads_q) || !rows_ok(q_out, q_out_stride, heads_q)) return SVDP_ERR_INVALID_ARG;
     if (heads > 0 && (!rows_ok(k, k_stride, heads) || !rows_ok(k_out, k_out_stride, heads))) return SVDP_ERR_INVALID_ARG;
     if ((q == q_out && q_stride != q_out_stride) || (heads > 0 && k == k_out && k_stride != k_out_stride)) return SVDP_ERR_INVALID_ARG;
+    const int bytes = bytes_of(dtype);
+    const int64_t q_row = (int64_t)heads_q * dim, k_row = (int64_t)heads * dim;
+    if (q != q_out && rows_meet(T, q_out, q_out_stride, q_row, q, q_stride, q_row, bytes)) return SVDP_ERR_INVALID_ARG;
+    if (heads > 0 && ((k != k_out && rows_meet(T, k_out, k_out_stride, k_row, k, k_stride, k_row, bytes)) ||
+                      rows_meet(T, q_out, q_out_stride, q_row, k_out, k_out_stride, k_row, bytes) ||
+                      rows_meet(T, q_out, q_out_stride, q_row, k, k_stride, k_row, bytes) || rows_meet(T, k_out, k_out_stride, k_row, q, q_stride, q_row, bytes)))
+        return SVDP_ERR_INVALID_ARG;
     if ((rot > 0 && (!places || !inv_freq)) || !aligned_to(places, 4) || !aligned_to(inv_freq, 4) || !aligned16(q_weight) || !aligned16(k_weight))
         return SVDP_ERR_INVALID_ARG;
     RopeArgs A{};

@@ -221,3 +221,33 @@ def test_read_refuses_rows_that_overlap(svdp):
         a = {**dict(kl=1 << 20, kr=1024, vl=1 << 20, vr=1024), **over}
         assert svdp.lib().svdp_kv_read(ctypes.byref(cache8(svdp)), P, 3, P, a["kl"], a["kr"], 1 << 40, a["vl"], a["vr"], None) == INVALID
 
+
+
+def test_rotation_refuses_rows_that_overlap(svdp):
+    """One buffer for both outputs, an output over the other input, an output moved against its own input: every such call is refused where the strides are
+    the same; what does not overlap is not (asked only where no GPU is there to follow the addresses)."""
+    import torch
+
+    rng, unit, dim = np.random.default_rng(7), 64, 64
+    refused = taken = 0
+
+    def elements(at, stride, heads, T):
+        return {at + t * stride + i for t in range(T) for i in range(0, heads * dim, 8)}       # addresses are whole 16 bytes apart
+
+    for _ in range(4000):
+        T, hq, h = int(rng.integers(1, 5)), int(rng.integers(1, 4)), int(rng.integers(0, 4))
+        stride = unit * int(rng.integers(max(hq, h), 9))
+        place = lambda: 8 * int(rng.integers(0, 8 * 8 * 3)) if rng.random() < 0.3 else unit * int(rng.integers(0, 40))
+        q, k, qo, ko = (place() for _ in range(4))
+        qo, ko = q if rng.random() < 0.5 else qo, k if rng.random() < 0.5 else ko
+        e = {n: elements(at, stride, heads, T) for n, at, heads in (("q", q, hq), ("k", k, h), ("qo", qo, hq), ("ko", ko, h))}
+        meet = bool((q != qo and e["qo"] & e["q"]) or (k != ko and e["ko"] & e["k"]) or e["qo"] & e["ko"] or e["qo"] & e["k"] or e["ko"] & e["q"])
+        at = lambda place: (1 << 20) + 2 * place
+        call = lambda: svdp.lib().svdp_qk_rope(1, dim, T, at(q), stride, hq, at(k), stride, h, P, P, dim, 0, None, None, 0.0, at(qo), stride, at(ko), stride, None)
+        if meet:
+            assert call() == INVALID, (T, hq, h, stride, q, k, qo, ko)
+            refused += 1
+        elif not torch.cuda.is_available():
+            assert call() != INVALID, (T, hq, h, stride, q, k, qo, ko)
+            taken += 1
+    assert refused > 500 and (taken > 500 or torch.cuda.is_available())
